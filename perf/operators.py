@@ -369,11 +369,11 @@ def _exact_read(q, scales, k):
     nibble[:, 0::2] = packed & 15
     nibble[:, 1::2] = packed >> 4
     exponent, mantissa = (nibble >> 1) & 3, nibble & 1
-    magnitude = torch.where(exponent == 0, mantissa * 0.5, torch.ldexp(1 + mantissa * 0.5, exponent - 1)).double()
+    magnitude = torch.where(exponent == 0, mantissa * 0.5, (1 + mantissa * 0.5) * torch.exp2(exponent - 1.0)).double()
     if scales == "tiles":
         s = torch.cat([part for part in s.view(-1, rows, 8)], 1)
     s = s.repeat_interleave(_BLOCK, 1)
-    v = torch.ldexp(torch.where(nibble >= 8, -magnitude, magnitude), (s - 127).double())
+    v = torch.where(nibble >= 8, -magnitude, magnitude) * torch.exp2((s - 127).double())
     v[s == 255] = math.nan
     return v[:, :k]
 
