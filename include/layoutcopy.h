@@ -35,6 +35,8 @@ typedef struct lc_layout lc_layout_t; /* opaque: a layout S:D */
 typedef struct lc_plan lc_plan_t;     /* opaque: a planned copy between two layouts */
 typedef struct lc_slayout lc_slayout_t; /* opaque: a layout whose strides come from an integer-semimodule (Sec. 2.3.2) */
 typedef struct lc_gemm_plan lc_gemm_plan_t; /* opaque: a planned GEMM over three layouts */
+typedef struct lc_mx_plan lc_mx_plan_t; /* opaque: a planned quantisation to or from microscaled 4-bit elements */
+typedef struct lc_mx_gemm_plan lc_mx_gemm_plan_t; /* opaque: a planned GEMM with microscaled 4-bit operands */
 
 typedef enum {
   LC_OK = 0,
@@ -56,13 +58,15 @@ typedef enum {
   LC_ERR_HIP = 16,                /* a HIP runtime call failed (no device, launch failure, ...) */
   LC_ERR_NEEDS_WORKSPACE = 17,    /* the plan needs scratch device memory: use lc_plan_execute_workspace */
   LC_ERR_WORKSPACE_TOO_SMALL = 18,/* the workspace is NULL, misaligned or smaller than lc_plan_workspace_bytes */
-  LC_ERR_SCRATCH_LIMIT = 19       /* lc_plan_execute_static: the plan needs more scratch than the library's static array holds */
+  LC_ERR_SCRATCH_LIMIT = 19,      /* lc_plan_execute_static: the plan needs more scratch than the library's static array holds */
+  LC_ERR_BLOCK_LAYOUT = 20        /* microscaled tensors: a block of 32 codes is not 16 contiguous, aligned bytes under its layout */
 } lc_status_t;
 
 /* Element types.  The copy moves bit patterns; the dtype only fixes the element width. */
 typedef enum {
   LC_F32 = 0, LC_F16 = 1, LC_BF16 = 2,
-  LC_B8 = 3, LC_B16 = 4, LC_B32 = 5, LC_B64 = 6, LC_B128 = 7 /* opaque elements of 1, 2, 4, 8, 16 bytes */
+  LC_B8 = 3, LC_B16 = 4, LC_B32 = 5, LC_B64 = 6, LC_B128 = 7, /* opaque elements of 1, 2, 4, 8, 16 bytes */
+  LC_MXFP4 = 8 /* codes of 4 bits under scales per block of 32: an operand of the lc_mx_ calls only, not an element of a copy */
 } lc_dtype_t;
 
 const char* lc_status_string(lc_status_t s);
@@ -321,6 +325,54 @@ lc_status_t lc_gemm_plan_time(const lc_gemm_plan_t* plan, const void* a, const v
  * tile, column-major.  which = 0: A, (64,8) -> m + 32 k of the (32,16) tile; 1: B, (64,8) -> n + 32 k;
  * 2: C, (64,16) -> m + 32 n of the (32,32) tile. */
 lc_status_t lc_mfma_fragment_layout(int which, lc_layout_t** out);
+
+/* ---------------------------------------------------------------------------------------------
+ * Microscaled 4-bit tensors (MXFP4).
+ * An element is a code of 4 bits -- sign (bit 3), two exponent bits, one mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
+ * negatives -- and the 32 codes of a block along one mode share a scale of 8 bits, s, that stands for 2^(s - 127); s = 255 makes
+ * all 32 elements NaN.  A tensor is two device pointers under two layouts of equal rank:
+ *   codes   strides count elements of 4 bits; element e lies in the low half of byte e / 2 where e is even, in the high half
+ *           where it is odd.  The blocked mode is padded to whole blocks (its size is a multiple of 32) and leads with a stride-1
+ *           leaf whose extent is a multiple of 32; every other stride is a multiple of 32, the pointer 16-byte aligned
+ *           (BLOCK_LAYOUT, MISALIGNED): a block is 16 aligned bytes.
+ *   scales  bytes, any strides >= 0; the blocked mode counts blocks (its size is the codes' over 32).
+ * lc_mx_scale_layout writes the layout of the scales of `rows` rows of `blocks` blocks that the products read best:
+ * (rows,(8,blocks/8)):(8,(1,8 rows)) where blocks is a multiple of 8 -- eight neighbouring blocks of a row together, then the next
+ * row's eight -- and (rows,blocks):(blocks,1) otherwise.
+ * Negative strides are refused for codes and scales (NEGATIVE_STRIDE); modes of more than 4 leaves after coalescing, or sizes of
+ * 2^31 or more, are TOO_LARGE.  All calls are asynchronous on `hip_stream`, allocate nothing and may be recorded into a HIP graph;
+ * tensors that a call writes may overlap none that it reads.
+ * ------------------------------------------------------------------------------------------- */
+
+/* Which power of two a block's scale is, for its largest magnitude a: FLOOR 2^(floor(log2 a) - 2) (what lies above 6 times the
+ * scale saturates), COVER the smallest with a <= 6 * scale.  Kept within 2^-127 .. 2^127; 2^-127 for a block of zeros. */
+typedef enum { LC_MX_FLOOR = 0, LC_MX_COVER = 1 } lc_mx_rule_t;
+
+lc_status_t lc_mx_scale_layout(int64_t rows, int64_t blocks, lc_layout_t** out);
+
+/* Quantisation: src over (R,K) in fp32, fp16 or bf16 (strides of either sign) -> codes over (R,P), scales over (R,P/32), P >= K.
+ * Each value over its block's scale is rounded to the nearest code, ties to the even one, larger ones saturate at 6; the sign is
+ * kept, that of zero included.  Elements past K are zeros.  A block with an infinity or a NaN gets the scale 255 and codes 0.
+ * Blocks run along the second mode; exchange the modes of all three layouts for the other one.
+ * Errors: SIZE_MISMATCH, BLOCK_LAYOUT, NEGATIVE_STRIDE, DST_ALIASES (two blocks, or two scales, share an address), UNSUPPORTED_DTYPE,
+ * INVALID_ARG (a layout that is not rank 2), TOO_LARGE (2^31 blocks or more). */
+lc_status_t lc_mx_quantize_plan_create(const lc_layout_t* src, const lc_layout_t* codes, const lc_layout_t* scales, lc_dtype_t src_dtype,
+                                       lc_mx_rule_t rule, lc_mx_plan_t** out);
+/* Dequantisation: codes over (R,P), scales over (R,P/32) -> dst over (R,K), K <= P, each value rounded to the nearest of dst's type
+ * (exact in fp32 and bf16; beyond a type's range infinite).  Errors as above (DST_ALIASES: two coordinates of dst share an offset). */
+lc_status_t lc_mx_dequantize_plan_create(const lc_layout_t* codes, const lc_layout_t* scales, const lc_layout_t* dst, lc_dtype_t dst_dtype,
+                                         lc_mx_plan_t** out);
+/* One line: how the 16- or 32-bit side is reached, the coalesced modes. */
+lc_status_t lc_mx_plan_describe(const lc_mx_plan_t* plan, char* buf, size_t cap, size_t* needed);
+void lc_mx_plan_destroy(lc_mx_plan_t* plan);
+/* src / dst: aligned to their elements; codes: to 16 bytes (MISALIGNED).  A plan of the other direction is an INVALID_ARG. */
+lc_status_t lc_mx_quantize_plan_execute(const lc_mx_plan_t* plan, const void* src, void* codes, void* scales, void* hip_stream);
+lc_status_t lc_mx_dequantize_plan_execute(const lc_mx_plan_t* plan, const void* codes, const void* scales, void* dst, void* hip_stream);
+/* Plan (kept between calls as lc_copy's are) and execute. */
+lc_status_t lc_mx_quantize(const void* src, const lc_layout_t* src_layout, void* codes, const lc_layout_t* codes_layout, void* scales,
+                           const lc_layout_t* scales_layout, lc_dtype_t src_dtype, lc_mx_rule_t rule, void* hip_stream);
+lc_status_t lc_mx_dequantize(const void* codes, const lc_layout_t* codes_layout, const void* scales, const lc_layout_t* scales_layout, void* dst,
+                             const lc_layout_t* dst_layout, lc_dtype_t dst_dtype, void* hip_stream);
 
 #ifdef __cplusplus
 }

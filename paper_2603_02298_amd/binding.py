@@ -112,6 +112,17 @@ def lib():
     L.lc_debug_gemm_replay_on_host.argtypes = [P, P, i64, P, i64, P, i64]
     L.lc_debug_gemm_lds_address.argtypes = [ctypes.c_int, ctypes.c_uint32, ctypes.c_uint32, ctypes.c_uint32, ctypes.c_uint32]
     L.lc_debug_gemm_lds_address.restype = i64
+    L.lc_mx_scale_layout.argtypes = [i64, i64, PP]
+    L.lc_mx_quantize_plan_create.argtypes = [P, P, P, ctypes.c_int, ctypes.c_int, PP]
+    L.lc_mx_dequantize_plan_create.argtypes = [P, P, P, ctypes.c_int, PP]
+    L.lc_mx_plan_describe.argtypes = [P, ctypes.c_char_p, sz, ctypes.POINTER(sz)]
+    L.lc_mx_plan_destroy.argtypes = [P]
+    L.lc_mx_plan_destroy.restype = None
+    L.lc_mx_quantize_plan_execute.argtypes = [P, P, P, P, P]
+    L.lc_mx_dequantize_plan_execute.argtypes = [P, P, P, P, P]
+    L.lc_mx_quantize.argtypes = [P, P, P, P, P, P, ctypes.c_int, ctypes.c_int, P]
+    L.lc_mx_dequantize.argtypes = [P, P, P, P, P, P, ctypes.c_int, P]
+    L.lc_debug_mx_walk_on_host.argtypes = [P, i64, i64, i64, i64, ctypes.POINTER(i64), ctypes.POINTER(i64)]
     _lib = L
     return L
 
@@ -459,3 +470,136 @@ def gemm_tensor(a, a_layout, b, b_layout, c, c_layout):
         raise ValueError("tensor smaller than the layout's cosize")
     lc_gemm(a.data_ptr(), la, b.data_ptr(), lb, c.data_ptr(), lc_, "bf16" if a.dtype == torch.bfloat16 else "f16",
             torch.cuda.current_stream().cuda_stream)
+
+
+# ---- microscaled 4-bit tensors (MXFP4) ----
+MX_RULES = {"floor": 0, "cover": 1}
+
+
+def lc_mx_scale_layout(rows, blocks):
+    """The layout of the scales of `rows` rows of `blocks` blocks that the products read best."""
+    h = ctypes.c_void_p()
+    _check(lib().lc_mx_scale_layout(rows, blocks, ctypes.byref(h)), "lc_mx_scale_layout(%d, %d)" % (rows, blocks))
+    return Layout(_handle=h)
+
+
+class _MxPlan:
+    """lc_mx_plan_t handle."""
+
+    def __del__(self):
+        if getattr(self, "_h", None) and _lib is not None:
+            _lib.lc_mx_plan_destroy(self._h)
+            self._h = None
+
+    def describe(self):
+        need = ctypes.c_size_t()
+        lib().lc_mx_plan_describe(self._h, None, 0, ctypes.byref(need))
+        buf = ctypes.create_string_buffer(need.value)
+        lib().lc_mx_plan_describe(self._h, buf, need.value, None)
+        return buf.value.decode()
+
+    def debug_walk_on_host(self, x_before, x_bytes, codes_bytes, scales_bytes):
+        """Test instrumentation: walk the plan's accesses on the host against the buffers' sizes (x_before: bytes of x below
+        offset 0); returns the bytes read and written."""
+        r, w = ctypes.c_int64(), ctypes.c_int64()
+        _check(lib().lc_debug_mx_walk_on_host(self._h, x_before, x_bytes, codes_bytes, scales_bytes, ctypes.byref(r), ctypes.byref(w)),
+               "lc_debug_mx_walk_on_host")
+        return r.value, w.value
+
+
+class MxQuantizePlan(_MxPlan):
+    """Quantisation of src over (R,K) to codes over (R,P) and scales over (R,P/32); dtype: f32, bf16, f16; rule: floor, cover."""
+
+    def __init__(self, src_layout, codes_layout, scales_layout, dtype, rule="floor"):
+        self.src_layout, self.codes_layout, self.scales_layout = _as_layout(src_layout), _as_layout(codes_layout), _as_layout(scales_layout)
+        self.dtype, self.rule = dtype, rule
+        self._h = ctypes.c_void_p()
+        _check(lib().lc_mx_quantize_plan_create(self.src_layout._h, self.codes_layout._h, self.scales_layout._h, DTYPES[dtype], MX_RULES[rule],
+                                                ctypes.byref(self._h)),
+               "lc_mx_quantize_plan_create(%s -> %s, %s, %s, %s)" % (self.src_layout, self.codes_layout, self.scales_layout, dtype, rule))
+
+    def execute(self, src_ptr, codes_ptr, scales_ptr, stream=0):
+        """Device addresses; stream: hipStream_t as int."""
+        _check(lib().lc_mx_quantize_plan_execute(self._h, src_ptr, codes_ptr, scales_ptr, stream), "lc_mx_quantize_plan_execute")
+
+
+class MxDequantizePlan(_MxPlan):
+    """Codes over (R,P) under scales over (R,P/32) to values over (R,K), K <= P; dtype: f32, bf16, f16."""
+
+    def __init__(self, codes_layout, scales_layout, dst_layout, dtype):
+        self.codes_layout, self.scales_layout, self.dst_layout = _as_layout(codes_layout), _as_layout(scales_layout), _as_layout(dst_layout)
+        self.dtype = dtype
+        self._h = ctypes.c_void_p()
+        _check(lib().lc_mx_dequantize_plan_create(self.codes_layout._h, self.scales_layout._h, self.dst_layout._h, DTYPES[dtype], ctypes.byref(self._h)),
+               "lc_mx_dequantize_plan_create(%s, %s -> %s, %s)" % (self.codes_layout, self.scales_layout, self.dst_layout, dtype))
+
+    def execute(self, codes_ptr, scales_ptr, dst_ptr, stream=0):
+        """Device addresses; stream: hipStream_t as int."""
+        _check(lib().lc_mx_dequantize_plan_execute(self._h, codes_ptr, scales_ptr, dst_ptr, stream), "lc_mx_dequantize_plan_execute")
+
+
+def lc_mx_quantize(src_ptr, src_layout, codes_ptr, codes_layout, scales_ptr, scales_layout, dtype, rule="floor", stream=0):
+    """Quantisation on the GPU for device pointers."""
+    a, q, s = _as_layout(src_layout), _as_layout(codes_layout), _as_layout(scales_layout)
+    status = lib().lc_mx_quantize(src_ptr, a._h, codes_ptr, q._h, scales_ptr, s._h, DTYPES[dtype], MX_RULES[rule], stream)
+    if status != 0:
+        raise LayoutCopyError(status, "lc_mx_quantize(%s -> %s, %s)" % (a, q, s))
+
+
+def lc_mx_dequantize(codes_ptr, codes_layout, scales_ptr, scales_layout, dst_ptr, dst_layout, dtype, stream=0):
+    """Dequantisation on the GPU for device pointers."""
+    q, s, d = _as_layout(codes_layout), _as_layout(scales_layout), _as_layout(dst_layout)
+    status = lib().lc_mx_dequantize(codes_ptr, q._h, scales_ptr, s._h, dst_ptr, d._h, DTYPES[dtype], stream)
+    if status != 0:
+        raise LayoutCopyError(status, "lc_mx_dequantize(%s, %s -> %s)" % (q, s, d))
+
+
+def _mx_device(what, tensors):
+    """The one GPU that all tensors are on, entered: the launch goes to that device's current stream."""
+    import torch
+    if not all(t.is_cuda for t in tensors):
+        raise RuntimeError(what + " needs GPU tensors: it only runs in the HIP kernels")
+    if len({t.device for t in tensors}) != 1:
+        raise ValueError("tensors on different devices")
+    return torch.cuda.device(tensors[0].device)
+
+
+def _mx_dtype(t):
+    import torch
+    names = {torch.float32: "f32", torch.bfloat16: "bf16", torch.float16: "f16"}
+    if t.dtype not in names:
+        raise ValueError("float32, bfloat16 or float16 expected")
+    return names[t.dtype]
+
+
+def _mx_covers(codes, codes_layout, scales, scales_layout):
+    import torch
+    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
+        raise ValueError("codes and scales: uint8")
+    if (codes_layout.cosize + 1) // 2 > codes.numel() or scales_layout.cosize > scales.numel():
+        raise ValueError("tensor smaller than the layout's cosize")
+
+
+def mx_quantize_tensor(src, src_layout, codes, codes_layout, scales, scales_layout, rule="floor", src_origin=0):
+    """Convenience for torch tensors on one GPU, on its current stream (codes, scales: uint8).  src_origin: the element of src that
+    offset 0 of its layout refers to (layouts with negative strides reach below it)."""
+    import torch
+    with _mx_device("mx_quantize_tensor", (src, codes, scales)):
+        a, q, s = _as_layout(src_layout), _as_layout(codes_layout), _as_layout(scales_layout)
+        _mx_covers(codes, q, scales, s)
+        if src_origin + a.min_offset < 0 or src_origin + a.cosize > src.numel():
+            raise ValueError("tensor does not cover the offsets the layout reaches")
+        lc_mx_quantize(src.data_ptr() + src_origin * src.element_size(), a, codes.data_ptr(), q, scales.data_ptr(), s, _mx_dtype(src), rule,
+                       torch.cuda.current_stream().cuda_stream)
+
+
+def mx_dequantize_tensor(codes, codes_layout, scales, scales_layout, dst, dst_layout, dst_origin=0):
+    """Convenience for torch tensors on one GPU, on its current stream."""
+    import torch
+    with _mx_device("mx_dequantize_tensor", (codes, scales, dst)):
+        q, s, d = _as_layout(codes_layout), _as_layout(scales_layout), _as_layout(dst_layout)
+        _mx_covers(codes, q, scales, s)
+        if dst_origin + d.min_offset < 0 or dst_origin + d.cosize > dst.numel():
+            raise ValueError("tensor does not cover the offsets the layout reaches")
+        lc_mx_dequantize(codes.data_ptr(), q, scales.data_ptr(), s, dst.data_ptr() + dst_origin * dst.element_size(), d, _mx_dtype(dst),
+                         torch.cuda.current_stream().cuda_stream)

@@ -76,6 +76,7 @@ const char* lc_status_string(lc_status_t s) {
     case LC_ERR_NEEDS_WORKSPACE: return "NEEDS_WORKSPACE";
     case LC_ERR_WORKSPACE_TOO_SMALL: return "WORKSPACE_TOO_SMALL";
     case LC_ERR_SCRATCH_LIMIT: return "SCRATCH_LIMIT";
+    case LC_ERR_BLOCK_LAYOUT: return "BLOCK_LAYOUT";
   }
   return "UNKNOWN";
 }
@@ -89,6 +90,7 @@ int lc_dtype_bytes(lc_dtype_t dt) {
     case LC_B8: return 1;
     case LC_B64: return 8;
     case LC_B128: return 16;
+    case LC_MXFP4: return 0;   // half a byte: no element of a copy
   }
   return 0;
 }
