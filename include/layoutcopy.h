@@ -374,6 +374,38 @@ lc_status_t lc_mx_quantize(const void* src, const lc_layout_t* src_layout, void*
 lc_status_t lc_mx_dequantize(const void* codes, const lc_layout_t* codes_layout, const void* scales, const lc_layout_t* scales_layout, void* dst,
                              const lc_layout_t* dst_layout, lc_dtype_t dst_dtype, void* hip_stream);
 
+/* GEMM with microscaled 4-bit operands on the matrix cores: C(m,n) = sum_k A(m,k) B(n,k), or C(m,n) += that sum (`accumulate` not 0), B in
+ * codes, A in codes too (a_dtype LC_MXFP4) or in 16 bits (LC_BF16, LC_F16; a_scales NULL).  Layouts of rank 2, or all of rank 3 for a
+ * batch of products (as lc_gemm; strides of 0 share an operand).  C holds fp32, fp16 or bf16 (c_dtype): sums are accumulated in fp32, in an
+ * order of their own but the same one every time, and rounded once.
+ *   Both in codes: A over (M,K), B over (N,K), C over (M,N), K whole blocks, both blocked along k.  Products are exact.
+ *   A in 16 bits, B blocked along k (its scales over (N,P/32)): A over (M,K), B over (N,P), P >= K: the forward product with quantised
+ *   weights.  B's elements past K are not used.
+ *   A in 16 bits, B blocked along its rows (its scales over (P/32,K)): A over (M,K), B over (P,K), C over (M,N), P >= N: the product with the
+ *   transposed weights, i.e. the gradient of the forward product's A.
+ *   B's elements are rounded to A's type before they are multiplied: exact in bf16; in fp16 for magnitudes from 2^-14 to 65504, beyond which
+ *   they are infinite, and below to within 2^-25.
+ * A block whose scale is 255 makes every element of C that it enters NaN.  No call allocates or needs a workspace.
+ * a / b / c_align_bytes: alignment the caller guarantees for the pointers (codes: 16 or more).  Errors: INVALID_ARG (ranks, a_scales),
+ * SIZE_MISMATCH, BLOCK_LAYOUT, NEGATIVE_STRIDE, DST_ALIASES (C), UNSUPPORTED_DTYPE, MISALIGNED, TOO_LARGE (an extent, or a cosize -- of codes
+ * in words of four -- of 2^31 or more), HIP. */
+lc_status_t lc_mx_gemm_plan_create(const lc_layout_t* a, const lc_layout_t* a_scales, const lc_layout_t* b, const lc_layout_t* b_scales,
+                                   const lc_layout_t* c, lc_dtype_t a_dtype, lc_dtype_t c_dtype, int accumulate, unsigned a_align_bytes,
+                                   unsigned b_align_bytes, unsigned c_align_bytes, lc_mx_gemm_plan_t** out);
+/* One line: kernel, tile, how the operands are loaded, the coalesced modes (codes in words of four). */
+lc_status_t lc_mx_gemm_plan_describe(const lc_mx_gemm_plan_t* plan, char* buf, size_t cap, size_t* needed);
+lc_status_t lc_mx_gemm_plan_execute(const lc_mx_gemm_plan_t* plan, const void* a, const void* a_scales, const void* b, const void* b_scales, void* c,
+                                    void* hip_stream);
+void lc_mx_gemm_plan_destroy(lc_mx_gemm_plan_t* plan);
+int64_t lc_mx_gemm_plan_flops(const lc_mx_gemm_plan_t* plan); /* 2 M N K (L) */
+/* Plan (kept between calls, alignment taken from the pointers) and execute. */
+lc_status_t lc_mx_gemm(const void* a, const lc_layout_t* a_layout, const void* a_scales, const lc_layout_t* a_scales_layout, const void* b,
+                       const lc_layout_t* b_layout, const void* b_scales, const lc_layout_t* b_scales_layout, void* c,
+                       const lc_layout_t* c_layout, lc_dtype_t a_dtype, lc_dtype_t c_dtype, int accumulate, void* hip_stream);
+/* Mean milliseconds of `iters` back-to-back executions after `warmup` untimed ones, by HIP events on `hip_stream`; synchronises the stream. */
+lc_status_t lc_mx_gemm_plan_time(const lc_mx_gemm_plan_t* plan, const void* a, const void* a_scales, const void* b, const void* b_scales, void* c,
+                                 int warmup, int iters, void* hip_stream, float* ms_per_iter);
+
 #ifdef __cplusplus
 }
 #endif

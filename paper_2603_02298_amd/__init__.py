@@ -9,4 +9,4 @@ from .binding import (GemmPlan, gemm_tensor, lc_gemm, lc_mfma_fragment_layout, D
                       lc_max_common_vector, lc_raked_product, lc_right_inverse, SLayout, lc_slayout_coalesce,
                       lc_slayout_composition, lc_slayout_right_inverse, lc_slayout_xor_right_inverse,
                       lc_zipped_divide, lib, MxDequantizePlan, MxQuantizePlan, lc_mx_dequantize, lc_mx_quantize, lc_mx_scale_layout,
-                      mx_dequantize_tensor, mx_quantize_tensor)
+                      mx_dequantize_tensor, mx_quantize_tensor, MxGemmPlan, lc_mx_gemm, mx_gemm_tensor)

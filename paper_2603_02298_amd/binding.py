@@ -8,7 +8,7 @@ from . import build as _build
 
 _lib = None
 
-DTYPES = {"f32": 0, "f16": 1, "bf16": 2, "b8": 3, "b16": 4, "b32": 5, "b64": 6, "b128": 7}
+DTYPES = {"f32": 0, "f16": 1, "bf16": 2, "b8": 3, "b16": 4, "b32": 5, "b64": 6, "b128": 7, "mxfp4": 8}
 DTYPE_BYTES = {"f32": 4, "f16": 2, "bf16": 2, "b8": 1, "b16": 2, "b32": 4, "b64": 8, "b128": 16}
 
 
@@ -122,6 +122,15 @@ def lib():
     L.lc_mx_dequantize_plan_execute.argtypes = [P, P, P, P, P]
     L.lc_mx_quantize.argtypes = [P, P, P, P, P, P, ctypes.c_int, ctypes.c_int, P]
     L.lc_mx_dequantize.argtypes = [P, P, P, P, P, P, ctypes.c_int, P]
+    L.lc_mx_gemm_plan_create.argtypes = [P, P, P, P, P, ctypes.c_int, ctypes.c_int, ctypes.c_int, u, u, u, PP]
+    L.lc_mx_gemm_plan_describe.argtypes = [P, ctypes.c_char_p, sz, ctypes.POINTER(sz)]
+    L.lc_mx_gemm_plan_execute.argtypes = [P, P, P, P, P, P, P]
+    L.lc_mx_gemm_plan_destroy.argtypes = [P]
+    L.lc_mx_gemm_plan_destroy.restype = None
+    L.lc_mx_gemm_plan_flops.argtypes = [P]
+    L.lc_mx_gemm_plan_flops.restype = i64
+    L.lc_mx_gemm.argtypes = [P, P, P, P, P, P, P, P, P, P, ctypes.c_int, ctypes.c_int, ctypes.c_int, P]
+    L.lc_mx_gemm_plan_time.argtypes = [P, P, P, P, P, P, ctypes.c_int, ctypes.c_int, P, ctypes.POINTER(ctypes.c_float)]
     L.lc_debug_mx_walk_on_host.argtypes = [P, i64, i64, i64, i64, ctypes.POINTER(i64), ctypes.POINTER(i64)]
     _lib = L
     return L
@@ -554,6 +563,61 @@ def lc_mx_dequantize(codes_ptr, codes_layout, scales_ptr, scales_layout, dst_ptr
         raise LayoutCopyError(status, "lc_mx_dequantize(%s, %s -> %s)" % (q, s, d))
 
 
+class MxGemmPlan:
+    """lc_mx_gemm_plan_t handle: C(m,n) = sum_k A(m,k) B(n,k) (accumulate: +=), B in codes, A in codes (a_dtype "mxfp4") or in 16
+    bits (a_dtype bf16, f16; a_scales_layout None); c_dtype: f32, bf16, f16."""
+
+    def __init__(self, a_layout, a_scales_layout, b_layout, b_scales_layout, c_layout, a_dtype="mxfp4", c_dtype="f32", accumulate=True,
+                 a_align=256, b_align=256, c_align=256):
+        self.a_layout, self.b_layout, self.c_layout = _as_layout(a_layout), _as_layout(b_layout), _as_layout(c_layout)
+        self.a_scales_layout = None if a_scales_layout is None else _as_layout(a_scales_layout)
+        self.b_scales_layout = _as_layout(b_scales_layout)
+        self.a_dtype, self.c_dtype, self.accumulate = a_dtype, c_dtype, accumulate
+        self._h = ctypes.c_void_p()
+        _check(lib().lc_mx_gemm_plan_create(self.a_layout._h, self.a_scales_layout._h if self.a_scales_layout else None, self.b_layout._h,
+                                            self.b_scales_layout._h, self.c_layout._h, DTYPES[a_dtype], DTYPES[c_dtype], int(accumulate), a_align, b_align,
+                                            c_align, ctypes.byref(self._h)),
+               "lc_mx_gemm_plan_create(%s, %s, %s, %s, %s, %s, %s)" % (self.a_layout, self.a_scales_layout, self.b_layout, self.b_scales_layout,
+                                                                       self.c_layout, a_dtype, c_dtype))
+
+    def __del__(self):
+        if getattr(self, "_h", None) and _lib is not None:
+            _lib.lc_mx_gemm_plan_destroy(self._h)
+            self._h = None
+
+    def describe(self):
+        need = ctypes.c_size_t()
+        lib().lc_mx_gemm_plan_describe(self._h, None, 0, ctypes.byref(need))
+        buf = ctypes.create_string_buffer(need.value)
+        lib().lc_mx_gemm_plan_describe(self._h, buf, need.value, None)
+        return buf.value.decode()
+
+    @property
+    def flops(self):
+        return lib().lc_mx_gemm_plan_flops(self._h)
+
+    def execute(self, a_ptr, a_scales_ptr, b_ptr, b_scales_ptr, c_ptr, stream=0):
+        """Device addresses (a_scales_ptr None for an A in 16 bits); stream: hipStream_t as int."""
+        _check(lib().lc_mx_gemm_plan_execute(self._h, a_ptr, a_scales_ptr, b_ptr, b_scales_ptr, c_ptr, stream), "lc_mx_gemm_plan_execute")
+
+    def time(self, a_ptr, a_scales_ptr, b_ptr, b_scales_ptr, c_ptr, warmup, iters, stream=0):
+        ms = ctypes.c_float()
+        _check(lib().lc_mx_gemm_plan_time(self._h, a_ptr, a_scales_ptr, b_ptr, b_scales_ptr, c_ptr, warmup, iters, stream, ctypes.byref(ms)),
+               "lc_mx_gemm_plan_time")
+        return ms.value
+
+
+def lc_mx_gemm(a_ptr, a_layout, a_scales_ptr, a_scales_layout, b_ptr, b_layout, b_scales_ptr, b_scales_layout, c_ptr, c_layout, a_dtype="mxfp4",
+               c_dtype="f32", accumulate=True, stream=0):
+    """GEMM with microscaled 4-bit operands on the GPU for device pointers."""
+    la, lb, lc_, sb = _as_layout(a_layout), _as_layout(b_layout), _as_layout(c_layout), _as_layout(b_scales_layout)
+    sa = None if a_scales_layout is None else _as_layout(a_scales_layout)
+    status = lib().lc_mx_gemm(a_ptr, la._h, a_scales_ptr, sa._h if sa else None, b_ptr, lb._h, b_scales_ptr, sb._h, c_ptr, lc_._h, DTYPES[a_dtype],
+                              DTYPES[c_dtype], int(accumulate), stream)
+    if status != 0:
+        raise LayoutCopyError(status, "lc_mx_gemm(%s, %s, %s, %s, %s)" % (la, sa, lb, sb, lc_))
+
+
 def _mx_device(what, tensors):
     """The one GPU that all tensors are on, entered: the launch goes to that device's current stream."""
     import torch
@@ -603,3 +667,24 @@ def mx_dequantize_tensor(codes, codes_layout, scales, scales_layout, dst, dst_la
             raise ValueError("tensor does not cover the offsets the layout reaches")
         lc_mx_dequantize(codes.data_ptr(), q, scales.data_ptr(), s, dst.data_ptr() + dst_origin * dst.element_size(), d, _mx_dtype(dst),
                          torch.cuda.current_stream().cuda_stream)
+
+
+def mx_gemm_tensor(a, a_layout, a_scales, a_scales_layout, b, b_layout, b_scales, b_scales_layout, c, c_layout, accumulate=True):
+    """Convenience for torch tensors on one GPU, on its current stream: b and b_scales uint8; a uint8 with a_scales, or bfloat16 or
+    float16 with None for its scales and their layout; c float32, bfloat16 or float16."""
+    import torch
+    codes = a_scales is not None
+    with _mx_device("mx_gemm_tensor", (a, b, b_scales, c) + ((a_scales,) if codes else ())):
+        la, lb, lc_, sb = _as_layout(a_layout), _as_layout(b_layout), _as_layout(c_layout), _as_layout(b_scales_layout)
+        sa = _as_layout(a_scales_layout) if codes else None
+        _mx_covers(b, lb, b_scales, sb)
+        if codes:
+            _mx_covers(a, la, a_scales, sa)
+        elif a.dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError("a: bfloat16 or float16, or uint8 with scales")
+        elif la.cosize > a.numel():
+            raise ValueError("tensor smaller than the layout's cosize")
+        if lc_.cosize > c.numel():
+            raise ValueError("tensor smaller than the layout's cosize")
+        lc_mx_gemm(a.data_ptr(), la, a_scales.data_ptr() if codes else None, sa, b.data_ptr(), lb, b_scales.data_ptr(), sb, c.data_ptr(), lc_,
+                   "mxfp4" if codes else _mx_dtype(a), _mx_dtype(c), accumulate, torch.cuda.current_stream().cuda_stream)

@@ -4,6 +4,7 @@
 #include <string>
 
 #include "layoutcopy.h"
+#include "mx_gemm_plan.hpp"
 #include "mx_plan.hpp"
 #include "plan_cache.hpp"
 
@@ -16,6 +17,12 @@ lc_status_t put_text(const std::string& s, char* buf, size_t cap, size_t* needed
     buf[n] = 0;
   }
   return LC_OK;
+}
+unsigned pointer_alignment(const void* p) {
+  uintptr_t v = reinterpret_cast<uintptr_t>(p);
+  unsigned a = 1;
+  while (a < 256 && (v % (2 * a)) == 0) a *= 2;
+  return a;
 }
 lc_status_t create(bool quantize, const lc_layout_t* x, const lc_layout_t* codes, const lc_layout_t* scales, int dtype, int rule, lc_mx_plan_t** out) {
   if (!x || !codes || !scales || !out) return LC_ERR_INVALID_ARG;
@@ -108,6 +115,72 @@ lc_status_t lc_mx_dequantize(const void* codes, const lc_layout_t* codes_layout,
   } catch (...) {
     return LC_ERR_INVALID_ARG;
   }
+}
+
+lc_status_t lc_mx_gemm_plan_create(const lc_layout_t* a, const lc_layout_t* a_scales, const lc_layout_t* b, const lc_layout_t* b_scales,
+                                   const lc_layout_t* c, lc_dtype_t a_dtype, lc_dtype_t c_dtype, int accumulate, unsigned a_align_bytes,
+                                   unsigned b_align_bytes, unsigned c_align_bytes, lc_mx_gemm_plan_t** out) {
+  if (!a || !b || !b_scales || !c || !out) return LC_ERR_INVALID_ARG;
+  try {
+    auto plan = std::make_unique<lc_mx_gemm_plan>();
+    lc_status_t st = lc::make_mx_gemm_plan(a->L, a_scales ? &a_scales->L : nullptr, b->L, b_scales->L, c->L, (int)a_dtype, (int)c_dtype, accumulate,
+                                           a_align_bytes, b_align_bytes, c_align_bytes, plan.get());
+    if (st == LC_OK) *out = plan.release();
+    return st;
+  } catch (...) {
+    return LC_ERR_INVALID_ARG;
+  }
+}
+lc_status_t lc_mx_gemm_plan_describe(const lc_mx_gemm_plan_t* plan, char* buf, size_t cap, size_t* needed) {
+  if (!plan) return LC_ERR_INVALID_ARG;
+  try {
+    return put_text(lc::describe(*plan), buf, cap, needed);
+  } catch (...) {
+    return LC_ERR_INVALID_ARG;
+  }
+}
+lc_status_t lc_mx_gemm_plan_execute(const lc_mx_gemm_plan_t* plan, const void* a, const void* a_scales, const void* b, const void* b_scales, void* c,
+                                    void* hip_stream) {
+  if (!plan) return LC_ERR_INVALID_ARG;
+  return lc::execute_mx_gemm_plan(*plan, a, a_scales, b, b_scales, c, hip_stream);
+}
+void lc_mx_gemm_plan_destroy(lc_mx_gemm_plan_t* plan) { delete plan; }
+int64_t lc_mx_gemm_plan_flops(const lc_mx_gemm_plan_t* plan) { return plan ? 2 * plan->M * plan->N * plan->K * plan->L : -1; }
+lc_status_t lc_mx_gemm(const void* a, const lc_layout_t* a_layout, const void* a_scales, const lc_layout_t* a_scales_layout, const void* b,
+                       const lc_layout_t* b_layout, const void* b_scales, const lc_layout_t* b_scales_layout, void* c,
+                       const lc_layout_t* c_layout, lc_dtype_t a_dtype, lc_dtype_t c_dtype, int accumulate, void* hip_stream) {
+  if (!a || !b || !b_scales || !c || !a_layout || !b_layout || !b_scales_layout || !c_layout || (a_scales == nullptr) != (a_scales_layout == nullptr))
+    return LC_ERR_INVALID_ARG;
+  try {
+    static thread_local std::string key;
+    key.clear();
+    for (const lc_layout_t* l : {a_layout, b_layout, b_scales_layout, c_layout}) lc::key_layout(&key, l->L);
+    lc::key_number(&key, a_scales_layout != nullptr);
+    if (a_scales_layout) lc::key_layout(&key, a_scales_layout->L);
+    for (int64_t v : {(int64_t)a_dtype, (int64_t)c_dtype, (int64_t)(accumulate != 0), (int64_t)pointer_alignment(a), (int64_t)pointer_alignment(b),
+                      (int64_t)pointer_alignment(c)})
+      lc::key_number(&key, v);
+    lc::key_tuning(&key);
+    static lc::PlanCache<lc_mx_gemm_plan> plans;
+    std::shared_ptr<const lc_mx_gemm_plan> plan = plans.find(key);
+    if (!plan) {
+      auto fresh = std::make_shared<lc_mx_gemm_plan>();
+      lc_status_t st = lc::make_mx_gemm_plan(a_layout->L, a_scales_layout ? &a_scales_layout->L : nullptr, b_layout->L, b_scales_layout->L, c_layout->L,
+                                             (int)a_dtype, (int)c_dtype, accumulate, pointer_alignment(a), pointer_alignment(b), pointer_alignment(c),
+                                             fresh.get());
+      if (st != LC_OK) return st;
+      plan = fresh;
+      plans.insert(key, plan);
+    }
+    return lc::execute_mx_gemm_plan(*plan, a, a_scales, b, b_scales, c, hip_stream);
+  } catch (...) {
+    return LC_ERR_INVALID_ARG;
+  }
+}
+lc_status_t lc_mx_gemm_plan_time(const lc_mx_gemm_plan_t* plan, const void* a, const void* a_scales, const void* b, const void* b_scales, void* c,
+                                 int warmup, int iters, void* hip_stream, float* ms_per_iter) {
+  if (!plan) return LC_ERR_INVALID_ARG;
+  return lc::time_mx_gemm_plan(*plan, a, a_scales, b, b_scales, c, warmup, iters, hip_stream, ms_per_iter);
 }
 
 // Checking device for tests: walks the plan's accesses on the host against the sizes of the buffers (see mx_plan.hpp).  Not in the

@@ -1,0 +1,219 @@
+// Device helpers of the GEMM kernels with microscaled 4-bit operands: the matrix instructions, scales, codes on their way to
+// 16 bits, and C.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "gemm_device.hpp"
+#include "kernarg.hpp"
+#include "layoutcopy.h"
+#include "mx_gemm_params.hpp"
+
+namespace lc {
+
+// What the products are made of: both operands codes, or the kernel's A codes and B 16-bit elements.
+enum MxMath : int { kMxCodes = 0, kMxBf16 = 1, kMxF16 = 2 };
+
+typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+// The matrix instruction of blocks of 32 codes takes a lane's block in four registers of the eight it has for 8-bit elements.
+__device__ __forceinline__ i32x8 mx_operand_of(u32x4 v) { return i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0}; }
+
+// acc += A(32 x 64) B(32 x 64): lane l holds block l / 32 of row l % 32; its scale is byte SEL of the lane's scale register.
+// (The fourth and fifth arguments name the operands' type: 4 = these codes.)
+template <int SEL>
+__device__ __forceinline__ f32x16 mx_mfma_32x32x64(u32x4 a, u32x4 b, f32x16 acc, uint32_t sa, uint32_t sb) {
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(mx_operand_of(a), mx_operand_of(b), acc, 4, 4, SEL, (int)sa, SEL, (int)sb);
+}
+// acc += A(16 x 128) B(16 x 128): lane l holds block l / 16 of row l % 16.
+__device__ __forceinline__ f32x4 mx_mfma_16x16x128(u32x4 a, u32x4 b, f32x4 acc, uint32_t sa, uint32_t sb) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx_operand_of(a), mx_operand_of(b), acc, 4, 4, 0, (int)sa, 0, (int)sb);
+}
+// acc += A(16 x 32) B(16 x 32) in 16 bits: lane l holds elements 8 (l / 16) .. + 7 of row l % 16.
+template <int MATH>
+__device__ __forceinline__ f32x4 mfma_16x16x32(u32x4 a, u32x4 b, f32x4 acc) {
+  if constexpr (MATH == kMxBf16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), acc, 0, 0, 0);
+}
+
+// The value a scale's byte stands for (2^-127 has no exponent bits of its own; 255 is NaN).
+__device__ __forceinline__ float mx_scale_value(uint32_t byte) {
+  const uint32_t bits = byte == 0u ? 0x00400000u : byte == 255u ? 0x7FC00000u : byte << 23;
+  return __builtin_bit_cast(float, bits);
+}
+// eight codes of a dword -> eight 16-bit elements, rounded to nearest (exact in bf16)
+template <int MATH>
+__device__ __forceinline__ u32x4 mx_expand(uint32_t codes, float scale) {
+  u32x4 v;
+  static_for<4>([&](auto i) {
+    if constexpr (MATH == kMxBf16) v[(int)i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, (int)decltype(i)::value));
+    else v[(int)i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, (int)decltype(i)::value));
+  });
+  return v;
+}
+
+// ---- C: sums are held in fp32 and rounded once, to nearest, where C has 16 bits ----
+__device__ __forceinline__ void mx_c_put(void* C, uint32_t off, float v, int32_t type, int32_t accumulate) {
+  if (type == LC_F32) {
+    float* p = static_cast<float*>(C) + off;
+    *p = accumulate ? *p + v : v;
+  } else if (type == LC_BF16) {
+    __bf16* p = static_cast<__bf16*>(C) + off;
+    *p = (__bf16)(accumulate ? (float)*p + v : v);
+  } else {
+    _Float16* p = static_cast<_Float16*>(C) + off;
+    *p = (_Float16)(accumulate ? (float)*p + v : v);
+  }
+}
+// four consecutive elements at an address aligned to them
+__device__ __forceinline__ void mx_c_put4(void* C, uint32_t off, f32x4 v, int32_t type, int32_t accumulate) {
+  typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+  typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+  if (type == LC_F32) {
+    f32x4* p = reinterpret_cast<f32x4*>(static_cast<float*>(C) + off);
+    *p = accumulate ? *p + v : v;
+  } else if (type == LC_BF16) {
+    bf16x4* p = reinterpret_cast<bf16x4*>(static_cast<__bf16*>(C) + off);
+    if (accumulate) v += __builtin_convertvector(*p, f32x4);
+    *p = __builtin_convertvector(v, bf16x4);
+  } else {
+    f16x4* p = reinterpret_cast<f16x4*>(static_cast<_Float16*>(C) + off);
+    if (accumulate) v += __builtin_convertvector(*p, f32x4);
+    *p = __builtin_convertvector(v, f16x4);
+  }
+}
+__device__ __forceinline__ void* mx_c_at(void* C, uint32_t off, int32_t type) { return static_cast<unsigned char*>(C) + (uint64_t)off * (type == LC_F32 ? 4u : 2u); }
+
+// The sums of a BM x BN tile, parked in LDS as gemm_sum_unit says, to C: consecutive lanes along the mode that C holds together.
+template <int BM, int BN, int LANES>
+__device__ __forceinline__ void mx_tile_to_c(const MxGemmParams& P, void* C, const unsigned char* lds, uint32_t m0, uint32_t n0, uint32_t tid) {
+  constexpr int N = BM * BN / 4 / LANES;
+  static_assert(BM * BN / 4 % LANES == 0, "whole units for every lane");
+  for (int j = 0; j < N; ++j) {
+    uint32_t m4, n;
+    gemm_sum_of(BM, BN, P.g.c_vec, tid + (uint32_t)j * LANES, &m4, &n);
+    const uint32_t m = m0 + 4u * m4;
+    if (m >= P.g.M || n0 + n >= P.g.N) continue;
+    const f32x4 v = *reinterpret_cast<const f32x4*>(lds + gemm_sum_unit(BM, BN, m4, n) * 16u);
+    const uint32_t n_off = gemm_mode_eval(P.g.c_n, n0 + n);
+    if (P.g.c_vec) {
+      mx_c_put4(C, gemm_mode_eval(P.g.c_m, m) + n_off, v, P.c_type, P.accumulate);
+    } else {
+      static_for<4>([&](auto e) {
+        if (m + (uint32_t)e < P.g.M) mx_c_put(C, gemm_mode_eval(P.g.c_m, m + (uint32_t)e) + n_off, v[(int)e], P.c_type, P.accumulate);
+      });
+    }
+  }
+}
+
+// ---- scales of fragments of 32 rows (32 x 32 x 64): a lane's blocks are 4 h .. 4 h + 3 of the k tile's eight, h = l / 32, so the
+// four k steps' scales are the bytes of one dword ----
+template <int FRAGS>
+struct MxScaleLoader {
+  const unsigned char* base;
+  int64_t off[FRAGS];        // of the lane's row
+  uint32_t blocks, h;
+  bool dwords;               // (uniform) the four scales are neighbours
+  uint32_t raw[FRAGS];
+
+  // (blocks: along k; rows past the operand's extent read its last row's)
+  __device__ __forceinline__ void init(const unsigned char* p, const GemmMode& rmode, uint32_t row0, uint32_t extent, uint32_t n_blocks, bool neighbours, uint32_t lane) {
+    base = p;
+    blocks = n_blocks;
+    dwords = neighbours;
+    h = lane >> 5;
+    static_for<FRAGS>([&](auto i) {
+      const uint32_t r = row0 + 32u * (uint32_t)i + (lane & 31u);
+      off[i] = (int64_t)gemm_mode_eval(rmode, r < extent ? r : extent - 1u);
+    });
+  }
+  // asks for k tile kt
+  __device__ __forceinline__ void fetch(const GemmMode& kmode, uint32_t kt) {
+    typedef uint32_t __attribute__((aligned(1))) u32_any;
+    const uint32_t first = kt * kMxTileBlocks + 4u * h;
+    if (dwords) {   // (four blocks that would reach past the last are read where they end with it)
+      const uint32_t from = first + 4u <= blocks ? first : blocks - 4u;
+      const uint32_t at = gemm_mode_eval(kmode, from);
+      static_for<FRAGS>([&](auto i) { raw[i] = *reinterpret_cast<const u32_any*>(base + off[i] + at); });
+    } else {
+      uint32_t at[4];
+      static_for<4>([&](auto e) {
+        const uint32_t b = first + (uint32_t)e;
+        at[(int)e] = gemm_mode_eval(kmode, b < blocks ? b : blocks - 1u);
+      });
+      static_for<FRAGS>([&](auto i) {
+        raw[i] = 0u;
+        static_for<4>([&](auto e) { raw[i] |= (uint32_t)base[off[i] + at[(int)e]] << (8 * e); });
+      });
+    }
+  }
+  // The scales of k tile kt, which was asked for last: blocks past the last one have the scale 2^-127 (their codes are zeros).
+  __device__ __forceinline__ void take(uint32_t kt, uint32_t (&out)[FRAGS]) const {
+    const uint32_t first = kt * kMxTileBlocks + 4u * h;
+    static_for<FRAGS>([&](auto i) { out[i] = raw[i]; });
+    if (kt * kMxTileBlocks + kMxTileBlocks > blocks) {   // (uniform)
+      const uint32_t from = first + 4u <= blocks ? first : blocks - 4u;
+      const uint32_t past = first >= blocks ? 4u : first + 4u > blocks ? first + 4u - blocks : 0u;   // of the lane's four blocks
+      const uint32_t moved = dwords ? first - from : 0u;
+      static_for<FRAGS>([&](auto i) {
+        uint32_t v = moved >= 4u ? 0u : out[i] >> (8u * moved);
+        if (past) v = past >= 4u ? 0u : v & (0xFFFFFFFFu >> (8u * past));
+        out[i] = v;
+      });
+    }
+  }
+};
+
+// ---- a tile of codes through registers into 16-bit elements in LDS ----
+// Blocks along k (BLOCKED 1): BR rows of 64 k in the arrangement of kLoadKDirect.  Lane t of 256 takes block t % 2 of rows t / 2 + 128 i.
+// Blocks along the rows (0): 64 k rows of BR elements in the arrangement of kLoadRDirect.  Lane t takes block t % (BR / 32) of k t / (BR / 32) + ..
+// K: elements along k; blocks (along k: at or past it) and k rows past K become zeros whatever their scales are.
+template <int MATH, int BR, int BLOCKED>
+struct MxTileLoader {
+  static constexpr int UNITS = BR * 2 / 256;   // blocks of a lane
+  static_assert(UNITS >= 1, "a block for every lane");
+  __amdgpu_buffer_rsrc_t codes, scales;
+  uint32_t off[UNITS], s_off[UNITS];   // 0xFFFFFFFF: no such row
+  uint32_t K, t;
+  u32x4 raw[UNITS];
+  uint32_t byte[UNITS];
+
+  __device__ __forceinline__ uint32_t row_of(uint32_t i) const { return BLOCKED ? (t >> 1) + 128u * i : 32u * (t % (BR / 32u)); }
+  __device__ __forceinline__ uint32_t k_of(uint32_t i) const { return BLOCKED ? 32u * (t & 1u) : t / (BR / 32u) + (256u / (BR / 32u)) * i; }
+  __device__ __forceinline__ void init(const unsigned char* p, const unsigned char* s, const MxGemmParams& P, uint32_t row0, uint32_t tid) {
+    codes = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(p), 0, 0xFFFFFFFFu, 0x00020000);
+    scales = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(s), 0, 0xFFFFFFFFu, 0x00020000);
+    K = P.g.K;
+    t = tid;
+    static_for<UNITS>([&](auto i) {
+      const uint32_t r = row0 + row_of((uint32_t)i);
+      // (blocks along the rows: words of four rows, whole blocks inside the operand)
+      off[i] = r < P.g.M ? 2u * gemm_mode_eval(P.g.a_r, BLOCKED ? r : r / 4u) : 0xFFFFFFFFu;
+      s_off[i] = r < P.g.M ? gemm_mode_eval(P.sa_r, BLOCKED ? r : r / kMxBlock) : 0xFFFFFFFFu;
+    });
+  }
+  __device__ __forceinline__ void fetch(const MxGemmParams& P, uint32_t kt) {
+    static_for<UNITS>([&](auto i) {
+      const uint32_t k = kt * kGemmBK + k_of((uint32_t)i);
+      const bool in = k < K && off[i] != 0xFFFFFFFFu;
+      const uint32_t at = in ? off[i] + 2u * gemm_mode_eval(P.g.a_k, BLOCKED ? k / 4u : k) : 0xFFFFFFFFu;
+      const uint32_t s_at = in ? s_off[i] + gemm_mode_eval(P.sa_k, BLOCKED ? k / kMxBlock : k) : 0xFFFFFFFFu;
+      raw[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(codes, (int)at, 0, 0));   // outside: zeros
+      byte[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(scales, (int)s_at, 0, 0) & 0xFFu;
+    });
+  }
+  // parks the k tile that was asked for last
+  __device__ __forceinline__ void park(unsigned char* tile) {
+    static_for<UNITS>([&](auto i) {
+      const float scale = mx_scale_value(byte[i]);
+      const uint32_t row = row_of((uint32_t)i), k = k_of((uint32_t)i);
+      static_for<4>([&](auto q) {
+        const uint32_t at = BLOCKED ? gemm_lds_offset(row, k / 8u + (uint32_t)q) : gemm_rdirect_lds_offset(BR, k, row + 8u * (uint32_t)q);
+        *reinterpret_cast<u32x4*>(tile + at) = mx_expand<MATH>(raw[i][(int)q], scale);
+      });
+    });
+  }
+};
+
+}  // namespace lc

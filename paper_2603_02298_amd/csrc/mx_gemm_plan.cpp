@@ -1,0 +1,246 @@
+#include "mx_gemm_plan.hpp"
+
+#include <algorithm>
+#include <cstdlib>
+
+#include "plan.hpp"
+
+namespace lc {
+
+namespace {
+
+int env_int(const char* name, int dflt) {
+  const char* v = std::getenv(name);
+  return (v && *v) ? std::atoi(v) : dflt;
+}
+
+lc_status_t fill_mode(const Modes& m, GemmMode* out) {
+  if (m.empty() || (int)m.size() > kGemmMaxLeaves) return LC_ERR_TOO_LARGE;
+  out->n = (int32_t)m.size();
+  for (const Mode& x : m)
+    if (x.extent >= (int64_t(1) << 31) || x.stride >= (int64_t(1) << 31)) return LC_ERR_TOO_LARGE;
+  for (int k = 0; k < kGemmMaxLeaves - 1; ++k) {
+    const bool reduced = k + 1 < (int)m.size();
+    out->div[k] = make_fastdiv(reduced ? (uint32_t)m[k].extent : 1u);
+    out->stride[k] = reduced ? (uint32_t)m[k].stride : 0u;
+  }
+  out->last_stride = (uint32_t)m.back().stride;
+  out->lead_stride = (uint32_t)m.front().stride;
+  return LC_OK;
+}
+
+// One operand as the kernels see it.
+struct Side {
+  Modes r, k, l;       // elements of 16 bits; codes: words of four
+  Modes s_r, s_k, s_l; // scales, bytes
+  bool dwords = false; // the scales of four neighbouring blocks are neighbours
+  int64_t rows = 0;    // of the caller's C
+  std::string text, s_text;
+};
+
+// A mode of codes in words of four: the blocked mode leads with consecutive codes.
+Modes in_words(const Modes& m, bool blocked) {
+  Modes w;
+  for (size_t i = 0; i < m.size(); ++i) w.push_back(blocked && i == 0 ? Mode{m[0].extent / 4, 1} : Mode{m[i].extent, m[i].extent > 1 ? m[i].stride / 4 : 0});
+  return coalesce_modes(w);
+}
+
+Modes batch_of(const Layout& L) { return L.rank() == 3 ? coalesce_modes(L.mode(2).leaves) : Modes{{1, 0}}; }
+std::string mode_text(const Modes& m) { return Layout::flat(m).str(); }
+
+lc_status_t side_of_codes(const Layout& codes, const Layout& scales, int blocked, Side* s) {
+  if (codes.rank() != scales.rank()) return LC_ERR_INVALID_ARG;
+  MxOperand op;
+  lc_status_t st = mx_operand(codes, scales, blocked, &op);
+  if (st != LC_OK) return st;
+  const Modes batch = batch_of(codes);
+  if (codes.rank() == 3) {
+    if (scales.mode(2).size() != codes.mode(2).size()) return LC_ERR_SIZE_MISMATCH;
+    for (const Mode& m : batch)
+      if (m.extent > 1 && m.stride % kMxBlock != 0) return LC_ERR_BLOCK_LAYOUT;
+  }
+  const int64_t lim = int64_t(1) << 31;
+  if ((codes.cosize() + 3) / 4 >= lim || scales.cosize() >= lim) return LC_ERR_TOO_LARGE;
+  s->r = in_words(coalesce_modes(codes.mode(0).leaves), blocked == 0);
+  s->k = in_words(coalesce_modes(codes.mode(1).leaves), blocked == 1);
+  s->l = in_words(batch, false);
+  s->s_r = op.s_r;
+  s->s_k = op.s_k;
+  s->s_l = batch_of(scales);
+  s->dwords = s->s_k[0].stride == 1 && (s->s_k.size() == 1 ? s->s_k[0].extent >= 4 : s->s_k[0].extent % 4 == 0);
+  s->text = mode_text(s->r) + " x " + mode_text(s->k);
+  s->s_text = mode_text(s->s_r) + " x " + mode_text(s->s_k);
+  return LC_OK;
+}
+
+bool leads_contiguous(const Modes& m, int64_t vec) { return m[0].stride == 1 && m[0].extent % vec == 0; }
+bool aligned(const Modes& m, int64_t vec, size_t from) {
+  for (size_t i = from; i < m.size(); ++i)
+    if (m[i].extent > 1 && m[i].stride % vec != 0) return false;
+  return true;
+}
+
+}  // namespace
+
+lc_status_t make_mx_gemm_plan(const Layout& A, const Layout* A_scales, const Layout& B, const Layout& B_scales, const Layout& C, int a_dtype, int c_dtype,
+                              int accumulate, unsigned a_align, unsigned b_align, unsigned c_align, lc_mx_gemm_plan* out) {
+  if (a_dtype != LC_MXFP4 && a_dtype != LC_BF16 && a_dtype != LC_F16) return LC_ERR_UNSUPPORTED_DTYPE;
+  if (c_dtype != LC_F32 && c_dtype != LC_BF16 && c_dtype != LC_F16) return LC_ERR_UNSUPPORTED_DTYPE;
+  const bool codes = a_dtype == LC_MXFP4;
+  if (codes != (A_scales != nullptr)) return LC_ERR_INVALID_ARG;
+  for (const Layout* L : {&A, &B, &B_scales, &C, A_scales}) {
+    if (!L) continue;
+    lc_status_t st = validate(*L);
+    if (st != LC_OK) return st;
+    if (L->is_leaf() || (L->rank() != 2 && L->rank() != 3) || L->rank() != A.rank()) return LC_ERR_INVALID_ARG;
+    if (L->has_negative_stride()) return LC_ERR_NEGATIVE_STRIDE;
+  }
+  for (unsigned align : {a_align, b_align, c_align})
+    if (align == 0 || (align & (align - 1)) != 0) return LC_ERR_INVALID_ARG;
+  const unsigned c_bytes = c_dtype == LC_F32 ? 4u : 2u;
+  if (b_align < kMxBlockBytes || a_align < (codes ? kMxBlockBytes : 2u) || c_align < c_bytes) return LC_ERR_MISALIGNED;
+  lc_mx_gemm_plan plan;
+  plan.a_dtype = a_dtype;
+  plan.c_dtype = c_dtype;
+  plan.accumulate = accumulate != 0;
+  plan.M = A.mode(0).size();
+  plan.N = C.mode(1).size();
+  plan.K = A.mode(1).size();
+  const int64_t M = plan.M, N = plan.N, K = plan.K, b_rows = B.mode(0).size(), b_k = B.mode(1).size();
+  if (C.mode(0).size() != M) return LC_ERR_SIZE_MISMATCH;
+  // B's blocks run along the mode that its scales count in blocks
+  if (B_scales.mode(0).size() == b_rows) plan.blocked = 1;
+  else if (B_scales.mode(1).size() == b_k && !codes) plan.blocked = 0;
+  else return LC_ERR_SIZE_MISMATCH;
+  // sizes: the blocked mode may be padded beyond what a 16-bit operand, or C, has
+  if (codes ? b_rows != N || b_k != K : plan.blocked ? b_rows != N || b_k < K : b_rows < N || b_k != K) return LC_ERR_SIZE_MISMATCH;
+  const bool batched = A.rank() == 3;
+  plan.L = batched ? A.mode(2).size() : 1;
+  if (batched && (B.mode(2).size() != plan.L || C.mode(2).size() != plan.L)) return LC_ERR_SIZE_MISMATCH;
+  const int64_t lim = int64_t(1) << 31;
+  if (M >= lim || N >= lim || K >= lim || plan.L > 65535 || C.cosize() >= lim || (!codes && A.cosize() >= lim)) return LC_ERR_TOO_LARGE;
+
+  Side a, b;
+  lc_status_t st = side_of_codes(B, B_scales, plan.blocked, &b);
+  if (st != LC_OK) return st;
+  if (codes) {
+    if ((st = side_of_codes(A, *A_scales, 1, &a)) != LC_OK) return st;
+  } else {
+    a.r = coalesce_modes(A.mode(0).leaves);
+    a.k = coalesce_modes(A.mode(1).leaves);
+    a.l = batch_of(A);
+    a.text = mode_text(a.r) + " x " + mode_text(a.k);
+  }
+  a.rows = M;
+  b.rows = N;
+  Modes c_m = coalesce_modes(C.mode(0).leaves), c_n = coalesce_modes(C.mode(1).leaves);
+  const Modes c_l = batch_of(C);
+  {
+    Modes all = c_m;
+    all.insert(all.end(), c_n.begin(), c_n.end());
+    all.insert(all.end(), c_l.begin(), c_l.end());
+    if (M * N * plan.L > 1 && !layout_is_injective(all, M * N * plan.L)) return LC_ERR_DST_ALIASES;
+  }
+  plan.a_text = a.text;
+  plan.b_text = b.text;
+  plan.sa_text = a.s_text;
+  plan.sb_text = b.s_text;
+  plan.c_text = mode_text(c_m) + " x " + mode_text(c_n);
+
+  // The kernel's A is the operand in codes; of two such, the one whose rows C holds together (its sums lie in fours along m).
+  auto c_vec_ok = [&](const Modes& lead, const Modes& other) {
+    return c_align % (4 * c_bytes) == 0 && leads_contiguous(lead, 4) && aligned(lead, 4, 1) && aligned(other, 4, 0) && aligned(c_l, 4, 0);
+  };
+  plan.exchanged = !codes || (c_m[0].stride != 1 && c_n[0].stride == 1);
+  if (plan.exchanged) {
+    std::swap(a, b);
+    std::swap(c_m, c_n);
+  }
+  MxGemmParams& P = plan.params;
+  GemmParams& G = P.g;
+  const Modes unit = {{1, 0}};
+  const bool b_scaled = codes;
+  if ((st = fill_mode(a.r, &G.a_r)) != LC_OK || (st = fill_mode(a.k, &G.a_k)) != LC_OK || (st = fill_mode(b.r, &G.b_r)) != LC_OK ||
+      (st = fill_mode(b.k, &G.b_k)) != LC_OK || (st = fill_mode(c_m, &G.c_m)) != LC_OK || (st = fill_mode(c_n, &G.c_n)) != LC_OK ||
+      (st = fill_mode(a.l, &G.a_l)) != LC_OK || (st = fill_mode(b.l, &G.b_l)) != LC_OK || (st = fill_mode(c_l, &G.c_l)) != LC_OK ||
+      (st = fill_mode(a.s_r, &P.sa_r)) != LC_OK || (st = fill_mode(a.s_k, &P.sa_k)) != LC_OK || (st = fill_mode(a.s_l, &P.sa_l)) != LC_OK ||
+      (st = fill_mode(b_scaled ? b.s_r : unit, &P.sb_r)) != LC_OK || (st = fill_mode(b_scaled ? b.s_k : unit, &P.sb_k)) != LC_OK ||
+      (st = fill_mode(b_scaled ? b.s_l : unit, &P.sb_l)) != LC_OK)
+    return st;
+  G.M = (uint32_t)a.rows;
+  G.N = (uint32_t)b.rows;
+  G.K = (uint32_t)(codes ? K / 4 : K);
+  G.L = (uint32_t)plan.L;
+  G.k_tiles = (G.K + kGemmBK - 1) / kGemmBK;
+  G.c_vec = c_vec_ok(c_m, c_n) ? 1 : 0;
+  G.group_m = 8;
+  P.blocks = (uint32_t)((K + kMxBlock - 1) / kMxBlock);
+  P.c_type = c_dtype;
+  P.accumulate = accumulate != 0;
+  P.a_dwords = a.dwords;
+  P.b_dwords = b.dwords;
+  plan.c_align = G.c_vec ? 4 * c_bytes : c_bytes;
+
+  // How the kernel's B is brought in.  Codes: straight into LDS, k tiles inside the k mode's first leaf or vector by vector.  16-bit elements: k vectors
+  // straight into LDS, k vectors at any alignment, or gathered.
+  auto whole_tiles = [](const Modes& k) { return k.size() == 1 || k[0].extent % kGemmBK == 0; };
+  unsigned x_align = 2;   // of the 16-bit operand's pointer
+  if (codes) {
+    plan.b_load = whole_tiles(a.k) && whole_tiles(b.k) && (G.K % kGemmBK == 0 || (a.k.size() == 1 && b.k.size() == 1)) ? kLoadKDirect : kLoadKLeaves;
+  } else if (a_align % 16 == 0 && b.k[0].stride == 1 && b.k.size() == 1 && K % 8 == 0 && aligned(b.r, 8, 0) && aligned(b.l, 8, 0)) {
+    plan.b_load = kLoadKDirect;
+    x_align = 16;
+  } else if (b.k.size() == 1 && b.k[0].stride == 1 && K >= 8) {
+    plan.b_load = kLoadKAny;
+  } else {
+    plan.b_load = kLoadKGather;
+    G.b_direct = 4;   // element by element, lanes along the rows
+  }
+  plan.a_align = codes ? kMxBlockBytes : x_align;
+  plan.b_align = kMxBlockBytes;
+
+  // Tiles.
+  auto tiles_of = [&](int64_t tm, int64_t tn) { return (a.rows + tm - 1) / tm * ((b.rows + tn - 1) / tn) * plan.L; };
+  auto take = [&](MxGemmKernel kernel, int tm, int tn, int waves) {
+    plan.kernel = kernel;
+    plan.tile_m = tm;
+    plan.tile_n = tn;
+    plan.waves = waves;
+  };
+  const bool can_direct = codes || (plan.blocked == 1 && plan.b_load == kLoadKDirect);
+  const int t_env = env_int("LC_TUNE_MX_TILE", 0);
+  if (t_env == 16 && can_direct) take(kMxDirect, 16, 16, 8);
+  else if (t_env == 3216 && can_direct) take(kMxDirect, 32, 16, 8);
+  else if (t_env == 32 && can_direct) take(kMxDirect, 32, 32, 8);
+  else if (t_env == 64 && codes) take(kMxStream, 64, 64, 4);
+  else if (t_env == 12864) take(kMxStream, 128, 64, 4);
+  else if (t_env == 128) take(kMxStream, 128, 128, 4);
+  else if (can_direct && b.rows <= 16) take(kMxDirect, tiles_of(32, 16) >= 256 ? 32 : 16, 16, 8);
+  else if (can_direct && tiles_of(32, 32) <= 512) take(kMxDirect, 32, 32, 8);
+  else if (codes && tiles_of(64, 64) <= 512) take(kMxStream, 64, 64, 4);
+  else if (tiles_of(128, 128) <= 256) take(kMxStream, 128, 64, 4);
+  else take(kMxStream, 128, 128, 4);
+  plan.lds_bytes = plan.kernel == kMxStream ? 2u * (unsigned)(plan.tile_m + plan.tile_n) * 128u : 0u;
+  G.tiles_m = (uint32_t)((a.rows + plan.tile_m - 1) / plan.tile_m);
+  G.tiles_n = (uint32_t)((b.rows + plan.tile_n - 1) / plan.tile_n);
+  // a grid counts its lanes in 32 bits
+  if ((uint64_t)tiles_of(plan.tile_m, plan.tile_n) * 64u * (unsigned)plan.waves > 0xFFFFFFFFull) return LC_ERR_TOO_LARGE;
+  *out = plan;
+  return LC_OK;
+}
+
+std::string describe(const lc_mx_gemm_plan& plan) {
+  static const char* kernels[] = {"direct", "stream", "ring"};
+  auto type = [](int t) { return t == LC_F32 ? "f32" : t == LC_BF16 ? "bf16" : t == LC_F16 ? "f16" : "mxfp4"; };
+  std::string s = std::string("class=mx-gemm kernel=") + kernels[plan.kernel] + " a=" + type(plan.a_dtype) + " b=mxfp4 c=" + type(plan.c_dtype);
+  s += plan.accumulate ? " accumulate=1" : " accumulate=0";
+  s += " M=" + std::to_string(plan.M) + " N=" + std::to_string(plan.N) + " K=" + std::to_string(plan.K) + " L=" + std::to_string(plan.L);
+  s += " b_blocks_along=" + std::string(plan.blocked ? "k" : "rows") + " exchanged=" + std::to_string((int)plan.exchanged);
+  s += " tile=" + std::to_string(plan.tile_m) + "x" + std::to_string(plan.tile_n) + " waves=" + std::to_string(plan.waves);
+  s += " tiles=" + std::to_string(plan.params.g.tiles_m) + "x" + std::to_string(plan.params.g.tiles_n) + " k_tiles=" + std::to_string(plan.params.g.k_tiles);
+  const char* load = plan.b_load == kLoadKDirect ? "k-vectors" : plan.b_load == kLoadKLeaves ? "k-vectors-over-leaves" : plan.b_load == kLoadKAny ? "unaligned-k-vectors" : "elements";
+  s += std::string(" load=") + load + " c_vec=" + std::to_string(plan.params.g.c_vec) + " lds_bytes=" + std::to_string(plan.lds_bytes);
+  return s + " A=[" + plan.a_text + "] A_scales=[" + plan.sa_text + "] B=[" + plan.b_text + "] B_scales=[" + plan.sb_text + "] C=[" + plan.c_text + "]";
+}
+
+}  // namespace lc

@@ -159,3 +159,85 @@ def test_every_access_lies_inside_and_every_byte_is_written_once(R, K, dtype, or
         q.debug_walk_on_host(before, behind, Q.cosize // 2, S.cosize - 1)
     with pytest.raises(lc.LayoutCopyError):
         d.debug_walk_on_host(before, behind - 1, Q.cosize // 2, S.cosize)
+
+
+# ---- products ----
+def _gemm(a, a_s, b, b_s, c, a_dtype="mxfp4", c_dtype="f32", **more):
+    return lc.MxGemmPlan(a, a_s, b, b_s, c, a_dtype, c_dtype, **more)
+
+
+@pytest.mark.parametrize("a,a_s,b,b_s,c,a_dtype,c_dtype,status", [
+    ("(4,96):(96,1)", "(4,3):(3,1)", "(5,96):(96,1)", "(5,3):(3,1)", "(4,6):(6,1)", "mxfp4", "f32", "SIZE_MISMATCH"),       # N
+    ("(4,96):(96,1)", "(4,3):(3,1)", "(5,64):(64,1)", "(5,2):(2,1)", "(4,5):(5,1)", "mxfp4", "f32", "SIZE_MISMATCH"),       # K
+    ("(4,96):(96,1)", "(4,3):(3,1)", "(5,96):(96,1)", "(5,3):(3,1)", "(3,5):(5,1)", "mxfp4", "f32", "SIZE_MISMATCH"),       # M
+    ("(4,96):(96,1)", "(4,2):(2,1)", "(5,96):(96,1)", "(5,3):(3,1)", "(4,5):(5,1)", "mxfp4", "f32", "SIZE_MISMATCH"),       # A's scales
+    ("(4,96):(96,1)", "(4,3):(3,1)", "(5,96):(96,1)", "(4,3):(3,1)", "(4,5):(5,1)", "mxfp4", "f32", "SIZE_MISMATCH"),       # B's scales
+    ("(4,96):(96,1)", "(4,3):(3,1)", "(32,96):(1,32)", "(1,96):(1,1)", "(4,32):(32,1)", "mxfp4", "f32", "SIZE_MISMATCH"),   # codes by codes blocked along the rows
+    ("(4,96):(96,1)", None, "(5,96):(96,1)", "(5,3):(3,1)", "(4,5):(5,1)", "mxfp4", "f32", "INVALID_ARG"),                  # no scales
+    ("(4,96):(96,1)", "(4,3):(3,1)", "(5,96):(96,1)", "(5,3):(3,1)", "(4,5):(5,1)", "bf16", "f32", "INVALID_ARG"),          # scales for 16 bits
+    ("(4,96):(96,1)", None, "(5,96):(96,1)", "(5,3):(3,1)", "(4,5):(5,1)", "f32", "f32", "UNSUPPORTED_DTYPE"),
+    ("(4,96):(96,1)", None, "(5,96):(96,1)", "(5,3):(3,1)", "(4,5):(5,1)", "bf16", "b16", "UNSUPPORTED_DTYPE"),
+    ("(4,97):(97,1)", None, "(5,96):(96,1)", "(5,3):(3,1)", "(4,5):(5,1)", "bf16", "f32", "SIZE_MISMATCH"),                 # K beyond B's
+    ("(4,97):(97,1)", None, "(96,97):(1,96)", "(3,97):(1,3)", "(4,97):(97,1)", "bf16", "f32", "SIZE_MISMATCH"),             # N beyond B's
+    ("(4,96):(96,1)", None, "(96,97):(1,96)", "(3,97):(1,3)", "(4,90):(90,1)", "bf16", "f32", "SIZE_MISMATCH"),             # K differs
+    ("(4,96):(96,1)", None, "(5,96):(96,1)", "(5,3):(3,1)", "(4,5):(0,1)", "bf16", "f32", "DST_ALIASES"),
+    ("(4,96):(96,1)", None, "(5,96):(96,1)", "(5,3):(3,1)", "(4,5):(4,1)", "bf16", "f32", "DST_ALIASES"),
+    ("(4,96):(-96,1)", None, "(5,96):(96,1)", "(5,3):(3,1)", "(4,5):(5,1)", "bf16", "f32", "NEGATIVE_STRIDE"),
+    ("(4,96):(96,1)", None, "(5,96):(96,1)", "(5,3):(3,1)", "(4,5):(5,-1)", "bf16", "f32", "NEGATIVE_STRIDE"),
+    ("(4,96):(96,1)", None, "(5,96):(98,1)", "(5,3):(3,1)", "(4,5):(5,1)", "bf16", "f32", "BLOCK_LAYOUT"),
+    ("(4,96):(96,1)", None, "(5,96):(1,5)", "(5,3):(3,1)", "(4,5):(5,1)", "bf16", "f32", "BLOCK_LAYOUT"),
+    ("(4,96,2):(96,1,384)", None, "(5,96,2):(96,1,500)", "(5,3,2):(3,1,15)", "(4,5,2):(5,1,20)", "bf16", "f32", "BLOCK_LAYOUT"),   # a batch off the grid
+    ("(4,96,2):(96,1,384)", None, "(5,96,3):(96,1,480)", "(5,3,3):(3,1,15)", "(4,5,2):(5,1,20)", "bf16", "f32", "SIZE_MISMATCH"),
+    ("(4,96,2):(96,1,384)", None, "(5,96,2):(96,1,480)", "(5,3,1):(3,1,15)", "(4,5,2):(5,1,20)", "bf16", "f32", "SIZE_MISMATCH"),
+    ("(4,96,2):(96,1,384)", None, "(5,96,2):(96,1,480)", "(5,3,2):(3,1,15)", "(4,5,2):(5,1,10)", "bf16", "f32", "DST_ALIASES"),
+    ("(4,96):(96,1)", None, "(5,96,2):(96,1,480)", "(5,3,2):(3,1,15)", "(4,5):(5,1)", "bf16", "f32", "INVALID_ARG"),
+    ("(4,96,2):(96,1,384)", None, "(5,96,2):(96,1,480)", "(5,3):(3,1)", "(4,5,2):(5,1,20)", "bf16", "f32", "INVALID_ARG"),
+    ("384:1", None, "(5,96):(96,1)", "(5,3):(3,1)", "(4,5):(5,1)", "bf16", "f32", "INVALID_ARG"),
+    ("(4,96):(1073741824,1)", None, "(5,96):(96,1)", "(5,3):(3,1)", "(4,5):(5,1)", "bf16", "f32", "TOO_LARGE"),
+    ("(4,96):(96,1)", None, "(5,96):(4294967296,1)", "(5,3):(3,1)", "(4,5):(5,1)", "bf16", "f32", "TOO_LARGE"),
+])
+def test_gemm_refusals(a, a_s, b, b_s, c, a_dtype, c_dtype, status):
+    with pytest.raises(lc.LayoutCopyError) as e:
+        _gemm(a, a_s, b, b_s, c, a_dtype, c_dtype)
+    assert e.value.status_name == status
+
+
+def test_gemm_alignments_and_null_arguments():
+    for more, status in (({"b_align": 8}, "MISALIGNED"), ({"a_align": 1}, "MISALIGNED"), ({"c_align": 2}, "MISALIGNED"), ({"a_align": 24}, "INVALID_ARG"),
+                         ({"a_align": 0}, "INVALID_ARG")):
+        with pytest.raises(lc.LayoutCopyError) as e:
+            _gemm("(4,96):(96,1)", None, "(5,96):(96,1)", "(5,3):(3,1)", "(4,5):(5,1)", "bf16", "f32", **more)
+        assert e.value.status_name == status
+    with pytest.raises(lc.LayoutCopyError) as e:
+        _gemm("(4,96):(96,1)", "(4,3):(3,1)", "(5,96):(96,1)", "(5,3):(3,1)", "(4,5):(5,1)", a_align=8)
+    assert e.value.status_name == "MISALIGNED"
+    L = lc.lib()
+    mixed = _gemm("(4,96):(96,1)", None, "(8,96):(96,1)", "(8,3):(3,1)", "(4,8):(8,1)", "bf16", "f32")
+    codes = _gemm("(4,96):(96,1)", "(4,3):(3,1)", "(8,96):(96,1)", "(8,3):(3,1)", "(4,8):(8,1)")
+    assert mixed.flops == codes.flops == 2 * 4 * 8 * 96
+    # refused before anything is launched: addresses that are never touched
+    assert L.lc_mx_gemm_plan_execute(None, 256, None, 256, 256, 256, None) == 1
+    assert L.lc_mx_gemm_plan_execute(mixed._h, 256, 256, 256, 256, 256, None) == 1   # scales for 16-bit elements
+    assert L.lc_mx_gemm_plan_execute(codes._h, 256, None, 256, 256, 256, None) == 1
+    assert L.lc_mx_gemm_plan_execute(mixed._h, 256, None, 256, 256, None, None) == 1
+    assert L.lc_mx_gemm_plan_execute(mixed._h, 258, None, 256, 256, 256, None) == 15   # planned for 16-byte vectors
+    assert L.lc_mx_gemm_plan_execute(mixed._h, 256, None, 264, 256, 256, None) == 15
+    assert L.lc_mx_gemm_plan_execute(mixed._h, 256, None, 256, 256, 260, None) == 15
+    assert L.lc_mx_gemm_plan_execute(codes._h, 264, 256, 256, 256, 256, None) == 15
+    assert L.lc_mx_gemm_plan_flops(None) == -1 and L.lc_mx_gemm_plan_describe(None, None, 0, None) == 1
+    ms = ctypes.c_float()
+    assert L.lc_mx_gemm_plan_time(mixed._h, 256, None, 256, 256, 256, 0, 0, None, ctypes.byref(ms)) == 1
+    a, b, s, c = (lc.Layout(t) for t in ("(4,96):(96,1)", "(8,96):(96,1)", "(8,3):(3,1)", "(4,8):(8,1)"))
+    assert L.lc_mx_gemm(256, a._h, None, None, 256, b._h, 256, s._h, None, c._h, 2, 0, 0, None) == 1
+    assert L.lc_mx_gemm(256, a._h, 256, None, 256, b._h, 256, s._h, 256, c._h, 2, 0, 0, None) == 1
+    assert L.lc_mx_gemm(256, a._h, None, None, 264, b._h, 256, s._h, 256, c._h, 2, 0, 0, None) == 15
+
+
+@pytest.mark.parametrize("a,a_dtype,load", [
+    ("(40,320):(320,1)", "bf16", "load=k-vectors "), ("(40,317):(320,1)", "bf16", "load=unaligned-k-vectors"), ("(40,320):(321,1)", "f16", "load=unaligned-k-vectors"),
+    ("(40,320):(1,40)", "bf16", "load=elements"), ("(40,(8,40)):(8,(1,320))", "bf16", "load=elements"), ("(40,7):(7,1)", "bf16", "load=elements")])
+def test_gemm_loads(a, a_dtype, load):
+    k = lc.Layout(a).size // 40
+    p = (k + 31) // 32 * 32
+    codes, scales = _rows(50, p)
+    assert load in _gemm(a, None, codes, scales, "(40,50):(50,1)", a_dtype).describe()
