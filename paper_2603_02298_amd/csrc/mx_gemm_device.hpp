@@ -54,57 +54,79 @@ __device__ __forceinline__ u32x4 mx_expand(uint32_t codes, float scale) {
 }
 
 // ---- C: sums are held in fp32 and rounded once, to nearest, where C has 16 bits ----
-__device__ __forceinline__ void mx_c_put(void* C, uint32_t off, float v, int32_t type, int32_t accumulate) {
-  if (type == LC_F32) {
-    float* p = static_cast<float*>(C) + off;
-    *p = accumulate ? *p + v : v;
-  } else if (type == LC_BF16) {
-    __bf16* p = static_cast<__bf16*>(C) + off;
-    *p = (__bf16)(accumulate ? (float)*p + v : v);
-  } else {
-    _Float16* p = static_cast<_Float16*>(C) + off;
-    *p = (_Float16)(accumulate ? (float)*p + v : v);
-  }
-}
-// four consecutive elements at an address aligned to them
-__device__ __forceinline__ void mx_c_put4(void* C, uint32_t off, f32x4 v, int32_t type, int32_t accumulate) {
-  typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-  typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-  if (type == LC_F32) {
-    f32x4* p = reinterpret_cast<f32x4*>(static_cast<float*>(C) + off);
-    *p = accumulate ? *p + v : v;
-  } else if (type == LC_BF16) {
-    bf16x4* p = reinterpret_cast<bf16x4*>(static_cast<__bf16*>(C) + off);
-    if (accumulate) v += __builtin_convertvector(*p, f32x4);
-    *p = __builtin_convertvector(v, bf16x4);
-  } else {
-    f16x4* p = reinterpret_cast<f16x4*>(static_cast<_Float16*>(C) + off);
-    if (accumulate) v += __builtin_convertvector(*p, f32x4);
-    *p = __builtin_convertvector(v, f16x4);
-  }
-}
 __device__ __forceinline__ void* mx_c_at(void* C, uint32_t off, int32_t type) { return static_cast<unsigned char*>(C) + (uint64_t)off * (type == LC_F32 ? 4u : 2u); }
 
-// The sums of a BM x BN tile, parked in LDS as gemm_sum_unit says, to C: consecutive lanes along the mode that C holds together.
-template <int BM, int BN, int LANES>
-__device__ __forceinline__ void mx_tile_to_c(const MxGemmParams& P, void* C, const unsigned char* lds, uint32_t m0, uint32_t n0, uint32_t tid) {
-  constexpr int N = BM * BN / 4 / LANES;
-  static_assert(BM * BN / 4 % LANES == 0, "whole units for every lane");
-  for (int j = 0; j < N; ++j) {
-    uint32_t m4, n;
-    gemm_sum_of(BM, BN, P.g.c_vec, tid + (uint32_t)j * LANES, &m4, &n);
-    const uint32_t m = m0 + 4u * m4;
-    if (m >= P.g.M || n0 + n >= P.g.N) continue;
-    const f32x4 v = *reinterpret_cast<const f32x4*>(lds + gemm_sum_unit(BM, BN, m4, n) * 16u);
-    const uint32_t n_off = gemm_mode_eval(P.g.c_n, n0 + n);
-    if (P.g.c_vec) {
-      mx_c_put4(C, gemm_mode_eval(P.g.c_m, m) + n_off, v, P.c_type, P.accumulate);
+template <int TYPE>
+using mx_c_elem = std::conditional_t<TYPE == LC_F32, float, std::conditional_t<TYPE == LC_BF16, __bf16, _Float16>>;
+
+// An offset along one of C's modes: a multiplication where the mode has one leaf.
+__device__ __forceinline__ uint32_t mx_c_eval(const GemmMode& mode, bool one_leaf, uint32_t i) { return one_leaf ? i * mode.last_stride : gemm_mode_eval(mode, i); }
+
+// The sums of a BM x BN tile, parked in LDS as gemm_sum_unit says, to C by LANES lanes: consecutive lanes along the mode that C holds together.
+// A lane stays in its row group (column), so it evaluates one of C's modes once; eight units are on their way at a time.
+template <int BM, int BN, int LANES, int TYPE, bool ADD, bool VEC>
+__device__ __forceinline__ void mx_tile_to_c_as(const MxGemmParams& P, void* C, const unsigned char* lds, uint32_t m0, uint32_t n0, uint32_t tid) {
+  using T = mx_c_elem<TYPE>;
+  typedef T Tx4 __attribute__((ext_vector_type(4)));
+  constexpr int N = BM * BN / 4 / LANES, U = N < 8 ? N : 8;
+  constexpr uint32_t ALONG = VEC ? BM / 4 : BN, STEP = LANES / ALONG;   // lanes along the contiguous mode; how far the other one moves per unit
+  static_assert(BM * BN / 4 % LANES == 0 && LANES % ALONG == 0 && N % U == 0, "whole units for every lane");
+  T* c = static_cast<T*>(C);
+  const uint32_t fast = tid % ALONG, slow = tid / ALONG;
+  if (VEC ? m0 + 4u * fast >= P.g.M : n0 + fast >= P.g.N) return;
+  const bool one_leaf = VEC ? P.g.c_n.n == 1 : P.g.c_m.n == 1;
+  c += VEC ? gemm_mode_eval(P.g.c_m, m0 + 4u * fast) : gemm_mode_eval(P.g.c_n, n0 + fast);
+  for (int first = 0; first < N; first += U) {
+    f32x4 v[U];
+    static_for<U>([&](auto u) {
+      const uint32_t at = slow + (uint32_t)(first + u) * STEP;
+      v[u] = *reinterpret_cast<const f32x4*>(lds + (VEC ? gemm_sum_unit(BM, BN, fast, at) : gemm_sum_unit(BM, BN, at, fast)) * 16u);
+    });
+    if constexpr (VEC) {
+      uint32_t off[U];
+      Tx4 old[U];
+      static_for<U>([&](auto u) {
+        const uint32_t n = n0 + slow + (uint32_t)(first + u) * STEP;
+        off[u] = mx_c_eval(P.g.c_n, one_leaf, n < P.g.N ? n : P.g.N - 1u);
+        if constexpr (ADD) old[u] = *reinterpret_cast<const Tx4*>(c + off[u]);
+      });
+      static_for<U>([&](auto u) {
+        if constexpr (ADD) v[u] += __builtin_convertvector(old[u], f32x4);
+        if (n0 + slow + (uint32_t)(first + u) * STEP < P.g.N) *reinterpret_cast<Tx4*>(c + off[u]) = __builtin_convertvector(v[u], Tx4);
+      });
     } else {
-      static_for<4>([&](auto e) {
-        if (m + (uint32_t)e < P.g.M) mx_c_put(C, gemm_mode_eval(P.g.c_m, m + (uint32_t)e) + n_off, v[(int)e], P.c_type, P.accumulate);
+      static_for<U>([&](auto u) {
+        const uint32_t m = m0 + 4u * (slow + (uint32_t)(first + u) * STEP);
+        uint32_t off[4];
+        float old[4];
+        static_for<4>([&](auto e) {
+          off[(int)e] = mx_c_eval(P.g.c_m, one_leaf, m + (uint32_t)e < P.g.M ? m + (uint32_t)e : P.g.M - 1u);
+          old[(int)e] = ADD ? (float)c[off[(int)e]] : 0.f;
+        });
+        static_for<4>([&](auto e) {
+          if (m + (uint32_t)e < P.g.M) c[off[(int)e]] = (T)(ADD ? old[(int)e] + v[u][(int)e] : v[u][(int)e]);
+        });
       });
     }
   }
+}
+// f(std::integral_constant<int, type>, std::bool_constant<accumulate>) for the plan's C
+template <typename F>
+__device__ __forceinline__ void mx_c_dispatch(const MxGemmParams& P, F&& f) {
+  auto typed = [&](auto add) {
+    if (P.c_type == LC_F32) f(std::integral_constant<int, LC_F32>{}, add);
+    else if (P.c_type == LC_BF16) f(std::integral_constant<int, LC_BF16>{}, add);
+    else f(std::integral_constant<int, LC_F16>{}, add);
+  };
+  if (P.accumulate) typed(std::true_type{});
+  else typed(std::false_type{});
+}
+template <int BM, int BN, int LANES>
+__device__ __forceinline__ void mx_tile_to_c(const MxGemmParams& P, void* C, const unsigned char* lds, uint32_t m0, uint32_t n0, uint32_t tid) {
+  mx_c_dispatch(P, [&](auto type, auto add) {
+    if (P.g.c_vec) mx_tile_to_c_as<BM, BN, LANES, decltype(type)::value, decltype(add)::value, true>(P, C, lds, m0, n0, tid);
+    else mx_tile_to_c_as<BM, BN, LANES, decltype(type)::value, decltype(add)::value, false>(P, C, lds, m0, n0, tid);
+  });
 }
 
 // ---- scales of fragments of 32 rows (32 x 32 x 64): a lane's blocks are 4 h .. 4 h + 3 of the k tile's eight, h = l / 32, so the
@@ -151,17 +173,11 @@ struct MxScaleLoader {
   // The scales of k tile kt, which was asked for last: blocks past the last one have the scale 2^-127 (their codes are zeros).
   __device__ __forceinline__ void take(uint32_t kt, uint32_t (&out)[FRAGS]) const {
     const uint32_t first = kt * kMxTileBlocks + 4u * h;
-    static_for<FRAGS>([&](auto i) { out[i] = raw[i]; });
-    if (kt * kMxTileBlocks + kMxTileBlocks > blocks) {   // (uniform)
-      const uint32_t from = first + 4u <= blocks ? first : blocks - 4u;
-      const uint32_t past = first >= blocks ? 4u : first + 4u > blocks ? first + 4u - blocks : 0u;   // of the lane's four blocks
-      const uint32_t moved = dwords ? first - from : 0u;
-      static_for<FRAGS>([&](auto i) {
-        uint32_t v = moved >= 4u ? 0u : out[i] >> (8u * moved);
-        if (past) v = past >= 4u ? 0u : v & (0xFFFFFFFFu >> (8u * past));
-        out[i] = v;
-      });
-    }
+    // (no branch: the loops around it stay one block of instructions)
+    const uint32_t past = first >= blocks ? 4u : first + 4u > blocks ? first + 4u - blocks : 0u;   // of the lane's four blocks
+    const uint32_t moved = dwords && first + 4u > blocks ? 8u * (first + 4u - blocks) : 0u;        // (32 bits and more: all of them are past the last)
+    const uint32_t mask = past >= 4u ? 0u : 0xFFFFFFFFu >> (8u * past);
+    static_for<FRAGS>([&](auto i) { out[i] = (raw[i] >> (moved & 31u)) & mask; });
   }
 };
 

@@ -208,6 +208,7 @@ lc_status_t make_mx_gemm_plan(const Layout& A, const Layout* A_scales, const Lay
     plan.waves = waves;
   };
   const bool can_direct = codes || (plan.blocked == 1 && plan.b_load == kLoadKDirect);
+  const bool can_ring = codes && plan.b_load == kLoadKDirect && a.dwords && b.dwords;
   const int t_env = env_int("LC_TUNE_MX_TILE", 0);
   if (t_env == 16 && can_direct) take(kMxDirect, 16, 16, 8);
   else if (t_env == 3216 && can_direct) take(kMxDirect, 32, 16, 8);
@@ -215,12 +216,14 @@ lc_status_t make_mx_gemm_plan(const Layout& A, const Layout* A_scales, const Lay
   else if (t_env == 64 && codes) take(kMxStream, 64, 64, 4);
   else if (t_env == 12864) take(kMxStream, 128, 64, 4);
   else if (t_env == 128) take(kMxStream, 128, 128, 4);
+  else if (t_env == 256 && can_ring) take(kMxRing, 256, 256, 4);
   else if (can_direct && b.rows <= 16) take(kMxDirect, tiles_of(32, 16) >= 256 ? 32 : 16, 16, 8);
   else if (can_direct && tiles_of(32, 32) <= 512) take(kMxDirect, 32, 32, 8);
   else if (codes && tiles_of(64, 64) <= 512) take(kMxStream, 64, 64, 4);
+  else if (can_ring && tiles_of(256, 256) >= 128) take(kMxRing, 256, 256, 4);
   else if (tiles_of(128, 128) <= 256) take(kMxStream, 128, 64, 4);
   else take(kMxStream, 128, 128, 4);
-  plan.lds_bytes = plan.kernel == kMxStream ? 2u * (unsigned)(plan.tile_m + plan.tile_n) * 128u : 0u;
+  plan.lds_bytes = plan.kernel == kMxStream ? 2u * (unsigned)(plan.tile_m + plan.tile_n) * 128u : plan.kernel == kMxRing ? 5u * 256u * 128u : 0u;
   G.tiles_m = (uint32_t)((a.rows + plan.tile_m - 1) / plan.tile_m);
   G.tiles_n = (uint32_t)((b.rows + plan.tile_n - 1) / plan.tile_n);
   // a grid counts its lanes in 32 bits

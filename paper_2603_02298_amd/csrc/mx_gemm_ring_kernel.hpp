@@ -1,0 +1,193 @@
+// Device code of the ring kernel of the GEMM with two operands in microscaled 4-bit codes: 256 x 256 tiles of C for problems that have enough of them.
+//
+// Four wavefronts own a tile, wavefront (wm, wn) a quarter of 128 x 128 as 4 x 4 fragments of 32 x 32.  The operand tiles of a k tile (256
+// codes, rows of 128 bytes) go straight into a ring of five slots of LDS of one operand tile each, in the order A(0), B(0), A(1), B(1), A(2), ..: the
+// schedule of the generic GEMM's ring of 16-bit tiles, whose bytes per matrix instruction and clocks per instruction these codes share (a
+// 32 x 32 x 64 instruction of codes reads what a 32 x 32 x 16 one of 16-bit elements reads, and takes as long).
+// A lane takes four neighbouring blocks of a row per k tile (4 h .. 4 h + 3, h the half of the wavefront it is in), one per k step, so its
+// four scales are one dword, fetched into registers a k tile ahead: ahead of the loads of A(t + 2), so that the wait for everything older than
+// those covers them.
+// The sums pass through LDS, a column of fragments of a wavefront at a time and each wavefront in a place of its own, so that C is written in
+// whole lines.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <atomic>
+
+#include "mx_gemm_device.hpp"
+#include "mx_gemm_plan.hpp"
+
+namespace lc {
+
+constexpr unsigned kMxRingLds = 5u * 256u * 128u;
+
+__global__ __launch_bounds__(kBlock, 1) void mx_ring_kernel(MxGemmParams P, const unsigned char* __restrict__ A, const unsigned char* __restrict__ SA,
+                                                            const unsigned char* __restrict__ B, const unsigned char* __restrict__ SB, void* __restrict__ C) {
+  constexpr int BM = 256, FM = 4, FN = 4, R = BM / 32, MFMAS = FM * FN;
+  constexpr uint32_t SLOT = BM * 128u;
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  touch_kernel_arguments<(int)sizeof(MxGemmParams) + 40>();
+
+  const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
+  const uint32_t wm = wave & 1u, wn = wave >> 1, h = lane >> 5, r = lane & 31u;
+  const uint32_t per_batch = P.g.tiles_m * P.g.tiles_n;
+  const uint32_t order = gemm_tile_order_of_block(blockIdx.x, per_batch * P.g.L);
+  const uint32_t batch = order / per_batch;
+  uint32_t tm, tn;
+  gemm_tile_of_order(P.g, order - batch * per_batch, &tm, &tn);
+  const uint32_t m0 = tm * BM, n0 = tn * BM;
+  A += 2u * (uint64_t)gemm_mode_eval(P.g.a_l, batch);
+  B += 2u * (uint64_t)gemm_mode_eval(P.g.b_l, batch);
+  SA += gemm_mode_eval(P.sa_l, batch);
+  SB += gemm_mode_eval(P.sb_l, batch);
+  C = mx_c_at(C, gemm_mode_eval(P.g.c_l, batch), P.c_type);
+
+  DirectTileLoader<BM, kLoadKDirect, 4> la, lb;
+  la.init(reinterpret_cast<const uint16_t*>(A), P.g.a_r, P.g.a_k, m0, P.g.M, P.g.K, tid);
+  lb.init(reinterpret_cast<const uint16_t*>(B), P.g.b_r, P.g.b_k, n0, P.g.N, P.g.K, tid);
+  MxScaleLoader<FM> lsa;
+  MxScaleLoader<FN> lsb;
+  lsa.init(SA, P.sa_r, m0 + wm * 128u, P.g.M, P.blocks, true, lane);
+  lsb.init(SB, P.sb_r, n0 + wn * 128u, P.g.N, P.blocks, true, lane);
+
+  f32x16 acc[FM][FN];
+  static_for<FM>([&](auto i) {
+    static_for<FN>([&](auto j) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+    });
+  });
+  u32x4 af[2][FM], bf[2][FN];   // fragments, double-buffered in registers (one wavefront per SIMD: nothing else covers the LDS latency)
+  uint32_t sa[FM], sb[FN];
+  // per fragment: the lane's LDS address for the k tile's first k step in the slot being multiplied; k step kk: address ^ 16 kk
+  uint32_t a_fr[FM], b_fr[FN];
+  static_for<FM>([&](auto i) { a_fr[i] = gemm_lds_offset(wm * 128u + 32u * (uint32_t)i + r, 4u * h); });
+  static_for<FN>([&](auto j) { b_fr[j] = SLOT + gemm_lds_offset(wn * 128u + 32u * (uint32_t)j + r, 4u * h); });
+  auto read_fragments = [&](auto kk, auto buf) {
+    static_for<FM>([&](auto i) { af[buf][i] = *reinterpret_cast<const u32x4*>(lds + (a_fr[i] ^ (16u * (uint32_t)kk))); });
+    static_for<FN>([&](auto j) { bf[buf][j] = *reinterpret_cast<const u32x4*>(lds + (b_fr[j] ^ (16u * (uint32_t)kk))); });
+  };
+  auto multiply = [&](auto kk, auto buf) {
+    static_for<FM>([&](auto i) {
+      static_for<FN>([&](auto j) { acc[i][j] = mx_mfma_32x32x64<(int)decltype(kk)::value>(af[buf][i], bf[buf][j], acc[i][j], sa[i], sb[j]); });
+    });
+  };
+  // issue order inside a k step: its loads and LDS reads spread evenly between the products (the reads over the first SPAN of them)
+  auto issue_order = [&](auto loads_c, auto span_c) {
+    constexpr int LOADS = loads_c, SPAN = span_c, READS = FM + FN;
+    static_for<MFMAS>([&](auto g) {
+      constexpr int loads = LOADS * (g + 1) / MFMAS - LOADS * g / MFMAS;
+      constexpr int reads = g < SPAN ? READS * (g + 1) / SPAN - READS * g / SPAN : 0;
+      if constexpr (loads > 0) __builtin_amdgcn_sched_group_barrier(0x010, loads, 0);
+      if constexpr (reads > 0) __builtin_amdgcn_sched_group_barrier(0x100, reads, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    });
+  };
+  auto next_slot = [](uint32_t slot) { return slot + 2u >= 5u ? slot + 2u - 5u : slot + 2u; };
+  // s_waitcnt vmcnt(n) lgkmcnt(0): all but the n youngest loads have landed, every LDS read has returned
+  auto wait_loads_but = [](auto n) {
+    constexpr int N = decltype(n)::value;
+    static_assert(N >= 0 && N < 64, "vmcnt has six bits");
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0070);
+  };
+  using Zero = std::integral_constant<int, 0>;
+  using One = std::integral_constant<int, 1>;
+  using Two = std::integral_constant<int, 2>;
+  using Three = std::integral_constant<int, 3>;
+
+  const uint32_t last = P.g.k_tiles - 1u, wave_at = wave * (R * 1024u);
+  // byte offset of a k tile (uniform).  Evaluated afresh every time, without a branch: the k loop has to stay one block of instructions, or the
+  // compiler moves the products of the k steps before a branch behind it, where no load or LDS read lies between them.
+  auto a_bytes = [&](uint32_t t) { return 2u * gemm_mode_eval(P.g.a_k, t * kGemmBK); };
+  auto b_bytes = [&](uint32_t t) { return 2u * gemm_mode_eval(P.g.b_k, t * kGemmBK); };
+  lsa.fetch(P.sa_k, 0u);
+  lsb.fetch(P.sb_k, 0u);
+  // (the last argument of a fetch: the k tile it asks for is the last one, which may be short)
+  la.fetch(a_bytes(0u), 0u * SLOT + wave_at, last == 0u);
+  lb.fetch(b_bytes(0u), 1u * SLOT + wave_at, last == 0u);
+  __builtin_amdgcn_sched_barrier(0x038F);   // k tile 0's loads stay the oldest: the first wait below counts from the youngest
+  la.fetch(a_bytes(last < 1u ? last : 1u), 2u * SLOT + wave_at, last <= 1u);
+  lb.template fetch<0, R / 2>(b_bytes(last < 1u ? last : 1u), 3u * SLOT + wave_at, last <= 1u);
+  wait_loads_but(std::integral_constant<int, R + R / 2>{});   // k tile 0 and its scales have landed
+  lsa.take(0u, sa);
+  lsb.take(0u, sb);
+  lds_barrier();
+  read_fragments(Zero{}, Zero{});
+  uint32_t s_a = 0u, s_b = 1u;   // slots of the k tile being multiplied
+  for (uint32_t kt = 0; kt < P.g.k_tiles; ++kt) {
+    const uint32_t s_b1 = next_slot(s_b), s_a2 = next_slot(next_slot(s_a));   // slots of B(kt + 1) and A(kt + 2)
+    const uint32_t t1 = kt < last ? kt + 1u : last, t2 = t1 < last ? t1 + 1u : last;
+    const uint32_t b1 = b_bytes(t1), a2 = a_bytes(t2), b2 = b_bytes(t2);
+    // k step 0: the next k tile's scales, second half of B(kt + 1); k steps 1 and 2: A(kt + 2).  Past the last k tile the loads repeat it
+    // (in bounds, into slots nobody reads again).
+    lsa.fetch(P.sa_k, t1);
+    lsb.fetch(P.sb_k, t1);
+    lb.template fetch<R / 2, R>(b1, s_b1 * SLOT + wave_at, kt + 1u >= last);
+    read_fragments(One{}, One{});
+    multiply(Zero{}, Zero{});
+    issue_order(std::integral_constant<int, FM + FN + R - R / 2>{}, std::integral_constant<int, MFMAS>{});
+    // The wait before the barrier counts loads: all but the R youngest must have landed, and those must be A(kt + 2)'s: nothing but vector
+    // memory instructions is held back here (mask: ALU, VALU, SALU, MFMA and LDS instructions may cross).
+    __builtin_amdgcn_sched_barrier(0x038F);
+    la.template fetch<0, R / 2>(a2, s_a2 * SLOT + wave_at, kt + 2u >= last);
+    read_fragments(Two{}, Zero{});
+    multiply(One{}, One{});
+    issue_order(std::integral_constant<int, R / 2>{}, std::integral_constant<int, MFMAS>{});
+    la.template fetch<R / 2, R>(a2, s_a2 * SLOT + wave_at, kt + 2u >= last);
+    read_fragments(Three{}, One{});
+    multiply(Two{}, Zero{});
+    // the reads before the barrier over the first half of the products, so that the last one has returned when the last is issued
+    issue_order(std::integral_constant<int, R - R / 2>{}, std::integral_constant<int, (MFMAS + 1) / 2>{});
+    wait_loads_but(std::integral_constant<int, R>{});   // k tile kt + 1 and its scales have landed; A(kt + 2) may still be on its way
+    lds_barrier();
+    // k step 3: first half of B(kt + 2), into the slot A(kt) leaves
+    lb.template fetch<0, R / 2>(b2, s_a * SLOT + wave_at, kt + 2u >= last);
+    const uint32_t sa_next = next_slot(s_a), sb_next = next_slot(s_b);
+    const uint32_t da = (sa_next - s_a) * SLOT, db = (sb_next - s_b) * SLOT;
+    static_for<FM>([&](auto i) { a_fr[i] += da; });
+    static_for<FN>([&](auto j) { b_fr[j] += db; });
+    s_a = sa_next;
+    s_b = sb_next;
+    read_fragments(Zero{}, Zero{});
+    multiply(Three{}, One{});
+    issue_order(std::integral_constant<int, R / 2>{}, std::integral_constant<int, MFMAS>{});
+    lsa.take(t1, sa);
+    lsb.take(t1, sb);
+  }
+  __builtin_amdgcn_s_waitcnt(0x0070);   // the repeated loads of the last k tile have landed, its fragments have been read
+  lds_barrier();
+
+  unsigned char* mine = lds + wave * (128u * 32u * 4u);
+  mx_c_dispatch(P, [&](auto type, auto add) {
+    static_for<FN>([&](auto j) {
+      static_for<FM>([&](auto i) {
+        static_for<4>([&](auto g) {
+          f32x4 v;
+          static_for<4>([&](auto e) { v[(int)e] = acc[i][j][4 * g + e]; });
+          *reinterpret_cast<f32x4*>(mine + gemm_sum_unit(128u, 32u, 8u * (uint32_t)i + mfma_c_row(lane, 4u * (uint32_t)g) / 4u, mfma_c_col(lane)) * 16u) = v;
+        });
+      });
+      asm volatile("" ::: "memory");   // (a wavefront's LDS accesses are carried out in order)
+      const uint32_t m = m0 + wm * 128u, n = n0 + wn * 128u + 32u * (uint32_t)j;
+      if (P.g.c_vec) mx_tile_to_c_as<128, 32, 64, decltype(type)::value, decltype(add)::value, true>(P, C, mine, m, n, lane);
+      else mx_tile_to_c_as<128, 32, 64, decltype(type)::value, decltype(add)::value, false>(P, C, mine, m, n, lane);
+      asm volatile("" ::: "memory");
+    });
+  });
+}
+
+static inline hipError_t launch_mx_ring(const lc_mx_gemm_plan& plan, const unsigned char* a, const unsigned char* sa, const unsigned char* b,
+                                        const unsigned char* sb, void* c, hipStream_t s) {
+  if (plan.lds_bytes != kMxRingLds || plan.b_load != kLoadKDirect || !plan.params.a_dwords || !plan.params.b_dwords) return hipErrorInvalidValue;
+  static std::atomic<bool> raised{false};
+  if (!raised.load(std::memory_order_acquire)) {
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&mx_ring_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    if (e != hipSuccess) return e;
+    raised.store(true, std::memory_order_release);
+  }
+  const unsigned grid = plan.params.g.tiles_m * plan.params.g.tiles_n * plan.params.g.L;
+  hipLaunchKernelGGL(mx_ring_kernel, dim3(grid), dim3(kBlock), plan.lds_bytes, s, plan.params, a, sa, b, sb, c);
+  return hipSuccess;
+}
+
+}  // namespace lc
