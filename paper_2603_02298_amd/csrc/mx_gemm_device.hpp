@@ -10,6 +10,16 @@
 
 namespace lc {
 
+// The kernel's arguments again, through a pointer that the compiler cannot trace back to them: what only the end of a kernel needs is then
+// loaded there, and not at the start, where the scalar registers it would be kept in until the end are taken from the k loop.  (MxGemmParams is the
+// first argument.)
+__device__ __forceinline__ const MxGemmParams& mx_params_again() {
+  typedef const MxGemmParams __attribute__((address_space(4))) * KernargPtr;
+  KernargPtr p = (KernargPtr)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const MxGemmParams*)p;
+}
+
 // What the products are made of: both operands codes, or the kernel's A codes and B 16-bit elements.
 enum MxMath : int { kMxCodes = 0, kMxBf16 = 1, kMxF16 = 2 };
 
@@ -181,6 +191,64 @@ struct MxScaleLoader {
   }
 };
 
+// ---- a tile of codes through registers into 16-bit elements in LDS, for k modes (of the codes and of their scales) that every k tile lies evenly in:
+// inside the first leaf, or a mode of one leaf ----
+// The units are MxTileLoader's.  What is the same for every k tile is worked out once: a lane's offsets from the tile's first k, and where its
+// elements go in LDS.
+template <int MATH, int BR, int BLOCKED>
+struct MxEvenTileLoader {
+  static constexpr int UNITS = BR * 2 / 256;
+  __amdgpu_buffer_rsrc_t codes, scales;
+  uint32_t off[UNITS], s_off[UNITS];   // 0xFFFFFFFF: no such row
+  uint32_t tail_mask;                  // bit i: block i of this lane lies below K in the last k tile
+  uint32_t put;                        // bytes into the tile
+  struct Raw {
+    u32x4 codes[UNITS];
+    uint8_t byte[UNITS];
+  };
+
+  __device__ __forceinline__ void init(const unsigned char* p, const unsigned char* s, const MxGemmParams& P, uint32_t row0, uint32_t t) {
+    codes = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(p), 0, 0xFFFFFFFFu, 0x00020000);
+    scales = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(s), 0, 0xFFFFFFFFu, 0x00020000);
+    const uint32_t k_rem = P.g.K - (P.g.K - 1u) / kGemmBK * kGemmBK;
+    tail_mask = 0u;
+    static_for<UNITS>([&](auto i) {
+      const uint32_t row = BLOCKED ? (t >> 1) + 128u * (uint32_t)i : 32u * (t % (BR / 32u));
+      const uint32_t k = BLOCKED ? 32u * (t & 1u) : t / (BR / 32u) + (256u / (BR / 32u)) * (uint32_t)i;
+      const uint32_t r = row0 + row;
+      off[i] = r < P.g.M ? 2u * (gemm_mode_eval(P.g.a_r, BLOCKED ? r : r / 4u) + (BLOCKED ? 8u * (t & 1u) : k * P.g.a_k.lead_stride)) : 0xFFFFFFFFu;
+      s_off[i] = r < P.g.M ? gemm_mode_eval(P.sa_r, BLOCKED ? r : r / kMxBlock) + (BLOCKED ? t & 1u : k) * P.sa_k.lead_stride : 0xFFFFFFFFu;
+      tail_mask |= (k < k_rem ? 1u : 0u) << (int)i;
+      // (unit i lies 128 rows, or 256 / (BR / 32) k, behind unit 0: a constant)
+      if constexpr (decltype(i)::value == 0) put = BLOCKED ? gemm_lds_offset(row, k / 8u) : gemm_rdirect_lds_offset(BR, k, row);
+    });
+  }
+  // where k tile kt begins along the codes' and along the scales' k mode, in bytes (uniform)
+  __device__ __forceinline__ static uint32_t codes_at(const MxGemmParams& P, uint32_t kt) { return 2u * gemm_mode_eval(P.g.a_k, kt * (BLOCKED ? kGemmBK / 4u : (uint32_t)kGemmBK)); }
+  __device__ __forceinline__ static uint32_t scales_at(const MxGemmParams& P, uint32_t kt) { return gemm_mode_eval(P.sa_k, kt * (BLOCKED ? kGemmBK / kMxBlock : (uint32_t)kGemmBK)); }
+  // tail: it is the short last one
+  __device__ __forceinline__ void fetch(uint32_t at, uint32_t s_at, bool tail, Raw& raw) const {
+    static_for<UNITS>([&](auto i) {
+      const bool out = tail && ((tail_mask >> (int)i) & 1u) == 0u;
+      raw.codes[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(codes, (int)(out ? 0xFFFFFFFFu : off[i]), (int)at, 0));   // outside: zeros
+      raw.byte[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(scales, (int)(out ? 0xFFFFFFFFu : s_off[i]), (int)s_at, 0);
+    });
+  }
+  // parks quarter q (eight elements) of block i of the lane's
+  template <int I, int Q>
+  __device__ __forceinline__ void park(unsigned char* tile, const Raw& raw) const {
+    constexpr uint32_t UNIT = BLOCKED ? 128u * 128u : 256u / (BR / 32u) * (BR * 2u);
+    static_assert(BLOCKED || (256u / (BR / 32u)) % 4u == 0u, "units of a lane fold alike");
+    // (the four 16-byte vectors of a block: the low bits of the slot)
+    *reinterpret_cast<u32x4*>(tile + (put ^ (16u * Q)) + I * UNIT) = mx_expand<MATH>(raw.codes[I][Q], mx_scale_value(raw.byte[I]));
+  }
+  __device__ __forceinline__ void park_all(unsigned char* tile, const Raw& raw) const {
+    static_for<UNITS>([&](auto i) {
+      static_for<4>([&](auto q) { park<(int)decltype(i)::value, (int)decltype(q)::value>(tile, raw); });
+    });
+  }
+};
+
 // ---- a tile of codes through registers into 16-bit elements in LDS ----
 // Blocks along k (BLOCKED 1): BR rows of 64 k in the arrangement of kLoadKDirect.  Lane t of 256 takes block t % 2 of rows t / 2 + 128 i.
 // Blocks along the rows (0): 64 k rows of BR elements in the arrangement of kLoadRDirect.  Lane t takes block t % (BR / 32) of k t / (BR / 32) + ..
@@ -192,8 +260,10 @@ struct MxTileLoader {
   __amdgpu_buffer_rsrc_t codes, scales;
   uint32_t off[UNITS], s_off[UNITS];   // 0xFFFFFFFF: no such row
   uint32_t K, t;
-  u32x4 raw[UNITS];
-  uint32_t byte[UNITS];
+  struct Raw {   // a k tile's codes and scales, as they were loaded
+    u32x4 codes[UNITS];
+    uint32_t byte[UNITS];
+  };
 
   __device__ __forceinline__ uint32_t row_of(uint32_t i) const { return BLOCKED ? (t >> 1) + 128u * i : 32u * (t % (BR / 32u)); }
   __device__ __forceinline__ uint32_t k_of(uint32_t i) const { return BLOCKED ? 32u * (t & 1u) : t / (BR / 32u) + (256u / (BR / 32u)) * i; }
@@ -209,24 +279,26 @@ struct MxTileLoader {
       s_off[i] = r < P.g.M ? gemm_mode_eval(P.sa_r, BLOCKED ? r : r / kMxBlock) : 0xFFFFFFFFu;
     });
   }
-  __device__ __forceinline__ void fetch(const MxGemmParams& P, uint32_t kt) {
+  __device__ __forceinline__ void fetch(const MxGemmParams& P, uint32_t kt, Raw& raw) const {
     static_for<UNITS>([&](auto i) {
       const uint32_t k = kt * kGemmBK + k_of((uint32_t)i);
       const bool in = k < K && off[i] != 0xFFFFFFFFu;
       const uint32_t at = in ? off[i] + 2u * gemm_mode_eval(P.g.a_k, BLOCKED ? k / 4u : k) : 0xFFFFFFFFu;
       const uint32_t s_at = in ? s_off[i] + gemm_mode_eval(P.sa_k, BLOCKED ? k / kMxBlock : k) : 0xFFFFFFFFu;
-      raw[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(codes, (int)at, 0, 0));   // outside: zeros
-      byte[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(scales, (int)s_at, 0, 0) & 0xFFu;
+      raw.codes[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(codes, (int)at, 0, 0));   // outside: zeros
+      raw.byte[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(scales, (int)s_at, 0, 0) & 0xFFu;
     });
   }
-  // parks the k tile that was asked for last
-  __device__ __forceinline__ void park(unsigned char* tile) {
-    static_for<UNITS>([&](auto i) {
-      const float scale = mx_scale_value(byte[i]);
+  // parks a k tile; FIRST, END: which of the lane's blocks
+  template <int FIRST = 0, int END = UNITS>
+  __device__ __forceinline__ void park(unsigned char* tile, const Raw& raw) const {
+    static_for<END - FIRST>([&](auto d) {
+      constexpr int i = FIRST + decltype(d)::value;
+      const float scale = mx_scale_value(raw.byte[i]);
       const uint32_t row = row_of((uint32_t)i), k = k_of((uint32_t)i);
       static_for<4>([&](auto q) {
         const uint32_t at = BLOCKED ? gemm_lds_offset(row, k / 8u + (uint32_t)q) : gemm_rdirect_lds_offset(BR, k, row + 8u * (uint32_t)q);
-        *reinterpret_cast<u32x4*>(tile + at) = mx_expand<MATH>(raw[i][(int)q], scale);
+        *reinterpret_cast<u32x4*>(tile + at) = mx_expand<MATH>(raw.codes[i][(int)q], scale);
       });
     });
   }

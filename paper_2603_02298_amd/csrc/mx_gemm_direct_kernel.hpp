@@ -120,15 +120,16 @@ __global__ __launch_bounds__(64 * WAVES) void mx_direct_kernel(MxGemmParams P, c
     static_for<FN>([&](auto j) { *reinterpret_cast<f32x4*>(mine + (16u * (uint32_t)j + row) * PITCH + 16u * (uint32_t)i + 4u * quarter) = acc[i][j]; });
   });
   __syncthreads();
-  const bool along_m = P.g.c_m.lead_stride == 1u;
-  mx_c_dispatch(P, [&](auto type, auto add) {
+  const MxGemmParams& E = mx_params_again();
+  const bool along_m = E.g.c_m.lead_stride == 1u;
+  mx_c_dispatch(E, [&](auto type, auto add) {
     mx_c_elem<decltype(type)::value>* c = static_cast<mx_c_elem<decltype(type)::value>*>(C);
     for (uint32_t e = tid; e < (uint32_t)(TM * TN); e += LANES) {
       const uint32_t m = along_m ? e % TM : e / TN, n = along_m ? e / TM : e % TN;
-      if (m0 + m >= P.g.M || n0 + n >= P.g.N) continue;
+      if (m0 + m >= E.g.M || n0 + n >= E.g.N) continue;
       float sum = part[n * PITCH + m];
       static_for<WAVES - 1>([&](auto w) { sum += part[((uint32_t)w + 1u) * (TN * PITCH) + n * PITCH + m]; });
-      auto* p = c + (gemm_mode_eval(P.g.c_m, m0 + m) + gemm_mode_eval(P.g.c_n, n0 + n));
+      auto* p = c + (gemm_mode_eval(E.g.c_m, m0 + m) + gemm_mode_eval(E.g.c_n, n0 + n));
       *p = (mx_c_elem<decltype(type)::value>)(decltype(add)::value ? (float)*p + sum : sum);
     }
   });

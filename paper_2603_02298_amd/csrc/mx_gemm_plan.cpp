@@ -209,6 +209,9 @@ lc_status_t make_mx_gemm_plan(const Layout& A, const Layout* A_scales, const Lay
   };
   const bool can_direct = codes || (plan.blocked == 1 && plan.b_load == kLoadKDirect);
   const bool can_ring = codes && plan.b_load == kLoadKDirect && a.dwords && b.dwords;
+  // (k tiles that lie evenly in the k modes of the codes and of their scales)
+  auto even = [](const Modes& k, int64_t per_tile) { return k.size() == 1 || k[0].extent % per_tile == 0; };
+  const bool can_wide = !codes && plan.b_load == kLoadKDirect && even(a.k, plan.blocked ? kGemmBK / 4 : kGemmBK) && even(a.s_k, plan.blocked ? kGemmBK / kMxBlock : kGemmBK);
   const int t_env = env_int("LC_TUNE_MX_TILE", 0);
   if (t_env == 16 && can_direct) take(kMxDirect, 16, 16, 8);
   else if (t_env == 3216 && can_direct) take(kMxDirect, 32, 16, 8);
@@ -217,13 +220,19 @@ lc_status_t make_mx_gemm_plan(const Layout& A, const Layout* A_scales, const Lay
   else if (t_env == 12864) take(kMxStream, 128, 64, 4);
   else if (t_env == 128) take(kMxStream, 128, 128, 4);
   else if (t_env == 256 && can_ring) take(kMxRing, 256, 256, 4);
+  else if (t_env == 256 && can_wide) take(kMxWide, 256, 256, 4);
+  else if (t_env == 256128 && can_wide) take(kMxWide, 256, 128, 4);
   else if (can_direct && b.rows <= 16) take(kMxDirect, tiles_of(32, 16) >= 256 ? 32 : 16, 16, 8);
   else if (can_direct && tiles_of(32, 32) <= 512) take(kMxDirect, 32, 32, 8);
   else if (codes && tiles_of(64, 64) <= 512) take(kMxStream, 64, 64, 4);
   else if (can_ring && tiles_of(256, 256) >= 128) take(kMxRing, 256, 256, 4);
+  else if (can_wide && tiles_of(256, 256) >= 192) take(kMxWide, 256, 256, 4);
+  else if (can_wide && tiles_of(256, 128) >= 96) take(kMxWide, 256, 128, 4);
   else if (tiles_of(128, 128) <= 256) take(kMxStream, 128, 64, 4);
   else take(kMxStream, 128, 128, 4);
-  plan.lds_bytes = plan.kernel == kMxStream ? 2u * (unsigned)(plan.tile_m + plan.tile_n) * 128u : plan.kernel == kMxRing ? 5u * 256u * 128u : 0u;
+  plan.lds_bytes = plan.kernel == kMxStream ? 2u * (unsigned)(plan.tile_m + plan.tile_n) * 128u
+                   : plan.kernel == kMxRing ? 5u * 256u * 128u
+                   : plan.kernel == kMxWide ? (2u * 256u + 3u * (unsigned)plan.tile_n) * 128u : 0u;
   G.tiles_m = (uint32_t)((a.rows + plan.tile_m - 1) / plan.tile_m);
   G.tiles_n = (uint32_t)((b.rows + plan.tile_n - 1) / plan.tile_n);
   // a grid counts its lanes in 32 bits
@@ -233,7 +242,7 @@ lc_status_t make_mx_gemm_plan(const Layout& A, const Layout* A_scales, const Lay
 }
 
 std::string describe(const lc_mx_gemm_plan& plan) {
-  static const char* kernels[] = {"direct", "stream", "ring"};
+  static const char* kernels[] = {"direct", "stream", "ring", "wide"};
   auto type = [](int t) { return t == LC_F32 ? "f32" : t == LC_BF16 ? "bf16" : t == LC_F16 ? "f16" : "mxfp4"; };
   std::string s = std::string("class=mx-gemm kernel=") + kernels[plan.kernel] + " a=" + type(plan.a_dtype) + " b=mxfp4 c=" + type(plan.c_dtype);
   s += plan.accumulate ? " accumulate=1" : " accumulate=0";

@@ -107,25 +107,24 @@ __global__ __launch_bounds__(kBlock, 1) void mx_ring_kernel(MxGemmParams P, cons
   lb.fetch(b_bytes(0u), 1u * SLOT + wave_at, last == 0u);
   __builtin_amdgcn_sched_barrier(0x038F);   // k tile 0's loads stay the oldest: the first wait below counts from the youngest
   la.fetch(a_bytes(last < 1u ? last : 1u), 2u * SLOT + wave_at, last <= 1u);
-  lb.template fetch<0, R / 2>(b_bytes(last < 1u ? last : 1u), 3u * SLOT + wave_at, last <= 1u);
-  wait_loads_but(std::integral_constant<int, R + R / 2>{});   // k tile 0 and its scales have landed
+  lb.fetch(b_bytes(last < 1u ? last : 1u), 3u * SLOT + wave_at, last <= 1u);
+  wait_loads_but(std::integral_constant<int, 2 * R>{});   // k tile 0 and its scales have landed
   lsa.take(0u, sa);
   lsb.take(0u, sb);
   lds_barrier();
   read_fragments(Zero{}, Zero{});
   uint32_t s_a = 0u, s_b = 1u;   // slots of the k tile being multiplied
   for (uint32_t kt = 0; kt < P.g.k_tiles; ++kt) {
-    const uint32_t s_b1 = next_slot(s_b), s_a2 = next_slot(next_slot(s_a));   // slots of B(kt + 1) and A(kt + 2)
+    const uint32_t s_a2 = next_slot(next_slot(s_a));   // slot of A(kt + 2)
     const uint32_t t1 = kt < last ? kt + 1u : last, t2 = t1 < last ? t1 + 1u : last;
-    const uint32_t b1 = b_bytes(t1), a2 = a_bytes(t2), b2 = b_bytes(t2);
-    // k step 0: the next k tile's scales, second half of B(kt + 1); k steps 1 and 2: A(kt + 2).  Past the last k tile the loads repeat it
+    const uint32_t a2 = a_bytes(t2), b2 = b_bytes(t2);
+    // k step 0: the next k tile's scales; k steps 1 and 2: A(kt + 2).  Past the last k tile the loads repeat it
     // (in bounds, into slots nobody reads again).
     lsa.fetch(P.sa_k, t1);
     lsb.fetch(P.sb_k, t1);
-    lb.template fetch<R / 2, R>(b1, s_b1 * SLOT + wave_at, kt + 1u >= last);
     read_fragments(One{}, One{});
     multiply(Zero{}, Zero{});
-    issue_order(std::integral_constant<int, FM + FN + R - R / 2>{}, std::integral_constant<int, MFMAS>{});
+    issue_order(std::integral_constant<int, FM + FN>{}, std::integral_constant<int, MFMAS>{});
     // The wait before the barrier counts loads: all but the R youngest must have landed, and those must be A(kt + 2)'s: nothing but vector
     // memory instructions is held back here (mask: ALU, VALU, SALU, MFMA and LDS instructions may cross).
     __builtin_amdgcn_sched_barrier(0x038F);
@@ -140,8 +139,8 @@ __global__ __launch_bounds__(kBlock, 1) void mx_ring_kernel(MxGemmParams P, cons
     issue_order(std::integral_constant<int, R - R / 2>{}, std::integral_constant<int, (MFMAS + 1) / 2>{});
     wait_loads_but(std::integral_constant<int, R>{});   // k tile kt + 1 and its scales have landed; A(kt + 2) may still be on its way
     lds_barrier();
-    // k step 3: first half of B(kt + 2), into the slot A(kt) leaves
-    lb.template fetch<0, R / 2>(b2, s_a * SLOT + wave_at, kt + 2u >= last);
+    // k step 3: B(kt + 2), into the slot A(kt) leaves
+    lb.fetch(b2, s_a * SLOT + wave_at, kt + 2u >= last);
     const uint32_t sa_next = next_slot(s_a), sb_next = next_slot(s_b);
     const uint32_t da = (sa_next - s_a) * SLOT, db = (sb_next - s_b) * SLOT;
     static_for<FM>([&](auto i) { a_fr[i] += da; });
@@ -150,7 +149,7 @@ __global__ __launch_bounds__(kBlock, 1) void mx_ring_kernel(MxGemmParams P, cons
     s_b = sb_next;
     read_fragments(Zero{}, Zero{});
     multiply(Three{}, One{});
-    issue_order(std::integral_constant<int, R / 2>{}, std::integral_constant<int, MFMAS>{});
+    issue_order(std::integral_constant<int, R>{}, std::integral_constant<int, MFMAS>{});
     lsa.take(t1, sa);
     lsb.take(t1, sb);
   }
@@ -158,7 +157,8 @@ __global__ __launch_bounds__(kBlock, 1) void mx_ring_kernel(MxGemmParams P, cons
   lds_barrier();
 
   unsigned char* mine = lds + wave * (128u * 32u * 4u);
-  mx_c_dispatch(P, [&](auto type, auto add) {
+  const MxGemmParams& E = mx_params_again();
+  mx_c_dispatch(E, [&](auto type, auto add) {
     static_for<FN>([&](auto j) {
       static_for<FM>([&](auto i) {
         static_for<4>([&](auto g) {
@@ -169,8 +169,8 @@ __global__ __launch_bounds__(kBlock, 1) void mx_ring_kernel(MxGemmParams P, cons
       });
       asm volatile("" ::: "memory");   // (a wavefront's LDS accesses are carried out in order)
       const uint32_t m = m0 + wm * 128u, n = n0 + wn * 128u + 32u * (uint32_t)j;
-      if (P.g.c_vec) mx_tile_to_c_as<128, 32, 64, decltype(type)::value, decltype(add)::value, true>(P, C, mine, m, n, lane);
-      else mx_tile_to_c_as<128, 32, 64, decltype(type)::value, decltype(add)::value, false>(P, C, mine, m, n, lane);
+      if (E.g.c_vec) mx_tile_to_c_as<128, 32, 64, decltype(type)::value, decltype(add)::value, true>(E, C, mine, m, n, lane);
+      else mx_tile_to_c_as<128, 32, 64, decltype(type)::value, decltype(add)::value, false>(E, C, mine, m, n, lane);
       asm volatile("" ::: "memory");
     });
   });

@@ -109,6 +109,7 @@ __global__ __launch_bounds__(kBlock, 160 * 1024 / (2 * (BM + BN) * 128)) void mx
     constexpr int A_LOAD = A_KIND ? kLoadKDirect : kLoadRDirect;   // how the expanded tile lies in LDS
     constexpr bool REGS = gemm_load_in_registers(B_LOAD);          // B through registers as well
     MxTileLoader<MATH, BM, A_KIND> la;
+    typename MxTileLoader<MATH, BM, A_KIND>::Raw raw;
     TileLoader<BN, B_LOAD, 4> lb;
     la.init(A, SA, P, m0, tid);
     init_loader<B_LOAD>(lb, B16, P.g.b_r, P.g.b_k, n0, P.g.N, P.g.K, tid, P.g.b_direct);
@@ -122,12 +123,12 @@ __global__ __launch_bounds__(kBlock, 160 * 1024 / (2 * (BM + BN) * 128)) void mx
         if (kt + 1u < P.g.k_tiles) kb.next(P.g.b_k, kt + 1u);
       }
     };
-    la.fetch(P, 0u);
+    la.fetch(P, 0u, raw);
     request_b(0u);
-    la.park(lds);
+    la.park(lds, raw);
     if constexpr (REGS) lb.park(lds + b_at, 0u);
     if (P.g.k_tiles > 1u) {
-      la.fetch(P, 1u);
+      la.fetch(P, 1u, raw);
       if constexpr (REGS) request_b(1u);
     }
     for (uint32_t t = 0; t < P.g.k_tiles; ++t) {
@@ -138,10 +139,10 @@ __global__ __launch_bounds__(kBlock, 160 * 1024 / (2 * (BM + BN) * 128)) void mx
       if (t + 1u < P.g.k_tiles) {
         unsigned char* next = lds + ((t + 1u) & 1u) * STAGE;
         if constexpr (!REGS) request_b(t + 1u);
-        la.park(next);
+        la.park(next, raw);
         if constexpr (REGS) lb.park(next + b_at, t + 1u);
         if (t + 2u < P.g.k_tiles) {
-          la.fetch(P, t + 2u);
+          la.fetch(P, t + 2u, raw);
           if constexpr (REGS) request_b(t + 2u);
         }
       }
@@ -171,7 +172,7 @@ __global__ __launch_bounds__(kBlock, 160 * 1024 / (2 * (BM + BN) * 128)) void mx
     });
   });
   __syncthreads();
-  mx_tile_to_c<BM, BN, kBlock>(P, C, lds, m0, n0, tid);
+  mx_tile_to_c<BM, BN, kBlock>(mx_params_again(), C, lds, m0, n0, tid);
 }
 
 template <int MATH, int BM, int BN, int A_KIND, int B_LOAD>
