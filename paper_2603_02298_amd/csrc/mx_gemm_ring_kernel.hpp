@@ -23,7 +23,7 @@ constexpr unsigned kMxRingLds = 5u * 256u * 128u;
 
 __global__ __launch_bounds__(kBlock, 1) void mx_ring_kernel(MxGemmParams P, const unsigned char* __restrict__ A, const unsigned char* __restrict__ SA,
                                                             const unsigned char* __restrict__ B, const unsigned char* __restrict__ SB, void* __restrict__ C) {
-  constexpr int BM = 256, FM = 4, FN = 4, R = BM / 32, MFMAS = FM * FN;
+  constexpr int BM = 256, FM = 4, FN = 4, R = BM / 32;
   constexpr uint32_t SLOT = BM * 128u;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   touch_kernel_arguments<(int)sizeof(MxGemmParams) + 40>();
@@ -63,24 +63,19 @@ __global__ __launch_bounds__(kBlock, 1) void mx_ring_kernel(MxGemmParams P, cons
   uint32_t a_fr[FM], b_fr[FN];
   static_for<FM>([&](auto i) { a_fr[i] = gemm_lds_offset(wm * 128u + 32u * (uint32_t)i + r, 4u * h); });
   static_for<FN>([&](auto j) { b_fr[j] = SLOT + gemm_lds_offset(wn * 128u + 32u * (uint32_t)j + r, 4u * h); });
-  auto read_fragments = [&](auto kk, auto buf) {
-    static_for<FM>([&](auto i) { af[buf][i] = *reinterpret_cast<const u32x4*>(lds + (a_fr[i] ^ (16u * (uint32_t)kk))); });
-    static_for<FN>([&](auto j) { bf[buf][j] = *reinterpret_cast<const u32x4*>(lds + (b_fr[j] ^ (16u * (uint32_t)kk))); });
-  };
-  auto multiply = [&](auto kk, auto buf) {
+  auto read_a = [&](auto i, auto kk, auto buf) { af[buf][i] = *reinterpret_cast<const u32x4*>(lds + (a_fr[i] ^ (16u * (uint32_t)kk))); };
+  auto read_b = [&](auto j, auto kk, auto buf) { bf[buf][j] = *reinterpret_cast<const u32x4*>(lds + (b_fr[j] ^ (16u * (uint32_t)kk))); };
+  // One k step in four parts, in this order: a row of products each, and before them in the first three the reads of the next k step's
+  // fragments, in every one what `more` does.  Nothing crosses the parts, so that what is not a product lies between products.
+  auto k_step = [&](auto kk, auto next_kk, auto&& more) {
+    constexpr int buf = decltype(kk)::value % 2;
+    using Other = std::integral_constant<int, 1 - buf>;
     static_for<FM>([&](auto i) {
+      if constexpr (i == 0) static_for<FN>([&](auto j) { read_b(j, next_kk, Other{}); });
+      if constexpr (i == 1 || i == 2) static_for<2>([&](auto d) { read_a(std::integral_constant<int, 2 * (decltype(i)::value - 1) + decltype(d)::value>{}, next_kk, Other{}); });
+      more(i);
       static_for<FN>([&](auto j) { acc[i][j] = mx_mfma_32x32x64<(int)decltype(kk)::value>(af[buf][i], bf[buf][j], acc[i][j], sa[i], sb[j]); });
-    });
-  };
-  // issue order inside a k step: its loads and LDS reads spread evenly between the products (the reads over the first SPAN of them)
-  auto issue_order = [&](auto loads_c, auto span_c) {
-    constexpr int LOADS = loads_c, SPAN = span_c, READS = FM + FN;
-    static_for<MFMAS>([&](auto g) {
-      constexpr int loads = LOADS * (g + 1) / MFMAS - LOADS * g / MFMAS;
-      constexpr int reads = g < SPAN ? READS * (g + 1) / SPAN - READS * g / SPAN : 0;
-      if constexpr (loads > 0) __builtin_amdgcn_sched_group_barrier(0x010, loads, 0);
-      if constexpr (reads > 0) __builtin_amdgcn_sched_group_barrier(0x100, reads, 0);
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_barrier(0);
     });
   };
   auto next_slot = [](uint32_t slot) { return slot + 2u >= 5u ? slot + 2u - 5u : slot + 2u; };
@@ -112,44 +107,34 @@ __global__ __launch_bounds__(kBlock, 1) void mx_ring_kernel(MxGemmParams P, cons
   lsa.take(0u, sa);
   lsb.take(0u, sb);
   lds_barrier();
-  read_fragments(Zero{}, Zero{});
-  uint32_t s_a = 0u, s_b = 1u;   // slots of the k tile being multiplied
+  static_for<FM>([&](auto i) { read_a(i, Zero{}, Zero{}); });
+  static_for<FN>([&](auto j) { read_b(j, Zero{}, Zero{}); });
+  uint32_t s_a = 0u, s_b = 1u, a2, b2;   // slots of the k tile being multiplied; where A(kt + 2) and B(kt + 2) begin
   for (uint32_t kt = 0; kt < P.g.k_tiles; ++kt) {
     const uint32_t s_a2 = next_slot(next_slot(s_a));   // slot of A(kt + 2)
     const uint32_t t1 = kt < last ? kt + 1u : last, t2 = t1 < last ? t1 + 1u : last;
-    const uint32_t a2 = a_bytes(t2), b2 = b_bytes(t2);
-    // k step 0: the next k tile's scales; k steps 1 and 2: A(kt + 2).  Past the last k tile the loads repeat it
-    // (in bounds, into slots nobody reads again).
-    lsa.fetch(P.sa_k, t1);
-    lsb.fetch(P.sb_k, t1);
-    read_fragments(One{}, One{});
-    multiply(Zero{}, Zero{});
-    issue_order(std::integral_constant<int, FM + FN>{}, std::integral_constant<int, MFMAS>{});
-    // The wait before the barrier counts loads: all but the R youngest must have landed, and those must be A(kt + 2)'s: nothing but vector
-    // memory instructions is held back here (mask: ALU, VALU, SALU, MFMA and LDS instructions may cross).
-    __builtin_amdgcn_sched_barrier(0x038F);
-    la.template fetch<0, R / 2>(a2, s_a2 * SLOT + wave_at, kt + 2u >= last);
-    read_fragments(Two{}, Zero{});
-    multiply(One{}, One{});
-    issue_order(std::integral_constant<int, R / 2>{}, std::integral_constant<int, MFMAS>{});
-    la.template fetch<R / 2, R>(a2, s_a2 * SLOT + wave_at, kt + 2u >= last);
-    read_fragments(Three{}, One{});
-    multiply(Two{}, Zero{});
-    // the reads before the barrier over the first half of the products, so that the last one has returned when the last is issued
-    issue_order(std::integral_constant<int, R - R / 2>{}, std::integral_constant<int, (MFMAS + 1) / 2>{});
+    // k step 0: the next k tile's scales; k steps 1 and 2: A(kt + 2).  Past the last k tile the loads repeat it (in bounds, into slots
+    // nobody reads again).
+    k_step(Zero{}, One{}, [&](auto i) {
+      if constexpr (i == 0) lsa.fetch(P.sa_k, t1);
+      if constexpr (i == 1) lsb.fetch(P.sb_k, t1);
+      if constexpr (i == 2) a2 = a_bytes(t2);
+      if constexpr (i == 3) b2 = b_bytes(t2);
+    });
+    asm volatile("" ::: "memory");
+    k_step(One{}, Two{}, [&](auto i) { la.template fetch<i * R / 8, (i + 1) * R / 8>(a2, s_a2 * SLOT + wave_at, kt + 2u >= last); });
+    k_step(Two{}, Three{}, [&](auto i) { la.template fetch<R / 2 + i * R / 8, R / 2 + (i + 1) * R / 8>(a2, s_a2 * SLOT + wave_at, kt + 2u >= last); });
+    // all but the R youngest have landed, and those are A(kt + 2)'s
     wait_loads_but(std::integral_constant<int, R>{});   // k tile kt + 1 and its scales have landed; A(kt + 2) may still be on its way
     lds_barrier();
-    // k step 3: B(kt + 2), into the slot A(kt) leaves
-    lb.fetch(b2, s_a * SLOT + wave_at, kt + 2u >= last);
     const uint32_t sa_next = next_slot(s_a), sb_next = next_slot(s_b);
-    const uint32_t da = (sa_next - s_a) * SLOT, db = (sb_next - s_b) * SLOT;
+    const uint32_t da = (sa_next - s_a) * SLOT, db = (sb_next - s_b) * SLOT, b_to = s_a * SLOT + wave_at;
     static_for<FM>([&](auto i) { a_fr[i] += da; });
     static_for<FN>([&](auto j) { b_fr[j] += db; });
     s_a = sa_next;
     s_b = sb_next;
-    read_fragments(Zero{}, Zero{});
-    multiply(Three{}, One{});
-    issue_order(std::integral_constant<int, R>{}, std::integral_constant<int, MFMAS>{});
+    // k step 3: B(kt + 2), into the slot A(kt) leaves
+    k_step(Three{}, Zero{}, [&](auto i) { lb.template fetch<i * R / 4, (i + 1) * R / 4>(b2, b_to, kt + 2u >= last); });
     lsa.take(t1, sa);
     lsb.take(t1, sb);
   }
