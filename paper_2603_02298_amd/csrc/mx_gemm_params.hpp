@@ -23,7 +23,12 @@ struct MxGemmParams {
   int32_t accumulate;
   int32_t a_dwords, b_dwords;    // 1: four blocks 4 c .. 4 c + 3 of a row have neighbouring scales
   uint32_t blocks;               // blocks along k that hold k < K
-  uint32_t pad;
+  uint32_t scale_pitch;          // direct kernel: bytes from one row's scales to the next in LDS; 0: they do not fit, and are read where they lie
 };
+
+// LDS of the direct kernel: the scales of a tile's rows, in whose place the wavefronts' partial tiles come afterwards.  The pitch is an odd number of
+// dwords, so that 16 rows' scales of one chunk lie in different banks.
+constexpr uint32_t kMxDirectScaleLimit = 64u << 10;
+LC_HD uint32_t mx_scale_pitch(uint32_t blocks) { return 4u * ((blocks + 3u) / 4u | 1u); }
 
 }  // namespace lc

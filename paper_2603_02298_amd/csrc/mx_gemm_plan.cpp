@@ -207,11 +207,11 @@ lc_status_t make_mx_gemm_plan(const Layout& A, const Layout* A_scales, const Lay
     plan.tile_n = tn;
     plan.waves = waves;
   };
-  const bool can_direct = codes || (plan.blocked == 1 && plan.b_load == kLoadKDirect);
   const bool can_ring = codes && plan.b_load == kLoadKDirect && a.dwords && b.dwords;
   // (k tiles that lie evenly in the k modes of the codes and of their scales)
   auto even = [](const Modes& k, int64_t per_tile) { return k.size() == 1 || k[0].extent % per_tile == 0; };
   const bool can_wide = !codes && plan.b_load == kLoadKDirect && even(a.k, plan.blocked ? kGemmBK / 4 : kGemmBK) && even(a.s_k, plan.blocked ? kGemmBK / kMxBlock : kGemmBK);
+  const bool can_direct = plan.blocked == 1 && even(a.k, 32) && even(a.s_k, 4) && (codes ? even(b.k, 32) && even(b.s_k, 4) : plan.b_load == kLoadKDirect);
   const int t_env = env_int("LC_TUNE_MX_TILE", 0);
   if (t_env == 16 && can_direct) take(kMxDirect, 16, 16, 8);
   else if (t_env == 3216 && can_direct) take(kMxDirect, 32, 16, 8);
@@ -233,6 +233,16 @@ lc_status_t make_mx_gemm_plan(const Layout& A, const Layout* A_scales, const Lay
   plan.lds_bytes = plan.kernel == kMxStream ? 2u * (unsigned)(plan.tile_m + plan.tile_n) * 128u
                    : plan.kernel == kMxRing ? 5u * 256u * 128u
                    : plan.kernel == kMxWide ? (2u * 256u + 3u * (unsigned)plan.tile_n) * 128u : 0u;
+  if (plan.kernel == kMxDirect) {
+    const int chunks = (int)((P.blocks + 3) / 4), w_env = env_int("LC_TUNE_MX_WAVES", 0);
+    plan.waves = w_env == 4 || w_env == 8 ? w_env : chunks <= 8 ? 4 : 8;
+    plan.x_quads = !codes && b.rows <= 4 && plan.tile_n == 16 ? 1 : plan.tile_n / 4;
+    // wavefronts' partial tiles, in whose place 16-bit elements pass through and the scales lie before
+    const unsigned part = (unsigned)(plan.waves * plan.tile_n * (plan.tile_m + 4) * 4), through = codes ? 0u : (unsigned)(plan.waves * plan.x_quads) * 1024u;
+    const uint64_t scales = (uint64_t)(plan.tile_m + (codes ? plan.tile_n : 0)) * mx_scale_pitch(P.blocks);
+    P.scale_pitch = scales <= kMxDirectScaleLimit ? mx_scale_pitch(P.blocks) : 0u;
+    plan.lds_bytes = std::max(part, through + (P.scale_pitch ? (unsigned)scales : 0u));
+  }
   G.tiles_m = (uint32_t)((a.rows + plan.tile_m - 1) / plan.tile_m);
   G.tiles_n = (uint32_t)((b.rows + plan.tile_n - 1) / plan.tile_n);
   // a grid counts its lanes in 32 bits

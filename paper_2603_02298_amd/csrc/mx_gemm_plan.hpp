@@ -13,6 +13,7 @@ struct lc_mx_gemm_plan {
   bool exchanged = false;                // the kernel's A is the caller's B (always where A holds 16-bit elements)
   lc::MxGemmKernel kernel = lc::kMxDirect;
   int tile_m = 0, tile_n = 0, waves = 0;
+  int x_quads = 0;                       // direct kernel: groups of four rows of the kernel's B that are loaded per tile
   int b_load = 0;                        // GemmLoad of the kernel's B (and of A where both are codes)
   unsigned a_align = 1, b_align = 1, c_align = 1;   // of the caller's pointers
   unsigned lds_bytes = 0;

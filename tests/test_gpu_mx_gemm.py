@@ -380,3 +380,15 @@ def test_helper_refusals():
                               ("c_layout", "(2,2):(1,1)", lc.LayoutCopyError)):
         with pytest.raises(error):
             lc.mx_gemm_tensor(**dict(args, **{key: value}))
+
+
+@pytest.mark.parametrize("a_dtype", ["mxfp4", "bf16"])
+@pytest.mark.parametrize("M", [1, 20])
+@pytest.mark.parametrize("s_text", ["(20,2304):(2304,1)", "(20,2304):(1,20)"])
+def test_long_k(a_dtype, M, s_text):
+    """More scales than the direct kernel keeps in LDS (2304 blocks), and just as many as it does (1020, 2044)."""
+    for blocks in (2304, 2044, 1020):
+        K, N = 32 * blocks, 20
+        s = s_text.replace("2304", str(blocks))
+        a, a_s = (_rows(M, K), _scales(M, K)) if a_dtype == "mxfp4" else (_rows(M, K), None)
+        _run(a, a_s, _rows(N, K), s, _rows(M, N), a_dtype, "f32", False, "wide", seed=blocks)
