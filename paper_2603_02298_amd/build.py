@@ -16,7 +16,8 @@ SOURCES = ["layout.cpp", "algebra.cpp", "semimodule.cpp", "plan.cpp", "replay.cp
            "gemm_inst_bf16_gather.hip", "gemm_inst_f16_gather.hip", "gemm_inst_bf16_leaves.hip", "gemm_inst_f16_leaves.hip",
            "gemm_inst_bf16_wide.hip", "gemm_inst_f16_wide.hip",
            "mx_plan.cpp", "mx_gemm_plan.cpp", "mx_capi.cpp", "mx_kernels.hip", "mx_gemm_kernels.hip",
-           "mx_gemm_inst_direct_codes.hip", "mx_gemm_inst_direct_bf16.hip", "mx_gemm_inst_direct_f16.hip", "mx_gemm_inst_stream_codes.hip", "mx_gemm_inst_ring_codes.hip", "mx_gemm_inst_wide_bf16.hip", "mx_gemm_inst_wide_f16.hip",
+           "mx_gemm_inst_direct_codes.hip", "mx_gemm_inst_direct_bf16.hip", "mx_gemm_inst_direct_f16.hip", "mx_gemm_inst_stream_codes.hip", "mx_gemm_inst_ring_codes.hip", "mx_gemm_inst_wide_bf16_k.hip", "mx_gemm_inst_wide_bf16_rows.hip",
+           "mx_gemm_inst_wide_f16_k.hip", "mx_gemm_inst_wide_f16_rows.hip",
            "mx_gemm_inst_stream_bf16_k.hip", "mx_gemm_inst_stream_bf16_rows.hip", "mx_gemm_inst_stream_f16_k.hip", "mx_gemm_inst_stream_f16_rows.hip"]
 HEADERS = ["layout.hpp", "algebra.hpp", "semimodule.hpp", "plan.hpp", "kernel_params.hpp", "gemm_plan.hpp", "gemm_params.hpp", "plan_cache.hpp", "kernarg.hpp"]
 # header -> the only sources that include it
@@ -27,7 +28,7 @@ _GATHER = ["gemm_inst_%s_%s.hip" % (t, g) for t in ("bf16", "f16") for g in ("ga
 _MX_DIRECT = ["mx_gemm_inst_direct_%s.hip" % t for t in ("codes", "bf16", "f16")]
 _MX_STREAM = ["mx_gemm_inst_stream_%s.hip" % t for t in ("codes", "bf16_k", "bf16_rows", "f16_k", "f16_rows")]
 _MX_RING = ["mx_gemm_inst_ring_codes.hip"]
-_MX_WIDE = ["mx_gemm_inst_wide_bf16.hip", "mx_gemm_inst_wide_f16.hip"]
+_MX_WIDE = ["mx_gemm_inst_wide_%s_%s.hip" % (t, k) for t in ("bf16", "f16") for k in ("k", "rows")]
 _WIDE = ["gemm_inst_%s_wide.hip" % t for t in ("bf16", "f16")]
 _MX_GEMM = _MX_DIRECT + _MX_STREAM + _MX_RING + _MX_WIDE + ["mx_gemm_plan.cpp", "mx_gemm_kernels.hip", "mx_capi.cpp"]
 _MX = _MX_GEMM + ["mx_plan.cpp", "mx_kernels.hip"]

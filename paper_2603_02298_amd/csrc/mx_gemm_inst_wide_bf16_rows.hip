@@ -1,0 +1,8 @@
+// Instantiates the wide kernel for codes with blocks along the rows beside bf16 elements.
+#include "mx_gemm_wide_kernel.hpp"
+
+namespace lc {
+hipError_t launch_mx_wide_bf16_rows(const lc_mx_gemm_plan& plan, const unsigned char* a, const unsigned char* sa, const unsigned char* b, const unsigned char*, void* c, hipStream_t s) {
+  return launch_mx_wide_shape<kMxBf16, 0>(plan, a, sa, b, c, s);
+}
+}  // namespace lc

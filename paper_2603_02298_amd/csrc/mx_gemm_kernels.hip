@@ -16,8 +16,10 @@ LC_MX_LAUNCHER(launch_mx_direct_bf16);
 LC_MX_LAUNCHER(launch_mx_direct_f16);
 LC_MX_LAUNCHER(launch_mx_stream_codes);
 LC_MX_LAUNCHER(launch_mx_ring_codes);
-LC_MX_LAUNCHER(launch_mx_wide_bf16);
-LC_MX_LAUNCHER(launch_mx_wide_f16);
+LC_MX_LAUNCHER(launch_mx_wide_bf16_k);
+LC_MX_LAUNCHER(launch_mx_wide_bf16_rows);
+LC_MX_LAUNCHER(launch_mx_wide_f16_k);
+LC_MX_LAUNCHER(launch_mx_wide_f16_rows);
 LC_MX_LAUNCHER(launch_mx_stream_bf16_k);
 LC_MX_LAUNCHER(launch_mx_stream_bf16_rows);
 LC_MX_LAUNCHER(launch_mx_stream_f16_k);
@@ -49,8 +51,10 @@ lc_status_t execute_mx_gemm_plan(const lc_mx_gemm_plan& plan, const void* a, con
     pre = codes ? launch_mx_direct_codes(plan, ka, ksa, kb, ksb, c, s) : bf16 ? launch_mx_direct_bf16(plan, ka, ksa, kb, ksb, c, s) : launch_mx_direct_f16(plan, ka, ksa, kb, ksb, c, s);
   else if (plan.kernel == kMxRing && codes)
     pre = launch_mx_ring_codes(plan, ka, ksa, kb, ksb, c, s);
+  else if (plan.kernel == kMxWide && !codes && plan.blocked)
+    pre = bf16 ? launch_mx_wide_bf16_k(plan, ka, ksa, kb, ksb, c, s) : launch_mx_wide_f16_k(plan, ka, ksa, kb, ksb, c, s);
   else if (plan.kernel == kMxWide && !codes)
-    pre = bf16 ? launch_mx_wide_bf16(plan, ka, ksa, kb, ksb, c, s) : launch_mx_wide_f16(plan, ka, ksa, kb, ksb, c, s);
+    pre = bf16 ? launch_mx_wide_bf16_rows(plan, ka, ksa, kb, ksb, c, s) : launch_mx_wide_f16_rows(plan, ka, ksa, kb, ksb, c, s);
   else if (plan.kernel == kMxStream && codes)
     pre = launch_mx_stream_codes(plan, ka, ksa, kb, ksb, c, s);
   else if (plan.kernel == kMxStream && plan.blocked)

@@ -222,17 +222,45 @@ lc_status_t make_mx_gemm_plan(const Layout& A, const Layout* A_scales, const Lay
   else if (t_env == 256 && can_ring) take(kMxRing, 256, 256, 4);
   else if (t_env == 256 && can_wide) take(kMxWide, 256, 256, 4);
   else if (t_env == 256128 && can_wide) take(kMxWide, 256, 128, 4);
-  else if (can_direct && b.rows <= 16) take(kMxDirect, tiles_of(32, 16) >= 256 ? 32 : 16, 16, 8);
-  else if (can_direct && tiles_of(32, 32) <= 512) take(kMxDirect, 32, 32, 8);
-  else if (codes && tiles_of(64, 64) <= 512) take(kMxStream, 64, 64, 4);
-  else if (can_ring && tiles_of(256, 256) >= 128) take(kMxRing, 256, 256, 4);
-  else if (can_wide && tiles_of(256, 256) >= 192) take(kMxWide, 256, 256, 4);
-  else if (can_wide && tiles_of(256, 128) >= 96) take(kMxWide, 256, 128, 4);
-  else if (tiles_of(128, 128) <= 256) take(kMxStream, 128, 64, 4);
-  else take(kMxStream, 128, 128, 4);
+  else if (t_env == 128128 && can_wide) take(kMxWide, 128, 128, 4);
+  else if (t_env == 128064 && can_wide) take(kMxWide, 128, 64, 4);
+  else {
+    // What a choice costs is how many rounds of 256 tiles (one a CU) there are times what a round takes, and not less than what a tile takes
+    // alone; in microseconds at K = 4096, which all of them follow alike.  Measured on MI355X (us; direct 32 x 32, then the tiles by size):
+    //   both codes (64 x 64, 128 x 64, 128 x 128, 256 x 256): 64 x 4096 x 4096 9.8, 13.7, 15.7, -, -; 256 x 4096 x 4096 32.7, 14.5, 16.1, 19.8, -; 512 x 4096 x 4096
+    //   63, 17.9, 17.6, 20.8, 35.1; 1024 x 4096 x 4096 -, 25.9, 24.2, 24.0, 37.5; 2048 x 4096 x 4096 -, -, 38.0, 31.9, 38.3; 3000^2 x 2048 -, -, 26.5, 27.7, 26.8;
+    //   4096 x 8192 x 4096 -, -, -, 110, 89; 8192^3 -, -, -, 391, 302; 512 x 1024 x 1024 7.7, 6.5, 7.9, 9.7, -; 256^3 5.6, 4.6, -, -, -.
+    //   one in 16 bits (128 x 64, 128 x 128, 256 x 128, 256 x 256): 128 x 2048 x 2048 9.1, 18.0, 21.0, -, -; 128 x 8192 x 8192 61, 60, -, -, -; 256 x 4096 x 4096 38.9, 31.4,
+    //   36.3, 57, -; 512 x 4096 x 4096 78, 35.8, 39.6, 61, -; 1024 x 4096 x 4096 -, 55, 46, 65, 92; 2048 x 4096 x 4096 -, 102, 75, 74, 96; along the rows -, -, 92, 82, 100;
+    //   3000 x 5000 x 1024 -, 59, 43, 48, 40; 2048 x 8192 x 4096 -, -, -, 144, 116.
+    struct Choice { MxGemmKernel kernel; int tm, tn; double round, alone; bool can; };
+    const Choice choices[] = {
+        {kMxDirect, 32, 32, 9.5, 9.5, can_direct && (!codes || G.k_tiles > 2)},   // (both codes over one or two k tiles: the stream kernel starts with less)
+        {kMxStream, 64, 64, 6.5, 14.0, codes}, {kMxStream, 128, 64, 9.5, 17.0, codes}, {kMxStream, 128, 128, 16.0, 22.0, codes},
+        {kMxRing, 256, 256, 44.5, 36.0, can_ring && tiles_of(256, 256) >= 96},
+        {kMxWide, 128, 64, 26.0, 34.0, can_wide}, {kMxWide, 128, 128, 37.5, 44.0, can_wide}, {kMxWide, 256, 128, 72.0, 72.0, can_wide}, {kMxWide, 256, 256, 112.0, 112.0, can_wide},
+        {kMxStream, 128, 64, 30.0, 44.0, !codes && !can_wide}, {kMxStream, 128, 128, 43.0, 57.0, !codes && !can_wide}};
+    auto cost = [&](const Choice& c) {
+      const double rounds = (double)((tiles_of(c.tm, c.tn) + 255) / 256);
+      return c.kernel == kMxRing && tiles_of(c.tm, c.tn) <= 128 ? c.alone : std::max(c.alone, rounds * c.round);
+    };
+    const Choice* best = nullptr;
+    for (const Choice& c : choices)
+      if (c.can && (!best || cost(c) < cost(*best))) best = &c;
+    take(best->kernel, best->tm, best->tn, 4);
+    // The direct kernel reads operands once per tile, but where CUs would be left over, smaller tiles give them work: the smallest that are
+    // at most one a CU.  (us; 16 x 16, 32 x 16, 32 x 32: both codes 256^2 x 2048 6.0, -, 7.5; 123 x 1001 x 544 6.8, 6.2, 6.7; one in 16 bits 64 x 512 x 2048 5.6, 6.9,
+    // 8.5; 16 x 1024 x 1024 4.8, 5.5, 6.2; 16 x 8192 x 8192 14.0, 12.9, 15.8.)  Up to four rows are loaded a quarter of a fragment at a time, which bears
+    // two tiles a CU (1 x 8192 x 8192 10.2, 11.0; 1 x 32768 x 8192 32.9, 27.9).
+    if (plan.kernel == kMxDirect) {
+      const int64_t most = !codes && b.rows <= 4 ? 512 : 256;
+      if (tiles_of(16, 16) <= most) take(kMxDirect, 16, 16, 8);
+      else if (tiles_of(32, 16) <= most || b.rows <= 16) take(kMxDirect, 32, 16, 8);
+    }
+  }
   plan.lds_bytes = plan.kernel == kMxStream ? 2u * (unsigned)(plan.tile_m + plan.tile_n) * 128u
                    : plan.kernel == kMxRing ? 5u * 256u * 128u
-                   : plan.kernel == kMxWide ? (2u * 256u + 3u * (unsigned)plan.tile_n) * 128u : 0u;
+                   : plan.kernel == kMxWide ? (2u * (unsigned)plan.tile_m + 3u * (unsigned)plan.tile_n) * 128u : 0u;
   if (plan.kernel == kMxDirect) {
     const int chunks = (int)((P.blocks + 3) / 4), w_env = env_int("LC_TUNE_MX_WAVES", 0);
     plan.waves = w_env == 4 || w_env == 8 ? w_env : chunks <= 8 ? 4 : 8;

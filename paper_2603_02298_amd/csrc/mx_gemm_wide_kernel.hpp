@@ -1,12 +1,12 @@
-// Device code of the wide kernel of the GEMM with one operand in microscaled 4-bit codes: tiles of 256 rows of codes by BN (256 or 128) rows of a
-// 16-bit operand, for problems with enough of them.
+// Device code of the wide kernel of the GEMM with one operand in microscaled 4-bit codes: tiles of BM rows of codes (256 or 128) by BN rows
+// of a 16-bit operand, for problems with enough of them.
 //
-// Four wavefronts own a tile, wavefront (wm, wn) 128 x BN / 2 of it.  A k tile is 64 k.  The 16-bit operand's tiles go straight into three
+// Four wavefronts own a tile, wavefront (wm, wn) BM / 2 x BN / 2 of it.  A k tile is 64 k.  The 16-bit operand's tiles go straight into three
 // places of LDS, two k tiles ahead.  The codes' tiles pass through registers: fetched two at a time a pair ahead (few workgroups share them, so they
 // come from further away), expanded to the other operand's type under the products of the k tile before theirs, and parked in one of two places.  One barrier per k tile, between its third and
 // fourth k step: by then every wavefront has its last fragments of the k tile, and the next one is complete.
-// The matrix cores take BN / 16 x 32 clocks per k step and wavefront and LDS delivers (4 + BN / 64) KiB to it meanwhile; expanding adds 32 conversions
-// and 8 writes per lane and k tile, which lie between products.
+// A wavefront's k step is FM FN products of 32 clocks and FM + FN fragments of 1 KiB from LDS; expanding adds 16 conversions and 4 writes per block of
+// a lane, which lie between products.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -17,12 +17,12 @@
 
 namespace lc {
 
-constexpr unsigned mx_wide_lds(int bn) { return (2u * 256u + 3u * (unsigned)bn) * 128u; }
+constexpr unsigned mx_wide_lds(int bm, int bn) { return (2u * (unsigned)bm + 3u * (unsigned)bn) * 128u; }
 
-template <int MATH, int BLOCKED, int BN>
-__global__ __launch_bounds__(kBlock, 1) void mx_wide_kernel(MxGemmParams P, const unsigned char* __restrict__ A, const unsigned char* __restrict__ SA,
+template <int MATH, int BLOCKED, int BM, int BN>
+__global__ __launch_bounds__(kBlock, 160 * 1024 / mx_wide_lds(BM, BN)) void mx_wide_kernel(MxGemmParams P, const unsigned char* __restrict__ A, const unsigned char* __restrict__ SA,
                                                             const unsigned char* __restrict__ B, void* __restrict__ C) {
-  constexpr int BM = 256, FM = 4, FN = BN / 64, RB = BN / 32, RA = 8, MFMAS = FM * FN;
+  constexpr int FM = BM / 64, FN = BN / 64, RB = BN / 32, UNITS = BM / 128, RA = 4 * UNITS;   // RB, RA: loads of a k tile's elements, of two k tiles' codes
   constexpr int A_LOAD = BLOCKED ? kLoadKDirect : kLoadRDirect;
   constexpr uint32_t A_SLOT = BM * 128u, B_AT = 2u * A_SLOT, B_SLOT = BN * 128u;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
@@ -59,7 +59,7 @@ __global__ __launch_bounds__(kBlock, 1) void mx_wide_kernel(MxGemmParams P, cons
   // tiles: a constant offset.
   uint32_t a_fr[FM], b_fr[FN];   // (b_fr: in the place of the k tile being multiplied)
   static_for<FM>([&](auto i) {
-    const uint32_t row = wm * 128u + 32u * (uint32_t)i;
+    const uint32_t row = wm * (BM / 2u) + 32u * (uint32_t)i;
     a_fr[i] = BLOCKED ? gemm_lds_offset(row + mfma_ab_row(lane), mfma_ab_kvec(lane)) : gemm_rdirect_frag_offset(BM, lane, row, 8u * mfma_ab_kvec(lane));
   });
   static_for<FN>([&](auto j) { b_fr[j] = B_AT + gemm_lds_offset(wn * (BN / 2u) + 32u * (uint32_t)j + mfma_ab_row(lane), mfma_ab_kvec(lane)); });
@@ -68,14 +68,15 @@ __global__ __launch_bounds__(kBlock, 1) void mx_wide_kernel(MxGemmParams P, cons
     else af[buf][i] = lds_read_tr_16x8<BM>(lds + a_fr[i] + decltype(a_slot)::value * A_SLOT, kk);
   };
   auto read_b = [&](auto j, auto kk, auto buf) { bf[buf][j] = *reinterpret_cast<const u32x4*>(lds + (b_fr[j] ^ (32u * (uint32_t)kk))); };
-  // One k step in four parts, in this order: a row of products each, and before them in the first three the reads of the next k step's
-  // fragments, in every one what `more` does.  Nothing crosses the parts, so that what is not a product lies between products.
+  // One k step in FM parts, in this order: a row of products each, and before them the reads of the next k step's fragments (in the first parts) and
+  // what `more` does.  Nothing crosses the parts, so that what is not a product lies between products.
   auto k_step = [&](auto buf, auto next_kk, auto a_slot, auto&& more) {
     constexpr int nbuf = 1 - decltype(buf)::value;
     using Other = std::integral_constant<int, nbuf>;
     static_for<FM>([&](auto i) {
       if constexpr (i == 0) static_for<FN>([&](auto j) { read_b(j, next_kk, Other{}); });
-      if constexpr (i == 1 || i == 2) static_for<2>([&](auto d) { read_a(std::integral_constant<int, 2 * (decltype(i)::value - 1) + decltype(d)::value>{}, next_kk, Other{}, a_slot); });
+      if constexpr (FM == 2 ? i == 0 : i == 1 || i == 2)
+        static_for<2>([&](auto d) { read_a(std::integral_constant<int, (FM == 2 ? 0 : 2 * (decltype(i)::value - 1)) + decltype(d)::value>{}, next_kk, Other{}, a_slot); });
       more(i);
       static_for<FN>([&](auto j) { acc[i][j] = mfma_32x32x16<MATH == kMxBf16>(af[buf][i], bf[buf][j], acc[i][j]); });
       __builtin_amdgcn_sched_barrier(0);
@@ -125,28 +126,36 @@ __global__ __launch_bounds__(kBlock, 1) void mx_wide_kernel(MxGemmParams P, cons
     unsigned char* a_next = lds + Next::value * A_SLOT;
     // k steps 0 and 1: the codes of kt + 1 are expanded and parked; before them, after an odd k tile, the codes of the pair after the next are
     // asked for; k steps 1 and 2: the 16-bit operand of k tile kt + 2
+    auto park = [&](auto part) {   // of the 4 UNITS parts
+      constexpr int p = decltype(part)::value;
+      la.template park<p / 4, p % 4>(a_next, codes);
+    };
+    auto ask_b = [&](auto part) {   // of 2 FM parts
+      constexpr int p = decltype(part)::value;
+      lb.template fetch<p * RB / (2 * FM), (p + 1) * RB / (2 * FM)>(b2, b_wave + b_far, kt + 2u >= last);
+    };
     k_step(Zero{}, One{}, Now{}, [&](auto i) {
       if constexpr (ASK && i < 2) la.fetch(codes_at[i], scales_at[i], kt + 3u + (uint32_t)i >= last, fill[i]);
-      la.template park<0, (int)decltype(i)::value>(a_next, codes);
+      park(std::integral_constant<int, decltype(i)::value>{});
     });
     asm volatile("" ::: "memory");   // the wait below counts the codes' loads as older than those that follow: no load is moved across
     k_step(One{}, Two{}, Now{}, [&](auto i) {
-      if constexpr (i % 2 == 0) lb.template fetch<i * RB / 8, (i + 2) * RB / 8>(b2, b_wave + b_far, kt + 2u >= last);
-      la.template park<1, (int)decltype(i)::value>(a_next, codes);
+      ask_b(std::integral_constant<int, decltype(i)::value>{});
+      park(std::integral_constant<int, FM + decltype(i)::value>{});
     });
-    k_step(Zero{}, Three{}, Now{}, [&](auto i) {
-      if constexpr (i % 2 == 0) lb.template fetch<RB / 2 + i * RB / 8, RB / 2 + (i + 2) * RB / 8>(b2, b_wave + b_far, kt + 2u >= last);
-    });
+    k_step(Zero{}, Three{}, Now{}, [&](auto i) { ask_b(std::integral_constant<int, FM + decltype(i)::value>{}); });
     // all but the 16-bit operand of k tile kt + 2 and the codes just asked for (they were before those; after an even k tile the codes have landed)
     wait_loads_but(std::integral_constant<int, RB + (ASK ? RA : 0)>{});
     lds_barrier();
     static_for<FN>([&](auto j) { b_fr[j] += b_next - b_now; });
     b_now = b_next;
     k_step(One{}, Zero{}, Next{}, [&](auto i) {
-      constexpr int pair = i / 2;
-      if constexpr (!ODD && i % 2 == 0) codes_at[pair] = CodesLoader::codes_at(P, at_most_last(kt + 4u + (uint32_t)pair));
-      if constexpr (!ODD && i % 2 == 1) scales_at[pair] = CodesLoader::scales_at(P, at_most_last(kt + 4u + (uint32_t)pair));
-      if constexpr (i == 3) b2 = b_bytes(at_most_last(kt + 3u));
+      static_for<4>([&](auto e) {
+        constexpr int pair = e / 2;
+        if constexpr (!ODD && e * FM / 4 == i && e % 2 == 0) codes_at[pair] = CodesLoader::codes_at(P, at_most_last(kt + 4u + (uint32_t)pair));
+        if constexpr (!ODD && e * FM / 4 == i && e % 2 == 1) scales_at[pair] = CodesLoader::scales_at(P, at_most_last(kt + 4u + (uint32_t)pair));
+      });
+      if constexpr (i == FM - 1) b2 = b_bytes(at_most_last(kt + 3u));
     });
   };
   uint32_t kt = 0;
@@ -167,7 +176,7 @@ __global__ __launch_bounds__(kBlock, 1) void mx_wide_kernel(MxGemmParams P, cons
   lds_barrier();
 
   // the sums through LDS, a column of fragments of a wavefront at a time and each wavefront in a place of its own
-  unsigned char* mine = lds + wave * (128u * 32u * 4u);
+  unsigned char* mine = lds + wave * (BM / 2u * 32u * 4u);
   const MxGemmParams& E = mx_params_again();
   mx_c_dispatch(E, [&](auto type, auto add) {
     static_for<FN>([&](auto j) {
@@ -175,37 +184,38 @@ __global__ __launch_bounds__(kBlock, 1) void mx_wide_kernel(MxGemmParams P, cons
         static_for<4>([&](auto g) {
           f32x4 v;
           static_for<4>([&](auto e) { v[(int)e] = acc[i][j][4 * g + e]; });
-          *reinterpret_cast<f32x4*>(mine + gemm_sum_unit(128u, 32u, 8u * (uint32_t)i + mfma_c_row(lane, 4u * (uint32_t)g) / 4u, mfma_c_col(lane)) * 16u) = v;
+          *reinterpret_cast<f32x4*>(mine + gemm_sum_unit(BM / 2u, 32u, 8u * (uint32_t)i + mfma_c_row(lane, 4u * (uint32_t)g) / 4u, mfma_c_col(lane)) * 16u) = v;
         });
       });
       asm volatile("" ::: "memory");   // (a wavefront's LDS accesses are carried out in order)
-      const uint32_t m = m0 + wm * 128u, n = n0 + wn * (BN / 2u) + 32u * (uint32_t)j;
-      if (E.g.c_vec) mx_tile_to_c_as<128, 32, 64, decltype(type)::value, decltype(add)::value, true>(E, C, mine, m, n, lane);
-      else mx_tile_to_c_as<128, 32, 64, decltype(type)::value, decltype(add)::value, false>(E, C, mine, m, n, lane);
+      const uint32_t m = m0 + wm * (BM / 2u), n = n0 + wn * (BN / 2u) + 32u * (uint32_t)j;
+      if (E.g.c_vec) mx_tile_to_c_as<BM / 2, 32, 64, decltype(type)::value, decltype(add)::value, true>(E, C, mine, m, n, lane);
+      else mx_tile_to_c_as<BM / 2, 32, 64, decltype(type)::value, decltype(add)::value, false>(E, C, mine, m, n, lane);
       asm volatile("" ::: "memory");
     });
   });
 }
 
-template <int MATH, int BLOCKED, int BN>
+template <int MATH, int BLOCKED, int BM, int BN>
 static inline hipError_t launch_mx_wide(const lc_mx_gemm_plan& plan, const unsigned char* a, const unsigned char* sa, const unsigned char* b, void* c, hipStream_t s) {
-  if (plan.lds_bytes != mx_wide_lds(BN) || plan.b_load != kLoadKDirect || plan.blocked != BLOCKED) return hipErrorInvalidValue;
+  if (plan.lds_bytes != mx_wide_lds(BM, BN) || plan.b_load != kLoadKDirect || plan.blocked != BLOCKED) return hipErrorInvalidValue;
   static std::atomic<bool> raised{false};   // one flag per instantiation: the attribute belongs to the kernel function
-  if (!raised.load(std::memory_order_acquire)) {
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&mx_wide_kernel<MATH, BLOCKED, BN>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+  if (plan.lds_bytes > 64 * 1024 && !raised.load(std::memory_order_acquire)) {
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&mx_wide_kernel<MATH, BLOCKED, BM, BN>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
     if (e != hipSuccess) return e;
     raised.store(true, std::memory_order_release);
   }
   const unsigned grid = plan.params.g.tiles_m * plan.params.g.tiles_n * plan.params.g.L;
-  hipLaunchKernelGGL((mx_wide_kernel<MATH, BLOCKED, BN>), dim3(grid), dim3(kBlock), plan.lds_bytes, s, plan.params, a, sa, b, c);
+  hipLaunchKernelGGL((mx_wide_kernel<MATH, BLOCKED, BM, BN>), dim3(grid), dim3(kBlock), plan.lds_bytes, s, plan.params, a, sa, b, c);
   return hipSuccess;
 }
-template <int MATH>
+template <int MATH, int BLOCKED>
 static inline hipError_t launch_mx_wide_shape(const lc_mx_gemm_plan& plan, const unsigned char* a, const unsigned char* sa, const unsigned char* b, void* c,
                                               hipStream_t s) {
-  if (plan.tile_m != 256) return hipErrorInvalidValue;
-  if (plan.tile_n == 256) return plan.blocked ? launch_mx_wide<MATH, 1, 256>(plan, a, sa, b, c, s) : launch_mx_wide<MATH, 0, 256>(plan, a, sa, b, c, s);
-  if (plan.tile_n == 128) return plan.blocked ? launch_mx_wide<MATH, 1, 128>(plan, a, sa, b, c, s) : launch_mx_wide<MATH, 0, 128>(plan, a, sa, b, c, s);
+  if (plan.tile_m == 256 && plan.tile_n == 256) return launch_mx_wide<MATH, BLOCKED, 256, 256>(plan, a, sa, b, c, s);
+  if (plan.tile_m == 256 && plan.tile_n == 128) return launch_mx_wide<MATH, BLOCKED, 256, 128>(plan, a, sa, b, c, s);
+  if (plan.tile_m == 128 && plan.tile_n == 128) return launch_mx_wide<MATH, BLOCKED, 128, 128>(plan, a, sa, b, c, s);
+  if (plan.tile_m == 128 && plan.tile_n == 64) return launch_mx_wide<MATH, BLOCKED, 128, 64>(plan, a, sa, b, c, s);
   return hipErrorInvalidValue;
 }
 

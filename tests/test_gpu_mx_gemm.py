@@ -152,7 +152,7 @@ MIXED = [(1, 1, 1), (1, 40, 64), (1, 1000, 1024), (2, 17, 100), (5, 33, 33), (16
 
 @pytest.mark.parametrize("M,N,K", MIXED)
 @pytest.mark.parametrize("a_dtype", ["bf16", "f16"])
-@pytest.mark.parametrize("tile", [0, 16, 3216, 32, 12864, 128, 256, 256128])
+@pytest.mark.parametrize("tile", [0, 16, 3216, 32, 12864, 128, 256, 256128, 128128, 128064])
 def test_weights(M, N, K, a_dtype, tile, monkeypatch):
     if tile:
         monkeypatch.setenv("LC_TUNE_MX_TILE", str(tile))
@@ -164,7 +164,7 @@ def test_weights(M, N, K, a_dtype, tile, monkeypatch):
 
 @pytest.mark.parametrize("M,K,N", MIXED)
 @pytest.mark.parametrize("a_dtype", ["bf16", "f16"])
-@pytest.mark.parametrize("tile", [0, 12864, 128, 256, 256128])
+@pytest.mark.parametrize("tile", [0, 12864, 128, 256, 256128, 128128, 128064])
 def test_transposed_weights(M, N, K, a_dtype, tile, monkeypatch):
     """The gradient of the forward product's A: the sum runs over N, B is blocked along the rows of the result."""
     if tile:
@@ -187,7 +187,7 @@ def test_transposed_weights(M, N, K, a_dtype, tile, monkeypatch):
     ("(70,90):(1,70)", "((32,10),90):((1,2880),32)", "(10,90):(90,1)", "(70,300):(1,70)", 0),
     ("(33,50,3):(56,1,2000)", "(320,50,3):(1,320,0)", "(10,50,3):(1,10,0)", "(33,304,3):(304,1,10032)", 0),
 ])
-@pytest.mark.parametrize("tile", [0, 32, 128, 256, 256128])
+@pytest.mark.parametrize("tile", [0, 32, 128, 256, 256128, 128128, 128064])
 @pytest.mark.parametrize("a_dtype", ["bf16", "f16"])
 def test_layouts_of_mixed_operands(a, b, b_s, c, blocked, tile, a_dtype, monkeypatch):
     if tile:
@@ -197,7 +197,7 @@ def test_layouts_of_mixed_operands(a, b, b_s, c, blocked, tile, a_dtype, monkeyp
 
 
 @pytest.mark.parametrize("a_dtype,blocked", [("mxfp4", 1), ("bf16", 1), ("f16", 1), ("bf16", 0), ("f16", 0)])
-@pytest.mark.parametrize("tile", [0, 32, 128, 256, 256128])
+@pytest.mark.parametrize("tile", [0, 32, 128, 256, 256128, 128128, 128064])
 def test_nan_scales_reach_what_they_enter_and_nothing_else(a_dtype, tile, blocked, monkeypatch):
     if tile:
         monkeypatch.setenv("LC_TUNE_MX_TILE", str(tile))
@@ -223,7 +223,7 @@ def test_nan_scales_reach_what_they_enter_and_nothing_else(a_dtype, tile, blocke
 
 
 @pytest.mark.parametrize("a_dtype", ["bf16", "f16"])
-@pytest.mark.parametrize("tile", [0, 32, 128, 256, 256128])
+@pytest.mark.parametrize("tile", [0, 32, 128, 256, 256128, 128128, 128064])
 def test_blocks_past_k_are_not_used(a_dtype, tile, monkeypatch):
     """K = 72 of 256: what lies in the blocks past it, NaN scales among it, stays out of the sum."""
     if tile:
