@@ -100,42 +100,59 @@ __device__ __forceinline__ uint32_t quad_swap1(uint32_t v) { return (uint32_t)__
 __device__ __forceinline__ uint32_t quad_swap2(uint32_t v) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true); }
 
 // ---------------------------------------------------------------------------------------------
-// Along k, or element by element: four lanes share a block, eight consecutive k each; kMxUnroll blocks' loads per lane are in
-// flight before the first is used.  WHOLE: K is a multiple of 8, so that a vector lies inside or outside as a whole.
+// Along k, or element by element: four lanes share a block, eight consecutive k each; kMxUnroll rows' loads per lane are in flight
+// before the first is used.  WHOLE: K is a multiple of 8, so that a vector lies inside or outside as a whole.
+// Memory bounds it.  8192 x 8192 bf16, scales in groups of eight blocks: quantised in 42 us, 4.0 TB/s, dequantised in 27.5 us, 6.2 TB/s
+// (codes still in the caches).  The order of the tiles decides: neighbouring workgroups along k write and read whole lines of a row, 50 and
+// 35 us became 42 and 27.5 when they no longer went along the rows.
 // ---------------------------------------------------------------------------------------------
+
+// Where a lane's rows are in a tensor: base + u * step where the rows' mode has one leaf, evaluated row by row otherwise.
+struct RowWalk {
+  const MxMode& mode;
+  int64_t first, step;
+  uint32_t row, rows;
+  __device__ __forceinline__ RowWalk(const MxMode& m, uint32_t row0, uint32_t rows_at_a_time, int64_t along)
+      : mode(m), first((m.n == 1 ? mx_mode_eval(m, row0) : 0) + along), step(m.last_stride * rows_at_a_time), row(row0), rows(rows_at_a_time) {}
+  __device__ __forceinline__ int64_t operator()(uint32_t u) const { return mode.n == 1 ? first + u * step : first + mx_mode_eval(mode, row + u * rows); }
+};
+
 template <int DT, bool VECTORS, bool WHOLE>
 __device__ __forceinline__ void quantize_along_k(const MxCopyParams& P, const unsigned char* x, unsigned char* q, unsigned char* s) {
   constexpr int ES = kElemBytes<DT>, DW = 2 * ES;   // dwords of eight elements
-  const uint32_t tid = threadIdx.x, part = tid & 3u, total = P.R * P.blocks;
+  const uint32_t tid = threadIdx.x, part = tid & 3u;
+  uint32_t row, block;
+  mx_unit_of(P, blockIdx.x, tid >> 2, &row, &block);
+  const uint32_t rows = mx_rows_at_a_time(P), k0 = block * kMxBlock + 8u * part;
+  if (block >= P.blocks || row >= P.R) return;   // (whole groups of four lanes)
+  const bool in = VECTORS && (WHOLE ? k0 < P.K : k0 + 8u <= P.K);   // a vector that lies inside
+  const RowWalk at(P.x_r, row, rows, in ? mx_mode_eval(P.x_k, k0) : 0);
   uint32_t v[kMxUnroll][DW];
-  uint32_t row[kMxUnroll], block[kMxUnroll];
-  static_for<(int)kMxUnroll>([&](auto u) {
-    const uint32_t id = blockIdx.x * kMxBlocksPerGroup + (uint32_t)u * 64u + (tid >> 2);
-    mx_block_of(P, id < total ? id : total - 1u, &row[u], &block[u]);
-    const uint32_t k0 = block[u] * kMxBlock + 8u * part;
-    const unsigned char* xr = x + mx_mode_eval(P.x_r, row[u]);
-    if constexpr (VECTORS && WHOLE) {
-      const bool in = k0 < P.K;   // (a vector outside reads the row's first instead)
-      const unsigned char* p = xr + mx_mode_eval(P.x_k, in ? k0 : 0u);
-      static_for<DW / 4>([&](auto d) {
-        const u32x4 w = select_or_zero(in, reinterpret_cast<const u32x4_any*>(p)[(int)d]);
-        static_for<4>([&](auto e) { v[u][4 * d + e] = w[(int)e]; });
-      });
-    } else if (VECTORS && k0 + 8u <= P.K) {
-      const unsigned char* p = xr + mx_mode_eval(P.x_k, k0);
-      static_for<DW / 4>([&](auto d) {
-        const u32x4 w = reinterpret_cast<const u32x4_any*>(p)[(int)d];
-        static_for<4>([&](auto e) { v[u][4 * d + e] = w[(int)e]; });
-      });
-    } else {
-      static_for<8>([&](auto j) {
-        const uint32_t k = k0 + (uint32_t)j;
-        const uint32_t e = k < P.K ? load_element<DT>(xr + mx_mode_eval(P.x_k, k)) : 0u;
-        if constexpr (DT == LC_F32) v[u][(int)j] = e;
-        else v[u][j / 2] = j % 2 ? v[u][j / 2] | (e << 16) : e;
-      });
-    }
-  });
+  if (in) {   // (no branch between the loads: a row past the last loads the lane's first again)
+    u32x4 w[kMxUnroll][DW / 4];
+    static_for<(int)kMxUnroll>([&](auto u) {
+      const unsigned char* p = x + at(row + (uint32_t)u * rows < P.R ? (uint32_t)u : 0u);
+      static_for<DW / 4>([&](auto d) { w[u][d] = reinterpret_cast<const u32x4_any*>(p)[(int)d]; });
+    });
+    __builtin_amdgcn_sched_barrier(0);
+    static_for<(int)kMxUnroll>([&](auto u) { static_for<DW>([&](auto d) { v[u][d] = w[u][d / 4][d % 4]; }); });
+  } else {
+    static_for<(int)kMxUnroll>([&](auto u) {
+      static_for<DW>([&](auto d) { v[u][d] = 0u; });
+      if constexpr (!(VECTORS && WHOLE)) {
+        if (row + (uint32_t)u * rows < P.R) {
+          const unsigned char* p = x + at((uint32_t)u);
+          static_for<8>([&](auto j) {
+            const uint32_t k = k0 + (uint32_t)j;
+            const uint32_t e = k < P.K ? load_element<DT>(p + mx_mode_eval(P.x_k, k)) : 0u;
+            if constexpr (DT == LC_F32) v[u][(int)j] = e;
+            else v[u][j / 2] = j % 2 ? v[u][j / 2] | (e << 16) : e;
+          });
+        }
+      }
+    });
+  }
+  const RowWalk q_at(P.q_r, row, rows, mx_mode_eval(P.q_b, block) + 4 * part), s_at(P.s_r, row, rows, mx_mode_eval(P.s_b, block));
   static_for<(int)kMxUnroll>([&](auto u) {
     uint32_t m = magnitude_of<DT>(v[u][0]);
     static_for<DW - 1>([&](auto d) { m = max_of<DT>(m, magnitude_of<DT>(v[u][d + 1])); });
@@ -146,9 +163,9 @@ __device__ __forceinline__ void quantize_along_k(const MxCopyParams& P, const un
     uint32_t codes = 0u;
     static_for<4>([&](auto i) { codes = pack_codes<DT, i>(codes, v[u][DT == LC_F32 ? 2 * i : i], v[u][DT == LC_F32 ? 2 * i + 1 : i], scale); });
     if (byte == 255u) codes = 0u;
-    if (blockIdx.x * kMxBlocksPerGroup + (uint32_t)u * 64u + (tid >> 2) < total) {
-      *reinterpret_cast<uint32_t*>(q + mx_mode_eval(P.q_r, row[u]) + mx_mode_eval(P.q_b, block[u]) + 4u * part) = codes;
-      if (part == 0u) s[mx_mode_eval(P.s_r, row[u]) + mx_mode_eval(P.s_b, block[u])] = (unsigned char)byte;
+    if (row + (uint32_t)u * rows < P.R) {
+      *reinterpret_cast<uint32_t*>(q + q_at((uint32_t)u)) = codes;
+      if (part == 0u) s[s_at((uint32_t)u)] = (unsigned char)byte;
     }
   });
 }
@@ -166,16 +183,23 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(MxCopyParams P, cons
                                                             unsigned char* __restrict__ x) {
   constexpr int ES = kElemBytes<DT>, DW = 2 * ES;
   touch_kernel_arguments<kMxKernargs>();
-  const uint32_t tid = threadIdx.x, part = tid & 3u, total = P.R * P.blocks;
-  uint32_t codes[kMxUnroll], byte[kMxUnroll], row[kMxUnroll], block[kMxUnroll];
+  const uint32_t tid = threadIdx.x, part = tid & 3u;
+  uint32_t row, block;
+  mx_unit_of(P, blockIdx.x, tid >> 2, &row, &block);
+  const uint32_t rows = mx_rows_at_a_time(P), k0 = block * kMxBlock + 8u * part;
+  if (block >= P.blocks || row >= P.R) return;
+  const bool in = VECTORS && k0 + 8u <= P.K;
+  const RowWalk q_at(P.q_r, row, rows, mx_mode_eval(P.q_b, block) + 4 * part), s_at(P.s_r, row, rows, mx_mode_eval(P.s_b, block));
+  uint32_t codes[kMxUnroll], byte[kMxUnroll];
   static_for<(int)kMxUnroll>([&](auto u) {
-    const uint32_t id = blockIdx.x * kMxBlocksPerGroup + (uint32_t)u * 64u + (tid >> 2);
-    mx_block_of(P, id < total ? id : total - 1u, &row[u], &block[u]);
-    codes[u] = *reinterpret_cast<const uint32_t*>(q + mx_mode_eval(P.q_r, row[u]) + mx_mode_eval(P.q_b, block[u]) + 4u * part);
-    byte[u] = s[mx_mode_eval(P.s_r, row[u]) + mx_mode_eval(P.s_b, block[u])];
+    const uint32_t from = row + (uint32_t)u * rows < P.R ? (uint32_t)u : 0u;   // (a row past the last reads the lane's first instead)
+    codes[u] = *reinterpret_cast<const uint32_t*>(q + q_at(from));
+    byte[u] = s[s_at(from)];
   });
+  __builtin_amdgcn_sched_barrier(0);
+  const RowWalk at(P.x_r, row, rows, in ? mx_mode_eval(P.x_k, k0) : 0);
   static_for<(int)kMxUnroll>([&](auto u) {
-    if (blockIdx.x * kMxBlocksPerGroup + (uint32_t)u * 64u + (tid >> 2) >= total) return;
+    if (row + (uint32_t)u * rows >= P.R) return;
     const float scale = scale_value(byte[u]);
     uint32_t v[DW];
     static_for<4>([&](auto i) {
@@ -183,110 +207,163 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(MxCopyParams P, cons
       if constexpr (DT == LC_F32) { v[2 * i] = w[0]; v[2 * i + 1] = w[1]; }
       else v[(int)i] = w[0];
     });
-    const uint32_t k0 = block[u] * kMxBlock + 8u * part;
-    unsigned char* xr = x + mx_mode_eval(P.x_r, row[u]);
-    if (VECTORS && k0 + 8u <= P.K) {
-      unsigned char* p = xr + mx_mode_eval(P.x_k, k0);
+    unsigned char* p = x + at((uint32_t)u);
+    if (in) {
       static_for<DW / 4>([&](auto d) { reinterpret_cast<u32x4_any*>(p)[(int)d] = u32x4{v[4 * d], v[4 * d + 1], v[4 * d + 2], v[4 * d + 3]}; });
     } else {
       static_for<8>([&](auto j) {
         const uint32_t k = k0 + (uint32_t)j;
-        if (k < P.K) store_element<DT>(xr + mx_mode_eval(P.x_k, k), DT == LC_F32 ? v[(int)j % DW] : v[j / 2] >> (16 * (j % 2)));
+        if (k < P.K) store_element<DT>(p + mx_mode_eval(P.x_k, k), DT == LC_F32 ? v[(int)j % DW] : v[j / 2] >> (16 * (j % 2)));
       });
     }
   });
 }
 
 // ---------------------------------------------------------------------------------------------
-// Along the rows: a lane holds the 32 k of a block for the rows of one 16-byte vector, so blocks and the transposition between
-// the two sides stay in its registers; 8 x 8 lanes read (write) whole lines on one side and whole lines on the other.
+// Along the rows: lanes hold 16 bytes of rows at eight k each, and four lanes transpose their codes among them (mx_row_vector).
+// Quantisation collects a workgroup's blocks in LDS, which gives rows of eight blocks' codes and scales one store of 128 and of 8 bytes:
+// 4100 x 5003 f32 from columns in 36 us with every lane storing its own, 32 us so (2.9 TB/s; reads that start in the middle of a line are what
+// is left).  A lane with all 32 k of a block needs neither and took 33 us there, but 9.6 us instead of 7 for 4096 x 2048 bf16: too few waves.
+// Dequantisation of 8192 x 8192 bf16 into columns: 39 us, 4.4 TB/s.
+// The tiles are dealt to the XCDs in stretches (gemm_tile_order_of_block): 55 -> 50 us for the 4100 x 5003 f32 there and back.
 // ---------------------------------------------------------------------------------------------
-template <int DT>
-__global__ __launch_bounds__(256) void mx_quantize_rows_kernel(MxCopyParams P, uint32_t tiles_r, const unsigned char* __restrict__ x,
-                                                               unsigned char* __restrict__ q, unsigned char* __restrict__ s) {
-  constexpr uint32_t ROWS = 16 / kElemBytes<DT>;
-  touch_kernel_arguments<kMxKernargs + 8>();
-  uint32_t start, first, block;
-  mx_row_vector(P, ROWS, tiles_r, blockIdx.x * 4u + (threadIdx.x >> 6), threadIdx.x & 63u, &start, &first, &block);
-  if (first >= P.R || block >= P.blocks) return;
-  const unsigned char* p = x + mx_mode_eval(P.x_r, start);
-  u32x4 v[kMxBlock];
-  static_for<(int)kMxBlock>([&](auto k) {
-    const uint32_t at = block * kMxBlock + (uint32_t)k;
-    const bool in = at < P.K;   // (a k outside reads k = 0 instead)
-    v[(int)k] = select_or_zero(in, *reinterpret_cast<const u32x4_any*>(p + mx_mode_eval(P.x_k, in ? at : 0u)));
+
+// 4 x 4 over the wave's four rows of 16 lanes: v[j] of row i becomes v[i] of row j.
+__device__ __forceinline__ void transpose_rows(uint32_t (&v)[4]) {
+  static_for<2>([&](auto i) {
+    const u32x2 t = __builtin_amdgcn_permlane16_swap(v[2 * i], v[2 * i + 1], false, false);
+    v[2 * i] = t[0];
+    v[2 * i + 1] = t[1];
   });
+  static_for<2>([&](auto i) {
+    const u32x2 t = __builtin_amdgcn_permlane32_swap(v[(int)i], v[i + 2], false, false);
+    v[(int)i] = t[0];
+    v[i + 2] = t[1];
+  });
+}
+template <int DT>
+__device__ __forceinline__ uint32_t max_of_rows(uint32_t m) {
+  const u32x2 t = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+  m = max_of<DT>(t[0], t[1]);
+  const u32x2 w = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+  return max_of<DT>(w[0], w[1]);
+}
+
+template <int ROWS>
+constexpr uint32_t kMxRowPieces = kMxRowWaves * kMxRowLanes * ROWS;   // blocks of a workgroup
+
+template <int DT>
+__global__ __launch_bounds__(64 * kMxRowWaves) void mx_quantize_rows_kernel(MxCopyParams P, const unsigned char* __restrict__ x,
+                                                                          unsigned char* __restrict__ q, unsigned char* __restrict__ s) {
+  constexpr int ROWS = 16 / kElemBytes<DT>;
+  touch_kernel_arguments<kMxKernargs>();
+  const uint32_t lane = threadIdx.x & 63u, part = lane / kMxRowLanes;
+  uint32_t start, first, block;
+  mx_row_vector(P, ROWS, gemm_tile_order_of_block(blockIdx.x, gridDim.x), threadIdx.x >> 6, lane, &start, &first, &block);
+  const uint32_t group_row = first - ((threadIdx.x >> 6 >> P.block_shift) * kMxRowLanes + lane % kMxRowLanes) * ROWS;   // the workgroup's first
+  const uint32_t group_block = block - ((threadIdx.x >> 6) & ((1u << P.block_shift) - 1u));
+  __shared__ u32x4 s_codes[kMxRowPieces<ROWS> + kMxRowPieces<ROWS> / 8];
+  __shared__ unsigned char s_bytes[kMxRowPieces<ROWS>];
+  const unsigned char* p = x + mx_mode_eval(P.x_r, start);
+  const uint32_t k0 = block * kMxBlock + 8u * part;
+  const RowWalk at(P.x_k, k0, 1, 0);
+  u32x4 v[8];
+  static_for<8>([&](auto k) { v[(int)k] = *reinterpret_cast<const u32x4_any*>(p + (k0 + (uint32_t)k < P.K ? at((uint32_t)k) : 0)); });   // (a k outside reads k = 0)
+  __builtin_amdgcn_sched_barrier(0);
+  static_for<8>([&](auto k) { v[(int)k] = select_or_zero(k0 + (uint32_t)k < P.K, v[(int)k]); });
   u32x4 m;
   static_for<4>([&](auto d) {
     m[(int)d] = magnitude_of<DT>(v[0][(int)d]);
-    static_for<(int)kMxBlock - 1>([&](auto k) { m[(int)d] = max_of<DT>(m[(int)d], magnitude_of<DT>(v[k + 1][(int)d])); });
+    static_for<7>([&](auto k) { m[(int)d] = max_of<DT>(m[(int)d], magnitude_of<DT>(v[k + 1][(int)d])); });
+    m[(int)d] = max_of_rows<DT>(m[(int)d]);
   });
-  static_for<(int)ROWS>([&](auto j) {
-    constexpr int d = DT == LC_F32 ? j : j / 2;
-    const uint32_t byte = scale_byte<DT>(DT == LC_F32 ? m[d] : (m[d] >> (16 * (j % 2))) & 0xFFFFu, P.cover);
-    const float scale = scale_value(byte);
-    u32x4 codes;
-    static_for<4>([&](auto w) {
+  static_for<ROWS / 4>([&](auto four) {
+    uint32_t codes[4], byte[4];
+    static_for<4>([&](auto i) {
+      constexpr int j = 4 * four + i, d = DT == LC_F32 ? j : j / 2;
+      byte[(int)i] = scale_byte<DT>(DT == LC_F32 ? m[d] : (m[d] >> (16 * (j % 2))) & 0xFFFFu, P.cover);
+      const float scale = scale_value(byte[(int)i]);
       uint32_t c = 0u;
-      static_for<4>([&](auto i) {
-        constexpr int k = 8 * w + 2 * i;
-        if constexpr (DT == LC_F32) c = pack_codes<DT, i>(c, v[k][d], v[k + 1][d], scale);
-        else c = pack_codes<DT, i>(c, __builtin_amdgcn_perm(v[k + 1][d], v[k][d], j % 2 ? 0x07060302u : 0x05040100u), 0u, scale);
+      static_for<4>([&](auto pair) {
+        constexpr int k = 2 * pair;
+        if constexpr (DT == LC_F32) c = pack_codes<DT, pair>(c, v[k][d], v[k + 1][d], scale);
+        else c = pack_codes<DT, pair>(c, __builtin_amdgcn_perm(v[k + 1][d], v[k][d], j % 2 ? 0x07060302u : 0x05040100u), 0u, scale);
       });
-      codes[(int)w] = byte == 255u ? 0u : c;
+      codes[(int)i] = byte[(int)i] == 255u ? 0u : c;
     });
-    const uint32_t row = start + (uint32_t)j;
-    if (row >= first) {
-      *reinterpret_cast<u32x4*>(q + mx_mode_eval(P.q_r, row) + mx_mode_eval(P.q_b, block)) = codes;
-      s[mx_mode_eval(P.s_r, row) + mx_mode_eval(P.s_b, block)] = (unsigned char)byte;
+    transpose_rows(codes);
+    const uint32_t row = start + 4u * (uint32_t)four + part, piece = ((row - group_row) << P.block_shift) + (block - group_block);
+    if (first < P.R && row >= first) {
+      s_codes[piece + piece / 8u] = u32x4{codes[0], codes[1], codes[2], codes[3]};
+      s_bytes[piece] = (unsigned char)(part < 2u ? part ? byte[1] : byte[0] : part == 2u ? byte[2] : byte[3]);
+    }
+  });
+  __syncthreads();
+  static_for<(int)(kMxRowPieces<ROWS> / (64 * kMxRowWaves))>([&](auto i) {
+    const uint32_t piece = threadIdx.x + 64u * kMxRowWaves * (uint32_t)i;
+    const uint32_t row = group_row + (piece >> P.block_shift), at_block = group_block + (piece & ((1u << P.block_shift) - 1u));
+    if (row < P.R && at_block < P.blocks) {
+      *reinterpret_cast<u32x4*>(q + mx_mode_eval(P.q_r, row) + mx_mode_eval(P.q_b, at_block)) = s_codes[piece + piece / 8u];
+      s[mx_mode_eval(P.s_r, row) + mx_mode_eval(P.s_b, at_block)] = s_bytes[piece];
     }
   });
 }
 
 template <int DT>
-__global__ __launch_bounds__(256) void mx_dequantize_rows_kernel(MxCopyParams P, uint32_t tiles_r, const unsigned char* __restrict__ q,
-                                                                 const unsigned char* __restrict__ s, unsigned char* __restrict__ x) {
+__global__ __launch_bounds__(64 * kMxRowWaves) void mx_dequantize_rows_kernel(MxCopyParams P, const unsigned char* __restrict__ q,
+                                                                            const unsigned char* __restrict__ s, unsigned char* __restrict__ x) {
   constexpr uint32_t ES = kElemBytes<DT>, ROWS = 16 / ES;
-  touch_kernel_arguments<kMxKernargs + 8>();
+  touch_kernel_arguments<kMxKernargs>();
+  const uint32_t lane = threadIdx.x & 63u, part = lane / kMxRowLanes;
   uint32_t start, first, block;
-  mx_row_vector(P, ROWS, tiles_r, blockIdx.x * 4u + (threadIdx.x >> 6), threadIdx.x & 63u, &start, &first, &block);
+  mx_row_vector(P, ROWS, gemm_tile_order_of_block(blockIdx.x, gridDim.x), threadIdx.x >> 6, lane, &start, &first, &block);
   if (first >= P.R || block >= P.blocks) return;
-  u32x4 codes[ROWS];
-  float scale[ROWS];
-  uint32_t byte[ROWS];
-  static_for<(int)ROWS>([&](auto j) {
-    const uint32_t row = start + (uint32_t)j;
-    codes[(int)j] = *reinterpret_cast<const u32x4*>(q + mx_mode_eval(P.q_r, row) + mx_mode_eval(P.q_b, block));
-    byte[(int)j] = s[mx_mode_eval(P.s_r, row) + mx_mode_eval(P.s_b, block)];
+  const RowWalk q_at(P.q_r, start + part, 4, mx_mode_eval(P.q_b, block)), s_at(P.s_r, start + part, 4, mx_mode_eval(P.s_b, block));
+  uint32_t codes[ROWS], byte[ROWS];
+  static_for<(int)ROWS / 4>([&](auto four) {
+    const u32x4 c = *reinterpret_cast<const u32x4*>(q + q_at((uint32_t)four));
+    const uint32_t b = s[s_at((uint32_t)four)];
+    static_for<4>([&](auto i) {
+      codes[4 * four + i] = c[(int)i];
+      byte[4 * four + i] = b;
+    });
   });
-  static_for<(int)ROWS>([&](auto j) { scale[(int)j] = scale_value(byte[(int)j]); });
-  unsigned char* p = x + mx_mode_eval(P.x_r, start);
-  static_for<(int)kMxBlock / 2>([&](auto pair) {
-    constexpr int w = pair / 4, sel = pair % 4;
-    u32x4 even, odd;   // the rows' values at k = 2 pair and at 2 pair + 1
+  __builtin_amdgcn_sched_barrier(0);
+  float scale[ROWS];
+  static_for<(int)ROWS / 4>([&](auto four) {
+    uint32_t c[4], b[4];
+    static_for<4>([&](auto i) { c[(int)i] = codes[4 * four + i]; b[(int)i] = byte[4 * four + i]; });
+    transpose_rows(c);
+    transpose_rows(b);
+    static_for<4>([&](auto i) { codes[4 * four + i] = c[(int)i]; scale[4 * four + i] = scale_value(b[(int)i]); });
+  });
+  const uint32_t k0 = block * kMxBlock + 8u * part;
+  const RowWalk at(P.x_k, k0, 1, mx_mode_eval(P.x_r, start));
+  static_for<4>([&](auto pair) {
+    u32x4 even, odd;   // the rows' values at k0 + 2 pair and at the next k
     if constexpr (DT == LC_F32) {
       static_for<4>([&](auto j) {
-        const u32x2 t = unpack_codes<DT, sel>(codes[(int)j][w], scale[(int)j]);
+        const u32x2 t = unpack_codes<DT, pair>(codes[(int)j], scale[(int)j]);
         even[(int)j] = t[0];
         odd[(int)j] = t[1];
       });
     } else {
       static_for<4>([&](auto d) {
-        const uint32_t lo = unpack_codes<DT, sel>(codes[2 * d][w], scale[2 * d])[0], hi = unpack_codes<DT, sel>(codes[2 * d + 1][w], scale[2 * d + 1])[0];
+        const uint32_t lo = unpack_codes<DT, pair>(codes[2 * d], scale[2 * d])[0], hi = unpack_codes<DT, pair>(codes[2 * d + 1], scale[2 * d + 1])[0];
         even[(int)d] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
         odd[(int)d] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
       });
     }
     static_for<2>([&](auto o) {
-      const uint32_t k = block * kMxBlock + 2u * (uint32_t)pair + (uint32_t)o;
+      constexpr uint32_t k = 2 * pair + o;
       const u32x4 v = o ? odd : even;
-      if (k < P.K) {
-        unsigned char* at = p + mx_mode_eval(P.x_k, k);
+      if (k0 + k < P.K) {
+        unsigned char* to = x + at(k);
         if (start == first) {
-          *reinterpret_cast<u32x4_any*>(at) = v;
+          *reinterpret_cast<u32x4_any*>(to) = v;
         } else {   // the vector that was started early: only the rows that are its own
           static_for<(int)ROWS>([&](auto j) {
-            if (start + (uint32_t)j >= first) store_element<DT>(at + (uint32_t)j * ES, DT == LC_F32 ? v[j % 4] : v[(j / 2) % 4] >> (16 * (j % 2)));
+            if (start + (uint32_t)j >= first) store_element<DT>(to + (uint32_t)j * ES, DT == LC_F32 ? v[j % 4] : v[(j / 2) % 4] >> (16 * (j % 2)));
           });
         }
       }
@@ -302,15 +379,15 @@ bool mx_hip_failed(hipError_t e, const char* what) {
 
 template <int DT>
 void launch_quantize(const lc_mx_plan& plan, const unsigned char* x, unsigned char* q, unsigned char* s, hipStream_t st) {
-  const dim3 grid(plan.groups), block(256);
-  if (plan.access == kMxAlongRows) hipLaunchKernelGGL((mx_quantize_rows_kernel<DT>), grid, block, 0, st, plan.params, plan.tiles_r, x, q, s);
+  const dim3 grid(plan.groups), block(plan.access == kMxAlongRows ? 64 * kMxRowWaves : 256);
+  if (plan.access == kMxAlongRows) hipLaunchKernelGGL((mx_quantize_rows_kernel<DT>), grid, block, 0, st, plan.params, x, q, s);
   else if (plan.access == kMxAlongK) hipLaunchKernelGGL((mx_quantize_kernel<DT, true>), grid, block, 0, st, plan.params, x, q, s);
   else hipLaunchKernelGGL((mx_quantize_kernel<DT, false>), grid, block, 0, st, plan.params, x, q, s);
 }
 template <int DT>
 void launch_dequantize(const lc_mx_plan& plan, const unsigned char* q, const unsigned char* s, unsigned char* x, hipStream_t st) {
-  const dim3 grid(plan.groups), block(256);
-  if (plan.access == kMxAlongRows) hipLaunchKernelGGL((mx_dequantize_rows_kernel<DT>), grid, block, 0, st, plan.params, plan.tiles_r, q, s, x);
+  const dim3 grid(plan.groups), block(plan.access == kMxAlongRows ? 64 * kMxRowWaves : 256);
+  if (plan.access == kMxAlongRows) hipLaunchKernelGGL((mx_dequantize_rows_kernel<DT>), grid, block, 0, st, plan.params, q, s, x);
   else if (plan.access == kMxAlongK) hipLaunchKernelGGL((mx_dequantize_kernel<DT, true>), grid, block, 0, st, plan.params, q, s, x);
   else hipLaunchKernelGGL((mx_dequantize_kernel<DT, false>), grid, block, 0, st, plan.params, q, s, x);
 }

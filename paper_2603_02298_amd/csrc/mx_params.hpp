@@ -46,33 +46,37 @@ struct MxCopyParams {
   MxMode s_r, s_b;
   uint32_t R, K;       // of x
   uint32_t blocks;     // blocks of a row that are gone over: all of the codes' (quantisation), those that hold k < K
-  // order of the blocks: `inner` neighbours of a row, then the next row's; then the next `inner` of every row.  Scales that lie
-  // in that order are read and written in whole runs.
-  uint32_t inner;
-  FastDiv inner_div, row_div;
+  // a workgroup goes over 2^block_shift blocks along k, and along the rows over kMxUnroll times 64 / 2^block_shift of them
+  // (kMxAlongRows: kMxRowLanes vectors times kMxRowWaves / 2^block_shift)
+  uint32_t block_shift;
+  uint32_t tiles_r, tiles_b;
+  FastDiv tiles_div;   // kMxAlongRows: of tiles_r, otherwise of tiles_b: neighbouring workgroups go along the memory
   int32_t cover;       // quantisation: the scale's rule
 };
-// block number id of the order above -> row, block along k
-LC_HD void mx_block_of(const MxCopyParams& P, uint32_t id, uint32_t* row, uint32_t* block) {
-  uint32_t rest, in, group;
-  fd_divmod(id, P.inner_div, &rest, &in);
-  fd_divmod(rest, P.row_div, &group, row);
-  *block = group * P.inner + in;
+// 256 lanes go over 64 blocks at a time; lane t takes elements 8 (t % 4) .. + 7 of block t / 4 of them.  From one time to the next the row
+// moves by the same step and the block stays: a lane works out where it begins once.
+constexpr uint32_t kMxUnroll = 4;
+LC_HD uint32_t mx_rows_at_a_time(const MxCopyParams& P) { return 64u >> P.block_shift; }
+// workgroup, lane / 4 -> the first row and the block
+LC_HD void mx_unit_of(const MxCopyParams& P, uint32_t group, uint32_t t, uint32_t* row, uint32_t* block) {
+  uint32_t tile_r, tile_b;
+  fd_divmod(group, P.tiles_div, &tile_r, &tile_b);
+  *block = (tile_b << P.block_shift) + (t & ((1u << P.block_shift) - 1u));
+  *row = tile_r * (mx_rows_at_a_time(P) * kMxUnroll) + (t >> P.block_shift);
 }
 
-// kMxAlongK, kMxElements: 256 lanes go over 64 blocks at a time, kMxUnroll times; lane t takes elements 8 (t % 4) .. + 7 of block t / 4.
-constexpr uint32_t kMxUnroll = 4;
-constexpr uint32_t kMxBlocksPerGroup = 64 * kMxUnroll;
-
-// kMxAlongRows: a wavefront takes 8 x 8 lanes: lane l the vector of rows l % 8 and block l / 8 of its tile, so that a load
-// instruction reads 128 consecutive bytes at each of 8 k and a store instruction writes 8 consecutive blocks of a row.
+// kMxAlongRows: a wavefront takes one block of 16 vectors of rows, lane l the vector l % 16 at the k 8 (l / 16) .. + 7 of the block: a load
+// instruction reads 256 consecutive bytes at each of four k.  Four lanes of a vector hold its rows' quarters of codes; transposed among
+// them, lane l has the whole block of the vector's row l / 16, and of every fourth after it.
 // row_vec: rows of a vector.  The last vector of a mode of one leaf starts early enough to end with the rows; *first is the
 // first row that is the lane's own.  (R >= row_vec, or whole vectors.)
-LC_HD void mx_row_vector(const MxCopyParams& P, uint32_t row_vec, uint32_t tiles_r, uint32_t wave, uint32_t lane, uint32_t* start, uint32_t* first, uint32_t* block) {
-  const uint32_t tile_b = wave / tiles_r, tile_r = wave % tiles_r;
-  *first = (tile_r * 8u + (lane & 7u)) * row_vec;
+constexpr uint32_t kMxRowLanes = 16, kMxRowWaves = 8;
+LC_HD void mx_row_vector(const MxCopyParams& P, uint32_t row_vec, uint32_t group, uint32_t wave, uint32_t lane, uint32_t* start, uint32_t* first, uint32_t* block) {
+  uint32_t tile_b, tile_r;
+  fd_divmod(group, P.tiles_div, &tile_b, &tile_r);
+  *first = ((tile_r * (kMxRowWaves >> P.block_shift) + (wave >> P.block_shift)) * kMxRowLanes + lane % kMxRowLanes) * row_vec;
   *start = *first + row_vec <= P.R ? *first : P.R - row_vec;
-  *block = tile_b * 8u + (lane >> 3);
+  *block = (tile_b << P.block_shift) + (wave & ((1u << P.block_shift) - 1u));
 }
 
 }  // namespace lc

@@ -122,27 +122,25 @@ lc_status_t make_mx_plan(bool quantize, const Layout& x, const Layout& codes, co
   P.cover = rule == LC_MX_COVER;
   const uint64_t total = (uint64_t)P.R * P.blocks;
   if (total >= (uint64_t(1) << 31)) return LC_ERR_TOO_LARGE;
-  // scales whose rows hold a few consecutive blocks and lie next to each other (mx_scale_layout): gone over in that order
-  const bool grouped = q.s_k.size() == 2 && q.s_k[0].stride == 1 && q.s_r[0].stride == q.s_k[0].extent && P.blocks % q.s_k[0].extent == 0;
-  P.inner = grouped ? (uint32_t)q.s_k[0].extent : P.blocks;
-  P.inner_div = make_fastdiv(P.inner);
-  P.row_div = make_fastdiv(P.R);
-
   // Vectors are loaded and stored at the elements' own alignment: the memory pipeline takes them anywhere.
   const int64_t row_vec = 16 / es;
   const bool k_vec = x_k[0].stride == 1 && (x_k.size() == 1 || x_k[0].extent % kMxBlock == 0);
   const bool r_vec = x_r[0].stride == 1 && (x_r.size() == 1 ? x_r[0].extent >= row_vec : x_r[0].extent % row_vec == 0);
   plan.access = k_vec ? kMxAlongK : r_vec ? kMxAlongRows : kMxElements;
-  if (plan.access == kMxAlongRows) {
-    plan.tiles_r = (uint32_t)((plan.R + 8 * row_vec - 1) / (8 * row_vec));
-    const uint64_t waves = (uint64_t)plan.tiles_r * ((P.blocks + 7) / 8);
-    if (waves >= (uint64_t(1) << 31)) return LC_ERR_TOO_LARGE;
-    plan.groups = (uint32_t)((waves + 3) / 4);
-  } else {
-    plan.groups = (uint32_t)((total + kMxBlocksPerGroup - 1) / kMxBlocksPerGroup);
-  }
-  // a grid counts its lanes in 32 bits
-  if ((uint64_t)plan.groups * 256u > 0xFFFFFFFFull) return LC_ERR_TOO_LARGE;
+  // Blocks of a workgroup along k: the most that waste an eighth at most; eight where a row keeps eight scales together and the next row's
+  // follow (mx_scale_layout): those are then read and written in runs of 256 bytes.  (8192 x 8192 bf16 quantised and
+  // back, with such scales: 70 us.)
+  const bool along_rows = plan.access == kMxAlongRows;
+  const bool grouped = q.s_k.size() == 2 && q.s_k[0].stride == 1 && q.s_k[0].extent == 8 && q.s_r[0].stride == 8;
+  P.block_shift = along_rows || grouped ? 3 : 6;
+  while (P.block_shift && (uint64_t)((P.blocks + (1u << P.block_shift) - 1) >> P.block_shift << P.block_shift) > (uint64_t)P.blocks + P.blocks / 8) --P.block_shift;
+  const int64_t rows = along_rows ? (kMxRowWaves >> P.block_shift) * kMxRowLanes * row_vec : mx_rows_at_a_time(P) * kMxUnroll;
+  P.tiles_b = (P.blocks + (1u << P.block_shift) - 1) >> P.block_shift;
+  P.tiles_r = (uint32_t)((plan.R + rows - 1) / rows);
+  const uint64_t groups = (uint64_t)P.tiles_r * P.tiles_b;
+  if (groups >= (uint64_t(1) << 23)) return LC_ERR_TOO_LARGE;   // a grid counts its lanes in 32 bits
+  plan.groups = (uint32_t)groups;
+  P.tiles_div = make_fastdiv(along_rows ? P.tiles_r : P.tiles_b);
   *out = plan;
   return LC_OK;
 }
@@ -153,7 +151,7 @@ std::string describe(const lc_mx_plan& plan) {
   s += plan.dtype == LC_F32 ? " x=f32" : plan.dtype == LC_BF16 ? " x=bf16" : " x=f16";
   s += " R=" + std::to_string(plan.R) + " K=" + std::to_string(plan.K) + " padded=" + std::to_string(plan.padded);
   if (plan.quantize) s += plan.params.cover ? " rule=cover" : " rule=floor";
-  s += std::string(" access=") + access[plan.access] + " inner=" + std::to_string(plan.params.inner) + " groups=" + std::to_string(plan.groups);
+  s += std::string(" access=") + access[plan.access] + " tiles=" + std::to_string(plan.params.tiles_r) + "x" + std::to_string(plan.params.tiles_b) + " groups=" + std::to_string(plan.groups);
   return s + " X=[" + plan.x_text + "] codes(blocks,bytes)=[" + plan.q_text + "] scales=[" + plan.s_text + "]";
 }
 
@@ -177,36 +175,40 @@ lc_status_t mx_walk_on_host(const lc_mx_plan& plan, int64_t x_before, int64_t x_
   };
   if (plan.access == kMxAlongRows) {
     const uint32_t row_vec = (uint32_t)(16 / es);
-    for (uint32_t wave = 0; wave < plan.groups * 4u && inside; ++wave)
+    for (uint32_t i = 0; i < plan.groups * kMxRowWaves && inside; ++i)
       for (uint32_t lane = 0; lane < 64u; ++lane) {
         uint32_t start, first, block;
-        mx_row_vector(P, row_vec, plan.tiles_r, wave, lane, &start, &first, &block);
+        mx_row_vector(P, row_vec, i / kMxRowWaves, i % kMxRowWaves, lane, &start, &first, &block);
         if (first >= P.R || block >= P.blocks) continue;
-        for (uint32_t k = block * kMxBlock; k < (block + 1) * kMxBlock && k < P.K; ++k) {
+        const uint32_t part = lane / kMxRowLanes;
+        for (uint32_t k = block * kMxBlock + 8 * part; k < block * kMxBlock + 8 * part + 8 && k < P.K; ++k) {
           const int64_t at = mx_mode_eval(P.x_r, start) + mx_mode_eval(P.x_k, k);
           if (plan.quantize) at_x(at, 16);
           else at_x(at + (first - start) * es, 16 - (first - start) * es);
         }
-        for (uint32_t j = first - start; j < row_vec; ++j) {
+        for (uint32_t j = part; j < row_vec; j += 4) {
+          if (plan.quantize && start + j < first) continue;
           at_q(mx_mode_eval(P.q_r, start + j) + mx_mode_eval(P.q_b, block), kMxBlockBytes, false);
           at_q(mx_mode_eval(P.s_r, start + j) + mx_mode_eval(P.s_b, block), 1, true);
         }
       }
   } else {
-    const uint32_t total = P.R * P.blocks;
-    for (uint32_t id = 0; id < plan.groups * kMxBlocksPerGroup && inside; ++id) {
-      if (id >= total) continue;
-      uint32_t row, block;
-      mx_block_of(P, id, &row, &block);
-      for (uint32_t part = 0; part < 4u; ++part) {
-        const uint32_t k0 = block * kMxBlock + 8u * part;
-        at_q(mx_mode_eval(P.q_r, row) + mx_mode_eval(P.q_b, block) + 4 * part, 4, false);
-        if (part == 0) at_q(mx_mode_eval(P.s_r, row) + mx_mode_eval(P.s_b, block), 1, true);
-        if (plan.access == kMxAlongK && k0 + 8u <= P.K) at_x(mx_mode_eval(P.x_r, row) + mx_mode_eval(P.x_k, k0), 8 * es);
-        else
-          for (uint32_t k = k0; k < k0 + 8u && k < P.K; ++k) at_x(mx_mode_eval(P.x_r, row) + mx_mode_eval(P.x_k, k), es);
-      }
-    }
+    for (uint32_t group = 0; group < plan.groups && inside; ++group)
+      for (uint32_t t = 0; t < 64u; ++t)
+        for (uint32_t u = 0; u < kMxUnroll; ++u) {
+          uint32_t row, block;
+          mx_unit_of(P, group, t, &row, &block);
+          row += u * mx_rows_at_a_time(P);
+          if (row >= P.R || block >= P.blocks) continue;
+          for (uint32_t part = 0; part < 4u; ++part) {
+            const uint32_t k0 = block * kMxBlock + 8u * part;
+            at_q(mx_mode_eval(P.q_r, row) + mx_mode_eval(P.q_b, block) + 4 * part, 4, false);
+            if (part == 0) at_q(mx_mode_eval(P.s_r, row) + mx_mode_eval(P.s_b, block), 1, true);
+            if (plan.access == kMxAlongK && k0 + 8u <= P.K) at_x(mx_mode_eval(P.x_r, row) + mx_mode_eval(P.x_k, k0), 8 * es);
+            else
+              for (uint32_t k = k0; k < k0 + 8u && k < P.K; ++k) at_x(mx_mode_eval(P.x_r, row) + mx_mode_eval(P.x_k, k), es);
+          }
+        }
   }
   if (reads) *reads = plan.quantize ? n_x : n_q;
   if (written) *written = plan.quantize ? n_q : n_x;
