@@ -138,7 +138,7 @@ lc_status_t make_mx_plan(bool quantize, const Layout& x, const Layout& codes, co
   P.tiles_b = (P.blocks + (1u << P.block_shift) - 1) >> P.block_shift;
   P.tiles_r = (uint32_t)((plan.R + rows - 1) / rows);
   const uint64_t groups = (uint64_t)P.tiles_r * P.tiles_b;
-  if (groups >= (uint64_t(1) << 23)) return LC_ERR_TOO_LARGE;   // a grid counts its lanes in 32 bits
+  if (groups * (along_rows ? 64u * kMxRowWaves : 256u) > 0xFFFFFFFFull) return LC_ERR_TOO_LARGE;   // a grid counts its lanes in 32 bits
   plan.groups = (uint32_t)groups;
   P.tiles_div = make_fastdiv(along_rows ? P.tiles_r : P.tiles_b);
   *out = plan;

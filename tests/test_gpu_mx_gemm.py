@@ -392,3 +392,65 @@ def test_long_k(a_dtype, M, s_text):
         s = s_text.replace("2304", str(blocks))
         a, a_s = (_rows(M, K), _scales(M, K)) if a_dtype == "mxfp4" else (_rows(M, K), None)
         _run(a, a_s, _rows(N, K), s, _rows(M, N), a_dtype, "f32", False, "wide", seed=blocks)
+
+
+@pytest.mark.parametrize("M,N,K,pitch", [(3, 40, 65, 70), (20, 70, 72, 80), (33, 100, 264, 272), (130, 140, 520, 528), (16, 128, 301, 301), (200, 129, 640, 648)])
+@pytest.mark.parametrize("order", ["k", "r"])
+@pytest.mark.parametrize("blocked", [1, 0])
+@pytest.mark.parametrize("tile", [0, 32, 12864, 128, 256, 256128, 128128, 128064])
+def test_nan_around_the_operands_stays_out(M, N, K, pitch, order, blocked, tile, monkeypatch):
+    """NaN before, behind and between the rows of A, scales of 255 between and behind B's, an origin of A off any vector for odd M."""
+    if tile:
+        monkeypatch.setenv("LC_TUNE_MX_TILE", str(tile))
+    dev = torch.device("cuda:0")
+    rng = np.random.default_rng(K)
+    pitch = pitch if order == "k" else M + 8
+    a_text = "(%d,%d):(%d,1)" % (M, K, pitch) if order == "k" else "(%d,%d):(1,%d)" % (M, K, pitch)
+    a = rng.integers(-4, 5, (M, K)).astype(np.float32)
+    before = 8 + M % 2
+    flat = np.full(before + lc.Layout(a_text).cosize + 600, np.nan, np.float32)
+    flat[before + mx.offsets(a_text)] = a
+    P = (K + 31) // 32 * 32 if blocked else (N + 31) // 32 * 32
+    rows, k = (N, P) if blocked else (K, P)
+    s_pitch = P // 32 + 3
+    codes = rng.integers(0, 16, (rows, k))
+    scales = np.full((rows + 9) * s_pitch + 1, 255, np.uint8)
+    used = 1 + np.arange(rows)[:, None] * s_pitch + np.arange(P // 32)   # at an odd address
+    scales[used] = rng.integers(126, 129, used.shape)
+    packed = np.zeros((rows, k // 2), np.uint8)
+    packed |= (codes[:, 0::2] | (codes[:, 1::2] << 4)).astype(np.uint8)
+    values = mx.LEVELS[codes] * np.repeat(np.ldexp(1.0, scales[used].astype(np.int64) - 127), 32, axis=1)
+    b_text, s_text = ("(%d,%d):(%d,1)" % (N, P, P), "(%d,%d):(%d,1)" % (N, P // 32, s_pitch)) if blocked else \
+                     ("(%d,%d):(1,%d)" % (P, K, P), "(%d,%d):(1,%d)" % (P // 32, K, s_pitch))
+    want = a.astype(np.float64) @ (values[:, :K].T if blocked else values[:, :N])
+    a_t = torch.from_numpy(flat).to(torch.bfloat16).to(dev)
+    b_t, s_t, c = torch.from_numpy(packed).to(dev), torch.from_numpy(scales).to(dev), torch.full((M, N), np.nan, device=dev)
+    lc.lc_mx_gemm(a_t.data_ptr() + 2 * before, a_text, None, None, b_t.data_ptr(), b_text, s_t.data_ptr() + 1, s_text, c.data_ptr(), _rows(M, N), "bf16", "f32", False,
+                  torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert (c.cpu().double().numpy() == want).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(5, 20, 96), (40, 70, 320), (130, 140, 544), (300, 260, 1056)])
+@pytest.mark.parametrize("tile", [0, 32, 64, 128, 256])
+def test_scales_between_the_rows_of_codes_stay_out(M, N, K, tile, monkeypatch):
+    """Scales of 255 between, before and behind the rows' own, which start at an odd address."""
+    if tile:
+        monkeypatch.setenv("LC_TUNE_MX_TILE", str(tile))
+    dev = torch.device("cuda:0")
+    rng = np.random.default_rng(K)
+    sides, s_pitch = [], K // 32 + 3
+    for rows in (M, N):
+        codes = rng.integers(0, 16, (rows, K))
+        scales = np.full((rows + 9) * s_pitch + 1, 255, np.uint8)
+        used = 1 + np.arange(rows)[:, None] * s_pitch + np.arange(K // 32)
+        scales[used] = rng.integers(126, 129, used.shape)
+        packed = (codes[:, 0::2] | (codes[:, 1::2] << 4)).astype(np.uint8)
+        values = mx.LEVELS[codes] * np.repeat(np.ldexp(1.0, scales[used].astype(np.int64) - 127), 32, axis=1)
+        sides.append((torch.from_numpy(packed).to(dev), _rows(rows, K), torch.from_numpy(scales).to(dev), "(%d,%d):(%d,1)" % (rows, K // 32, s_pitch), values))
+    (a, a_l, a_s, a_sl, av), (b, b_l, b_s, b_sl, bv) = sides
+    c = torch.full((M, N), np.nan, device=dev)
+    lc.lc_mx_gemm(a.data_ptr(), a_l, a_s.data_ptr() + 1, a_sl, b.data_ptr(), b_l, b_s.data_ptr() + 1, b_sl, c.data_ptr(), _rows(M, N), "mxfp4", "f32", False,
+                  torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert (c.cpu().double().numpy() == av @ bv.T).all()
