@@ -69,23 +69,26 @@ __device__ __forceinline__ void* mx_c_at(void* C, uint32_t off, int32_t type) { 
 template <int TYPE>
 using mx_c_elem = std::conditional_t<TYPE == LC_F32, float, std::conditional_t<TYPE == LC_BF16, __bf16, _Float16>>;
 
-// An offset along one of C's modes: a multiplication where the mode has one leaf.
-__device__ __forceinline__ uint32_t mx_c_eval(const GemmMode& mode, bool one_leaf, uint32_t i) { return one_leaf ? i * mode.last_stride : gemm_mode_eval(mode, i); }
-
 // The sums of a BM x BN tile, parked in LDS as gemm_sum_unit says, to C by LANES lanes: consecutive lanes along the mode that C holds together.
-// A lane stays in its row group (column), so it evaluates one of C's modes once; eight units are on their way at a time.
-template <int BM, int BN, int LANES, int TYPE, bool ADD, bool VEC>
+// A lane stays in its row group (column), so it evaluates one of C's modes once; U units are on their way at a time.
+// ONE: the other mode has one leaf, so that its offsets are one multiplication.  A loop, not unrolled, and few units where offsets take divisions: six
+// types and forms of C times all units with their divisions in line would be more instructions than the instruction cache holds.
+template <int BM, int BN, int LANES, int TYPE, bool ADD, bool VEC, bool ONE>
 __device__ __forceinline__ void mx_tile_to_c_as(const MxGemmParams& P, void* C, const unsigned char* lds, uint32_t m0, uint32_t n0, uint32_t tid) {
   using T = mx_c_elem<TYPE>;
   typedef T Tx4 __attribute__((ext_vector_type(4)));
-  constexpr int N = BM * BN / 4 / LANES, U = N < 8 ? N : 8;
+  constexpr int N = BM * BN / 4 / LANES, MOST = ONE ? 8 : VEC ? 4 : 1, U = N < MOST ? N : MOST;
   constexpr uint32_t ALONG = VEC ? BM / 4 : BN, STEP = LANES / ALONG;   // lanes along the contiguous mode; how far the other one moves per unit
   static_assert(BM * BN / 4 % LANES == 0 && LANES % ALONG == 0 && N % U == 0, "whole units for every lane");
   T* c = static_cast<T*>(C);
   const uint32_t fast = tid % ALONG, slow = tid / ALONG;
   if (VEC ? m0 + 4u * fast >= P.g.M : n0 + fast >= P.g.N) return;
-  const bool one_leaf = VEC ? P.g.c_n.n == 1 : P.g.c_m.n == 1;
   c += VEC ? gemm_mode_eval(P.g.c_m, m0 + 4u * fast) : gemm_mode_eval(P.g.c_n, n0 + fast);
+  auto offset = [&](uint32_t i) {
+    if constexpr (VEC) return ONE ? i * P.g.c_n.last_stride : gemm_mode_eval(P.g.c_n, i);
+    else return ONE ? i * P.g.c_m.last_stride : gemm_mode_eval(P.g.c_m, i);
+  };
+#pragma unroll 1
   for (int first = 0; first < N; first += U) {
     f32x4 v[U];
     static_for<U>([&](auto u) {
@@ -97,7 +100,7 @@ __device__ __forceinline__ void mx_tile_to_c_as(const MxGemmParams& P, void* C, 
       Tx4 old[U];
       static_for<U>([&](auto u) {
         const uint32_t n = n0 + slow + (uint32_t)(first + u) * STEP;
-        off[u] = mx_c_eval(P.g.c_n, one_leaf, n < P.g.N ? n : P.g.N - 1u);
+        off[u] = offset(n < P.g.N ? n : P.g.N - 1u);
         if constexpr (ADD) old[u] = *reinterpret_cast<const Tx4*>(c + off[u]);
       });
       static_for<U>([&](auto u) {
@@ -105,16 +108,19 @@ __device__ __forceinline__ void mx_tile_to_c_as(const MxGemmParams& P, void* C, 
         if (n0 + slow + (uint32_t)(first + u) * STEP < P.g.N) *reinterpret_cast<Tx4*>(c + off[u]) = __builtin_convertvector(v[u], Tx4);
       });
     } else {
+      uint32_t off[U][4];
+      float old[U][4];
       static_for<U>([&](auto u) {
         const uint32_t m = m0 + 4u * (slow + (uint32_t)(first + u) * STEP);
-        uint32_t off[4];
-        float old[4];
         static_for<4>([&](auto e) {
-          off[(int)e] = mx_c_eval(P.g.c_m, one_leaf, m + (uint32_t)e < P.g.M ? m + (uint32_t)e : P.g.M - 1u);
-          old[(int)e] = ADD ? (float)c[off[(int)e]] : 0.f;
+          off[u][(int)e] = offset(m + (uint32_t)e < P.g.M ? m + (uint32_t)e : P.g.M - 1u);
+          if constexpr (ADD) old[u][(int)e] = (float)c[off[u][(int)e]];
         });
+      });
+      static_for<U>([&](auto u) {
+        const uint32_t m = m0 + 4u * (slow + (uint32_t)(first + u) * STEP);
         static_for<4>([&](auto e) {
-          if (m + (uint32_t)e < P.g.M) c[off[(int)e]] = (T)(ADD ? old[(int)e] + v[u][(int)e] : v[u][(int)e]);
+          if (m + (uint32_t)e < P.g.M) c[off[u][(int)e]] = (T)(ADD ? old[u][(int)e] + v[u][(int)e] : v[u][(int)e]);
         });
       });
     }
@@ -134,8 +140,14 @@ __device__ __forceinline__ void mx_c_dispatch(const MxGemmParams& P, F&& f) {
 template <int BM, int BN, int LANES>
 __device__ __forceinline__ void mx_tile_to_c(const MxGemmParams& P, void* C, const unsigned char* lds, uint32_t m0, uint32_t n0, uint32_t tid) {
   mx_c_dispatch(P, [&](auto type, auto add) {
-    if (P.g.c_vec) mx_tile_to_c_as<BM, BN, LANES, decltype(type)::value, decltype(add)::value, true>(P, C, lds, m0, n0, tid);
-    else mx_tile_to_c_as<BM, BN, LANES, decltype(type)::value, decltype(add)::value, false>(P, C, lds, m0, n0, tid);
+    auto to_c = [&](auto vec, auto one) { mx_tile_to_c_as<BM, BN, LANES, decltype(type)::value, decltype(add)::value, decltype(vec)::value, decltype(one)::value>(P, C, lds, m0, n0, tid); };
+    if (P.g.c_vec) {
+      if (P.g.c_n.n == 1) to_c(std::true_type{}, std::true_type{});
+      else to_c(std::true_type{}, std::false_type{});
+    } else {
+      if (P.g.c_m.n == 1) to_c(std::false_type{}, std::true_type{});
+      else to_c(std::false_type{}, std::false_type{});
+    }
   });
 }
 
@@ -202,6 +214,7 @@ struct MxEvenTileLoader {
   uint32_t off[UNITS], s_off[UNITS];   // 0xFFFFFFFF: no such row
   uint32_t tail_mask;                  // bit i: block i of this lane lies below K in the last k tile
   uint32_t put;                        // bytes into the tile
+  uint32_t turn;                       // blocks along the rows: the lane parks quarter Q ^ turn where others park theirs
   struct Raw {
     u32x4 codes[UNITS];
     uint8_t byte[UNITS];
@@ -212,6 +225,7 @@ struct MxEvenTileLoader {
     scales = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(s), 0, 0xFFFFFFFFu, 0x00020000);
     const uint32_t k_rem = P.g.K - (P.g.K - 1u) / kGemmBK * kGemmBK;
     tail_mask = 0u;
+    turn = BLOCKED ? 0u : (t + (t >> 2)) & 3u;
     static_for<UNITS>([&](auto i) {
       const uint32_t row = BLOCKED ? (t >> 1) + 128u * (uint32_t)i : 32u * (t % (BR / 32u));
       const uint32_t k = BLOCKED ? 32u * (t & 1u) : t / (BR / 32u) + (256u / (BR / 32u)) * (uint32_t)i;
@@ -220,7 +234,7 @@ struct MxEvenTileLoader {
       s_off[i] = r < P.g.M ? gemm_mode_eval(P.sa_r, BLOCKED ? r : r / kMxBlock) + (BLOCKED ? t & 1u : k) * P.sa_k.lead_stride : 0xFFFFFFFFu;
       tail_mask |= (k < k_rem ? 1u : 0u) << (int)i;
       // (unit i lies 128 rows, or 256 / (BR / 32) k, behind unit 0: a constant)
-      if constexpr (decltype(i)::value == 0) put = BLOCKED ? gemm_lds_offset(row, k / 8u) : gemm_rdirect_lds_offset(BR, k, row);
+      if constexpr (decltype(i)::value == 0) put = BLOCKED ? gemm_lds_offset(row, k / 8u) : gemm_rdirect_lds_offset(BR, k, row) ^ (16u * turn);
     });
   }
   // where k tile kt begins along the codes' and along the scales' k mode, in bytes (uniform)
@@ -234,13 +248,19 @@ struct MxEvenTileLoader {
       raw.byte[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(scales, (int)(out ? 0xFFFFFFFFu : s_off[i]), (int)s_at, 0);
     });
   }
-  // parks quarter q (eight elements) of block i of the lane's
+  // parks a quarter (eight elements) of block i of the lane's.  Along the rows neighbouring lanes' blocks are 64 bytes apart: were all of them to
+  // park the same quarter, eight lanes would share four of the sixteen places that LDS writes at once; in turns they have eight (2048 x 4096 x 4096 along the rows: 74 -> 66 us).
   template <int I, int Q>
   __device__ __forceinline__ void park(unsigned char* tile, const Raw& raw) const {
+    uint32_t eight = raw.codes[I][Q];
+    if constexpr (!BLOCKED) {
+      const uint32_t even = turn & 2u ? raw.codes[I][Q ^ 2] : raw.codes[I][Q], odd = turn & 2u ? raw.codes[I][Q ^ 3] : raw.codes[I][Q ^ 1];
+      eight = turn & 1u ? odd : even;
+    }
     constexpr uint32_t UNIT = BLOCKED ? 128u * 128u : 256u / (BR / 32u) * (BR * 2u);
     static_assert(BLOCKED || (256u / (BR / 32u)) % 4u == 0u, "units of a lane fold alike");
     // (the four 16-byte vectors of a block: the low bits of the slot)
-    *reinterpret_cast<u32x4*>(tile + (put ^ (16u * Q)) + I * UNIT) = mx_expand<MATH>(raw.codes[I][Q], mx_scale_value(raw.byte[I]));
+    *reinterpret_cast<u32x4*>(tile + (put ^ (16u * Q)) + I * UNIT) = mx_expand<MATH>(eight, mx_scale_value(raw.byte[I]));
   }
   __device__ __forceinline__ void park_all(unsigned char* tile, const Raw& raw) const {
     static_for<UNITS>([&](auto i) {

@@ -12,8 +12,8 @@ constexpr uint32_t kMxTileBlocks = 8;   // blocks along k of a tile of codes: on
 enum MxGemmKernel : int32_t {
   kMxDirect = 0,   // operands straight into registers, the k loop shared out to the wavefronts
   kMxStream = 1,   // tiles through LDS, two pairs of them
-  kMxRing = 2,     // both operands codes: 256 x 256 tiles through a ring of five in LDS
-  kMxWide = 3      // one operand in 16 bits: tiles of 256 rows of codes by 256 or 128
+  kMxRing = 2,     // both operands codes: 256 x 256 or 128 x 128 tiles through a ring of five operand tiles in LDS
+  kMxWide = 3      // one operand in 16 bits: tiles of 256 or 128 rows of codes by 256 to 64
 };
 
 struct MxGemmParams {

@@ -222,27 +222,30 @@ lc_status_t make_mx_gemm_plan(const Layout& A, const Layout* A_scales, const Lay
   else if (t_env == 256 && can_ring) take(kMxRing, 256, 256, 4);
   else if (t_env == 256 && can_wide) take(kMxWide, 256, 256, 4);
   else if (t_env == 256128 && can_wide) take(kMxWide, 256, 128, 4);
+  else if (t_env == 128128 && can_ring) take(kMxRing, 128, 128, 4);
   else if (t_env == 128128 && can_wide) take(kMxWide, 128, 128, 4);
   else if (t_env == 128064 && can_wide) take(kMxWide, 128, 64, 4);
   else {
     // What a choice costs is how many rounds of 256 tiles (one a CU) there are times what a round takes, and not less than what a tile takes
     // alone; in microseconds at K = 4096, which all of them follow alike.  Measured on MI355X (us; direct 32 x 32, then the tiles by size):
-    //   both codes (64 x 64, 128 x 64, 128 x 128, 256 x 256): 64 x 4096 x 4096 9.8, 13.7, 15.7, -, -; 256 x 4096 x 4096 32.7, 14.5, 16.1, 19.8, -; 512 x 4096 x 4096
-    //   63, 17.9, 17.6, 20.8, 35.1; 1024 x 4096 x 4096 -, 25.9, 24.2, 24.0, 37.5; 2048 x 4096 x 4096 -, -, 38.0, 31.9, 38.3; 3000^2 x 2048 -, -, 26.5, 27.7, 26.8;
-    //   4096 x 8192 x 4096 -, -, -, 110, 89; 8192^3 -, -, -, 391, 302; 512 x 1024 x 1024 7.7, 6.5, 7.9, 9.7, -; 256^3 5.6, 4.6, -, -, -.
+    //   both codes (stream 64 x 64, 128 x 64, ring 128 x 128, 256 x 256): 256 x 4096 x 4096 32.7, 13.4, 14.7, 17.0, 35; 512 x 4096 x 4096 63, 16.8, 15.5, 17.1, 36;
+    //   1024 x 4096 x 4096 -, 25.1, 20.8, 19.3, 37; 2048 x 4096 x 4096 -, 45.3, 37.0, 28.8, 40; 4096 x 2048 x 2048 -, 28.1, 23.0, 20.9, 29.1; 3000^2 x 2048 -, 28.8, 24.5, 26.4,
+    //   27.4; 4096 x 8192 x 4096 -, 155, 118, 101, 89; 8192^3 -, 573, 461, 363, 299; 2048^2 x 512 -, 9.7, 9.0, 10.4, 17.8; 64 x 4096 x 4096 9.8, 13.7, -, -, -; 512 x 1024 x 1024
+    //   7.7, 6.5, 8.1, 9.0, -; 256^3 5.6, 4.6, 5.7, -, -.  Stream 128 x 128 (where the ring's loads do not apply): 22.1 at 1024 x 4096 x 4096, 30.5 at 2048 x 4096 x 4096.
     //   one in 16 bits (128 x 64, 128 x 128, 256 x 128, 256 x 256): 128 x 2048 x 2048 9.1, 18.0, 21.0, -, -; 128 x 8192 x 8192 61, 60, -, -, -; 256 x 4096 x 4096 38.9, 31.4,
     //   36.3, 57, -; 512 x 4096 x 4096 78, 35.8, 39.6, 61, -; 1024 x 4096 x 4096 -, 55, 46, 65, 92; 2048 x 4096 x 4096 -, 102, 75, 74, 96; along the rows -, -, 92, 82, 100;
     //   3000 x 5000 x 1024 -, 59, 43, 48, 40; 2048 x 8192 x 4096 -, -, -, 144, 116.
     struct Choice { MxGemmKernel kernel; int tm, tn; double round, alone; bool can; };
     const Choice choices[] = {
         {kMxDirect, 32, 32, 9.5, 9.5, can_direct && (!codes || G.k_tiles > 2)},   // (both codes over one or two k tiles: the stream kernel starts with less)
-        {kMxStream, 64, 64, 6.5, 14.0, codes}, {kMxStream, 128, 64, 9.5, 17.0, codes}, {kMxStream, 128, 128, 16.0, 22.0, codes},
+        {kMxStream, 64, 64, 9.0, 13.5, codes}, {kMxStream, 128, 64, 10.3, 15.0, codes}, {kMxStream, 128, 128, 16.0, 22.0, codes && !(can_ring && G.k_tiles > 2)},
+        {kMxRing, 128, 128, 14.8, 19.5, can_ring && G.k_tiles > 2},   // (over one or two k tiles its first loads are all there is)
         {kMxRing, 256, 256, 44.5, 36.0, can_ring && tiles_of(256, 256) >= 96},
         {kMxWide, 128, 64, 26.0, 34.0, can_wide}, {kMxWide, 128, 128, 37.5, 44.0, can_wide}, {kMxWide, 256, 128, 72.0, 72.0, can_wide}, {kMxWide, 256, 256, 112.0, 112.0, can_wide},
         {kMxStream, 128, 64, 30.0, 44.0, !codes && !can_wide}, {kMxStream, 128, 128, 43.0, 57.0, !codes && !can_wide}};
     auto cost = [&](const Choice& c) {
       const double rounds = (double)((tiles_of(c.tm, c.tn) + 255) / 256);
-      return c.kernel == kMxRing && tiles_of(c.tm, c.tn) <= 128 ? c.alone : std::max(c.alone, rounds * c.round);
+      return c.kernel == kMxRing && c.tm == 256 && tiles_of(c.tm, c.tn) <= 128 ? c.alone : std::max(c.alone, rounds * c.round);
     };
     const Choice* best = nullptr;
     for (const Choice& c : choices)
@@ -259,7 +262,7 @@ lc_status_t make_mx_gemm_plan(const Layout& A, const Layout* A_scales, const Lay
     }
   }
   plan.lds_bytes = plan.kernel == kMxStream ? 2u * (unsigned)(plan.tile_m + plan.tile_n) * 128u
-                   : plan.kernel == kMxRing ? 5u * 256u * 128u
+                   : plan.kernel == kMxRing ? 5u * (unsigned)plan.tile_m * 128u
                    : plan.kernel == kMxWide ? (2u * (unsigned)plan.tile_m + 3u * (unsigned)plan.tile_n) * 128u : 0u;
   if (plan.kernel == kMxDirect) {
     const int chunks = (int)((P.blocks + 3) / 4), w_env = env_int("LC_TUNE_MX_WAVES", 0);

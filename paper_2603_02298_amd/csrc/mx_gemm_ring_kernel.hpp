@@ -1,6 +1,7 @@
-// Device code of the ring kernel of the GEMM with two operands in microscaled 4-bit codes: 256 x 256 tiles of C for problems that have enough of them.
+// Device code of the ring kernel of the GEMM with two operands in microscaled 4-bit codes: BM x BM tiles of C, 256 for problems
+// that have enough of them, 128 (two workgroups a CU) for those that fill the card with these.
 //
-// Four wavefronts own a tile, wavefront (wm, wn) a quarter of 128 x 128 as 4 x 4 fragments of 32 x 32.  The operand tiles of a k tile (256
+// Four wavefronts own a tile, wavefront (wm, wn) a quarter of it as 4 x 4 (2 x 2) fragments of 32 x 32.  The operand tiles of a k tile (256
 // codes, rows of 128 bytes) go straight into a ring of five slots of LDS of one operand tile each, in the order A(0), B(0), A(1), B(1), A(2), ..: the
 // schedule of the generic GEMM's ring of 16-bit tiles, whose bytes per matrix instruction and clocks per instruction these codes share (a
 // 32 x 32 x 64 instruction of codes reads what a 32 x 32 x 16 one of 16-bit elements reads, and takes as long).
@@ -9,6 +10,10 @@
 // those covers them.
 // The sums pass through LDS, a column of fragments of a wavefront at a time and each wavefront in a place of its own, so that C is written in
 // whole lines.
+// What it measures, and what bounds it: 8192^3 into f32 300 us, 3.7 PFLOP/s, the matrix cores busy 45 % of clocks that the power limit holds at 1.93 GHz
+// (operands of random codes; they reach 6.5 PFLOP/s with nothing but these instructions).  A k tile of 256 x 256 takes 1.15 us, its 64 KiB at 58 GB/s
+// per CU, and every tile 17 us more: all CUs write their 256 KiB of C at the same time (13 us of that), then load the next first k tile.
+// A k step's products go in parts with everything else between them: in one piece, 8192^3 took 340 us.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -19,11 +24,11 @@
 
 namespace lc {
 
-constexpr unsigned kMxRingLds = 5u * 256u * 128u;
-
-__global__ __launch_bounds__(kBlock, 1) void mx_ring_kernel(MxGemmParams P, const unsigned char* __restrict__ A, const unsigned char* __restrict__ SA,
-                                                            const unsigned char* __restrict__ B, const unsigned char* __restrict__ SB, void* __restrict__ C) {
-  constexpr int BM = 256, FM = 4, FN = 4, R = BM / 32;
+template <int BM>
+__global__ __launch_bounds__(kBlock, BM == 256 ? 1 : 2) void mx_ring_kernel(MxGemmParams P, const unsigned char* __restrict__ A, const unsigned char* __restrict__ SA,
+                                                                               const unsigned char* __restrict__ B, const unsigned char* __restrict__ SB, void* __restrict__ C) {
+  constexpr int FM = BM / 64, FN = FM, R = BM / 32;
+  constexpr uint32_t W = BM / 2;   // rows of a wavefront
   constexpr uint32_t SLOT = BM * 128u;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   touch_kernel_arguments<(int)sizeof(MxGemmParams) + 40>();
@@ -47,8 +52,8 @@ __global__ __launch_bounds__(kBlock, 1) void mx_ring_kernel(MxGemmParams P, cons
   lb.init(reinterpret_cast<const uint16_t*>(B), P.g.b_r, P.g.b_k, n0, P.g.N, P.g.K, tid);
   MxScaleLoader<FM> lsa;
   MxScaleLoader<FN> lsb;
-  lsa.init(SA, P.sa_r, m0 + wm * 128u, P.g.M, P.blocks, true, lane);
-  lsb.init(SB, P.sb_r, n0 + wn * 128u, P.g.N, P.blocks, true, lane);
+  lsa.init(SA, P.sa_r, m0 + wm * W, P.g.M, P.blocks, true, lane);
+  lsb.init(SB, P.sb_r, n0 + wn * W, P.g.N, P.blocks, true, lane);
 
   f32x16 acc[FM][FN];
   static_for<FM>([&](auto i) {
@@ -61,8 +66,8 @@ __global__ __launch_bounds__(kBlock, 1) void mx_ring_kernel(MxGemmParams P, cons
   uint32_t sa[FM], sb[FN];
   // per fragment: the lane's LDS address for the k tile's first k step in the slot being multiplied; k step kk: address ^ 16 kk
   uint32_t a_fr[FM], b_fr[FN];
-  static_for<FM>([&](auto i) { a_fr[i] = gemm_lds_offset(wm * 128u + 32u * (uint32_t)i + r, 4u * h); });
-  static_for<FN>([&](auto j) { b_fr[j] = SLOT + gemm_lds_offset(wn * 128u + 32u * (uint32_t)j + r, 4u * h); });
+  static_for<FM>([&](auto i) { a_fr[i] = gemm_lds_offset(wm * W + 32u * (uint32_t)i + r, 4u * h); });
+  static_for<FN>([&](auto j) { b_fr[j] = SLOT + gemm_lds_offset(wn * W + 32u * (uint32_t)j + r, 4u * h); });
   auto read_a = [&](auto i, auto kk, auto buf) { af[buf][i] = *reinterpret_cast<const u32x4*>(lds + (a_fr[i] ^ (16u * (uint32_t)kk))); };
   auto read_b = [&](auto j, auto kk, auto buf) { bf[buf][j] = *reinterpret_cast<const u32x4*>(lds + (b_fr[j] ^ (16u * (uint32_t)kk))); };
   // One k step in four parts, in this order: a row of products each, and before them in the first three the reads of the next k step's
@@ -72,7 +77,8 @@ __global__ __launch_bounds__(kBlock, 1) void mx_ring_kernel(MxGemmParams P, cons
     using Other = std::integral_constant<int, 1 - buf>;
     static_for<FM>([&](auto i) {
       if constexpr (i == 0) static_for<FN>([&](auto j) { read_b(j, next_kk, Other{}); });
-      if constexpr (i == 1 || i == 2) static_for<2>([&](auto d) { read_a(std::integral_constant<int, 2 * (decltype(i)::value - 1) + decltype(d)::value>{}, next_kk, Other{}); });
+      constexpr int from = FM == 4 ? 2 * (decltype(i)::value - 1) : 2 * decltype(i)::value;   // (four rows: under the second and third, two: the first)
+      if constexpr (from >= 0 && from < FM) static_for<2>([&](auto d) { read_a(std::integral_constant<int, from + decltype(d)::value>{}, next_kk, Other{}); });
       more(i);
       static_for<FN>([&](auto j) { acc[i][j] = mx_mfma_32x32x64<(int)decltype(kk)::value>(af[buf][i], bf[buf][j], acc[i][j], sa[i], sb[j]); });
       __builtin_amdgcn_sched_barrier(0);
@@ -118,12 +124,12 @@ __global__ __launch_bounds__(kBlock, 1) void mx_ring_kernel(MxGemmParams P, cons
     k_step(Zero{}, One{}, [&](auto i) {
       if constexpr (i == 0) lsa.fetch(P.sa_k, t1);
       if constexpr (i == 1) lsb.fetch(P.sb_k, t1);
-      if constexpr (i == 2) a2 = a_bytes(t2);
-      if constexpr (i == 3) b2 = b_bytes(t2);
+      if constexpr (i == 2 % FM) a2 = a_bytes(t2);
+      if constexpr (i == 3 % FM) b2 = b_bytes(t2);
     });
     asm volatile("" ::: "memory");
-    k_step(One{}, Two{}, [&](auto i) { la.template fetch<i * R / 8, (i + 1) * R / 8>(a2, s_a2 * SLOT + wave_at, kt + 2u >= last); });
-    k_step(Two{}, Three{}, [&](auto i) { la.template fetch<R / 2 + i * R / 8, R / 2 + (i + 1) * R / 8>(a2, s_a2 * SLOT + wave_at, kt + 2u >= last); });
+    k_step(One{}, Two{}, [&](auto i) { la.template fetch<i * R / (2 * FM), (i + 1) * R / (2 * FM)>(a2, s_a2 * SLOT + wave_at, kt + 2u >= last); });
+    k_step(Two{}, Three{}, [&](auto i) { la.template fetch<R / 2 + i * R / (2 * FM), R / 2 + (i + 1) * R / (2 * FM)>(a2, s_a2 * SLOT + wave_at, kt + 2u >= last); });
     // all but the R youngest have landed, and those are A(kt + 2)'s
     wait_loads_but(std::integral_constant<int, R>{});   // k tile kt + 1 and its scales have landed; A(kt + 2) may still be on its way
     lds_barrier();
@@ -134,45 +140,52 @@ __global__ __launch_bounds__(kBlock, 1) void mx_ring_kernel(MxGemmParams P, cons
     s_a = sa_next;
     s_b = sb_next;
     // k step 3: B(kt + 2), into the slot A(kt) leaves
-    k_step(Three{}, Zero{}, [&](auto i) { lb.template fetch<i * R / 4, (i + 1) * R / 4>(b2, b_to, kt + 2u >= last); });
+    k_step(Three{}, Zero{}, [&](auto i) { lb.template fetch<i * R / FM, (i + 1) * R / FM>(b2, b_to, kt + 2u >= last); });
     lsa.take(t1, sa);
     lsb.take(t1, sb);
   }
   __builtin_amdgcn_s_waitcnt(0x0070);   // the repeated loads of the last k tile have landed, its fragments have been read
   lds_barrier();
 
-  unsigned char* mine = lds + wave * (128u * 32u * 4u);
+  unsigned char* mine = lds + wave * (W * 32u * 4u);
   const MxGemmParams& E = mx_params_again();
-  mx_c_dispatch(E, [&](auto type, auto add) {
-    static_for<FN>([&](auto j) {
-      static_for<FM>([&](auto i) {
-        static_for<4>([&](auto g) {
-          f32x4 v;
-          static_for<4>([&](auto e) { v[(int)e] = acc[i][j][4 * g + e]; });
-          *reinterpret_cast<f32x4*>(mine + gemm_sum_unit(128u, 32u, 8u * (uint32_t)i + mfma_c_row(lane, 4u * (uint32_t)g) / 4u, mfma_c_col(lane)) * 16u) = v;
+#pragma unroll 1   // (mx_tile_to_c_as: once in the code)
+  for (uint32_t j = 0; j < (uint32_t)FN; ++j) {
+    static_for<FN>([&](auto column) {
+      if (j == (uint32_t)column)
+        static_for<FM>([&](auto i) {
+          static_for<4>([&](auto g) {
+            f32x4 v;
+            static_for<4>([&](auto e) { v[(int)e] = acc[i][column][4 * g + e]; });
+            *reinterpret_cast<f32x4*>(mine + gemm_sum_unit(W, 32u, 8u * (uint32_t)i + mfma_c_row(lane, 4u * (uint32_t)g) / 4u, mfma_c_col(lane)) * 16u) = v;
+          });
         });
-      });
-      asm volatile("" ::: "memory");   // (a wavefront's LDS accesses are carried out in order)
-      const uint32_t m = m0 + wm * 128u, n = n0 + wn * 128u + 32u * (uint32_t)j;
-      if (E.g.c_vec) mx_tile_to_c_as<128, 32, 64, decltype(type)::value, decltype(add)::value, true>(E, C, mine, m, n, lane);
-      else mx_tile_to_c_as<128, 32, 64, decltype(type)::value, decltype(add)::value, false>(E, C, mine, m, n, lane);
-      asm volatile("" ::: "memory");
     });
-  });
+    asm volatile("" ::: "memory");   // (a wavefront's LDS accesses are carried out in order)
+    mx_tile_to_c<(int)W, 32, 64>(E, C, mine, m0 + wm * W, n0 + wn * W + 32u * j, lane);
+    asm volatile("" ::: "memory");
+  }
 }
 
-static inline hipError_t launch_mx_ring(const lc_mx_gemm_plan& plan, const unsigned char* a, const unsigned char* sa, const unsigned char* b,
-                                        const unsigned char* sb, void* c, hipStream_t s) {
-  if (plan.lds_bytes != kMxRingLds || plan.b_load != kLoadKDirect || !plan.params.a_dwords || !plan.params.b_dwords) return hipErrorInvalidValue;
-  static std::atomic<bool> raised{false};
+template <int BM>
+static inline hipError_t launch_mx_ring_of(const lc_mx_gemm_plan& plan, const unsigned char* a, const unsigned char* sa, const unsigned char* b,
+                                           const unsigned char* sb, void* c, hipStream_t s) {
+  if (plan.lds_bytes != 5u * BM * 128u || plan.b_load != kLoadKDirect || !plan.params.a_dwords || !plan.params.b_dwords) return hipErrorInvalidValue;
+  static std::atomic<bool> raised{false};   // one flag per instantiation: the attribute belongs to the kernel function
   if (!raised.load(std::memory_order_acquire)) {
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&mx_ring_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&mx_ring_kernel<BM>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
     if (e != hipSuccess) return e;
     raised.store(true, std::memory_order_release);
   }
   const unsigned grid = plan.params.g.tiles_m * plan.params.g.tiles_n * plan.params.g.L;
-  hipLaunchKernelGGL(mx_ring_kernel, dim3(grid), dim3(kBlock), plan.lds_bytes, s, plan.params, a, sa, b, sb, c);
+  hipLaunchKernelGGL((mx_ring_kernel<BM>), dim3(grid), dim3(kBlock), plan.lds_bytes, s, plan.params, a, sa, b, sb, c);
   return hipSuccess;
+}
+static inline hipError_t launch_mx_ring(const lc_mx_gemm_plan& plan, const unsigned char* a, const unsigned char* sa, const unsigned char* b,
+                                        const unsigned char* sb, void* c, hipStream_t s) {
+  if (plan.tile_m == 256 && plan.tile_n == 256) return launch_mx_ring_of<256>(plan, a, sa, b, sb, c, s);
+  if (plan.tile_m == 128 && plan.tile_n == 128) return launch_mx_ring_of<128>(plan, a, sa, b, sb, c, s);
+  return hipErrorInvalidValue;
 }
 
 }  // namespace lc

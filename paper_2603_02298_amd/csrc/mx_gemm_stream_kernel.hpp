@@ -7,6 +7,10 @@
 // One operand in 16 bits: a k tile is 64 k.  The codes pass through registers, where they are expanded to the other operand's type, into the
 // arrangement of the generic GEMM's k vectors (blocks along k) or row vectors (blocks along the rows); the 16-bit operand goes into
 // LDS as the generic GEMM's does.
+// It takes what the ring (both codes) and the wide kernel (one in 16 bits) do not: k modes of several leaves, scales that four neighbouring blocks do not
+// keep together, 16-bit operands off the 16-byte grid or not contiguous along k; and of two operands in codes the problems of few tiles.  A k tile's
+// loads are asked for one k tile ahead, so its time is theirs: 256 x 4096 x 4096 both codes 13.4 us (64 x 64 tiles), 512 x 4096 x 4096 15.5 us (128 x 64),
+// 1.1 PFLOP/s.
 #pragma once
 #include <hip/hip_runtime.h>
 

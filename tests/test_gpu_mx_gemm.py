@@ -113,7 +113,7 @@ CODES = [(1, 1, 32), (1, 40, 64), (3, 17, 96), (16, 16, 128), (17, 33, 160), (64
 
 
 @pytest.mark.parametrize("M,N,K", CODES)
-@pytest.mark.parametrize("tile", [0, 16, 3216, 32, 64, 12864, 128, 256])
+@pytest.mark.parametrize("tile", [0, 16, 3216, 32, 64, 12864, 128, 256, 128128])
 def test_codes_by_codes(M, N, K, tile, monkeypatch):
     if tile:
         monkeypatch.setenv("LC_TUNE_MX_TILE", str(tile))
@@ -138,7 +138,7 @@ def test_codes_by_codes(M, N, K, tile, monkeypatch):
     # batches: A's matrices apart, B's shared, scales shared
     ("(33,320,3):(320,1,16000)", "(33,10,3):(10,1,330)", "(50,320,3):(320,1,0)", "(50,10,3):(10,1,0)", "(33,50,3):(50,1,1700)"),
 ])
-@pytest.mark.parametrize("tile", [0, 32, 64, 128, 256])
+@pytest.mark.parametrize("tile", [0, 32, 64, 128, 256, 128128])
 def test_layouts_of_codes(a, a_s, b, b_s, c, tile, monkeypatch):
     if tile:
         monkeypatch.setenv("LC_TUNE_MX_TILE", str(tile))
@@ -432,7 +432,7 @@ def test_nan_around_the_operands_stays_out(M, N, K, pitch, order, blocked, tile,
 
 
 @pytest.mark.parametrize("M,N,K", [(5, 20, 96), (40, 70, 320), (130, 140, 544), (300, 260, 1056)])
-@pytest.mark.parametrize("tile", [0, 32, 64, 128, 256])
+@pytest.mark.parametrize("tile", [0, 32, 64, 128, 256, 128128])
 def test_scales_between_the_rows_of_codes_stay_out(M, N, K, tile, monkeypatch):
     """Scales of 255 between, before and behind the rows' own, which start at an odd address."""
     if tile:
