@@ -222,8 +222,9 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(MxCopyParams P, cons
 // ---------------------------------------------------------------------------------------------
 // Along the rows: lanes hold 16 bytes of rows at eight k each, and four lanes transpose their codes among them (mx_row_vector).
 // Quantisation collects a workgroup's blocks in LDS, which gives rows of eight blocks' codes and scales one store of 128 and of 8 bytes:
-// 4100 x 5003 f32 from columns in 36 us with every lane storing its own, 32 us so (2.9 TB/s: the reads are no more than the matrix, 81 MB, the writes
-// 15.5 MB for 10.9, since rows of 2512 and 157 bytes end inside lines).  A lane with all 32 k of a block needs neither and took 33 us there, but 9.6 us instead of 7 for 4096 x 2048 bf16: too few waves.
+// 4100 x 5003 f32 from columns in 36 us with every lane storing its own, 32 us so (2.9 TB/s: the reads are no more than the matrix, 82 MB, the
+// writes 15.5 MB for 10.9, since rows of 2512 and 157 bytes end inside lines).  A lane with all 32 k of a block needs neither and took 33 us there,
+// but 9.6 us instead of 7 for 4096 x 2048 bf16: too few wavefronts.
 // Dequantisation of 8192 x 8192 bf16 into columns: 39 us, 4.4 TB/s.
 // The tiles are dealt to the XCDs in stretches (gemm_tile_order_of_block): 55 -> 50 us for the 4100 x 5003 f32 there and back.
 // ---------------------------------------------------------------------------------------------
