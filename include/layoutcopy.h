@@ -380,7 +380,8 @@ lc_status_t lc_mx_dequantize(const void* codes, const lc_layout_t* codes_layout,
  * order of their own but the same one every time, and rounded once.
  *   Both in codes: A over (M,K), B over (N,K), C over (M,N), K whole blocks, both blocked along k.  Products are exact.
  *   A in 16 bits, B blocked along k (its scales over (N,P/32)): A over (M,K), B over (N,P), P >= K: the forward product with quantised
- *   weights.  B's elements past K are not used.
+ *   weights.  B's elements past K do not enter; where K ends inside a block, those of that block have to be finite in A's type (lc_mx_quantize
+ *   writes zeros there).
  *   A in 16 bits, B blocked along its rows (its scales over (P/32,K)): A over (M,K), B over (P,K), C over (M,N), P >= N: the product with the
  *   transposed weights, i.e. the gradient of the forward product's A.
  *   B's elements are rounded to A's type before they are multiplied: exact in bf16; in fp16 for magnitudes from 2^-14 to 65504, beyond which

@@ -24,7 +24,7 @@ struct MxOperand {
   int64_t rows = 0, k = 0;       // extents of the codes' modes
   Modes q_r, q_k, s_r, s_k;      // of the blocked mode: blocks
 };
-// Checks that blocks of 32 codes are whole 16-byte words and that the scales fit; batched: a third mode on both.
+// Checks that blocks of 32 codes are whole 16-byte words and that the scales fit.
 lc_status_t mx_operand(const Layout& codes, const Layout& scales, int blocked, MxOperand* out);
 
 lc_status_t make_mx_plan(bool quantize, const Layout& x, const Layout& codes, const Layout& scales, int dtype, int rule, lc_mx_plan* out);
