@@ -73,7 +73,8 @@ using mx_c_elem = std::conditional_t<TYPE == LC_F32, float, std::conditional_t<T
 // A lane stays in its row group (column), so it evaluates one of C's modes once; U units are on their way at a time.
 // ONE: the other mode has one leaf, so that its offsets are one multiplication.  A loop, not unrolled, and few units where offsets take divisions: six
 // types and forms of C times all units with their divisions in line would be more instructions than the instruction cache holds.
-template <int BM, int BN, int LANES, int TYPE, bool ADD, bool VEC, bool ONE>
+// PAST: written past the caches (MxGemmParams::past_caches).
+template <int BM, int BN, int LANES, int TYPE, bool ADD, bool VEC, bool ONE, bool PAST>
 __device__ __forceinline__ void mx_tile_to_c_as(const MxGemmParams& P, void* C, const unsigned char* lds, uint32_t m0, uint32_t n0, uint32_t tid) {
   using T = mx_c_elem<TYPE>;
   typedef T Tx4 __attribute__((ext_vector_type(4)));
@@ -105,7 +106,10 @@ __device__ __forceinline__ void mx_tile_to_c_as(const MxGemmParams& P, void* C, 
       });
       static_for<U>([&](auto u) {
         if constexpr (ADD) v[u] += __builtin_convertvector(old[u], f32x4);
-        if (n0 + slow + (uint32_t)(first + u) * STEP < P.g.N) *reinterpret_cast<Tx4*>(c + off[u]) = __builtin_convertvector(v[u], Tx4);
+        if (n0 + slow + (uint32_t)(first + u) * STEP < P.g.N) {
+          if constexpr (PAST) __builtin_nontemporal_store(__builtin_convertvector(v[u], Tx4), reinterpret_cast<Tx4*>(c + off[u]));
+          else *reinterpret_cast<Tx4*>(c + off[u]) = __builtin_convertvector(v[u], Tx4);
+        }
       });
     } else {
       uint32_t off[U][4];
@@ -140,13 +144,20 @@ __device__ __forceinline__ void mx_c_dispatch(const MxGemmParams& P, F&& f) {
 template <int BM, int BN, int LANES>
 __device__ __forceinline__ void mx_tile_to_c(const MxGemmParams& P, void* C, const unsigned char* lds, uint32_t m0, uint32_t n0, uint32_t tid) {
   mx_c_dispatch(P, [&](auto type, auto add) {
-    auto to_c = [&](auto vec, auto one) { mx_tile_to_c_as<BM, BN, LANES, decltype(type)::value, decltype(add)::value, decltype(vec)::value, decltype(one)::value>(P, C, lds, m0, n0, tid); };
+    auto to_c = [&](auto vec, auto one, auto past) {
+      mx_tile_to_c_as<BM, BN, LANES, decltype(type)::value, decltype(add)::value, decltype(vec)::value, decltype(one)::value, decltype(past)::value>(P, C, lds, m0, n0, tid);
+    };
+    using Yes = std::true_type;
+    using No = std::false_type;
     if (P.g.c_vec) {
-      if (P.g.c_n.n == 1) to_c(std::true_type{}, std::true_type{});
-      else to_c(std::true_type{}, std::false_type{});
+      if constexpr (!decltype(add)::value) {
+        if (P.past_caches && reinterpret_cast<uintptr_t>(C) % kMxLine == 0) return to_c(Yes{}, Yes{}, Yes{});
+      }
+      if (P.g.c_n.n == 1) to_c(Yes{}, Yes{}, No{});
+      else to_c(Yes{}, No{}, No{});
     } else {
-      if (P.g.c_m.n == 1) to_c(std::false_type{}, std::true_type{});
-      else to_c(std::false_type{}, std::false_type{});
+      if (P.g.c_m.n == 1) to_c(No{}, Yes{}, No{});
+      else to_c(No{}, No{}, No{});
     }
   });
 }

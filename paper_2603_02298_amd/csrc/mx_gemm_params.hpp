@@ -21,6 +21,7 @@ struct MxGemmParams {
   GemmMode sa_r, sa_k, sb_r, sb_k, sa_l, sb_l;   // scales in bytes; the blocked mode counts blocks
   int32_t c_type;                // LC_F32, LC_F16, LC_BF16
   int32_t accumulate;
+  int32_t past_caches;           // C is written past the caches: as large as the L2s or larger, in vectors that make whole lines
   int32_t a_dwords, b_dwords;    // 1: four blocks 4 c .. 4 c + 3 of a row have neighbouring scales
   uint32_t blocks;               // blocks along k that hold k < K
   uint32_t scale_pitch;          // direct kernel: bytes from one row's scales to the next in LDS; 0: they do not fit, and are read where they lie

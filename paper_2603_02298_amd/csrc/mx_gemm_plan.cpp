@@ -179,6 +179,10 @@ lc_status_t make_mx_gemm_plan(const Layout& A, const Layout* A_scales, const Lay
   P.accumulate = accumulate != 0;
   P.a_dwords = a.dwords;
   P.b_dwords = b.dwords;
+  // A C as large as the L2s or larger is written past the caches where its contiguous stretches begin on lines (if C does: the kernel looks); a smaller
+  // one stays there for whoever reads it next, and old values to be added bring their lines in anyway.  8192^3 into f32 305 -> 296 us, 4096 x 8192 x
+  // 4096 into bf16, its quantisation included, 97 -> 93.
+  P.past_caches = G.c_vec && !accumulate && c_n.size() == 1 && c_n[0].stride * c_bytes % kMxLine == 0 && M * N * plan.L * c_bytes >= (int64_t(32) << 20);
   plan.c_align = G.c_vec ? 4 * c_bytes : c_bytes;
 
   // How the kernel's B is brought in.  Codes: straight into LDS, k tiles inside the k mode's first leaf or vector by vector.  16-bit elements: k vectors

@@ -10,9 +10,9 @@
 // those covers them.
 // The sums pass through LDS, a column of fragments of a wavefront at a time and each wavefront in a place of its own, so that C is written in
 // whole lines.
-// What it measures, and what bounds it: 8192^3 into f32 300 us, 3.7 PFLOP/s, the matrix cores busy 45 % of clocks that the power limit holds at 1.93 GHz
+// What it measures, and what bounds it: 8192^3 into f32 296 us, 3.7 PFLOP/s, the matrix cores busy 45 % of clocks that the power limit holds at 1.93 GHz
 // (operands of random codes; they reach 6.5 PFLOP/s with nothing but these instructions).  A k tile of 256 x 256 takes 1.15 us, its 64 KiB at 58 GB/s
-// per CU, and every tile 17 us more: all CUs write their 256 KiB of C at the same time (13 us of that), then load the next first k tile.
+// per CU, and every tile 15 us more: all CUs write their 256 KiB of C at the same time (11 us of that), then load the next first k tile.
 // A k step's products go in parts with everything else between them: in one piece, 8192^3 took 340 us.
 #pragma once
 #include <hip/hip_runtime.h>

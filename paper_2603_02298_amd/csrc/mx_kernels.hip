@@ -81,6 +81,14 @@ __device__ __forceinline__ u32x2 unpack_codes(uint32_t codes, float scale) {
 
 // vectors at the elements' own alignment
 typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+// Elements to be quantised are read once, past the caches: 8192 x 8192 bf16 in 33 us instead of 42, 4100 x 5003 f32 from columns in 22 instead of 32.
+__device__ __forceinline__ u32x4 load_vector(const unsigned char* p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(p)); }
+// Dequantised ones are written past the caches where that pays (lc_mx_plan::large_lines).
+template <bool PAST>
+__device__ __forceinline__ void store_vector(unsigned char* p, u32x4 v) {
+  if constexpr (PAST) __builtin_nontemporal_store((u32x4_any)v, reinterpret_cast<u32x4_any*>(p));
+  else *reinterpret_cast<u32x4_any*>(p) = v;
+}
 
 template <int DT>
 __device__ __forceinline__ uint32_t load_element(const unsigned char* p) {
@@ -102,9 +110,9 @@ __device__ __forceinline__ uint32_t quad_swap2(uint32_t v) { return (uint32_t)__
 // ---------------------------------------------------------------------------------------------
 // Along k, or element by element: four lanes share a block, eight consecutive k each; kMxUnroll rows' loads per lane are in flight
 // before the first is used.  WHOLE: K is a multiple of 8, so that a vector lies inside or outside as a whole.
-// Memory bounds it.  8192 x 8192 bf16, scales in groups of eight blocks: quantised in 42 us, 4.0 TB/s, dequantised in 27.5 us, 6.2 TB/s
+// Memory bounds it.  8192 x 8192 bf16, scales in groups of eight blocks: quantised in 33 us, 5.1 TB/s, dequantised in 26.6 us, 6.4 TB/s
 // (codes still in the caches).  The order of the tiles decides: neighbouring workgroups along k write and read whole lines of a row, 50 and
-// 35 us became 42 and 27.5 when they no longer went along the rows.
+// 35 us became 42 and 27.5 when they no longer went along the rows; reading past the caches made 33 of the 42.
 // ---------------------------------------------------------------------------------------------
 
 // Where a lane's rows are in a tensor: base + u * step where the rows' mode has one leaf, evaluated row by row otherwise.
@@ -132,7 +140,7 @@ __device__ __forceinline__ void quantize_along_k(const MxCopyParams& P, const un
     u32x4 w[kMxUnroll][DW / 4];
     static_for<(int)kMxUnroll>([&](auto u) {
       const unsigned char* p = x + at(row + (uint32_t)u * rows < P.R ? (uint32_t)u : 0u);
-      static_for<DW / 4>([&](auto d) { w[u][d] = reinterpret_cast<const u32x4_any*>(p)[(int)d]; });
+      static_for<DW / 4>([&](auto d) { w[u][d] = load_vector(p + 16 * (int)d); });
     });
     __builtin_amdgcn_sched_barrier(0);
     static_for<(int)kMxUnroll>([&](auto u) { static_for<DW>([&](auto d) { v[u][d] = w[u][d / 4][d % 4]; }); });
@@ -178,7 +186,7 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(MxCopyParams P, const 
   else quantize_along_k<DT, VECTORS, false>(P, x, q, s);
 }
 
-template <int DT, bool VECTORS>
+template <int DT, bool VECTORS, bool PAST>
 __global__ __launch_bounds__(256) void mx_dequantize_kernel(MxCopyParams P, const unsigned char* __restrict__ q, const unsigned char* __restrict__ s,
                                                             unsigned char* __restrict__ x) {
   constexpr int ES = kElemBytes<DT>, DW = 2 * ES;
@@ -209,7 +217,7 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(MxCopyParams P, cons
     });
     unsigned char* p = x + at((uint32_t)u);
     if (in) {
-      static_for<DW / 4>([&](auto d) { reinterpret_cast<u32x4_any*>(p)[(int)d] = u32x4{v[4 * d], v[4 * d + 1], v[4 * d + 2], v[4 * d + 3]}; });
+      static_for<DW / 4>([&](auto d) { store_vector<PAST>(p + 16 * (int)d, u32x4{v[4 * d], v[4 * d + 1], v[4 * d + 2], v[4 * d + 3]}); });
     } else {
       static_for<8>([&](auto j) {
         const uint32_t k = k0 + (uint32_t)j;
@@ -222,11 +230,11 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(MxCopyParams P, cons
 // ---------------------------------------------------------------------------------------------
 // Along the rows: lanes hold 16 bytes of rows at eight k each, and four lanes transpose their codes among them (mx_row_vector).
 // Quantisation collects a workgroup's blocks in LDS, which gives rows of eight blocks' codes and scales one store of 128 and of 8 bytes:
-// 4100 x 5003 f32 from columns in 36 us with every lane storing its own, 32 us so (2.9 TB/s: the reads are no more than the matrix, 82 MB, the
-// writes 15.5 MB for 10.9, since rows of 2512 and 157 bytes end inside lines).  A lane with all 32 k of a block needs neither and took 33 us there,
-// but 9.6 us instead of 7 for 4096 x 2048 bf16: too few wavefronts.
-// Dequantisation of 8192 x 8192 bf16 into columns: 39 us, 4.4 TB/s.
-// The tiles are dealt to the XCDs in stretches (gemm_tile_order_of_block): 55 -> 50 us for the 4100 x 5003 f32 there and back.
+// 4100 x 5003 f32 from columns in 36 us with every lane storing its own, 32 us so, 22 us with reads past the caches (4.2 TB/s: the reads are no more
+// than the matrix, 82 MB, the writes 15.5 MB for 10.9, since rows of 2512 and 157 bytes end inside lines).  A lane with all 32 k of a block needs
+// neither exchange and took 9.6 us instead of 7 for 4096 x 2048 bf16: too few wavefronts.
+// Dequantisation of 8192 x 8192 bf16 into columns: 28 us, 6.1 TB/s (39 us when it was written through the caches).
+// The tiles are dealt to the XCDs in stretches (gemm_tile_order_of_block): 55 -> 50 us for the 4100 x 5003 f32 there and back, then.
 // ---------------------------------------------------------------------------------------------
 
 // 4 x 4 over the wave's four rows of 16 lanes: v[j] of row i becomes v[i] of row j.
@@ -269,7 +277,7 @@ __global__ __launch_bounds__(64 * kMxRowWaves) void mx_quantize_rows_kernel(MxCo
   const uint32_t k0 = block * kMxBlock + 8u * part;
   const RowWalk at(P.x_k, k0, 1, 0);
   u32x4 v[8];
-  static_for<8>([&](auto k) { v[(int)k] = *reinterpret_cast<const u32x4_any*>(p + (k0 + (uint32_t)k < P.K ? at((uint32_t)k) : 0)); });   // (a k outside reads k = 0)
+  static_for<8>([&](auto k) { v[(int)k] = load_vector(p + (k0 + (uint32_t)k < P.K ? at((uint32_t)k) : 0)); });   // (a k outside reads k = 0)
   __builtin_amdgcn_sched_barrier(0);
   static_for<8>([&](auto k) { v[(int)k] = select_or_zero(k0 + (uint32_t)k < P.K, v[(int)k]); });
   u32x4 m;
@@ -310,7 +318,7 @@ __global__ __launch_bounds__(64 * kMxRowWaves) void mx_quantize_rows_kernel(MxCo
   });
 }
 
-template <int DT>
+template <int DT, bool PAST>
 __global__ __launch_bounds__(64 * kMxRowWaves) void mx_dequantize_rows_kernel(MxCopyParams P, const unsigned char* __restrict__ q,
                                                                             const unsigned char* __restrict__ s, unsigned char* __restrict__ x) {
   constexpr uint32_t ES = kElemBytes<DT>, ROWS = 16 / ES;
@@ -361,7 +369,7 @@ __global__ __launch_bounds__(64 * kMxRowWaves) void mx_dequantize_rows_kernel(Mx
       if (k0 + k < P.K) {
         unsigned char* to = x + at(k);
         if (start == first) {
-          *reinterpret_cast<u32x4_any*>(to) = v;
+          store_vector<PAST>(to, v);
         } else {   // the vector that was started early: only the rows that are its own
           static_for<(int)ROWS>([&](auto j) {
             if (start + (uint32_t)j >= first) store_element<DT>(to + (uint32_t)j * ES, DT == LC_F32 ? v[j % 4] : v[(j / 2) % 4] >> (16 * (j % 2)));
@@ -388,9 +396,12 @@ void launch_quantize(const lc_mx_plan& plan, const unsigned char* x, unsigned ch
 template <int DT>
 void launch_dequantize(const lc_mx_plan& plan, const unsigned char* q, const unsigned char* s, unsigned char* x, hipStream_t st) {
   const dim3 grid(plan.groups), block(plan.access == kMxAlongRows ? 64 * kMxRowWaves : 256);
-  if (plan.access == kMxAlongRows) hipLaunchKernelGGL((mx_dequantize_rows_kernel<DT>), grid, block, 0, st, plan.params, q, s, x);
-  else if (plan.access == kMxAlongK) hipLaunchKernelGGL((mx_dequantize_kernel<DT, true>), grid, block, 0, st, plan.params, q, s, x);
-  else hipLaunchKernelGGL((mx_dequantize_kernel<DT, false>), grid, block, 0, st, plan.params, q, s, x);
+  const bool past = plan.large_lines && reinterpret_cast<uintptr_t>(x) % kMxLine == 0;
+  if (plan.access == kMxAlongRows && past) hipLaunchKernelGGL((mx_dequantize_rows_kernel<DT, true>), grid, block, 0, st, plan.params, q, s, x);
+  else if (plan.access == kMxAlongRows) hipLaunchKernelGGL((mx_dequantize_rows_kernel<DT, false>), grid, block, 0, st, plan.params, q, s, x);
+  else if (plan.access == kMxAlongK && past) hipLaunchKernelGGL((mx_dequantize_kernel<DT, true, true>), grid, block, 0, st, plan.params, q, s, x);
+  else if (plan.access == kMxAlongK) hipLaunchKernelGGL((mx_dequantize_kernel<DT, true, false>), grid, block, 0, st, plan.params, q, s, x);
+  else hipLaunchKernelGGL((mx_dequantize_kernel<DT, false, false>), grid, block, 0, st, plan.params, q, s, x);
 }
 
 }  // namespace

@@ -10,6 +10,7 @@ namespace lc {
 
 constexpr uint32_t kMxBlock = 32;       // codes that share a scale
 constexpr uint32_t kMxBlockBytes = 16;  // of codes
+constexpr uint32_t kMxLine = 128;       // bytes of a cache line
 
 // One coalesced mode, integral coordinate -> byte offset of 64 bits (copies reach whole memories).
 struct MxMode {

@@ -12,6 +12,7 @@ struct lc_mx_plan {
   lc::MxAccess access = lc::kMxElements;
   lc::MxCopyParams params{};
   uint32_t groups = 0;           // workgroups of the launch
+  bool large_lines = false;      // x is as large as the L2s or larger, and its contiguous stretches begin on lines where x does
   int64_t x_min = 0, x_cosize = 0, q_cosize = 0, s_cosize = 0;   // x in elements (smallest offset, largest + 1), codes in elements of 4 bits
   std::string x_text, q_text, s_text;
 };

@@ -194,3 +194,26 @@ def test_tensor_helpers_refuse_what_does_not_fit():
         lc.mx_dequantize_tensor(codes.cpu(), text, scales, "(2,2):(2,1)", x, text)
     with pytest.raises(lc.LayoutCopyError):
         lc.mx_quantize_tensor(x, text, codes.repeat(2)[8:], text, scales, "(2,2):(2,1)")   # codes off the 16-byte grid
+
+
+@pytest.mark.parametrize("R,K,x", [(2101, 4100, "k"), (2101, 4128, "k"), (2101, 4100, "r"), (2104, 4100, "r"), (3, 2900000, "r3"), (4100, 2050, "strided")])
+@pytest.mark.parametrize("origin", [0, 1])
+def test_large_tensors_on_and_off_cache_lines(R, K, x, origin):
+    """More than 32 MiB of fp32, rows or columns that begin on lines and (origin 1) that do not."""
+    dev = torch.device("cuda:0")
+    text = {"k": "(%d,%d):(%d,1)" % (R, K, 4128), "r": "(%d,%d):(1,%d)" % (R, K, 2112), "r3": "(%d,%d):(1,4)" % (R, K),
+            "strided": "(%d,%d):(%d,1)" % (R, K, 2051)}[x]
+    P = (K + 31) // 32 * 32
+    g = torch.Generator().manual_seed(K)
+    codes = torch.randint(0, 256, (R, P // 2), dtype=torch.uint8, generator=g)
+    scales = torch.randint(100, 150, (R, P // 32), dtype=torch.uint8, generator=g)
+    size = lc.Layout(text).cosize + origin + 9
+    dst = torch.full((size,), 77.0, device=dev)
+    lc.mx_dequantize_tensor(codes.to(dev), "(%d,%d):(%d,1)" % (R, P, P), scales.to(dev), "(%d,%d):(%d,1)" % (R, P // 32, P // 32), dst, text, dst_origin=origin)
+    torch.cuda.synchronize()
+    levels = torch.from_numpy(mx.LEVELS).float()   # (codes times powers of two: exact in fp32)
+    want = levels[torch.stack([codes & 15, codes >> 4], 2).long().reshape(R, P)] * torch.exp2(scales.float() - 127).repeat_interleave(32, 1)
+    off = torch.from_numpy(mx.offsets(text)).reshape(R, K) + origin
+    expect = torch.full((size,), 77.0)
+    expect[off] = want[:, :K]
+    assert torch.equal(dst.cpu(), expect)

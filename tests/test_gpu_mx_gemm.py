@@ -454,3 +454,27 @@ def test_scales_between_the_rows_of_codes_stay_out(M, N, K, tile, monkeypatch):
                   torch.cuda.current_stream().cuda_stream)
     torch.cuda.synchronize()
     assert (c.cpu().double().numpy() == av @ bv.T).all()
+
+
+@pytest.mark.parametrize("a_dtype", ["mxfp4", "bf16"])
+@pytest.mark.parametrize("tile", [0, 12864, 128, 256, 256128, 128128, 128064])
+@pytest.mark.parametrize("pitch,c_dtype", [(4128, "f32"), (4130, "f32"), (8256, "f16")])
+def test_large_c(a_dtype, tile, pitch, c_dtype, monkeypatch):
+    """More than 32 MiB of C, with rows that begin on cache lines and with ones that do not."""
+    if tile:
+        monkeypatch.setenv("LC_TUNE_MX_TILE", str(tile))
+    M, N, K = 2101, pitch - 5, 64
+    a, a_s = (_rows(M, K), _scales(M, K)) if a_dtype == "mxfp4" else (_rows(M, K), None)
+    _run(a, a_s, _rows(N, K), _scales(N, K), "(%d,%d):(%d,1)" % (M, N, pitch), a_dtype, c_dtype, False, "exact")
+
+
+def test_large_c_off_a_cache_line():
+    dev = torch.device("cuda:0")
+    M, N, K = 2050, 4096, 32
+    a, b = torch.full((M * K // 2,), 0x22, dtype=torch.uint8, device=dev), torch.full((N * K // 2,), 0x22, dtype=torch.uint8, device=dev)
+    s = torch.full((4096,), 127, dtype=torch.uint8, device=dev)
+    c = torch.zeros(M * N + 64, device=dev)
+    plan = lc.MxGemmPlan(_rows(M, K), _scales(M, K), _rows(N, K), _scales(N, K), _rows(M, N), accumulate=False)
+    plan.execute(a.data_ptr(), s.data_ptr(), b.data_ptr(), s.data_ptr(), c.data_ptr() + 16, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert (c[:4] == 0).all() and (c[4:4 + M * N] == K).all() and (c[4 + M * N:] == 0).all()
