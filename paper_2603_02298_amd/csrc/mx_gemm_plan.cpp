@@ -239,9 +239,13 @@ lc_status_t make_mx_gemm_plan(const Layout& A, const Layout* A_scales, const Lay
     //   one in 16 bits (128 x 64, 128 x 128, 256 x 128, 256 x 256): 128 x 2048 x 2048 9.1, 18.0, 21.0, -, -; 128 x 8192 x 8192 61, 60, -, -, -; 256 x 4096 x 4096 38.9, 31.4,
     //   36.3, 57, -; 512 x 4096 x 4096 78, 35.8, 39.6, 61, -; 1024 x 4096 x 4096 -, 55, 46, 65, 92; 2048 x 4096 x 4096 -, 102, 75, 74, 96; along the rows -, -, 92, 82, 100;
     //   3000 x 5000 x 1024 -, 59, 43, 48, 40; 2048 x 8192 x 4096 -, -, -, 144, 116.
+    // The direct kernel beside 16-bit elements loads up to four rows of them a quarter of a fragment at a time and up to 16 in tiles of 32 x 16: what a round
+    // takes goes with the rows.  (direct, 128 x 64: 1 x 32768 x 8192 28.4, 59; 16 x 32768 x 8192 44.6, 60.6; 16 x 16384 x 4096 16.4, 31.5; 32 x 16384 x 8192 31.9, 58;
+    // 32 x 32768 x 8192 61, 60.5; 64 x 16384 x 4096 42.3, 32.4; 96 x 8192 x 4096 29.4, 30.7.)
+    const double direct_round = codes || b.rows > 16 ? 9.5 : b.rows > 4 ? 6.0 : 3.6;
     struct Choice { MxGemmKernel kernel; int tm, tn; double round, alone; bool can; };
     const Choice choices[] = {
-        {kMxDirect, 32, 32, 9.5, 9.5, can_direct && (!codes || G.k_tiles > 2)},   // (both codes over one or two k tiles: the stream kernel starts with less)
+        {kMxDirect, 32, 32, direct_round, 9.5, can_direct && (!codes || G.k_tiles > 2)},   // (both codes over one or two k tiles: the stream kernel starts with less)
         {kMxStream, 64, 64, 9.0, 13.5, codes}, {kMxStream, 128, 64, 10.3, 15.0, codes}, {kMxStream, 128, 128, 16.0, 22.0, codes && !(can_ring && G.k_tiles > 2)},
         {kMxRing, 128, 128, 14.8, 19.5, can_ring && G.k_tiles > 2},   // (over one or two k tiles its first loads are all there is)
         {kMxRing, 256, 256, 44.5, 36.0, can_ring && tiles_of(256, 256) >= 96},
