@@ -393,16 +393,26 @@ def lc_copy(src_ptr, src_layout, dst_ptr, dst_layout, dtype, stream=0):
         raise LayoutCopyError(status, "lc_copy(%s -> %s)" % (sl, dl))
 
 
+def _memory_of(t):
+    """Elements of memory from a tensor's first to its last, both counted: what the offsets of a layout may reach.  The layout alone says where
+    elements lie there, the tensor's strides only how far its memory reaches: a view with gaps covers them, one that repeats elements
+    (expand) covers no more than those."""
+    if t.is_contiguous() or t.numel() == 0:
+        return t.numel()
+    return 1 + sum((extent - 1) * stride for extent, stride in zip(t.shape, t.stride()))
+
+
 def copy_tensor(src, src_layout, dst, dst_layout, dtype=None, src_origin=0, dst_origin=0):
     """Convenience for torch tensors on the GPU: takes data pointers and torch's current stream.  src_origin / dst_origin:
-    the element of each tensor that offset 0 of its layout refers to (layouts with negative strides reach below it)."""
+    the element of each tensor that offset 0 of its layout refers to (layouts with negative strides reach below it).  Offsets count
+    the elements of memory from the tensor's first one on, whatever its strides are; so they do in the helpers below."""
     import torch
     if not (src.is_cuda and dst.is_cuda):
         raise RuntimeError("copy_tensor needs GPU tensors: the copy only runs in the HIP kernels")
     if dtype is None:
         dtype = {4: "b32", 2: "b16", 1: "b8", 8: "b64"}[src.element_size()]
     sl, dl = _as_layout(src_layout), _as_layout(dst_layout)
-    if src_origin + sl.min_offset < 0 or src_origin + sl.cosize > src.numel() or dst_origin + dl.min_offset < 0 or dst_origin + dl.cosize > dst.numel():
+    if src_origin + sl.min_offset < 0 or src_origin + sl.cosize > _memory_of(src) or dst_origin + dl.min_offset < 0 or dst_origin + dl.cosize > _memory_of(dst):
         raise ValueError("tensor does not cover the offsets the layout reaches")
     lc_copy(src.data_ptr() + src_origin * src.element_size(), sl, dst.data_ptr() + dst_origin * dst.element_size(), dl, dtype,
             torch.cuda.current_stream().cuda_stream)
@@ -475,7 +485,7 @@ def gemm_tensor(a, a_layout, b, b_layout, c, c_layout):
     if a.dtype != b.dtype or a.dtype not in (torch.bfloat16, torch.float16) or c.dtype != torch.float32:
         raise ValueError("a, b: both bfloat16 or both float16; c: float32")
     la, lb, lc_ = _as_layout(a_layout), _as_layout(b_layout), _as_layout(c_layout)
-    if la.cosize > a.numel() or lb.cosize > b.numel() or lc_.cosize > c.numel():
+    if la.cosize > _memory_of(a) or lb.cosize > _memory_of(b) or lc_.cosize > _memory_of(c):
         raise ValueError("tensor smaller than the layout's cosize")
     lc_gemm(a.data_ptr(), la, b.data_ptr(), lb, c.data_ptr(), lc_, "bf16" if a.dtype == torch.bfloat16 else "f16",
             torch.cuda.current_stream().cuda_stream)
@@ -640,7 +650,7 @@ def _mx_covers(codes, codes_layout, scales, scales_layout):
     import torch
     if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
         raise ValueError("codes and scales: uint8")
-    if (codes_layout.cosize + 1) // 2 > codes.numel() or scales_layout.cosize > scales.numel():
+    if (codes_layout.cosize + 1) // 2 > _memory_of(codes) or scales_layout.cosize > _memory_of(scales):
         raise ValueError("tensor smaller than the layout's cosize")
 
 
@@ -651,7 +661,7 @@ def mx_quantize_tensor(src, src_layout, codes, codes_layout, scales, scales_layo
     with _mx_device("mx_quantize_tensor", (src, codes, scales)):
         a, q, s = _as_layout(src_layout), _as_layout(codes_layout), _as_layout(scales_layout)
         _mx_covers(codes, q, scales, s)
-        if src_origin + a.min_offset < 0 or src_origin + a.cosize > src.numel():
+        if src_origin + a.min_offset < 0 or src_origin + a.cosize > _memory_of(src):
             raise ValueError("tensor does not cover the offsets the layout reaches")
         lc_mx_quantize(src.data_ptr() + src_origin * src.element_size(), a, codes.data_ptr(), q, scales.data_ptr(), s, _mx_dtype(src), rule,
                        torch.cuda.current_stream().cuda_stream)
@@ -663,7 +673,7 @@ def mx_dequantize_tensor(codes, codes_layout, scales, scales_layout, dst, dst_la
     with _mx_device("mx_dequantize_tensor", (codes, scales, dst)):
         q, s, d = _as_layout(codes_layout), _as_layout(scales_layout), _as_layout(dst_layout)
         _mx_covers(codes, q, scales, s)
-        if dst_origin + d.min_offset < 0 or dst_origin + d.cosize > dst.numel():
+        if dst_origin + d.min_offset < 0 or dst_origin + d.cosize > _memory_of(dst):
             raise ValueError("tensor does not cover the offsets the layout reaches")
         lc_mx_dequantize(codes.data_ptr(), q, scales.data_ptr(), s, dst.data_ptr() + dst_origin * dst.element_size(), d, _mx_dtype(dst),
                          torch.cuda.current_stream().cuda_stream)
@@ -682,9 +692,9 @@ def mx_gemm_tensor(a, a_layout, a_scales, a_scales_layout, b, b_layout, b_scales
             _mx_covers(a, la, a_scales, sa)
         elif a.dtype not in (torch.bfloat16, torch.float16):
             raise ValueError("a: bfloat16 or float16, or uint8 with scales")
-        elif la.cosize > a.numel():
+        elif la.cosize > _memory_of(a):
             raise ValueError("tensor smaller than the layout's cosize")
-        if lc_.cosize > c.numel():
+        if lc_.cosize > _memory_of(c):
             raise ValueError("tensor smaller than the layout's cosize")
         lc_mx_gemm(a.data_ptr(), la, a_scales.data_ptr() if codes else None, sa, b.data_ptr(), lb, b_scales.data_ptr(), sb, c.data_ptr(), lc_,
                    "mxfp4" if codes else _mx_dtype(a), _mx_dtype(c), accumulate, torch.cuda.current_stream().cuda_stream)
