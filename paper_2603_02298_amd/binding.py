@@ -684,6 +684,8 @@ def mx_gemm_tensor(a, a_layout, a_scales, a_scales_layout, b, b_layout, b_scales
     float16 with None for its scales and their layout; c float32, bfloat16 or float16."""
     import torch
     codes = a_scales is not None
+    if codes != (a_scales_layout is not None):
+        raise ValueError("a_scales and a_scales_layout: both or neither")
     with _mx_device("mx_gemm_tensor", (a, b, b_scales, c) + ((a_scales,) if codes else ())):
         la, lb, lc_, sb = _as_layout(a_layout), _as_layout(b_layout), _as_layout(c_layout), _as_layout(b_scales_layout)
         sa = _as_layout(a_scales_layout) if codes else None

@@ -95,3 +95,12 @@ def test_other_orders_of_the_same_memory_and_empty_tensors(call, key, calls):
     with pytest.raises(ValueError, match="cover|smaller"):
         helper(**dict(args, **{key: t[:0]}))
     assert len(calls) == 1
+
+
+def test_scales_and_their_layout_come_together(calls):
+    """A layout without scales, or scales without a layout, is refused as the C call refuses it, not left out."""
+    for call, change in (("product", dict(a_scales_layout="(4,3):(3,1)")), ("product of codes", dict(a_scales=None)), ("product of codes", dict(a_scales_layout=None))):
+        helper, args = CALLS[call]
+        with pytest.raises(ValueError, match="a_scales and a_scales_layout"):
+            helper(**dict(args, **change))
+    assert calls == []
