@@ -378,14 +378,15 @@ lc_status_t lc_mx_dequantize(const void* codes, const lc_layout_t* codes_layout,
  * codes, A in codes too (a_dtype LC_MXFP4) or in 16 bits (LC_BF16, LC_F16; a_scales NULL).  Layouts of rank 2, or all of rank 3 for a
  * batch of products (as lc_gemm; strides of 0 share an operand).  C holds fp32, fp16 or bf16 (c_dtype): sums are accumulated in fp32, in an
  * order of their own but the same one every time, and rounded once.
- *   Both in codes: A over (M,K), B over (N,K), C over (M,N), K whole blocks, both blocked along k.  Products are exact.
+ *   Both in codes: A over (M,K), B over (N,K), C over (M,N), K whole blocks, both blocked along k.  Products are exact within fp32's range.
  *   A in 16 bits, B blocked along k (its scales over (N,P/32)): A over (M,K), B over (N,P), P >= K: the forward product with quantised
  *   weights.  B's elements past K do not enter; where K ends inside a block, those of that block have to be finite in A's type (lc_mx_quantize
  *   writes zeros there).
  *   A in 16 bits, B blocked along its rows (its scales over (P/32,K)): A over (M,K), B over (P,K), C over (M,N), P >= N: the product with the
  *   transposed weights, i.e. the gradient of the forward product's A.
- *   B's elements are rounded to A's type before they are multiplied: exact in bf16; in fp16 for magnitudes from 2^-14 to 65504, beyond which
- *   they are infinite, and below to within 2^-25.
+ *   B's elements are rounded to A's type before they are multiplied: in bf16 exact below 2^128 and infinite from there on (scales of 253 and
+ *   254, which only COVER gives, to values from 3.5 * 2^126 on); in fp16 exact for magnitudes from 2^-14 to 65504, beyond which they are infinite, and
+ *   below to within 2^-25.
  * A block whose scale is 255 makes every element of C that it enters NaN.  No call allocates or needs a workspace.
  * a / b / c_align_bytes: alignment the caller guarantees for the pointers (codes: 16 or more).  Errors: INVALID_ARG (ranks, a_scales),
  * SIZE_MISMATCH, BLOCK_LAYOUT, NEGATIVE_STRIDE, DST_ALIASES (C), UNSUPPORTED_DTYPE, MISALIGNED, TOO_LARGE (an extent, or a cosize -- of codes

@@ -52,7 +52,7 @@ __device__ __forceinline__ float mx_scale_value(uint32_t byte) {
   const uint32_t bits = byte == 0u ? 0x00400000u : byte == 255u ? 0x7FC00000u : byte << 23;
   return __builtin_bit_cast(float, bits);
 }
-// eight codes of a dword -> eight 16-bit elements, rounded to nearest (exact in bf16)
+// eight codes of a dword -> eight 16-bit elements, rounded to nearest (in bf16 exact, but infinite from 2^128 on)
 template <int MATH>
 __device__ __forceinline__ u32x4 mx_expand(uint32_t codes, float scale) {
   u32x4 v;

@@ -5,7 +5,7 @@
 // w, w + WAVES, .. of 128 k.  Nothing passes through LDS on the way in.  The order of k inside a chunk is free as long as both operands
 // have the same, so lane l takes block l / 16 of the chunk for row l % 16 of either operand: 16 bytes of codes, which are a whole
 // operand of the 16 x 16 x 128 instruction -- or, beside 16-bit elements, four operands of the 16 x 16 x 32 one, each eight consecutive k
-// of the block, once the codes are expanded to that type (exactly, for bf16).  DEPTH chunks are on their way while one is multiplied.
+// of the block, once the codes are expanded to that type (exactly, for bf16 below 2^128).  DEPTH chunks are on their way while one is multiplied.
 // The scales of the tile's rows are brought into LDS first, under the first codes' way: read where they lie, each would cost the vector memory path
 // a line of its own per row and chunk, as much as the codes do.
 // Needs k modes that chunks lie evenly in (inside the first leaf, or one leaf): then all that changes from chunk to chunk is one scalar per tensor.
