@@ -32,7 +32,8 @@ _MX_WIDE = ["mx_gemm_inst_wide_%s_%s.hip" % (t, k) for t in ("bf16", "f16") for 
 _WIDE = ["gemm_inst_%s_wide.hip" % t for t in ("bf16", "f16")]
 _MX_GEMM = _MX_DIRECT + _MX_STREAM + _MX_RING + _MX_WIDE + ["mx_gemm_plan.cpp", "mx_gemm_kernels.hip", "mx_capi.cpp"]
 _MX = _MX_GEMM + ["mx_plan.cpp", "mx_kernels.hip"]
-KERNEL_HEADERS = {"mx_params.hpp": _MX, "mx_plan.hpp": _MX, "mx_gemm_params.hpp": _MX_GEMM, "mx_gemm_plan.hpp": _MX_GEMM, "gemm_kernel.hpp": _TILE, "gemm_split_kernel.hpp": _SPLIT + _GATHER, "gemm_stream_kernel.hpp": _STREAM + _GATHER, "gemm_wide_kernel.hpp": _WIDE,
+KERNEL_HEADERS = {"lds_limit.hpp": _TILE + _SPLIT + _STREAM + _GATHER + _WIDE + _MX_DIRECT + _MX_STREAM + _MX_RING + _MX_WIDE + ["kernels.hip", "capi.cpp"],
+                  "mx_params.hpp": _MX, "mx_plan.hpp": _MX, "mx_gemm_params.hpp": _MX_GEMM, "mx_gemm_plan.hpp": _MX_GEMM, "gemm_kernel.hpp": _TILE, "gemm_split_kernel.hpp": _SPLIT + _GATHER, "gemm_stream_kernel.hpp": _STREAM + _GATHER, "gemm_wide_kernel.hpp": _WIDE,
                   "gemm_device.hpp": _TILE + _SPLIT + _STREAM + _GATHER + _WIDE + _MX_DIRECT + _MX_STREAM + _MX_RING + _MX_WIDE + ["mx_kernels.hip"],
                   "mx_gemm_device.hpp": _MX_DIRECT + _MX_STREAM + _MX_RING + _MX_WIDE, "mx_gemm_ring_kernel.hpp": _MX_RING, "mx_gemm_wide_kernel.hpp": _MX_WIDE, "mx_gemm_direct_kernel.hpp": _MX_DIRECT, "mx_gemm_stream_kernel.hpp": _MX_STREAM}
 

@@ -5,6 +5,7 @@
 
 #include "algebra.hpp"
 #include "layoutcopy.h"
+#include "lds_limit.hpp"
 #include "plan.hpp"
 #include "plan_cache.hpp"
 #include "semimodule.hpp"
@@ -312,6 +313,15 @@ size_t lc_debug_tuning_key(char* buf, size_t cap) {
   lc::key_tuning(&key);
   if (buf) std::memcpy(buf, key.data(), std::min(cap, key.size()));
   return key.size();
+}
+
+// Whether something done once per device was due (1) or done before (0) on each of a row of devices (test instrumentation, see lds_limit.hpp).
+void lc_debug_due_on_devices(const int* devices, int n, unsigned char* due) {
+  lc::DevicesDone done;
+  for (int i = 0; i < n; ++i) {
+    due[i] = !done.has(devices[i]);
+    done.add(devices[i]);
+  }
 }
 
 // Checking device for tests: replays the plan's index arithmetic on HOST buffers (see plan.hpp).

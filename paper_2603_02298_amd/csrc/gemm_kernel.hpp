@@ -13,11 +13,11 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
-#include <atomic>
 #include <string>
 
 #include "gemm_device.hpp"
 #include "gemm_plan.hpp"
+#include "lds_limit.hpp"
 #include "plan.hpp"
 
 namespace lc {
@@ -421,13 +421,9 @@ __global__ __launch_bounds__(kBlock, (WMB <= 2 ? 2 : 1)) void gemm_kernel(GemmPa
 template <bool BF16, int WB, int A_LOAD, int B_LOAD, bool KTAIL>
 static inline hipError_t launch_gemm_abk(const lc_gemm_plan& plan, const uint16_t* a, const uint16_t* b, float* c, hipStream_t s) {
   if (plan.lds_bytes > 64 * 1024) {
-    static std::atomic<bool> raised{false};   // one flag per instantiation: the attribute belongs to the kernel function
-    if (!raised.load(std::memory_order_acquire)) {
-      hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_kernel<BF16, WB, WB, A_LOAD, B_LOAD, KTAIL>),
-                                         hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-      if (e != hipSuccess) return e;
-      raised.store(true, std::memory_order_release);
-    }
+    static DevicesDone raised;
+    hipError_t e = raise_lds_limit(&raised, &gemm_kernel<BF16, WB, WB, A_LOAD, B_LOAD, KTAIL>);
+    if (e != hipSuccess) return e;
   }
   const unsigned grid = plan.params.tiles_m * plan.params.tiles_n;
   hipLaunchKernelGGL((gemm_kernel<BF16, WB, WB, A_LOAD, B_LOAD, KTAIL>), dim3(grid, plan.params.L), dim3(kBlock), plan.lds_bytes, s, plan.params, a, b, c);

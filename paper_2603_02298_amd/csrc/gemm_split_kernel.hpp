@@ -15,10 +15,9 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
-#include <atomic>
-
 #include "gemm_device.hpp"
 #include "gemm_plan.hpp"
+#include "lds_limit.hpp"
 #include "kernarg.hpp"
 
 namespace lc {
@@ -166,12 +165,10 @@ template <bool BF16, int TM, int TN, int WAVES, int STAGES, int A_LOAD, int B_LO
 static inline hipError_t launch_split_abc(const lc_gemm_plan& plan, const uint16_t* a, const uint16_t* b, float* c, hipStream_t s) {
   static_assert(WAVES * STAGES * (TM + TN) * 128 <= 160 * 1024, "the rings fit LDS");
   if (plan.lds_bytes != (unsigned)(WAVES * STAGES * (TM + TN) * 128) || plan.split_waves != WAVES) return hipErrorInvalidValue;
-  static std::atomic<bool> raised{false};   // one flag per instantiation: the attribute belongs to the kernel function
-  if (plan.lds_bytes > 64 * 1024 && !raised.load(std::memory_order_acquire)) {
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_split_kernel<BF16, TM, TN, WAVES, STAGES, A_LOAD, B_LOAD, C_VEC>),
-                                       hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+  static DevicesDone raised;
+  if (plan.lds_bytes > 64 * 1024) {
+    hipError_t e = raise_lds_limit(&raised, &gemm_split_kernel<BF16, TM, TN, WAVES, STAGES, A_LOAD, B_LOAD, C_VEC>);
     if (e != hipSuccess) return e;
-    raised.store(true, std::memory_order_release);
   }
   const unsigned grid = plan.params.tiles_m * plan.params.tiles_n * plan.params.L;
   hipLaunchKernelGGL((gemm_split_kernel<BF16, TM, TN, WAVES, STAGES, A_LOAD, B_LOAD, C_VEC>), dim3(grid), dim3(64 * WAVES), plan.lds_bytes, s, plan.params, a, b, c);

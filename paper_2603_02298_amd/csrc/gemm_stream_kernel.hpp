@@ -17,10 +17,9 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
-#include <atomic>
-
 #include "gemm_device.hpp"
 #include "gemm_plan.hpp"
+#include "lds_limit.hpp"
 #include "kernarg.hpp"
 
 namespace lc {
@@ -203,12 +202,10 @@ __global__ __launch_bounds__(kBlock, 160 * 1024 / (kStreamStages * (BM + BN) * 1
 template <bool BF16, int BM, int BN, int A_LOAD, int B_LOAD, bool C_VEC, bool PIECES = false>
 static inline hipError_t launch_stream_abc(const lc_gemm_plan& plan, const uint16_t* a, const uint16_t* b, float* c, hipStream_t s) {
   if (plan.lds_bytes != (unsigned)(kStreamStages * (BM + BN) * 128)) return hipErrorInvalidValue;
-  static std::atomic<bool> raised{false};   // one flag per instantiation: the attribute belongs to the kernel function
-  if (plan.lds_bytes > 64 * 1024 && !raised.load(std::memory_order_acquire)) {
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_stream_kernel<BF16, BM, BN, A_LOAD, B_LOAD, C_VEC, PIECES>),
-                                       hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+  static DevicesDone raised;
+  if (plan.lds_bytes > 64 * 1024) {
+    hipError_t e = raise_lds_limit(&raised, &gemm_stream_kernel<BF16, BM, BN, A_LOAD, B_LOAD, C_VEC, PIECES>);
     if (e != hipSuccess) return e;
-    raised.store(true, std::memory_order_release);
   }
   const unsigned grid = plan.params.tiles_m * plan.params.tiles_n * plan.params.L;
   hipLaunchKernelGGL((gemm_stream_kernel<BF16, BM, BN, A_LOAD, B_LOAD, C_VEC, PIECES>), dim3(grid), dim3(kBlock), plan.lds_bytes, s, plan.params, a, b, c);

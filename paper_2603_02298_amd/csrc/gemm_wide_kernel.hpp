@@ -14,10 +14,9 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
-#include <atomic>
-
 #include "gemm_device.hpp"
 #include "gemm_plan.hpp"
+#include "lds_limit.hpp"
 #include "kernarg.hpp"
 
 namespace lc {
@@ -192,13 +191,9 @@ __global__ __launch_bounds__(kBlock, 1) void gemm_wide_kernel(GemmParams P, cons
 template <bool BF16, int WMB, int WNB, int A_LOAD, int B_LOAD>
 static inline hipError_t launch_wide_ab(const lc_gemm_plan& plan, const uint16_t* a, const uint16_t* b, float* c, hipStream_t s) {
   if (plan.lds_bytes != 5u * 256u * 128u || !plan.params.c_vec) return hipErrorInvalidValue;
-  static std::atomic<bool> raised{false};   // one flag per instantiation: the attribute belongs to the kernel function
-  if (!raised.load(std::memory_order_acquire)) {
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_wide_kernel<BF16, WMB, WNB, A_LOAD, B_LOAD>),
-                                       hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-    if (e != hipSuccess) return e;
-    raised.store(true, std::memory_order_release);
-  }
+  static DevicesDone raised;
+  hipError_t e = raise_lds_limit(&raised, &gemm_wide_kernel<BF16, WMB, WNB, A_LOAD, B_LOAD>);
+  if (e != hipSuccess) return e;
   const unsigned grid = plan.params.tiles_m * plan.params.tiles_n * plan.params.L;
   hipLaunchKernelGGL((gemm_wide_kernel<BF16, WMB, WNB, A_LOAD, B_LOAD>), dim3(grid), dim3(kBlock), plan.lds_bytes, s, plan.params, a, b, c);
   return hipSuccess;

@@ -13,6 +13,7 @@
 
 #include "kernarg.hpp"
 #include "kernel_params.hpp"
+#include "lds_limit.hpp"
 #include "plan.hpp"
 
 namespace lc {
@@ -949,20 +950,11 @@ static PreLaunch launch_transpose_f(const lc_plan& plan, const void* src, void* 
     if (queue) lds_bytes += 16;   // the word that carries the next tile to the other lanes
   }
   if (lds_bytes > 64 * 1024) {   // what this launch asks for, the queue's word included
-    static std::atomic<bool> raised{false};   // one flag per instantiation: the attribute belongs to the kernel function
-    if (!raised.load(std::memory_order_acquire)) {
-      pre.call = "hipFuncSetAttribute";
-      pre.status = hipFuncSetAttribute(reinterpret_cast<const void*>(&transpose_kernel<ES, V, MT, NT, FULL, 0>),
-                                       hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-      if (pre.status == hipSuccess && FULL)
-        pre.status = hipFuncSetAttribute(reinterpret_cast<const void*>(&transpose_kernel<ES, V, MT, NT, FULL, FULL ? 1 : 0>),
-                                         hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-      if (pre.status == hipSuccess && FULL)
-        pre.status = hipFuncSetAttribute(reinterpret_cast<const void*>(&transpose_kernel<ES, V, MT, NT, FULL, FULL ? 2 : 0>),
-                                         hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-      if (pre.status != hipSuccess) return pre;
-      raised.store(true, std::memory_order_release);
-    }
+    static DevicesDone raised;
+    pre.call = "LDS limit";
+    pre.status = raise_lds_limit(&raised, &transpose_kernel<ES, V, MT, NT, FULL, 0>, &transpose_kernel<ES, V, MT, NT, FULL, FULL ? 1 : 0>,
+                                 &transpose_kernel<ES, V, MT, NT, FULL, FULL ? 2 : 0>);
+    if (pre.status != hipSuccess) return pre;
   }
   const uint32_t counters = (uint32_t)std::max(1, std::min(plan.queue_counters, kQueueLines - 1));
   // whole rounds of the grid that go by index before the queue takes over (at least one, never past the last whole round)
@@ -1024,15 +1016,10 @@ static PreLaunch launch_shifted_m(const lc_plan& plan, const void* src, void* ds
     if (queue) lds_bytes += 16;   // the word that carries the next tile to the other lanes
   }
   if (lds_bytes > 64 * 1024) {
-    static std::atomic<bool> raised{false};
-    if (!raised.load(std::memory_order_acquire)) {
-      pre.call = "hipFuncSetAttribute";
-      pre.status = hipFuncSetAttribute(reinterpret_cast<const void*>(&transpose_kernel<ES, V, MT, 0, true, 0, true>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-      if (pre.status == hipSuccess)
-        pre.status = hipFuncSetAttribute(reinterpret_cast<const void*>(&transpose_kernel<ES, V, MT, 0, true, 1, true>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-      if (pre.status != hipSuccess) return pre;
-      raised.store(true, std::memory_order_release);
-    }
+    static DevicesDone raised;
+    pre.call = "LDS limit";
+    pre.status = raise_lds_limit(&raised, &transpose_kernel<ES, V, MT, 0, true, 0, true>, &transpose_kernel<ES, V, MT, 0, true, 1, true>);
+    if (pre.status != hipSuccess) return pre;
   }
   const uint32_t grab = (uint32_t)std::max(1, plan.tile_queue);
   if (queue)

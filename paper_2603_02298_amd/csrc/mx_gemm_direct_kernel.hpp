@@ -15,8 +15,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
-#include <atomic>
-
+#include "lds_limit.hpp"
 #include "mx_gemm_device.hpp"
 #include "mx_gemm_plan.hpp"
 
@@ -211,12 +210,10 @@ static inline hipError_t launch_mx_direct_as(const lc_mx_gemm_plan& plan, const 
   constexpr int TM = 16 * FM, TN = 16 * ((XQ + 3) / 4);
   const unsigned through = MATH == kMxCodes ? 0u : WAVES * XQ * 1024u, scales = (unsigned)(TM + (MATH == kMxCodes ? TN : 0)) * plan.params.scale_pitch;
   if (plan.lds_bytes < WAVES * TN * (TM + 4) * 4u || plan.lds_bytes < through + scales || plan.lds_bytes > 160u * 1024u) return hipErrorInvalidValue;
-  static std::atomic<bool> raised{false};   // one flag per instantiation: the attribute belongs to the kernel function
-  if (plan.lds_bytes > 64 * 1024 && !raised.load(std::memory_order_acquire)) {
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&mx_direct_kernel<MATH, FM, XQ, WAVES, DEPTH, IN_LDS>),
-                                       hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+  static DevicesDone raised;
+  if (plan.lds_bytes > 64 * 1024) {
+    hipError_t e = raise_lds_limit(&raised, &mx_direct_kernel<MATH, FM, XQ, WAVES, DEPTH, IN_LDS>);
     if (e != hipSuccess) return e;
-    raised.store(true, std::memory_order_release);
   }
   const unsigned grid = plan.params.g.tiles_m * plan.params.g.tiles_n * plan.params.g.L;
   hipLaunchKernelGGL((mx_direct_kernel<MATH, FM, XQ, WAVES, DEPTH, IN_LDS>), dim3(grid), dim3(64 * WAVES), plan.lds_bytes, s, plan.params, a, sa, b, sb, c);

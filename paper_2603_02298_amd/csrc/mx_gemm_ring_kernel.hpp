@@ -17,8 +17,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
-#include <atomic>
-
+#include "lds_limit.hpp"
 #include "mx_gemm_device.hpp"
 #include "mx_gemm_plan.hpp"
 
@@ -171,12 +170,9 @@ template <int BM>
 static inline hipError_t launch_mx_ring_of(const lc_mx_gemm_plan& plan, const unsigned char* a, const unsigned char* sa, const unsigned char* b,
                                            const unsigned char* sb, void* c, hipStream_t s) {
   if (plan.lds_bytes != 5u * BM * 128u || plan.b_load != kLoadKDirect || !plan.params.a_dwords || !plan.params.b_dwords) return hipErrorInvalidValue;
-  static std::atomic<bool> raised{false};   // one flag per instantiation: the attribute belongs to the kernel function
-  if (!raised.load(std::memory_order_acquire)) {
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&mx_ring_kernel<BM>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-    if (e != hipSuccess) return e;
-    raised.store(true, std::memory_order_release);
-  }
+  static DevicesDone raised;
+  hipError_t e = raise_lds_limit(&raised, &mx_ring_kernel<BM>);
+  if (e != hipSuccess) return e;
   const unsigned grid = plan.params.g.tiles_m * plan.params.g.tiles_n * plan.params.g.L;
   hipLaunchKernelGGL((mx_ring_kernel<BM>), dim3(grid), dim3(kBlock), plan.lds_bytes, s, plan.params, a, sa, b, sb, c);
   return hipSuccess;

@@ -14,8 +14,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
-#include <atomic>
-
+#include "lds_limit.hpp"
 #include "mx_gemm_device.hpp"
 #include "mx_gemm_plan.hpp"
 
@@ -183,12 +182,10 @@ template <int MATH, int BM, int BN, int A_KIND, int B_LOAD>
 static inline hipError_t launch_mx_stream(const lc_mx_gemm_plan& plan, const unsigned char* a, const unsigned char* sa, const unsigned char* b,
                                           const unsigned char* sb, void* c, hipStream_t s) {
   if (plan.lds_bytes != (unsigned)(2 * (BM + BN) * 128)) return hipErrorInvalidValue;
-  static std::atomic<bool> raised{false};   // one flag per instantiation: the attribute belongs to the kernel function
-  if (plan.lds_bytes > 64 * 1024 && !raised.load(std::memory_order_acquire)) {
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&mx_stream_kernel<MATH, BM, BN, A_KIND, B_LOAD>),
-                                       hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+  static DevicesDone raised;
+  if (plan.lds_bytes > 64 * 1024) {
+    hipError_t e = raise_lds_limit(&raised, &mx_stream_kernel<MATH, BM, BN, A_KIND, B_LOAD>);
     if (e != hipSuccess) return e;
-    raised.store(true, std::memory_order_release);
   }
   const unsigned grid = plan.params.g.tiles_m * plan.params.g.tiles_n * plan.params.g.L;
   hipLaunchKernelGGL((mx_stream_kernel<MATH, BM, BN, A_KIND, B_LOAD>), dim3(grid), dim3(kBlock), plan.lds_bytes, s, plan.params, a, sa, b, sb, c);

@@ -14,8 +14,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
-#include <atomic>
-
+#include "lds_limit.hpp"
 #include "mx_gemm_device.hpp"
 #include "mx_gemm_plan.hpp"
 
@@ -203,11 +202,10 @@ __global__ __launch_bounds__(kBlock, 160 * 1024 / mx_wide_lds(BM, BN)) void mx_w
 template <int MATH, int BLOCKED, int BM, int BN>
 static inline hipError_t launch_mx_wide(const lc_mx_gemm_plan& plan, const unsigned char* a, const unsigned char* sa, const unsigned char* b, void* c, hipStream_t s) {
   if (plan.lds_bytes != mx_wide_lds(BM, BN) || plan.b_load != kLoadKDirect || plan.blocked != BLOCKED) return hipErrorInvalidValue;
-  static std::atomic<bool> raised{false};   // one flag per instantiation: the attribute belongs to the kernel function
-  if (plan.lds_bytes > 64 * 1024 && !raised.load(std::memory_order_acquire)) {
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&mx_wide_kernel<MATH, BLOCKED, BM, BN>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+  static DevicesDone raised;
+  if (plan.lds_bytes > 64 * 1024) {
+    hipError_t e = raise_lds_limit(&raised, &mx_wide_kernel<MATH, BLOCKED, BM, BN>);
     if (e != hipSuccess) return e;
-    raised.store(true, std::memory_order_release);
   }
   const unsigned grid = plan.params.g.tiles_m * plan.params.g.tiles_n * plan.params.g.L;
   hipLaunchKernelGGL((mx_wide_kernel<MATH, BLOCKED, BM, BN>), dim3(grid), dim3(kBlock), plan.lds_bytes, s, plan.params, a, sa, b, c);
