@@ -300,7 +300,7 @@ std::string describe(const lc_mx_gemm_plan& plan) {
   s += " tile=" + std::to_string(plan.tile_m) + "x" + std::to_string(plan.tile_n) + " waves=" + std::to_string(plan.waves);
   s += " tiles=" + std::to_string(plan.params.g.tiles_m) + "x" + std::to_string(plan.params.g.tiles_n) + " k_tiles=" + std::to_string(plan.params.g.k_tiles);
   const char* load = plan.b_load == kLoadKDirect ? "k-vectors" : plan.b_load == kLoadKLeaves ? "k-vectors-over-leaves" : plan.b_load == kLoadKAny ? "unaligned-k-vectors" : "elements";
-  s += std::string(" load=") + load + " c_vec=" + std::to_string(plan.params.g.c_vec) + " lds_bytes=" + std::to_string(plan.lds_bytes);
+  s += std::string(" load=") + load + " c_vec=" + std::to_string(plan.params.g.c_vec) + " past_caches=" + std::to_string(plan.params.past_caches) + " lds_bytes=" + std::to_string(plan.lds_bytes);
   return s + " A=[" + plan.a_text + "] A_scales=[" + plan.sa_text + "] B=[" + plan.b_text + "] B_scales=[" + plan.sb_text + "] C=[" + plan.c_text + "]";
 }
 

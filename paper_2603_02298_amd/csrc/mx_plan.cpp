@@ -158,6 +158,7 @@ std::string describe(const lc_mx_plan& plan) {
   s += " R=" + std::to_string(plan.R) + " K=" + std::to_string(plan.K) + " padded=" + std::to_string(plan.padded);
   if (plan.quantize) s += plan.params.cover ? " rule=cover" : " rule=floor";
   s += std::string(" access=") + access[plan.access] + " tiles=" + std::to_string(plan.params.tiles_r) + "x" + std::to_string(plan.params.tiles_b) + " groups=" + std::to_string(plan.groups);
+  if (!plan.quantize) s += " large_lines=" + std::to_string((int)plan.large_lines);
   return s + " X=[" + plan.x_text + "] codes(blocks,bytes)=[" + plan.q_text + "] scales=[" + plan.s_text + "]";
 }
 
