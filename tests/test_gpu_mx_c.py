@@ -1,10 +1,11 @@
-"""How the products with microscaled 4-bit operands write C: past the caches or not, as the plan says; and how dequantisation writes large tensors."""
+"""How the products with microscaled 4-bit operands write C: past the caches or not, as the plan says, and under modes of several leaves (the definition in 64
+bits and the bounds there are test_gpu_mx_gemm's); and how dequantisation writes large tensors."""
 import numpy as np
 import pytest
 
 import paper_2603_02298_amd as lc
 from oracle import mx_oracle as mx
-from test_gpu_mx_gemm import TORCH, _codes_and_scales, _elements, _rows, _scales
+from test_gpu_mx_gemm import TORCH, _codes_and_scales, _elements, _rows, _run, _scales
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -74,6 +75,34 @@ def test_large_batches_past_the_caches(a_dtype, tile, monkeypatch):
     plan = lc.MxGemmPlan(a, a_s if a_dtype == "mxfp4" else None, b, b_s, "(%d,%d,%d):(%d,1,%d)" % (M, N, L, pitch, M * pitch), a_dtype, "f32", False)
     assert _taken(plan, a_dtype, tile) and _words(plan)["past_caches"] == "1", plan.describe()
     _large(plan, (pitch, 1, M * pitch))
+
+
+# C's modes; which of the two the kernel's vectors would lie along (n: of both operands in codes and of 16-bit elements beside codes; m: of two in codes)
+LEAVES = {
+    "vectors along n": ("((9,31),(8,33)):((520,4688),(1,16))", True),
+    "vectors along m": ("((8,33),(9,31)):((1,16),(520,4688))", False),
+    "single elements along n": ("((9,31),(7,37)):((335,3017),(1,9))", False),
+    "single elements along m": ("((7,37),(9,31)):((1,9),(335,3017))", False),
+    "one leaf beside two": ("(260,(8,33)):(520,(1,16))", True),
+    "two leaves beside one": ("((9,31),264):((268,2416),1)", True),
+}
+
+
+@pytest.mark.parametrize("a_dtype,tile", FORCED)
+@pytest.mark.parametrize("case", LEAVES)
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_c_under_modes_of_several_leaves(case, a_dtype, tile, accumulate, monkeypatch):
+    monkeypatch.setenv("LC_TUNE_MX_TILE", str(tile))
+    c, vectors = LEAVES[case]
+    vectors = vectors or (case == "vectors along m" and a_dtype == "mxfp4")
+    M, N = mx.offsets(c).shape
+    for kind, c_dtype in (("exact", "f32"), ("wide", "bf16")):
+        args = _operands(M, N, 160, a_dtype) + (c, a_dtype, c_dtype, accumulate)
+        plan = lc.MxGemmPlan(*args)
+        assert _taken(plan, a_dtype, tile) and _words(plan)["c_vec"] == str(int(vectors))
+        text = plan.describe().split(" C=[")[1]
+        assert text.count(",") == c.count(",") - 2, text   # every leaf is still there
+        _run(*args, kind, seed=tile)
 
 
 @pytest.mark.parametrize("R,K,x", [(2101, 8203, "k"), (2101, 8300, "r"), (2104, 8300, "r")])
