@@ -231,7 +231,10 @@ lc_status_t make_mx_gemm_plan(const Layout& A, const Layout* A_scales, const Lay
   else if (t_env == 128064 && can_wide) take(kMxWide, 128, 64, 4);
   else {
     // What a choice costs is how many rounds of 256 tiles (one a CU) there are times what a round takes, and not less than what a tile takes
-    // alone; in microseconds at K = 4096, which all of them follow alike.  Measured on MI355X (us; direct 32 x 32, then the tiles by size):
+    // alone; in microseconds at K = 4096.  Other K scale all of them, though not quite alike: a start does not grow with K.  Over K = 512 to 16384 and N = 1024 to
+    // 16384 the choice takes 1.6 % longer than the fastest tile in the geometric mean of 212 calls with both operands codes (1 to 4096 rows; the most 46 us for 27, 1 x
+    // 16384 x 16384, where direct tiles of 32 x 16 would be the faster ones), 1.1 % in that of 287 beside 16 bits (1 to 2048 rows; the most 6.7 us for 4.5, 1 x 8192 x
+    // 512), nothing in that of 164 along the rows.  Measured on MI355X (us; direct 32 x 32, then the tiles by size):
     //   both codes (stream 64 x 64, 128 x 64, ring 128 x 128, 256 x 256): 256 x 4096 x 4096 32.7, 13.4, 14.7, 17.0, 35; 512 x 4096 x 4096 63, 16.8, 15.5, 17.1, 36;
     //   1024 x 4096 x 4096 -, 25.1, 20.8, 19.3, 37; 2048 x 4096 x 4096 -, 45.3, 37.0, 28.8, 40; 4096 x 2048 x 2048 -, 28.1, 23.0, 20.9, 29.1; 3000^2 x 2048 -, 28.8, 24.5, 26.4,
     //   27.4; 4096 x 8192 x 4096 -, 155, 118, 101, 89; 8192^3 -, 573, 461, 363, 299; 2048^2 x 512 -, 9.7, 9.0, 10.4, 17.8; 64 x 4096 x 4096 9.8, 13.7, -, -, -; 512 x 1024 x 1024

@@ -10,9 +10,11 @@
 // those covers them.
 // The sums pass through LDS, a column of fragments of a wavefront at a time and each wavefront in a place of its own, so that C is written in
 // whole lines.
-// What it measures, and what bounds it: 8192^3 into f32 296 us, 3.7 PFLOP/s, the matrix cores busy 45 % of clocks that the power limit holds at 1.93 GHz
-// (operands of random codes; they reach 6.5 PFLOP/s with nothing but these instructions).  A k tile of 256 x 256 takes 1.15 us, its 64 KiB at 58 GB/s
-// per CU, and every tile 15 us more: all CUs write their 256 KiB of C at the same time (11 us of that), then load the next first k tile.
+// What it measures, and what bounds it: 8192^3 into f32 295 us, 3.7 PFLOP/s: four rounds of 256 tiles, each 32 k tiles of 1.83 us and 16 us beside them
+// (from K = 512 to 32768: 82, 94, 121, 178, 295, 537, 1038 us).  A k tile takes about 3400 clocks, 2048 of them matrix instructions; the others wait for
+// LDS and for a turn to issue.  Those clocks are 1.4 us for a tile alone on the chip, and for all of them on operands of zeros; random codes on all CUs
+// take the chip to its power limit, 1.93 GHz, and the k tile to 1.83.  The 16 us: all CUs write their 256 KiB of C at the same time (11 us), then load
+// the next first k tile.  (The matrix cores are busy 45 % of the time; they reach 6.5 PFLOP/s on random codes with nothing but these instructions.)
 // A k step's products go in parts with everything else between them: in one piece, 8192^3 took 340 us.
 #pragma once
 #include <hip/hip_runtime.h>
