@@ -384,9 +384,9 @@ lc_status_t lc_mx_dequantize(const void* codes, const lc_layout_t* codes_layout,
  *   writes zeros there).
  *   A in 16 bits, B blocked along its rows (its scales over (P/32,K)): A over (M,K), B over (P,K), C over (M,N), P >= N: the product with the
  *   transposed weights, i.e. the gradient of the forward product's A.
- *   B's elements are rounded to A's type before they are multiplied: in bf16 exact below 2^128 and infinite from there on (scales of 253 and
- *   254, which only COVER gives, to values from 3.5 * 2^126 on); in fp16 exact for magnitudes from 2^-14 to 65504, beyond which they are infinite, and
- *   below to within 2^-25.
+ *   B's elements are rounded to A's type before they are multiplied: in bf16 exact below 2^128 and infinite from there on (4 and 6 under a
+ *   scale of 253, 2 and more under 254; lc_mx_quantize makes such elements of values from 3.5 * 2^126 on, by COVER only); in fp16 exact for
+ *   magnitudes from 2^-14 to 65504, beyond which they are infinite, and below to within 2^-25.
  * A block whose scale is 255 makes every element of C that it enters NaN.  No call allocates or needs a workspace.
  * a / b / c_align_bytes: alignment the caller guarantees for the pointers (codes: 16 or more).  Errors: INVALID_ARG (ranks, a_scales),
  * SIZE_MISMATCH, BLOCK_LAYOUT, NEGATIVE_STRIDE, DST_ALIASES (C), UNSUPPORTED_DTYPE, MISALIGNED, TOO_LARGE (an extent, or a cosize -- of codes
