@@ -37,6 +37,9 @@ typedef struct lc_slayout lc_slayout_t; /* opaque: a layout whose strides come f
 typedef struct lc_gemm_plan lc_gemm_plan_t; /* opaque: a planned GEMM over three layouts */
 typedef struct lc_mx_plan lc_mx_plan_t; /* opaque: a planned quantisation to or from microscaled 4-bit elements */
 typedef struct lc_mx_gemm_plan lc_mx_gemm_plan_t; /* opaque: a planned GEMM with microscaled 4-bit operands */
+typedef struct lc_rope_plan lc_rope_plan_t; /* opaque: a planned copy that turns pairs of elements by their token's position */
+typedef struct lc_mx_cache_plan lc_mx_cache_plan_t; /* opaque: a planned write into, or read from, slots of a microscaled 4-bit cache */
+typedef struct lc_mx_attention_plan lc_mx_attention_plan_t; /* opaque: a planned attention over a microscaled 4-bit cache */
 
 typedef enum {
   LC_OK = 0,
@@ -407,6 +410,113 @@ lc_status_t lc_mx_gemm(const void* a, const lc_layout_t* a_layout, const void* a
 /* Mean milliseconds of `iters` back-to-back executions after `warmup` untimed ones, by HIP events on `hip_stream`; synchronises the stream. */
 lc_status_t lc_mx_gemm_plan_time(const lc_mx_gemm_plan_t* plan, const void* a, const void* a_scales, const void* b, const void* b_scales, void* c,
                                  int warmup, int iters, void* hip_stream, float* ms_per_iter);
+
+/* ---------------------------------------------------------------------------------------------
+ * Rotary positions: a copy over (tokens T, heads H, elements D) that turns pairs of a head's first `rotary` elements.
+ * Pair i of rotary / 2, elements (a, b), of a token at position p becomes (a c - b s, b c + a s) with c = factor cos(p f_i),
+ * s = factor sin(p f_i); the elements from `rotary` on are copied.  Transposed, the pair is turned the other way
+ * (a c + b s, b c - a s): the gradient of the call without it, under the same positions, frequencies and factor.
+ *   HALF        element i with element i + rotary / 2
+ *   NEIGHBOURS  element 2 i with element 2 i + 1
+ * Positions: 32-bit integers of either sign, one per token.  Frequencies: rotary / 2 fp32 numbers (radians a position).  Both are device
+ * arrays read by the call.  The angle is the exact product of the two, reduced in 64 bits; c and s are within 2^-24 of it in
+ * fp32 (|factor| <= 1), each result is rounded once.
+ * ------------------------------------------------------------------------------------------- */
+typedef enum { LC_ROPE_HALF = 0, LC_ROPE_NEIGHBOURS = 1 } lc_rope_pairs_t;
+
+/* Frequencies of `rotary` / 2 pairs, f_i = base^(-2 i / rotary), stretched by `stretch` >= 1 to contexts longer than the `context`
+ * positions that a model was trained on:
+ *   PLAIN   as they are (stretch 1)
+ *   LINEAR  every f_i / stretch
+ *   BASE    the base times stretch^(rotary / (rotary - 2)): the slowest pair as by LINEAR, the fastest as it is (rotary >= 4)
+ *   PARTS   f_i m + f_i / stretch (1 - m); m falls from 1 to 0 in even steps between the pairs that go round `fast` and `slow` times
+ *           within `context` positions (the first rounded down, the second up)
+ *   BANDS   the same with m = (turns - slow) / (fast - slow), kept within 0 .. 1, of a pair that goes round `turns` times
+ * `out` is a host array of rotary / 2 floats, worked out in 64 bits and rounded once.  Errors: INVALID_ARG (rotary odd or < 2, base <= 1, stretch < 1,
+ * and for PARTS and BANDS context < 1 or not 0 < slow < fast). */
+typedef enum { LC_ROPE_PLAIN = 0, LC_ROPE_LINEAR = 1, LC_ROPE_BASE = 2, LC_ROPE_PARTS = 3, LC_ROPE_BANDS = 4 } lc_rope_stretch_t;
+lc_status_t lc_rope_frequencies(int rotary, double base, lc_rope_stretch_t rule, double stretch, int64_t context, double slow, double fast, float* out);
+
+/* x and y over (T,H,D), strides of either sign, in fp32, fp16 or bf16 (the same for both).  Errors: INVALID_ARG (ranks; rotary odd, < 2 or > D),
+ * SIZE_MISMATCH, UNSUPPORTED_DTYPE, DST_ALIASES (two coordinates of y share an offset), TOO_LARGE (a mode of 2^31 or more, or of more than 4
+ * leaves after coalescing). */
+lc_status_t lc_rope_plan_create(const lc_layout_t* x, const lc_layout_t* y, lc_dtype_t dtype, int rotary, lc_rope_pairs_t pairs, int transposed,
+                                lc_rope_plan_t** out);
+lc_status_t lc_rope_plan_describe(const lc_rope_plan_t* plan, char* buf, size_t cap, size_t* needed);
+void lc_rope_plan_destroy(lc_rope_plan_t* plan);
+/* Asynchronous on `hip_stream`, allocates nothing, may be recorded into a HIP graph.  y may be x under x's layout; any other overlap is
+ * undefined.  Errors: MISALIGNED (x, y: to their elements; positions, frequencies: to 4 bytes), INVALID_ARG, HIP. */
+lc_status_t lc_rope_plan_execute(const lc_rope_plan_t* plan, const void* x, const int32_t* positions, const float* frequencies, void* y, double factor,
+                                 void* hip_stream);
+/* Plan (kept between calls as lc_copy's are) and execute. */
+lc_status_t lc_rope(const void* x, const lc_layout_t* x_layout, const int32_t* positions, const float* frequencies, void* y, const lc_layout_t* y_layout,
+                    lc_dtype_t dtype, int rotary, lc_rope_pairs_t pairs, int transposed, double factor, void* hip_stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * A cache of keys and values in microscaled 4-bit elements: a pool of N slots, one token each, as codes over (N,H,P) and scales over
+ * (N,H,P/32), blocks along a head's elements, under the rules of the microscaled tensors above.  (Pages are a mode of the layouts: slot
+ * page * page_size + offset under "((page_size,pages),H,P):..".)
+ * Written: rows x over (T,H,D), D <= P, go to the slots that a device array of T 32-bit integers names, quantised as lc_mx_quantize does
+ * (elements past D are zeros).  Read: the other way, rounded as lc_mx_dequantize does.
+ * A token whose slot lies outside 0 .. N - 1 is left out: nothing is written for it, its row of x is left as it was.
+ * A slot must not be named twice by one write: its blocks then hold the codes of one and the scale of one of the tokens, not always the same one's.
+ * One call takes keys and values, both under the plan's layouts, or one tensor (the second's three pointers NULL).
+ * Asynchronous on `hip_stream`, allocate nothing, may be recorded into a HIP graph; tensors written may overlap none that is read.
+ * Errors: those of lc_mx_quantize / lc_mx_dequantize; ranks are 3. x: strides of either sign.  TOO_LARGE: modes of 2^31 or more.
+ * ------------------------------------------------------------------------------------------- */
+lc_status_t lc_mx_cache_write_plan_create(const lc_layout_t* x, const lc_layout_t* codes, const lc_layout_t* scales, lc_dtype_t x_dtype, lc_mx_rule_t rule,
+                                          lc_mx_cache_plan_t** out);
+lc_status_t lc_mx_cache_read_plan_create(const lc_layout_t* codes, const lc_layout_t* scales, const lc_layout_t* x, lc_dtype_t x_dtype, lc_mx_cache_plan_t** out);
+lc_status_t lc_mx_cache_plan_describe(const lc_mx_cache_plan_t* plan, char* buf, size_t cap, size_t* needed);
+void lc_mx_cache_plan_destroy(lc_mx_cache_plan_t* plan);
+lc_status_t lc_mx_cache_write_plan_execute(const lc_mx_cache_plan_t* plan, const void* k, void* k_codes, void* k_scales, const void* v, void* v_codes,
+                                           void* v_scales, const int32_t* slots, void* hip_stream);
+lc_status_t lc_mx_cache_read_plan_execute(const lc_mx_cache_plan_t* plan, const void* k_codes, const void* k_scales, void* k, const void* v_codes,
+                                          const void* v_scales, void* v, const int32_t* slots, void* hip_stream);
+/* Plan (kept between calls) and execute. */
+lc_status_t lc_mx_cache_write(const void* k, const void* v, const lc_layout_t* x_layout, void* k_codes, void* v_codes, const lc_layout_t* codes_layout,
+                              void* k_scales, void* v_scales, const lc_layout_t* scales_layout, const int32_t* slots, lc_dtype_t x_dtype, lc_mx_rule_t rule,
+                              void* hip_stream);
+lc_status_t lc_mx_cache_read(const void* k_codes, const void* v_codes, const lc_layout_t* codes_layout, const void* k_scales, const void* v_scales,
+                             const lc_layout_t* scales_layout, void* k, void* v, const lc_layout_t* x_layout, const int32_t* slots, lc_dtype_t x_dtype,
+                             void* hip_stream);
+
+/* Attention over that cache: o(t,h) = sum_j p_j v(j) / sum_j p_j with p_j = exp(scale q(t,h) . k(j)) over the cached tokens j that query t
+ * sees, of head h / (Hq / Hkv).  q over (T,Hq,D) in bf16 or fp16, o over (T,Hq,D) in q's type or fp32; keys' and values' codes over (N,Hkv,P),
+ * scales over (N,Hkv,P/32), D <= 256, the same layouts for both.
+ *   starts   (sequences + 1) tokens: sequence b's queries are rows starts[b] .. starts[b + 1] - 1 of q.  NULL: T / sequences each (T a multiple).
+ *   lengths  (sequences) cached tokens of each, its queries' own among them: query i of n stands at position length - n + i.
+ *   pages    (sequences, pages_per_sequence): token j of sequence b lies in slot pages[b, j / page] * page + j % page.  NULL: in slot
+ *            b * pages_per_sequence * page + j (then sequences * pages_per_sequence * page <= N).
+ * All three are device arrays of 32-bit integers, read by the call: a captured call follows them.
+ * causal: a query sees no token behind its position; window > 0 (only with causal): and none before the last `window` up to its own.
+ * A query that sees nothing (none cached, or a position before the first) gets zeros, and minus infinity in lse.  So does one whose
+ * every score is minus infinity.  Rows of q outside every sequence leave o and lse as they were.
+ * Numbers that do not fit are cut to what does: lengths to 0 .. pages_per_sequence * page, starts to 0 .. T, a sequence's queries to its
+ * first max_queries (the rows of the others are left as they were); tokens on a page outside 0 .. N / page - 1 are seen by nobody.
+ * Keys and values are rounded to q's type before they are multiplied (see lc_mx_gemm: exact in bf16 below 2^128); scores, sums and o's parts are
+ * fp32, probabilities are rounded to q's type.  Elements of a block past D have to be finite in q's type.  What nobody sees (slots behind a sequence's
+ * length, masked tokens) may hold anything, scales of 255 among it.
+ * lse (may be NULL): fp32 (T,Hq), row-major: log(sum_j p_j), natural.
+ * A call needs lc_mx_attention_plan_workspace_bytes(plan) bytes of scratch device memory, aligned to 16 bytes, its contents before and after
+ * meaningless (0: none, NULL will do); two executions that overlap in time need two.
+ * Asynchronous on `hip_stream`, allocates nothing, may be recorded into a HIP graph; o and lse may overlap nothing that is read.  Results do not depend on
+ * timing.
+ * Errors: INVALID_ARG (ranks, Hq no multiple of Hkv, T no multiple of `sequences` without starts, page, sequences, pages_per_sequence or
+ * max_queries < 1, window without causal or < 0, scale not finite, D > 256, N no multiple of page), SIZE_MISMATCH, BLOCK_LAYOUT,
+ * NEGATIVE_STRIDE (codes, scales), DST_ALIASES (o), UNSUPPORTED_DTYPE, TOO_LARGE (modes of 2^31 or more, more than 4 leaves, tokens of a sequence
+ * of 2^31 or more, more than 65535 sequences or heads), MISALIGNED (q, o to their elements, codes to 16 bytes, lse and integers to 4),
+ * WORKSPACE_TOO_SMALL, HIP. */
+lc_status_t lc_mx_attention_plan_create(const lc_layout_t* q, const lc_layout_t* codes, const lc_layout_t* scales, const lc_layout_t* o, lc_dtype_t q_dtype,
+                                        lc_dtype_t o_dtype, int64_t sequences, int64_t page, int64_t pages_per_sequence, int64_t max_queries, float scale,
+                                        int causal, int64_t window, lc_mx_attention_plan_t** out);
+/* One line: kernel, tile, parts that a sequence's tokens are shared out in, how q and the cache are reached. */
+lc_status_t lc_mx_attention_plan_describe(const lc_mx_attention_plan_t* plan, char* buf, size_t cap, size_t* needed);
+void lc_mx_attention_plan_destroy(lc_mx_attention_plan_t* plan);
+int64_t lc_mx_attention_plan_workspace_bytes(const lc_mx_attention_plan_t* plan);
+lc_status_t lc_mx_attention_plan_execute(const lc_mx_attention_plan_t* plan, const void* q, const void* k_codes, const void* k_scales, const void* v_codes,
+                                         const void* v_scales, const int32_t* pages, const int32_t* lengths, const int32_t* starts, void* o, float* lse,
+                                         void* workspace, size_t workspace_bytes, void* hip_stream);
 
 #ifdef __cplusplus
 }

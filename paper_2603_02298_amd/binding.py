@@ -1,7 +1,9 @@
 """ctypes binding of liblayoutcopy.so: the same entry points as include/layoutcopy.h, with
 argument marshalling only.  Every step of a copy runs in the library's HIP kernels; there is no
 Python or CPU fallback, and a missing library is an error."""
+import ast
 import ctypes
+import math
 import os
 
 from . import build as _build
@@ -132,6 +134,28 @@ def lib():
     L.lc_mx_gemm_plan_flops.argtypes = [P]
     L.lc_mx_gemm_plan_flops.restype = i64
     L.lc_mx_gemm.argtypes = [P, P, P, P, P, P, P, P, P, P, ctypes.c_int, ctypes.c_int, ctypes.c_int, P]
+    f64, i32, f32 = ctypes.c_double, ctypes.c_int, ctypes.c_float
+    L.lc_rope_frequencies.argtypes = [i32, f64, i32, f64, i64, f64, f64, P]
+    L.lc_rope_plan_create.argtypes = [P, P, i32, i32, i32, i32, PP]
+    L.lc_rope_plan_execute.argtypes = [P, P, P, P, P, f64, P]
+    L.lc_rope.argtypes = [P, P, P, P, P, P, i32, i32, i32, i32, f64, P]
+    L.lc_mx_cache_write_plan_create.argtypes = [P, P, P, i32, i32, PP]
+    L.lc_mx_cache_read_plan_create.argtypes = [P, P, P, i32, PP]
+    L.lc_mx_cache_write_plan_execute.argtypes = [P] * 9
+    L.lc_mx_cache_read_plan_execute.argtypes = [P] * 9
+    L.lc_mx_cache_write.argtypes = [P] * 10 + [i32, i32, P]
+    L.lc_mx_cache_read.argtypes = [P] * 10 + [i32, P]
+    L.lc_mx_attention_plan_create.argtypes = [P, P, P, P, i32, i32, i64, i64, i64, i64, f32, i32, i64, PP]
+    L.lc_mx_attention_plan_workspace_bytes.argtypes = [P]
+    L.lc_mx_attention_plan_workspace_bytes.restype = i64
+    L.lc_mx_attention_plan_execute.argtypes = [P] * 12 + [sz, P]
+    for n in ("rope", "mx_cache", "mx_attention"):
+        getattr(L, "lc_%s_plan_describe" % n).argtypes = [P, ctypes.c_char_p, sz, ctypes.POINTER(sz)]
+        getattr(L, "lc_%s_plan_destroy" % n).argtypes = [P]
+        getattr(L, "lc_%s_plan_destroy" % n).restype = None
+    L.lc_debug_rope_walk_on_host.argtypes = [P, i64, i64, i64, i64, ctypes.POINTER(i64)]
+    L.lc_debug_mx_cache_walk_on_host.argtypes = [P, P, i64, i64, i64, i64, ctypes.POINTER(i64)]
+    L.lc_debug_mx_attention_walk_on_host.argtypes = [P, P, P, P, i64, i64, i64, i64, ctypes.POINTER(i64)]
     L.lc_mx_gemm_plan_time.argtypes = [P, P, P, P, P, P, ctypes.c_int, ctypes.c_int, P, ctypes.POINTER(ctypes.c_float)]
     L.lc_debug_mx_walk_on_host.argtypes = [P, i64, i64, i64, i64, ctypes.POINTER(i64), ctypes.POINTER(i64)]
     _lib = L
@@ -702,3 +726,264 @@ def mx_gemm_tensor(a, a_layout, a_scales, a_scales_layout, b, b_layout, b_scales
             raise ValueError("tensor smaller than the layout's cosize")
         lc_mx_gemm(a.data_ptr(), la, a_scales.data_ptr() if codes else None, sa, b.data_ptr(), lb, b_scales.data_ptr(), sb, c.data_ptr(), lc_,
                    "mxfp4" if codes else _mx_dtype(a), _mx_dtype(c), accumulate, torch.cuda.current_stream().cuda_stream)
+
+
+# ---- rotary positions, and a cache of keys and values in microscaled 4-bit elements ----
+ROPE_PAIRS = {"half": 0, "neighbours": 1}
+ROPE_STRETCHES = {"plain": 0, "linear": 1, "base": 2, "parts": 3, "bands": 4}
+
+
+def lc_rope_frequencies(rotary, base=10000.0, rule="plain", stretch=1.0, context=0, slow=1.0, fast=32.0):
+    """Frequencies (radians a position) of rotary / 2 pairs, as a list of numbers that fp32 holds."""
+    out = (ctypes.c_float * max(1, rotary // 2))()
+    _check(lib().lc_rope_frequencies(rotary, base, ROPE_STRETCHES[rule], stretch, context, slow, fast, out), "lc_rope_frequencies(%d, %g, %s)" % (rotary, base, rule))
+    return list(out)
+
+
+class _ServePlan:
+    """A plan handle of the calls below; `_kind`: how its C entry points are called."""
+    _kind = None
+
+    def __del__(self):
+        if getattr(self, "_h", None) and _lib is not None:
+            getattr(_lib, "lc_%s_plan_destroy" % self._kind)(self._h)
+            self._h = None
+
+    def describe(self):
+        call, need = getattr(lib(), "lc_%s_plan_describe" % self._kind), ctypes.c_size_t()
+        call(self._h, None, 0, ctypes.byref(need))
+        buf = ctypes.create_string_buffer(need.value)
+        call(self._h, buf, need.value, None)
+        return buf.value.decode()
+
+
+class RopePlan(_ServePlan):
+    """A copy over (tokens, heads, elements) that turns pairs of the first `rotary` elements of a head by their token's position; pairs: half, neighbours;
+    transposed: the other way (the gradient); dtype: f32, bf16, f16."""
+    _kind = "rope"
+
+    def __init__(self, x_layout, y_layout, dtype, rotary, pairs="half", transposed=False):
+        self.x_layout, self.y_layout = _as_layout(x_layout), _as_layout(y_layout)
+        self.dtype, self.rotary, self.pairs, self.transposed = dtype, rotary, pairs, transposed
+        self._h = ctypes.c_void_p()
+        _check(lib().lc_rope_plan_create(self.x_layout._h, self.y_layout._h, DTYPES[dtype], rotary, ROPE_PAIRS[pairs], int(transposed), ctypes.byref(self._h)),
+               "lc_rope_plan_create(%s -> %s, %s, %d, %s)" % (self.x_layout, self.y_layout, dtype, rotary, pairs))
+
+    def execute(self, x_ptr, positions_ptr, frequencies_ptr, y_ptr, factor=1.0, stream=0):
+        """Device addresses (positions: 32-bit integers, frequencies: fp32); stream: hipStream_t as int."""
+        _check(lib().lc_rope_plan_execute(self._h, x_ptr, positions_ptr, frequencies_ptr, y_ptr, factor, stream), "lc_rope_plan_execute")
+
+    def debug_walk_on_host(self, x_before, x_bytes, y_before, y_bytes):
+        """Test instrumentation: walk the plan's accesses on the host against the buffers' sizes; returns the bytes written."""
+        n = ctypes.c_int64()
+        _check(lib().lc_debug_rope_walk_on_host(self._h, x_before, x_bytes, y_before, y_bytes, ctypes.byref(n)), "lc_debug_rope_walk_on_host")
+        return n.value
+
+
+def lc_rope(x_ptr, x_layout, positions_ptr, frequencies_ptr, y_ptr, y_layout, dtype, rotary, pairs="half", transposed=False, factor=1.0, stream=0):
+    """Rotary positions on the GPU for device pointers."""
+    x, y = _as_layout(x_layout), _as_layout(y_layout)
+    status = lib().lc_rope(x_ptr, x._h, positions_ptr, frequencies_ptr, y_ptr, y._h, DTYPES[dtype], rotary, ROPE_PAIRS[pairs], int(transposed), factor, stream)
+    if status != 0:
+        raise LayoutCopyError(status, "lc_rope(%s -> %s)" % (x, y))
+
+
+class _MxCachePlan(_ServePlan):
+    _kind = "mx_cache"
+
+    def debug_walk_on_host(self, slots, x_before, x_bytes, codes_bytes, scales_bytes):
+        """Test instrumentation: walk the plan's accesses for these slots (an int32 array) on the host against the buffers' sizes; returns the bytes written."""
+        n = ctypes.c_int64()
+        _check(lib().lc_debug_mx_cache_walk_on_host(self._h, slots.ctypes.data_as(ctypes.c_void_p), x_before, x_bytes, codes_bytes, scales_bytes, ctypes.byref(n)),
+               "lc_debug_mx_cache_walk_on_host")
+        return n.value
+
+
+class MxCacheWritePlan(_MxCachePlan):
+    """Rows over (T,H,D) quantised into slots of codes over (N,H,P) and scales over (N,H,P/32); dtype: f32, bf16, f16; rule: floor, cover."""
+
+    def __init__(self, x_layout, codes_layout, scales_layout, dtype, rule="floor"):
+        self.x_layout, self.codes_layout, self.scales_layout = _as_layout(x_layout), _as_layout(codes_layout), _as_layout(scales_layout)
+        self.dtype, self.rule = dtype, rule
+        self._h = ctypes.c_void_p()
+        _check(lib().lc_mx_cache_write_plan_create(self.x_layout._h, self.codes_layout._h, self.scales_layout._h, DTYPES[dtype], MX_RULES[rule], ctypes.byref(self._h)),
+               "lc_mx_cache_write_plan_create(%s -> %s, %s, %s, %s)" % (self.x_layout, self.codes_layout, self.scales_layout, dtype, rule))
+
+    def execute(self, k_ptr, k_codes_ptr, k_scales_ptr, v_ptr, v_codes_ptr, v_scales_ptr, slots_ptr, stream=0):
+        """Device addresses (slots: T 32-bit integers; the v_ three None for one tensor); stream: hipStream_t as int."""
+        _check(lib().lc_mx_cache_write_plan_execute(self._h, k_ptr, k_codes_ptr, k_scales_ptr, v_ptr, v_codes_ptr, v_scales_ptr, slots_ptr, stream),
+               "lc_mx_cache_write_plan_execute")
+
+
+class MxCacheReadPlan(_MxCachePlan):
+    """Slots of codes over (N,H,P) and scales over (N,H,P/32) to rows over (T,H,D); dtype: f32, bf16, f16."""
+
+    def __init__(self, codes_layout, scales_layout, x_layout, dtype):
+        self.codes_layout, self.scales_layout, self.x_layout = _as_layout(codes_layout), _as_layout(scales_layout), _as_layout(x_layout)
+        self.dtype = dtype
+        self._h = ctypes.c_void_p()
+        _check(lib().lc_mx_cache_read_plan_create(self.codes_layout._h, self.scales_layout._h, self.x_layout._h, DTYPES[dtype], ctypes.byref(self._h)),
+               "lc_mx_cache_read_plan_create(%s, %s -> %s, %s)" % (self.codes_layout, self.scales_layout, self.x_layout, dtype))
+
+    def execute(self, k_codes_ptr, k_scales_ptr, k_ptr, v_codes_ptr, v_scales_ptr, v_ptr, slots_ptr, stream=0):
+        """Device addresses (slots: T 32-bit integers; the v_ three None for one tensor); stream: hipStream_t as int."""
+        _check(lib().lc_mx_cache_read_plan_execute(self._h, k_codes_ptr, k_scales_ptr, k_ptr, v_codes_ptr, v_scales_ptr, v_ptr, slots_ptr, stream),
+               "lc_mx_cache_read_plan_execute")
+
+
+def lc_mx_cache_write(k_ptr, v_ptr, x_layout, k_codes_ptr, v_codes_ptr, codes_layout, k_scales_ptr, v_scales_ptr, scales_layout, slots_ptr, dtype, rule="floor", stream=0):
+    """Rows into slots on the GPU for device pointers (the v_ three None for one tensor)."""
+    x, q, s = _as_layout(x_layout), _as_layout(codes_layout), _as_layout(scales_layout)
+    status = lib().lc_mx_cache_write(k_ptr, v_ptr, x._h, k_codes_ptr, v_codes_ptr, q._h, k_scales_ptr, v_scales_ptr, s._h, slots_ptr, DTYPES[dtype], MX_RULES[rule], stream)
+    if status != 0:
+        raise LayoutCopyError(status, "lc_mx_cache_write(%s -> %s, %s)" % (x, q, s))
+
+
+def lc_mx_cache_read(k_codes_ptr, v_codes_ptr, codes_layout, k_scales_ptr, v_scales_ptr, scales_layout, k_ptr, v_ptr, x_layout, slots_ptr, dtype, stream=0):
+    """Slots to rows on the GPU for device pointers (the v_ three None for one tensor)."""
+    x, q, s = _as_layout(x_layout), _as_layout(codes_layout), _as_layout(scales_layout)
+    status = lib().lc_mx_cache_read(k_codes_ptr, v_codes_ptr, q._h, k_scales_ptr, v_scales_ptr, s._h, k_ptr, v_ptr, x._h, slots_ptr, DTYPES[dtype], stream)
+    if status != 0:
+        raise LayoutCopyError(status, "lc_mx_cache_read(%s, %s -> %s)" % (q, s, x))
+
+
+class MxAttentionPlan(_ServePlan):
+    """o(t,h) = softmax(scale q(t,h) . k) v over the cached tokens of t's sequence: q and o over (T,Hq,D), keys' and values' codes over (N,Hkv,P) and scales
+    over (N,Hkv,P/32).  page tokens a page, pages_per_sequence places of a sequence in the page table, at most max_queries queries of one."""
+    _kind = "mx_attention"
+
+    def __init__(self, q_layout, codes_layout, scales_layout, o_layout, q_dtype="bf16", o_dtype=None, *, sequences, page, pages_per_sequence, max_queries, scale,
+                 causal=True, window=0):
+        self.q_layout, self.o_layout = _as_layout(q_layout), _as_layout(o_layout)
+        self.codes_layout, self.scales_layout = _as_layout(codes_layout), _as_layout(scales_layout)
+        self.q_dtype, self.o_dtype = q_dtype, o_dtype or q_dtype
+        self.sequences, self.page, self.pages_per_sequence, self.max_queries = sequences, page, pages_per_sequence, max_queries
+        self.scale, self.causal, self.window = scale, causal, window
+        self._h = ctypes.c_void_p()
+        _check(lib().lc_mx_attention_plan_create(self.q_layout._h, self.codes_layout._h, self.scales_layout._h, self.o_layout._h, DTYPES[q_dtype], DTYPES[self.o_dtype],
+                                                 sequences, page, pages_per_sequence, max_queries, scale, int(causal), window, ctypes.byref(self._h)),
+               "lc_mx_attention_plan_create(%s, %s, %s -> %s, %s)" % (self.q_layout, self.codes_layout, self.scales_layout, self.o_layout, q_dtype))
+
+    @property
+    def workspace_bytes(self):
+        """Scratch device memory that a call needs (16-byte aligned)."""
+        return lib().lc_mx_attention_plan_workspace_bytes(self._h)
+
+    def execute(self, q_ptr, k_codes_ptr, k_scales_ptr, v_codes_ptr, v_scales_ptr, pages_ptr, lengths_ptr, starts_ptr, o_ptr, lse_ptr=None, workspace_ptr=None,
+                workspace_bytes=0, stream=0):
+        """Device addresses (pages, lengths, starts: 32-bit integers; pages, starts and lse may be None); stream: hipStream_t as int."""
+        _check(lib().lc_mx_attention_plan_execute(self._h, q_ptr, k_codes_ptr, k_scales_ptr, v_codes_ptr, v_scales_ptr, pages_ptr, lengths_ptr, starts_ptr, o_ptr, lse_ptr,
+                                                  workspace_ptr, workspace_bytes, stream), "lc_mx_attention_plan_execute")
+
+    def debug_walk_on_host(self, pages, lengths, starts, q_bytes, codes_bytes, scales_bytes, o_bytes):
+        """Test instrumentation: walk a call's accesses on the host (int32 arrays; pages and starts may be None) against the buffers' sizes; returns
+        how many pairs of a row and a token it sees its workgroups go over."""
+        n = ctypes.c_int64()
+        at = [None if a is None else a.ctypes.data_as(ctypes.c_void_p) for a in (pages, lengths, starts)]
+        _check(lib().lc_debug_mx_attention_walk_on_host(self._h, *at, q_bytes, codes_bytes, scales_bytes, o_bytes, ctypes.byref(n)), "lc_debug_mx_attention_walk_on_host")
+        return n.value
+
+
+def _mode_size(layout, i):
+    """Size of top-level mode i of a layout of rank 2 or more."""
+    def size(shape):
+        return math.prod(size(part) for part in shape) if isinstance(shape, tuple) else shape
+    return size(ast.literal_eval(str(layout).split(":")[0])[i])
+
+
+def _integers(t, n, what):
+    import torch
+    if t.dtype != torch.int32 or not t.is_contiguous() or t.numel() < n:
+        raise ValueError("%s: %d contiguous int32" % (what, n))
+
+
+def rope_tensor(x, x_layout, positions, frequencies, y, y_layout, rotary, pairs="half", transposed=False, factor=1.0, x_origin=0, y_origin=0):
+    """Convenience for torch tensors on one GPU, on its current stream (positions: int32, frequencies: float32).  x_origin / y_origin: the element of each
+    tensor that offset 0 of its layout refers to.  y may be x under the same layout."""
+    import torch
+    with _mx_device("rope_tensor", (x, positions, frequencies, y)):
+        a, b = _as_layout(x_layout), _as_layout(y_layout)
+        if x.dtype != y.dtype:
+            raise ValueError("x and y of one type")
+        if a.rank != 3:
+            raise ValueError("layouts over (tokens, heads, elements)")
+        _integers(positions, _mode_size(a, 0), "positions")
+        if frequencies.dtype != torch.float32 or not frequencies.is_contiguous() or 2 * frequencies.numel() < rotary:
+            raise ValueError("frequencies: rotary / 2 contiguous float32")
+        for t, layout, origin in ((x, a, x_origin), (y, b, y_origin)):
+            if origin + layout.min_offset < 0 or origin + layout.cosize > _memory_of(t):
+                raise ValueError("tensor does not cover the offsets the layout reaches")
+        lc_rope(x.data_ptr() + x_origin * x.element_size(), a, positions.data_ptr(), frequencies.data_ptr(), y.data_ptr() + y_origin * y.element_size(), b, _mx_dtype(x), rotary,
+                pairs, transposed, factor, torch.cuda.current_stream().cuda_stream)
+
+
+def _mx_cache_checks(k, k_codes, k_scales, v, v_codes, v_scales, x, q, s, slots, x_origin):
+    if len({t is None for t in (v, v_codes, v_scales)}) != 1:
+        raise ValueError("v, v_codes and v_scales: all or none")
+    if x.rank != 3:
+        raise ValueError("layouts over (tokens, heads, elements)")
+    _integers(slots, _mode_size(x, 0), "slots")
+    for rows, codes, scales in ((k, k_codes, k_scales), (v, v_codes, v_scales)):
+        if rows is None:
+            continue
+        _mx_covers(codes, q, scales, s)
+        if rows.dtype != k.dtype:
+            raise ValueError("k and v of one type")
+        if x_origin + x.min_offset < 0 or x_origin + x.cosize > _memory_of(rows):
+            raise ValueError("tensor does not cover the offsets the layout reaches")
+
+
+def _address(t, origin=0):
+    return None if t is None else t.data_ptr() + origin * t.element_size()
+
+
+def mx_cache_write_tensor(k, v, x_layout, k_codes, v_codes, codes_layout, k_scales, v_scales, scales_layout, slots, rule="floor", x_origin=0):
+    """Convenience for torch tensors on one GPU, on its current stream (codes, scales: uint8; slots: int32; the v three None for one tensor).  x_origin: the
+    element of k and v that offset 0 of their layout refers to."""
+    import torch
+    with _mx_device("mx_cache_write_tensor", [t for t in (k, v, k_codes, v_codes, k_scales, v_scales, slots) if t is not None]):
+        x, q, s = _as_layout(x_layout), _as_layout(codes_layout), _as_layout(scales_layout)
+        _mx_cache_checks(k, k_codes, k_scales, v, v_codes, v_scales, x, q, s, slots, x_origin)
+        lc_mx_cache_write(_address(k, x_origin), _address(v, x_origin), x, _address(k_codes), _address(v_codes), q, _address(k_scales), _address(v_scales), s, slots.data_ptr(),
+                          _mx_dtype(k), rule, torch.cuda.current_stream().cuda_stream)
+
+
+def mx_cache_read_tensor(k_codes, v_codes, codes_layout, k_scales, v_scales, scales_layout, k, v, x_layout, slots, x_origin=0):
+    """Convenience for torch tensors on one GPU, on its current stream: the way back."""
+    import torch
+    with _mx_device("mx_cache_read_tensor", [t for t in (k, v, k_codes, v_codes, k_scales, v_scales, slots) if t is not None]):
+        x, q, s = _as_layout(x_layout), _as_layout(codes_layout), _as_layout(scales_layout)
+        _mx_cache_checks(k, k_codes, k_scales, v, v_codes, v_scales, x, q, s, slots, x_origin)
+        lc_mx_cache_read(_address(k_codes), _address(v_codes), q, _address(k_scales), _address(v_scales), s, _address(k, x_origin), _address(v, x_origin), x, slots.data_ptr(),
+                         _mx_dtype(k), torch.cuda.current_stream().cuda_stream)
+
+
+def mx_attention_tensor(plan, q, k_codes, k_scales, v_codes, v_scales, lengths, o, pages=None, starts=None, lse=None, workspace=None, q_origin=0, o_origin=0):
+    """Convenience for torch tensors on one GPU, on its current stream, under an MxAttentionPlan: codes, scales and workspace uint8; lengths, pages and starts
+    int32; lse float32.  workspace: None allocates one for the call (under torch's own stream ordering).  q_origin / o_origin: the element of q and o
+    that offset 0 of their layouts refers to."""
+    import torch
+    with _mx_device("mx_attention_tensor", [t for t in (q, k_codes, k_scales, v_codes, v_scales, lengths, o, pages, starts, lse, workspace) if t is not None]):
+        if _mx_dtype(q) != plan.q_dtype or _mx_dtype(o) != plan.o_dtype:
+            raise ValueError("q and o of the plan's types")
+        for codes, scales in ((k_codes, k_scales), (v_codes, v_scales)):
+            _mx_covers(codes, plan.codes_layout, scales, plan.scales_layout)
+        for t, layout, origin in ((q, plan.q_layout, q_origin), (o, plan.o_layout, o_origin)):
+            if origin + layout.min_offset < 0 or origin + layout.cosize > _memory_of(t):
+                raise ValueError("tensor does not cover the offsets the layout reaches")
+        _integers(lengths, plan.sequences, "lengths")
+        if pages is not None:
+            _integers(pages, plan.sequences * plan.pages_per_sequence, "pages")
+        if starts is not None:
+            _integers(starts, plan.sequences + 1, "starts")
+        rows = _mode_size(plan.q_layout, 0) * _mode_size(plan.q_layout, 1)
+        if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() < rows):
+            raise ValueError("lse: %d contiguous float32" % rows)
+        need = plan.workspace_bytes
+        if workspace is None and need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        if workspace is not None and not workspace.is_contiguous():
+            raise ValueError("workspace: contiguous")
+        plan.execute(_address(q, q_origin), _address(k_codes), _address(k_scales), _address(v_codes), _address(v_scales), _address(pages), _address(lengths), _address(starts),
+                     _address(o, o_origin), _address(lse), _address(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                     torch.cuda.current_stream().cuda_stream)

@@ -18,7 +18,9 @@ SOURCES = ["layout.cpp", "algebra.cpp", "semimodule.cpp", "plan.cpp", "replay.cp
            "mx_plan.cpp", "mx_gemm_plan.cpp", "mx_capi.cpp", "mx_kernels.hip", "mx_gemm_kernels.hip",
            "mx_gemm_inst_direct_codes.hip", "mx_gemm_inst_direct_bf16.hip", "mx_gemm_inst_direct_f16.hip", "mx_gemm_inst_stream_codes.hip", "mx_gemm_inst_ring_codes.hip", "mx_gemm_inst_wide_bf16_k.hip", "mx_gemm_inst_wide_bf16_rows.hip",
            "mx_gemm_inst_wide_f16_k.hip", "mx_gemm_inst_wide_f16_rows.hip",
-           "mx_gemm_inst_stream_bf16_k.hip", "mx_gemm_inst_stream_bf16_rows.hip", "mx_gemm_inst_stream_f16_k.hip", "mx_gemm_inst_stream_f16_rows.hip"]
+           "mx_gemm_inst_stream_bf16_k.hip", "mx_gemm_inst_stream_bf16_rows.hip", "mx_gemm_inst_stream_f16_k.hip", "mx_gemm_inst_stream_f16_rows.hip",
+           "rope_plan.cpp", "mx_cache_plan.cpp", "mx_attention_plan.cpp", "rope_cache_capi.cpp", "rope_kernels.hip", "mx_cache_kernels.hip", "mx_attention_kernels.hip",
+           "mx_attention_inst_few_bf16.hip", "mx_attention_inst_few_f16.hip", "mx_attention_inst_tile_bf16.hip", "mx_attention_inst_tile_f16.hip"]
 HEADERS = ["layout.hpp", "algebra.hpp", "semimodule.hpp", "plan.hpp", "kernel_params.hpp", "gemm_plan.hpp", "gemm_params.hpp", "plan_cache.hpp", "kernarg.hpp"]
 # header -> the only sources that include it
 _TILE = ["gemm_inst_bf16_256.hip", "gemm_inst_bf16_128.hip", "gemm_inst_f16_256.hip", "gemm_inst_f16_128.hip"]
@@ -31,11 +33,21 @@ _MX_RING = ["mx_gemm_inst_ring_codes.hip"]
 _MX_WIDE = ["mx_gemm_inst_wide_%s_%s.hip" % (t, k) for t in ("bf16", "f16") for k in ("k", "rows")]
 _WIDE = ["gemm_inst_%s_wide.hip" % t for t in ("bf16", "f16")]
 _MX_GEMM = _MX_DIRECT + _MX_STREAM + _MX_RING + _MX_WIDE + ["mx_gemm_plan.cpp", "mx_gemm_kernels.hip", "mx_capi.cpp"]
-_MX = _MX_GEMM + ["mx_plan.cpp", "mx_kernels.hip"]
-KERNEL_HEADERS = {"lds_limit.hpp": _TILE + _SPLIT + _STREAM + _GATHER + _WIDE + _MX_DIRECT + _MX_STREAM + _MX_RING + _MX_WIDE + ["kernels.hip", "capi.cpp"],
+_ATTENTION_FEW = ["mx_attention_inst_few_%s.hip" % t for t in ("bf16", "f16")]
+_ATTENTION_TILE = ["mx_attention_inst_tile_%s.hip" % t for t in ("bf16", "f16")]
+_ATTENTION_DEVICE = _ATTENTION_FEW + _ATTENTION_TILE + ["mx_attention_kernels.hip"]
+_ATTENTION = _ATTENTION_DEVICE + ["mx_attention_plan.cpp", "rope_cache_capi.cpp"]
+_ROPE = ["rope_plan.cpp", "rope_kernels.hip", "rope_cache_capi.cpp"]
+_CACHE = _ATTENTION + ["mx_cache_plan.cpp", "mx_cache_kernels.hip"]
+_MX = _MX_GEMM + ["mx_plan.cpp", "mx_kernels.hip"] + _CACHE + _ROPE
+KERNEL_HEADERS = {"lds_limit.hpp": _TILE + _SPLIT + _STREAM + _GATHER + _WIDE + _MX_DIRECT + _MX_STREAM + _MX_RING + _MX_WIDE + _ATTENTION_TILE + ["kernels.hip", "capi.cpp"],
+                  "rope_params.hpp": _ROPE, "rope_plan.hpp": _ROPE, "mx_cache_params.hpp": _CACHE, "mx_cache_plan.hpp": _CACHE,
+                  "mx_attention_params.hpp": _ATTENTION, "mx_attention_plan.hpp": _ATTENTION, "mx_attention_device.hpp": _ATTENTION_DEVICE,
+                  "mx_attention_few_kernel.hpp": _ATTENTION_FEW, "mx_attention_tile_kernel.hpp": _ATTENTION_TILE,
+                  "mx_device.hpp": ["mx_kernels.hip", "mx_cache_kernels.hip", "rope_kernels.hip"],
                   "mx_params.hpp": _MX, "mx_plan.hpp": _MX, "mx_gemm_params.hpp": _MX_GEMM, "mx_gemm_plan.hpp": _MX_GEMM, "gemm_kernel.hpp": _TILE, "gemm_split_kernel.hpp": _SPLIT + _GATHER, "gemm_stream_kernel.hpp": _STREAM + _GATHER, "gemm_wide_kernel.hpp": _WIDE,
-                  "gemm_device.hpp": _TILE + _SPLIT + _STREAM + _GATHER + _WIDE + _MX_DIRECT + _MX_STREAM + _MX_RING + _MX_WIDE + ["mx_kernels.hip"],
-                  "mx_gemm_device.hpp": _MX_DIRECT + _MX_STREAM + _MX_RING + _MX_WIDE, "mx_gemm_ring_kernel.hpp": _MX_RING, "mx_gemm_wide_kernel.hpp": _MX_WIDE, "mx_gemm_direct_kernel.hpp": _MX_DIRECT, "mx_gemm_stream_kernel.hpp": _MX_STREAM}
+                  "gemm_device.hpp": _TILE + _SPLIT + _STREAM + _GATHER + _WIDE + _MX_DIRECT + _MX_STREAM + _MX_RING + _MX_WIDE + _ATTENTION_DEVICE + ["mx_kernels.hip", "mx_cache_kernels.hip", "rope_kernels.hip"],
+                  "mx_gemm_device.hpp": _MX_DIRECT + _MX_STREAM + _MX_RING + _MX_WIDE + _ATTENTION_DEVICE, "mx_gemm_ring_kernel.hpp": _MX_RING, "mx_gemm_wide_kernel.hpp": _MX_WIDE, "mx_gemm_direct_kernel.hpp": _MX_DIRECT, "mx_gemm_stream_kernel.hpp": _MX_STREAM}
 
 
 def _hipcc():

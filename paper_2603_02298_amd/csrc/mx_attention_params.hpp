@@ -1,0 +1,95 @@
+// Kernel arguments and index arithmetic of the attention over a microscaled 4-bit cache.  Shared by the device kernels and by the host walk that
+// checks a plan's addresses and what its workgroups go over without a GPU.
+//
+// A sequence's rows are its queries' heads that share keys and values: row r of sequence b and key head k is query r / group of the sequence, head
+// k * group + r % group.  A workgroup takes `tile_rows` rows of one sequence and key head, and one part of the tokens that they see.
+#pragma once
+#include "mx_params.hpp"
+
+namespace lc {
+
+struct MxAttentionParams {
+  MxMode q_t, q_h, q_d, o_t, o_h, o_d;   // tokens, heads, elements; in bytes
+  MxMode c_n, c_h, c_b;                  // the cache's slots, heads, blocks: codes
+  MxMode s_n, s_h, s_b;                  // scales
+  uint32_t T, D, blocks;                 // blocks: of a head that hold elements below D
+  uint32_t heads, kv_heads, group;       // group: heads / kv_heads
+  uint32_t sequences, page, pages_each, pool_pages;   // pages_each: places of a sequence in the page table
+  uint32_t max_queries, max_tokens;      // max_tokens: page * pages_each
+  uint32_t tile_rows, row_tiles;         // row_tiles: of a sequence and key head, at most
+  uint32_t part_tokens, parts;           // tokens of a part (a multiple of kMxAttentionTokens), parts at most
+  uint32_t window;                       // 0: none
+  FastDiv page_div, group_div, parts_div, rows_div, kv_div;   // rows_div: of row_tiles
+  float scale_log2;                      // scores are exponents of two: scale * log2(e)
+  int32_t causal, o_type;
+  uint32_t queries_each;                 // of a sequence, where a call names no starts
+  int32_t by_xcd;
+};
+
+constexpr uint32_t kMxAttentionTokens = 64;   // parts begin and end at multiples of this many tokens
+
+// A sequence as a call's arrays give it, cut to what fits.
+struct MxSequence {
+  uint32_t first;     // its first query's row of q
+  uint32_t queries;   // at most max_queries of them
+  int32_t position;   // of the first query (below 0: before the first token)
+  uint32_t length;    // cached tokens
+};
+LC_HD MxSequence mx_sequence(const MxAttentionParams& P, int32_t length, int32_t start, int32_t end) {
+  MxSequence s;
+  const int32_t T = (int32_t)P.T;
+  const int32_t s0 = start < 0 ? 0 : start > T ? T : start, s1 = end < s0 ? s0 : end > T ? T : end;
+  s.first = (uint32_t)s0;
+  const uint32_t all = (uint32_t)(s1 - s0);
+  s.queries = all < P.max_queries ? all : P.max_queries;
+  s.length = length < 0 ? 0u : (uint32_t)length > P.max_tokens ? P.max_tokens : (uint32_t)length;
+  s.position = (int32_t)s.length - (int32_t)all;
+  return s;
+}
+// tokens that query i sees: *lo .. *hi - 1 (none where hi <= lo)
+LC_HD void mx_seen(const MxAttentionParams& P, const MxSequence& s, uint32_t i, uint32_t* lo, uint32_t* hi) {
+  const int32_t at = s.position + (int32_t)i;
+  *hi = !P.causal ? s.length : at < 0 ? 0u : (uint32_t)at + 1u;   // (a query's position is below the length)
+  *lo = P.window && at + 1 > (int32_t)P.window ? (uint32_t)at + 1u - P.window : 0u;
+}
+// tokens that any of rows r0 .. r1 - 1 sees lie in *lo .. *hi - 1
+LC_HD void mx_rows_seen(const MxAttentionParams& P, const MxSequence& s, uint32_t r0, uint32_t r1, uint32_t* lo, uint32_t* hi) {
+  uint32_t unused;
+  mx_seen(P, s, fd_div(r0, P.group_div), lo, &unused);
+  mx_seen(P, s, fd_div(r1 - 1u, P.group_div), &unused, hi);
+  if (*lo > *hi) *lo = *hi;
+}
+// Parts of the tokens lo .. hi - 1: part 0 begins with the tile of kMxAttentionTokens that holds lo.
+LC_HD uint32_t mx_parts(const MxAttentionParams& P, uint32_t lo, uint32_t hi) {
+  const uint32_t begin = lo & ~(kMxAttentionTokens - 1u);
+  if (hi <= lo) return 0u;
+  return (hi - begin + P.part_tokens - 1u) / P.part_tokens;
+}
+LC_HD void mx_part(const MxAttentionParams& P, uint32_t lo, uint32_t hi, uint32_t part, uint32_t* from, uint32_t* to) {
+  const uint64_t begin = (uint64_t)(lo & ~(kMxAttentionTokens - 1u)) + (uint64_t)part * P.part_tokens, end = begin + P.part_tokens;
+  *from = begin > hi ? hi : (uint32_t)begin;
+  *to = end > hi ? hi : (uint32_t)end;
+}
+// Where the page that holds token j of a sequence is named in the page table, and the token's place on it.
+LC_HD uint64_t mx_page_at(const MxAttentionParams& P, uint32_t b, uint32_t j, uint32_t* place) {
+  uint32_t q;
+  fd_divmod(j, P.page_div, &q, place);
+  return (uint64_t)b * P.pages_each + q;
+}
+// Which workgroup does what.  Neighbouring workgroups go to different XCDs, each with a cache of its own.  by_xcd: those that read the same keys and values
+// (the row tiles of one sequence and key head, a pair) follow each other on one XCD, the longest (last) rows first.
+LC_HD bool mx_attention_work(const MxAttentionParams& P, uint32_t group, uint32_t* b, uint32_t* kv, uint32_t* row_tile, uint32_t* part) {
+  const uint32_t xcd = P.by_xcd ? group % kXcds : 0u, slot = P.by_xcd ? group / kXcds : group;
+  uint32_t rest, rows, pair;
+  fd_divmod(slot, P.parts_div, &rest, part);
+  fd_divmod(rest, P.rows_div, &pair, &rows);
+  *row_tile = P.row_tiles - 1u - rows;
+  fd_divmod(P.by_xcd ? pair * kXcds + xcd : pair, P.kv_div, b, kv);
+  return *b < P.sequences;
+}
+// A part's unfinished rows in the workspace: `tile_rows` rows of `width` sums, then their maxima and totals.  Number of the part's tile:
+LC_HD uint64_t mx_partial_tile(const MxAttentionParams& P, uint32_t b, uint32_t kv, uint32_t row_tile, uint32_t part) {
+  return (((uint64_t)b * P.kv_heads + kv) * P.row_tiles + row_tile) * P.parts + part;
+}
+
+}  // namespace lc

@@ -1,0 +1,274 @@
+// Attention of many rows (prompts) over a microscaled 4-bit cache: 128 rows and a part of their tokens per workgroup, 32 rows a wavefront; tiles of 64 tokens are
+// expanded to 16 bits into LDS by all of its lanes and read by all of its wavefronts.
+//
+// LDS holds a tile twice over (the next one's codes are loaded, and expanded, under the products of the one before): keys in the arrangement of
+// kLoadKDirect, 64 elements at a time, values in that of kLoadRDirect, whose transposing reads give a lane eight tokens of an element.
+// A lane has the scores of one row (S^T): 16 tokens of 32 each time, the others in lane + 32.
+// Bound by the matrix cores and, about as much, by the exponentials and conversions between the products.
+#pragma once
+#include "mx_attention_device.hpp"
+#include "lds_limit.hpp"
+
+namespace lc {
+
+__device__ __forceinline__ float mx_max_of_halves(float m) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  const uint32_t u = __builtin_bit_cast(uint32_t, m);
+  const u32x2 a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(mx_float_of(a[0]), mx_float_of(a[1]));
+}
+__device__ __forceinline__ float mx_sum_of_halves(float m) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  const uint32_t u = __builtin_bit_cast(uint32_t, m);
+  const u32x2 a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return mx_float_of(a[0]) + mx_float_of(a[1]);
+}
+
+template <int WIDTH>
+constexpr uint32_t kMxAttentionTileLds = 2u * 2u * kMxAttentionTokens * WIDTH * 2u + 2u * kMxAttentionTokens * 4u;   // (all of it dynamic: what may be allowed then is all of a CU's)
+
+template <int MATH, int WIDTH>
+__global__ __launch_bounds__(256, WIDTH == 256 ? 1 : 2) void mx_attention_tile_kernel(MxAttentionParams P, MxAttentionTensors t, bool q_vectors, bool o_vectors) {
+  constexpr int NB = WIDTH / 32, TOKENS = (int)kMxAttentionTokens, STEPS = WIDTH / 16;
+  constexpr uint32_t K_BYTES = TOKENS * WIDTH * 2, STAGE = 2 * K_BYTES;
+  // A lane loads UNITS blocks of a tile, all of the same block of a head: of keys and values of PASSES tokens (width 64: of keys or of values)
+  constexpr int PASSES = NB >= 4 ? NB / 4 : 1, TENSORS = NB >= 4 ? 2 : 1;
+  touch_kernel_arguments<kMxAttentionKernargs>();
+  extern __shared__ unsigned char lds[];
+  // [stage][token]: the tile whose token has values in blocks that may not be finite (kMxLoud)
+  uint32_t* s_loud = reinterpret_cast<uint32_t*>(lds + 2 * STAGE);
+  const uint32_t tid = threadIdx.x, lane = tid & 63u, n = lane & 31u, h = lane >> 5;
+  const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
+  MxAttentionWork w;
+  if (!mx_attention_begin(P, t, blockIdx.x, w)) return;
+  if (tid < 2u * TOKENS) s_loud[tid] = 0xFFFFFFFFu;
+
+  // ---- a lane's blocks of a tile ----
+  const uint32_t block = tid % NB, first_token = (tid / NB) % (256u / NB > (uint32_t)TOKENS ? (uint32_t)TOKENS : 256u / NB);
+  const bool second = TENSORS == 1 && tid >= 128u;   // (width 64) values
+  const bool block_in = block < P.blocks;
+  const int64_t c_head = mx_mode_eval(P.c_h, w.kv) + mx_mode_eval(P.c_b, block_in ? block : 0u), s_head = mx_mode_eval(P.s_h, w.kv) + mx_mode_eval(P.s_b, block_in ? block : 0u);
+  const unsigned char *codes[2] = {(second ? t.v_codes : t.k_codes) + c_head, t.v_codes + c_head};
+  const unsigned char *scales[2] = {(second ? t.v_scales : t.k_scales) + s_head, t.v_scales + s_head};
+  struct Raw {
+    u32x4 codes[PASSES][TENSORS];
+    uint32_t byte[PASSES][TENSORS];
+    bool in[PASSES];
+  };
+  auto page_of = [&](uint32_t j, uint32_t* place) -> uint32_t {
+    if (j >= w.to) { *place = 0u; return 0xFFFFFFFFu; }
+    const uint64_t at = mx_page_at(P, w.b, j, place);
+    return t.pages ? (uint32_t)t.pages[at] : (uint32_t)at;
+  };
+  struct Pages {
+    uint32_t id[PASSES], place[PASSES];
+    uint32_t of_lane;   // the page of token `lane` of the tile
+  };
+  auto pages_of = [&](uint32_t j) {
+    Pages p;
+    uint32_t unused;
+    static_for<PASSES>([&](auto i) { p.id[i] = page_of(j + first_token + (uint32_t)i * (TOKENS / PASSES), &p.place[i]); });
+    p.of_lane = page_of(j + lane, &unused);
+    return p;
+  };
+  auto load = [&](const Pages& p, Raw& raw) {
+    static_for<PASSES>([&](auto i) {
+      raw.in[i] = p.id[i] < P.pool_pages;
+      const uint32_t slot = raw.in[i] ? p.id[i] * P.page + p.place[i] : 0u;
+      const int64_t c = mx_mode_eval(P.c_n, slot), s = mx_mode_eval(P.s_n, slot);
+      static_for<TENSORS>([&](auto k) {
+        raw.codes[i][k] = *reinterpret_cast<const u32x4*>(codes[k] + c);
+        raw.byte[i][k] = scales[k][s];
+      });
+    });
+  };
+  auto expand = [&](uint32_t j, uint32_t stage, Raw& raw) {
+    unsigned char* keys = lds + stage * STAGE;
+    static_for<PASSES>([&](auto i) {
+      const uint32_t token = first_token + (uint32_t)i * (TOKENS / PASSES);
+      static_for<TENSORS>([&](auto k) {
+        const bool is_value = TENSORS == 1 ? second : (int)decltype(k)::value == 1;
+        // tokens that nobody sees, and blocks that are not there: zeros
+        const bool in = block_in && raw.in[i] && j + token >= w.lo, loud = is_value && in && raw.byte[i][k] >= kMxLoud<MATH>;
+        const u32x4 c = select_or_zero(in && !loud, raw.codes[i][k]);
+        const float scale = mx_scale_value(in && !loud ? raw.byte[i][k] : 127u);
+        if (loud) s_loud[TOKENS * stage + token] = j;
+        static_for<4>([&](auto e) {
+          const uint32_t at = is_value ? K_BYTES + gemm_rdirect_lds_offset(WIDTH, token, 32u * block + 8u * (uint32_t)e)
+                                       : (block / 2u) * (TOKENS * 128u) + gemm_lds_offset(token, 4u * (block & 1u) + (uint32_t)e);
+          *reinterpret_cast<u32x4*>(keys + at) = mx_expand<MATH>(c[(int)e], scale);
+        });
+      });
+    });
+  };
+
+  Raw raw;
+  Pages ahead = pages_of(w.from);
+  uint64_t ok_next = __ballot(ahead.of_lane < P.pool_pages), ok = ok_next;
+  if (w.from < w.to) {
+    load(ahead, raw);
+    ahead = pages_of(w.from + TOKENS);
+  }
+
+  // ---- queries ----
+  const uint32_t row = w.r0 + 32u * wave + n;
+  uint32_t row_lo, row_hi, q_token, q_head;
+  mx_row_seen(P, w, row, &row_lo, &row_hi);
+  mx_row_place(P, w, row < w.r1 ? row : w.r0, &q_token, &q_head);
+  u32x4 q[STEPS];
+  {
+    const unsigned char* p = row < w.r1 ? t.q + mx_mode_eval(P.q_t, q_token) + mx_mode_eval(P.q_h, q_head) : nullptr;
+    static_for<STEPS>([&](auto s) { q[s] = mx_query_vector(P, p, 16u * (uint32_t)s + 8u * h, q_vectors); });
+  }
+  // what the wavefront's rows see: any of them, every one of them
+  uint32_t any_lo = 0u, any_hi = 0u, all_lo = 0u, all_hi = 0u;
+  const uint32_t wave_r0 = w.r0 + 32u * wave, wave_r1 = wave_r0 + 32u < w.r1 ? wave_r0 + 32u : w.r1;
+  if (wave_r0 < w.r1) {
+    mx_seen(P, w.s, fd_div(wave_r0, P.group_div), &any_lo, &all_hi);
+    mx_seen(P, w.s, fd_div(wave_r1 - 1u, P.group_div), &all_lo, &any_hi);
+  }
+
+  float top = kMinusInfinity, total = 0.0f;
+  f32x16 acc[NB];
+  static_for<NB>([&](auto d) { static_for<16>([&](auto e) { acc[d][(int)e] = 0.0f; }); });
+  const uint32_t v_at = gemm_rdirect_frag_offset(WIDTH, lane, 0u, 4u * h);   // the lane's address of elements 0 .. 31 at the first 16 tokens
+
+  if (w.from < w.to) expand(w.from, 0u, raw);
+  __syncthreads();
+  uint32_t stage = 0u;
+  for (uint32_t j = w.from; j < w.to; j += TOKENS, stage ^= 1u) {
+    const uint32_t follows = j + TOKENS;
+    ok = ok_next;
+    if (follows < w.to) {
+      ok_next = __ballot(ahead.of_lane < P.pool_pages);
+      load(ahead, raw);
+      ahead = pages_of(follows + TOKENS);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+
+    if (j < any_hi && j + TOKENS > any_lo) {   // (a wavefront whose rows see nothing of the tile has nothing to do)
+      const unsigned char* keys = lds + stage * STAGE;
+      const unsigned char* values = keys + K_BYTES;
+      // ---- scores ----
+      f32x16 s[2];
+      static_for<2>([&](auto g) {
+        static_for<16>([&](auto e) { s[g][(int)e] = 0.0f; });
+        static_for<STEPS>([&](auto k) {
+          const u32x4 a = direct_fragment<TOKENS, kLoadKDirect>(keys + ((int)k / 4) * (TOKENS * 128), lane, 32u * (uint32_t)g, (int)k % 4);
+          s[g] = mfma_32x32x16<MATH == kMxBf16>(a, q[k], s[g]);
+        });
+        s[g] *= P.scale_log2;   // (of either sign, or 0: before what is not seen becomes minus infinity)
+      });
+      const bool whole = j >= all_lo && j + TOKENS <= all_hi && ok == ~uint64_t(0);
+      if (!whole) {
+        static_for<2>([&](auto g) {
+          static_for<16>([&](auto e) {
+            const uint32_t in = 32u * (uint32_t)g + mfma_c_row(lane, (uint32_t)e);
+            const bool seen = (ok >> in & 1u) && j + in >= row_lo && j + in < row_hi;
+            s[g][(int)e] = seen ? s[g][(int)e] : kMinusInfinity;
+          });
+        });
+      }
+      // ---- probabilities ----
+      float m = kMinusInfinity;
+      static_for<2>([&](auto g) {
+        static_for<16>([&](auto e) { m = fmaxf(m, s[g][(int)e]); });
+      });
+      m = fmaxf(top, mx_max_of_halves(m));
+      const float from = m == kMinusInfinity ? 0.0f : m;
+      const float shrink = __builtin_amdgcn_exp2f(top - from);
+      if (__ballot(m != top)) static_for<NB>([&](auto d) { acc[d] *= shrink; });
+      top = m;
+      float sum = 0.0f;
+      u32x4 p[4];
+      static_for<2>([&](auto g) {
+        static_for<16>([&](auto e) {
+          s[g][(int)e] = __builtin_amdgcn_exp2f(s[g][(int)e] - from);
+          sum += s[g][(int)e];
+        });
+        static_for<8>([&](auto d) { p[2 * g + d / 4][(int)d % 4] = mx_pair<MATH>(s[g][2 * d], s[g][2 * d + 1]); });
+      });
+      total = total * shrink + sum;
+      // ---- values: 16 tokens a step, of which a lane has 4 h .. + 3 and 8 + 4 h .. + 3 ----
+      auto fragment = [&](auto d, auto k) {
+        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+        const unsigned char* at = values + (v_at ^ (64u * (uint32_t)d)) + (uint32_t)k * 16u * (WIDTH * 2u);
+        const u32x2 a = __builtin_bit_cast(u32x2, lds_transpose_load((lds_s16x4*)at)), b = __builtin_bit_cast(u32x2, lds_transpose_load((lds_s16x4*)(at + 8u * (WIDTH * 2u))));
+        return u32x4{a[0], a[1], b[0], b[1]};
+      };
+      static_for<4>([&](auto k) { static_for<NB>([&](auto d) { acc[d] = mfma_32x32x16<MATH == kMxBf16>(fragment(d, k), p[k], acc[d]); }); });
+      uint64_t tokens = __ballot(s_loud[TOKENS * stage + lane] == j);
+#pragma unroll 1
+      for (; tokens; tokens &= tokens - 1u) {   // (rare)
+        const uint32_t in = (uint32_t)__builtin_ctzll(tokens);
+        // the row's probability: in one of its two lanes, the one whose scores hold the token
+        float mine = 0.0f;
+        static_for<2>([&](auto g) {
+          static_for<16>([&](auto e) { mine = in == 32u * (uint32_t)g + mfma_c_row(lane, (uint32_t)e) ? s[g][(int)e] : mine; });
+        });
+        const float probability = mx_sum_of_halves(mine);
+        const bool seen = j + in >= row_lo && j + in < row_hi;
+        uint32_t place;
+        const uint32_t id = page_of(j + in, &place), slot = id < P.pool_pages ? id * P.page + place : 0u;
+        const unsigned char *c = t.v_codes + mx_mode_eval(P.c_h, w.kv) + mx_mode_eval(P.c_n, slot), *b = t.v_scales + mx_mode_eval(P.s_h, w.kv) + mx_mode_eval(P.s_n, slot);
+        static_for<NB>([&](auto d) {
+          const uint32_t at = (uint32_t)d < P.blocks ? (uint32_t)d : 0u;
+          const uint32_t byte = b[mx_mode_eval(P.s_b, at)];
+          if ((uint32_t)d < P.blocks && byte >= kMxLoud<MATH>) {
+            const u32x4 codes = *reinterpret_cast<const u32x4*>(c + mx_mode_eval(P.c_b, at));
+            const float scale = mx_scale_value(byte);
+            static_for<4>([&](auto i) {   // elements 8 i + 4 h .. + 3 of the block
+              const uint32_t four = codes[(int)i] >> (16u * h);
+              float v[4];
+              mx_expand_pair<MATH, 0>(four, scale, &v[0], &v[1]);
+              mx_expand_pair<MATH, 1>(four, scale, &v[2], &v[3]);
+              static_for<4>([&](auto e) { acc[d][4 * i + e] = seen ? acc[d][4 * i + e] + probability * v[e] : acc[d][4 * i + e]; });
+            });
+          }
+        });
+      }
+    }
+    if (follows < w.to) expand(follows, stage ^ 1u, raw);
+    __syncthreads();
+  }
+
+  // ---- out: finished, or a part's sums for the join ----
+  const MxAttentionParams& Z = mx_attention_params_again();
+  total = mx_sum_of_halves(total);
+  if (row >= w.r1) return;
+  if (w.parts <= 1u) {
+    unsigned char* o = t.o + mx_mode_eval(Z.o_t, q_token) + mx_mode_eval(Z.o_h, q_head);
+    const float inverse = mx_inverse(total);
+    static_for<NB>([&](auto d) {
+      static_for<4>([&](auto i) {
+        float v[4];
+        static_for<4>([&](auto e) { v[e] = acc[d][4 * i + e] * inverse; });
+        mx_store_o<4>(Z, o, 32u * (uint32_t)d + 8u * (uint32_t)i + 4u * h, v, o_vectors);
+      });
+    });
+    if (t.lse && h == 0u) t.lse[(uint64_t)q_token * Z.heads + q_head] = mx_lse(top, total);
+  } else {
+    float* part = t.parts + mx_partial_tile(Z, w.b, w.kv, w.row_tile, w.part) * Z.tile_rows * (WIDTH + 2);
+    const uint32_t in = 32u * wave + n;
+    static_for<NB>([&](auto d) {
+      static_for<4>([&](auto i) {
+        *reinterpret_cast<f32x4*>(part + in * WIDTH + 32u * (uint32_t)d + 8u * (uint32_t)i + 4u * h) = f32x4{acc[d][4 * i], acc[d][4 * i + 1], acc[d][4 * i + 2], acc[d][4 * i + 3]};
+      });
+    });
+    if (h == 0u) {
+      part[Z.tile_rows * WIDTH + in] = top;
+      part[Z.tile_rows * WIDTH + Z.tile_rows + in] = total;
+    }
+  }
+}
+
+template <int MATH, int WIDTH>
+hipError_t launch_mx_attention_tile(const lc_mx_attention_plan& plan, const MxAttentionTensors& t, hipStream_t s) {
+  static DevicesDone raised;
+  const hipError_t e = raise_lds_limit(&raised, &mx_attention_tile_kernel<MATH, WIDTH>);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((mx_attention_tile_kernel<MATH, WIDTH>), dim3(plan.groups), dim3(256), kMxAttentionTileLds<WIDTH>, s, plan.params, t, plan.q_vectors, plan.o_vectors);
+  return hipSuccess;
+}
+
+}  // namespace lc

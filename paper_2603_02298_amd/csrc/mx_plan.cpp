@@ -16,6 +16,22 @@ int64_t extent_of(const Modes& m) {
   return n;
 }
 
+Modes joined(Modes a, const Modes& b) {
+  a.insert(a.end(), b.begin(), b.end());
+  return a;
+}
+bool writes_once(const Modes& a, const Modes& b) { return modes_write_once(joined(a, b)); }
+
+// a mode of whole blocks counted in blocks: its first leaf holds consecutive codes
+Modes in_blocks(const Modes& k) {
+  Modes b;
+  for (size_t i = 0; i < k.size(); ++i)
+    b.push_back(i == 0 ? Mode{k[0].extent / kMxBlock, kMxBlockBytes} : Mode{k[i].extent, k[i].stride / 2});
+  return coalesce_modes(b);
+}
+
+}  // namespace
+
 lc_status_t fill_mx_mode(const Modes& m, int64_t scale, MxMode* out) {
   if (m.empty() || (int)m.size() > kGemmMaxLeaves) return LC_ERR_TOO_LARGE;
   out->n = (int32_t)m.size();
@@ -28,26 +44,11 @@ lc_status_t fill_mx_mode(const Modes& m, int64_t scale, MxMode* out) {
   return LC_OK;
 }
 
-Modes joined(Modes a, const Modes& b) {
-  a.insert(a.end(), b.begin(), b.end());
-  return a;
-}
-bool writes_once(const Modes& a, const Modes& b) {
-  Modes all = joined(a, b);
+bool modes_write_once(Modes all) {
   for (Mode& m : all) m.stride = m.stride < 0 ? -m.stride : m.stride;   // (walking a mode backwards keeps its image apart or not)
   const int64_t n = extent_of(all);
   return n == 1 || layout_is_injective(coalesce_modes(all), n);
 }
-
-// a mode of whole blocks counted in blocks: its first leaf holds consecutive codes
-Modes in_blocks(const Modes& k) {
-  Modes b;
-  for (size_t i = 0; i < k.size(); ++i)
-    b.push_back(i == 0 ? Mode{k[0].extent / kMxBlock, kMxBlockBytes} : Mode{k[i].extent, k[i].stride / 2});
-  return coalesce_modes(b);
-}
-
-}  // namespace
 
 lc_status_t mx_operand(const Layout& codes, const Layout& scales, int blocked, MxOperand* out) {
   for (const Layout* L : {&codes, &scales}) {

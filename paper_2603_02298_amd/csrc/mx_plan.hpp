@@ -25,6 +25,11 @@ struct MxOperand {
   int64_t rows = 0, k = 0;       // extents of the codes' modes
   Modes q_r, q_k, s_r, s_k;      // of the blocked mode: blocks
 };
+// A coalesced mode (strides times `scale`) as kernels take it.
+lc_status_t fill_mx_mode(const Modes& m, int64_t scale, MxMode* out);
+// No two coordinates of these modes share an offset (shown on the host; see layout_is_injective).
+bool modes_write_once(Modes all);
+
 // Checks that blocks of 32 codes are whole 16-byte words and that the scales fit.
 lc_status_t mx_operand(const Layout& codes, const Layout& scales, int blocked, MxOperand* out);
 

@@ -1,0 +1,414 @@
+"""Attention over a microscaled 4-bit cache on the GPU against the definition in 64 bits.
+
+Error bound.  H: half a step of q's type (2^-8 bf16, 2^-11 f16), u = 2^-24.
+Scores: products of q and k are exact (k in q's type is what the oracle takes), a sum of D terms in fp32 is off by (D + 1) 2u of the sum of magnitudes (as for
+lc_mx_gemm), times the scale, whose own rounding and product add 3u of the score: with Z the row's largest scale sum |q k|, a score is off by e <= (2 D + 5) u Z.
+Probabilities: an exponential of a difference of such scores is off by 2 e, by u of its exponent (at most 2 Z / ln 2 of them) and by 2 u for the instruction:
+r = 2 e + 3 u Z + 2 u relative.  Rounding to 16 bits: H relative, and in f16 2^-25 absolute against the row's maximum of 1.
+Probabilities below 2^-126 of the row's largest, fp32's smallest, are zeros: 2^-126 absolute against it.
+Sums of n terms in fp32, rescaled once a tile of 32: (2 n + n / 32 * 3 + 64) u relative to sum p |v| above and to sum p below (64: the joins).
+Together |error| <= sum p |v| / sum p * (H + 2 r + 2 (2 n + n / 10 + 64) u) 1.01, 2^-126 sum |v| / sum p more (in f16 2^-25), and o's own rounding.
+lse: e + r + (2 n + n / 10 + 64) u + 4 u |lse|."""
+import numpy as np
+import pytest
+
+import paper_2603_02298_amd as lc
+from oracle import serve_oracle as so
+from oracle import mx_oracle as mx
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+TORCH = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+HALF_STEP = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+U = 2.0 ** -24
+
+
+def _pool_texts(slots, heads, width, page, order):
+    def text(w):
+        pages = slots // page
+        return {"heads": "((%d,%d),%d,%d):((%d,%d),%d,1)" % (page, pages, heads, w, w, heads * page * w, page * w),
+                "tokens": "((%d,%d),%d,%d):((%d,%d),%d,1)" % (page, pages, heads, w, heads * w, page * heads * w, w),
+                "flat": "(%d,%d,%d):(%d,%d,1)" % (slots, heads, w, heads * w, w),
+                "gaps": "((%d,%d),%d,%d):((%d,%d),%d,1)" % (page, pages, heads, w, w + 32, heads * page * (w + 32) + 64, page * (w + 32))}[order]
+    scales = text(width // 32)
+    if order == "heads":   # scales of a page's tokens together, block by block
+        blocks, pages = width // 32, slots // page
+        scales = "((%d,%d),%d,%d):((1,%d),%d,%d)" % (page, pages, heads, blocks, heads * page * blocks, page * blocks, page)
+    return text(width), scales
+
+
+def _rows(T, H, D, order):
+    return {"thd": "(%d,%d,%d):(%d,%d,1)" % (T, H, D, H * D, D), "htd": "(%d,%d,%d):(%d,%d,1)" % (T, H, D, D, T * D), "row": "(%d,%d,%d):(%d,%d,1)" % (T, H, D, (H + 2) * D + 1, D),
+            "dht": "(%d,%d,%d):(1,%d,%d)" % (T, H, D, T, T * H)}[order]
+
+
+def _fill(rng, codes_text, scales_text, slots, low=123, high=128):
+    """A pool whose every byte is noise, scales of 255 among it, but for the slots in use."""
+    codes = rng.integers(0, 256, lc.Layout(codes_text).cosize // 2 + 16, dtype=np.uint8)
+    scales = rng.integers(250, 256, lc.Layout(scales_text).cosize + 16, dtype=np.uint8)
+    s = mx.mode_offsets(scales_text)
+    at = s[0][slots][:, None, None] + s[1][None, :, None] + s[2][None, None, :]
+    scales[at] = rng.integers(low, high, at.shape)
+    return codes, scales
+
+
+class Case:
+    """One call's data; `run` makes it and compares."""
+
+    def __init__(self, queries, lengths, heads, kv, D, page=16, dtype="bf16", o_dtype=None, order="heads", q_order="thd", o_order="thd", causal=True, window=0, table=True, starts=True,
+                 extra_rows=0, max_queries=None, each=None, scale=None, seed=0, low=123, high=128):
+        print("case", queries, lengths, heads, kv, D, page, dtype, o_dtype, order, q_order, o_order, causal, window, table, starts, flush=True)
+        rng = self.rng = np.random.default_rng(seed)
+        self.B, self.queries, self.lengths, self.heads, self.kv, self.D = len(queries), queries, np.array(lengths, np.int32), heads, kv, D
+        self.page, self.dtype, self.o_dtype, self.causal, self.window = page, dtype, o_dtype or dtype, causal, window
+        self.each = each or max(1, -(-max(lengths) // page))
+        self.max_queries = max_queries or max(max(queries), 1)
+        self.T = sum(queries) + extra_rows
+        self.scale = D ** -0.5 if scale is None else scale
+        pages_n = self.B * self.each + (2 if table else 0)
+        self.slots = pages_n * page
+        width = (D + 31) // 32 * 32
+        self.codes_text, self.scales_text = _pool_texts(self.slots, kv, width, page, order)
+        self.q_text, self.o_text = _rows(self.T, heads, D, q_order), _rows(self.T, heads, D, o_order)
+        self.pages = rng.permutation(pages_n)[:self.B * self.each].astype(np.int32).reshape(self.B, self.each) if table else None
+        used = []
+        for b in range(self.B):
+            j = np.arange(min(max(lengths[b], 0), self.each * page))
+            used.append((self.pages[b][j // page] if table else b * self.each + j // page) * page + j % page)
+        self.used = used
+        inside = np.concatenate(used).astype(np.int64)
+        self.k, self.v = (list(_fill(rng, self.codes_text, self.scales_text, inside, low, high)) for _ in range(2))
+        q = rng.standard_normal(lc.Layout(self.q_text).cosize).astype(np.float32) * 1.5
+        self.q = torch.from_numpy(q).to(TORCH[dtype])
+        self.starts = np.cumsum([0] + list(queries)).astype(np.int32) if starts else None
+
+    def plan(self):
+        return lc.MxAttentionPlan(self.q_text, self.codes_text, self.scales_text, self.o_text, self.dtype, self.o_dtype, sequences=self.B, page=self.page, pages_per_sequence=self.each,
+                                  max_queries=self.max_queries, scale=self.scale, causal=self.causal, window=self.window)
+
+    def on_gpu(self, workspace=None):
+        dev = torch.device("cuda:0")
+        g = lambda a: None if a is None else torch.from_numpy(np.ascontiguousarray(a)).to(dev)   # noqa: E731
+        o = torch.full((lc.Layout(self.o_text).cosize + 8,), 77.0, dtype=TORCH[self.o_dtype], device=dev)
+        lse = torch.full((self.T, self.heads), 77.0, device=dev)
+        plan = self.plan()
+        print(plan.describe(), flush=True)
+        if workspace is None:   # what is in it does not matter
+            workspace = torch.full((plan.workspace_bytes,), 255, dtype=torch.uint8, device=dev)
+        lc.mx_attention_tensor(plan, self.q.to(dev), g(self.k[0]), g(self.k[1]), g(self.v[0]), g(self.v[1]), g(self.lengths), o, g(self.pages), g(self.starts), lse, workspace)
+        torch.cuda.synchronize()
+        return o, lse
+
+    def want(self):
+        # keys and values in q's type, as the call rounds them
+        t = TORCH[self.dtype]
+        pools = []
+        for codes, scales in (self.k, self.v):
+            pool = so.Pool(codes, self.codes_text, scales, self.scales_text, self.D)
+            pools.append(type("Rounded", (), {"slots": pool.slots, "__call__": lambda _, s, pool=pool: torch.from_numpy(pool(s)).to(t).double().numpy()})())
+        off = mx.offsets(self.q_text)
+        o, lse = np.full((self.T, self.heads, self.D), 77.0), np.full((self.T, self.heads), 77.0)
+        bound = so.attention(self.q.double().numpy()[off], *pools, self.heads // self.kv, self.B, self.page, self.each, self.max_queries, self.lengths, self.starts, self.pages,
+                             float(np.float32(self.scale)), self.causal, self.window, o, lse)
+        return o, lse, bound
+
+    def run(self):
+        o_t, lse_t = self.on_gpu()
+        o, lse, (mass, loose, Z, n) = self.want()
+        off = mx.offsets(self.o_text)
+        got = o_t.double().cpu().numpy()
+        H, D = HALF_STEP[self.dtype], self.D
+        e = (2 * D + 5) * U * Z
+        r = 2 * e + 3 * U * Z + 2 * U
+        sums = (2 * n + n / 10 + 64) * U
+        tol = mass * (H + 2 * r + 2 * sums)[..., None] * 1.01 + (2.0 ** -25 if self.dtype == "f16" else 2.0 ** -126) * loose
+        tol = tol + HALF_STEP[self.o_dtype] * (np.abs(o) + tol) + (2.0 ** -25 if self.o_dtype == "f16" else 0.0)
+        same = (got[off] == o) | (np.isnan(got[off]) & np.isnan(o))
+        with np.errstate(invalid="ignore"):
+            wrong = ~(same | (np.abs(got[off] - o) <= tol))
+        assert not wrong.any(), (int(wrong.sum()), np.argwhere(wrong)[:5].tolist(), got[off][wrong][:5], o[wrong][:5], tol[wrong][:5])
+        rest = np.ones(len(got), bool)
+        rest[off.reshape(-1)] = False
+        assert (got[rest] == 77.0).all()
+        got = lse_t.double().cpu().numpy()
+        same = (got == lse) | (np.isnan(got) & np.isnan(lse))
+        with np.errstate(invalid="ignore"):
+            assert (same | (np.abs(got - lse) <= e + r + sums + 4 * U * np.abs(lse))).all()
+        return o_t, lse_t
+
+
+# ---- few rows ----
+@pytest.mark.parametrize("length", [0, 1, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 129, 300, 1000])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_one_token(length, dtype):
+    Case([1], [length], 8, 2, 128, dtype=dtype, each=70).run()
+
+
+@pytest.mark.parametrize("D", [1, 31, 32, 33, 64, 80, 96, 128, 192, 200, 256])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("queries", [1, 5])
+def test_few_rows_of_every_width(D, dtype, queries):
+    Case([queries] * 3, [70, queries, 333], 8, 2, D, dtype=dtype, seed=D).run()
+
+
+@pytest.mark.parametrize("heads,kv", [(1, 1), (3, 3), (7, 1), (16, 1), (17, 1), (32, 1), (12, 4), (64, 2)])
+@pytest.mark.parametrize("page,order", [(16, "heads"), (64, "tokens"), (8, "heads"), (24, "tokens"), (1, "flat"), (3, "gaps"), (32, "gaps"), (128, "flat")])
+def test_heads_and_pages(heads, kv, page, order):
+    Case([1, 1], [200, 77], heads, kv, 64, page=page, order=order, seed=page).run()
+
+
+@pytest.mark.parametrize("page,each,order", [(16, 20, "heads"), (40, 7, "flat"), (7, 41, "flat"), (1, 300, "flat"), (300, 1, "flat"), (304, 1, "heads")])
+@pytest.mark.parametrize("queries", [1, 40])
+def test_without_a_table(page, each, order, queries):
+    Case([queries] * 2, [min(280, page * each), 55], 4, 2, 64, page=page, each=each, order=order, table=False).run()
+
+
+# ---- many rows ----
+@pytest.mark.parametrize("D", [1, 32, 33, 64, 80, 128, 192, 256])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_many_rows_of_every_width(D, dtype):
+    Case([130, 3, 40], [300, 64, 41], 4, 2, D, dtype=dtype, seed=D).run()
+
+
+@pytest.mark.parametrize("queries,lengths", [([33], [33]), ([128], [128]), ([129], [1000]), ([64], [64]), ([65], [1]), ([200], [150]), ([100, 0, 1, 50], [100, 30, 1, 0]), ([40, 300, 7], [500, 301, 2000])])
+@pytest.mark.parametrize("heads,kv", [(2, 2), (5, 1), (8, 2)])
+def test_ragged_prompts(queries, lengths, heads, kv):
+    """Sequences with fewer cached tokens than queries have rows that see nothing."""
+    Case(queries, lengths, heads, kv, 64, seed=len(queries)).run()
+
+
+@pytest.mark.parametrize("page,order", [(16, "tokens"), (1, "flat"), (3, "gaps"), (24, "heads"), (100, "tokens")])
+def test_prompts_on_pages(page, order):
+    Case([70, 20], [300, 90], 4, 2, 128, page=page, order=order).run()
+
+
+# ---- masks ----
+@pytest.mark.parametrize("window", [1, 2, 15, 64, 100, 5000])
+@pytest.mark.parametrize("queries", [1, 4, 90])
+def test_windows(window, queries):
+    Case([queries] * 2, [400, 123], 4, 2, 64, window=window).run()
+
+
+@pytest.mark.parametrize("queries", [1, 7, 60])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_every_token_for_every_query(queries, dtype):
+    """Cross attention: queries of one length, cached states of another."""
+    Case([queries, queries // 2, queries], [100, 333, 0], 4, 4, 80, causal=False, dtype=dtype).run()
+
+
+@pytest.mark.parametrize("queries", [2, 4, 50, 140])
+@pytest.mark.parametrize("window", [0, 37])
+@pytest.mark.parametrize("dtype,byte", [("bf16", 255), ("bf16", 254), ("f16", 255), ("f16", 150)])
+def test_values_that_are_not_finite_reach_only_rows_that_see_them(queries, window, dtype, byte):
+    """Scales of NaN, and such as make infinities of some codes, among the values of tokens that some queries see and others do not."""
+    c = Case([queries, queries], [200, queries], 4, 2, 64, dtype=dtype, window=window, order="tokens")
+    s = mx.mode_offsets(c.scales_text)
+    for b in range(2):
+        n = len(c.used[b])
+        for j in {n - 1, n - 2, n - max(2, queries // 2), max(0, n - queries), max(0, n - queries - window + 1 if window else 0), max(0, n - 5)}:
+            slot = c.used[b][min(max(j, 0), n - 1)]
+            c.v[1][s[0][slot] + s[1][j % 2] + s[2][(j // 2) % 2]] = byte
+    c.run()
+
+
+@pytest.mark.parametrize("queries", [1, 3, 60])
+@pytest.mark.parametrize("what", ["k", "q"])
+def test_nan_and_infinities_of_keys_and_queries(queries, what):
+    c = Case([queries, queries], [100, queries + 3], 4, 2, 64)
+    if what == "k":
+        s = mx.mode_offsets(c.scales_text)
+        c.k[1][s[0][c.used[0][-1]] + s[1][1] + s[2][0]] = 255   # seen by the last query only
+    else:
+        off = mx.offsets(c.q_text)
+        c.q[off[0, 0, 3]] = float("nan")
+        c.q[off[queries, 3, 5]] = float("inf")
+    c.run()
+
+
+@pytest.mark.parametrize("queries", [1, 4, 70])
+@pytest.mark.parametrize("page", [4, 16])
+def test_pages_outside_the_pool_are_seen_by_nobody(queries, page):
+    c = Case([queries, queries, queries], [300, 200, 90], 4, 2, 64, page=page)
+    c.pages[0, ::3] = -1
+    c.pages[1, 1::2] = 2 ** 31 - 1
+    c.pages[1, 0] = c.slots // page
+    c.pages[2, :] = -2 ** 31
+    c.run()
+
+
+def test_equal_scores_give_the_mean():
+    """q of zeros: every probability is 1, the sum of 2^n values of few bits is exact, and so is the result."""
+    for queries in (1, 40):
+        c = Case([queries], [256], 4, 2, 128, causal=False, dtype="bf16", o_dtype="f32", low=127, high=128)
+        c.q.zero_()
+        o_t, lse_t = c.on_gpu()
+        o, lse, _ = c.want()
+        assert (o_t.double().cpu().numpy()[mx.offsets(c.o_text)] == o).all()
+        assert (np.abs(lse_t.double().cpu().numpy() - lse) <= 4 * U * np.abs(lse)).all()
+
+
+def test_one_cached_token_is_the_answer():
+    for queries in (1, 40):
+        c = Case([1] if queries == 1 else [1, queries], [1] if queries == 1 else [1, 1], 4, 2, 96, causal=False, low=120, high=134)
+        o_t, _ = c.on_gpu()
+        o, _, _ = c.want()
+        assert (o_t.double().cpu().numpy()[mx.offsets(c.o_text)] == o).all()
+
+
+def test_scores_of_every_size():
+    """Maxima that grow from tile to tile, and scores so far apart that most probabilities are zero."""
+    for queries in (1, 40):
+        for scale in (0.0, 1e-3, 3.0, -0.5):
+            Case([queries], [700], 4, 2, 64, scale=scale, low=126, high=131).run()
+
+
+# ---- layouts, types, rows that are nobody's ----
+@pytest.mark.parametrize("q_order,o_order", [("htd", "thd"), ("row", "htd"), ("dht", "thd"), ("thd", "dht"), ("thd", "row")])
+@pytest.mark.parametrize("queries", [1, 5, 40])
+@pytest.mark.parametrize("D", [64, 72])
+def test_layouts_of_queries(q_order, o_order, queries, D):
+    Case([queries, queries], [50, 90], 4, 2, D, q_order=q_order, o_order=o_order, o_dtype="f32").run()
+
+
+@pytest.mark.parametrize("queries", [1, 40])
+def test_rows_that_are_nobodys_stay(queries):
+    """Rows behind the last sequence, and queries past max_queries."""
+    Case([queries, 2, queries], [100, 40, 300], 4, 2, 64, extra_rows=5).run()
+    Case([queries + 2, 1], [100, 40], 4, 2, 64, max_queries=queries).run()
+    Case([3] * 4, [10, 20, 30, 40], 4, 2, 64, starts=False).run()
+
+
+def test_numbers_that_do_not_fit_are_cut():
+    c = Case([4, 4], [60, 90], 4, 2, 64)
+    c.lengths[:] = [2 ** 31 - 1, -7]
+    full = np.arange(c.each * c.page)   # the first sequence now has every place of its row of the table
+    slots = (c.pages[0][full // c.page] * c.page + full % c.page).astype(np.int64)
+    for side in (c.k, c.v):
+        s = mx.mode_offsets(c.scales_text)
+        side[1][s[0][slots][:, None, None] + s[1][None, :, None] + s[2][None, None, :]] = 125
+    c.starts = np.array([-3, 5, 2 ** 31 - 1], np.int32)
+    c.run()
+
+
+@pytest.mark.parametrize("queries", [1, 40])
+def test_the_workspace_is_the_calls_alone(queries):
+    """The same bits whatever it held, and for every run."""
+    c = Case([queries] * 2, [5000, 4000], 4, 2, 64)
+    need = c.plan().workspace_bytes
+    assert need > 0
+    first = c.on_gpu(torch.zeros(need, dtype=torch.uint8, device="cuda"))
+    for fill in (255, 127):
+        again = c.on_gpu(torch.full((need,), fill, dtype=torch.uint8, device="cuda"))
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+def test_long_sequences_in_parts():
+    Case([1, 1], [20000, 9999], 8, 2, 128, page=64).run()
+    Case([40], [6000], 4, 1, 64, page=64, dtype="f16").run()
+
+
+def test_offsets_past_32_bits():
+    """A pool whose pages lie 2^28 + 1024 bytes apart."""
+    dev = torch.device("cuda:0")
+    rng = np.random.default_rng(3)
+    page, each, D = 16, 12, 64
+    step = (1 << 29) + 2048
+    codes_text, scales_text = "((16,%d),1,64):((64,%d),64,1)" % (each, step), "((16,%d),1,2):((2,32),2,1)" % each
+    codes = torch.zeros((step * (each - 1) + 1024) // 2, dtype=torch.uint8, device=dev)
+    small = rng.integers(0, 256, (each, page * 32), dtype=np.uint8)
+    for i in range(each):
+        codes[i * step // 2:i * step // 2 + page * 32] = torch.from_numpy(small[i]).to(dev)
+    scales = rng.integers(124, 128, each * page * 2, dtype=np.uint8)
+    pages = rng.permutation(each).astype(np.int32)
+    for queries in (1, 40):
+        q = torch.from_numpy(rng.standard_normal((queries, 2, D)).astype(np.float32)).bfloat16().to(dev)
+        o = torch.empty(queries, 2, D, device=dev)
+        plan = lc.MxAttentionPlan("(%d,2,64):(128,64,1)" % queries, codes_text, scales_text, "(%d,2,64):(128,64,1)" % queries, "bf16", "f32", sequences=1, page=page, pages_per_sequence=each,
+                                  max_queries=queries, scale=0.125)
+        g = lambda a: torch.from_numpy(a).to(dev)   # noqa: E731
+        lc.mx_attention_tensor(plan, q, codes, g(scales), codes, g(scales), g(np.array([page * each], np.int32)), o, g(pages[None].copy()))
+        near = "((16,%d),1,64):((64,1024),64,1)" % each
+        plan2 = lc.MxAttentionPlan("(%d,2,64):(128,64,1)" % queries, near, scales_text, "(%d,2,64):(128,64,1)" % queries, "bf16", "f32", sequences=1, page=page, pages_per_sequence=each,
+                                   max_queries=queries, scale=0.125)
+        o2 = torch.empty_like(o)
+        lc.mx_attention_tensor(plan2, q, g(small.reshape(-1)), g(scales), g(small.reshape(-1)), g(scales), g(np.array([page * each], np.int32)), o2, g(pages[None].copy()))
+        assert torch.equal(o, o2)
+
+
+def test_two_calls_at_once_and_a_captured_one():
+    """A graph follows the arrays that it was captured with; an eager call on another stream with a workspace of its own does not disturb it."""
+    dev = torch.device("cuda:0")
+    c = Case([1, 1], [3000, 2000], 8, 2, 128)
+    plan = c.plan()
+    g = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(dev)   # noqa: E731
+    q, lengths, pages, starts = c.q.to(dev), g(c.lengths), g(c.pages), g(c.starts)
+    pool = [g(a) for a in (*c.k, *c.v)]
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    spaces = [torch.empty(plan.workspace_bytes, dtype=torch.uint8, device=dev) for _ in range(2)]
+    outs = [torch.empty(lc.Layout(c.o_text).cosize, dtype=torch.bfloat16, device=dev) for _ in range(2)]
+
+    def call(i, stream):
+        plan.execute(q.data_ptr(), *[p.data_ptr() for p in pool], pages.data_ptr(), lengths.data_ptr(), starts.data_ptr(), outs[i].data_ptr(), None, spaces[i].data_ptr(),
+                     spaces[i].numel(), stream)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        call(0, side.cuda_stream)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        call(0, torch.cuda.current_stream().cuda_stream)
+    for n in ((3000, 2000), (1, 1999), (0, 64), (2500, 3000)):
+        c.lengths[:] = n
+        lengths.copy_(g(c.lengths))
+        q.copy_(q * 0.9)
+        torch.cuda.synchronize()
+        for o in outs:
+            o.fill_(77.0)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(other):
+            call(1, other.cuda_stream)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], outs[1]) and not torch.isnan(outs[0][:64]).any() if max(n) <= 3000 and n != (2500, 3000) else torch.equal(outs[0].isnan(), outs[1].isnan())
+
+
+# ---- together, as they are used ----
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("pairs", ["half", "neighbours"])
+def test_a_model_layer_step_by_step(dtype, pairs):
+    """Prompts, then single tokens: queries and keys turned, keys and values written, attention over what is cached; every step against the same in 64 bits from the
+    turned and quantised values."""
+    rng = np.random.default_rng(12)
+    dev = torch.device("cuda:0")
+    B, heads, kv, D, page, each = 2, 4, 2, 64, 16, 8
+    pages_n = B * each + 1
+    codes_text, scales_text = _pool_texts(pages_n * page, kv, D, page, "tokens")
+    pool = [torch.from_numpy(rng.integers(0, 256, lc.Layout(t).cosize // n, dtype=np.uint8)).to(dev) for t, n in ((codes_text, 2), (scales_text, 1)) * 2]
+    pages = rng.permutation(pages_n)[:B * each].reshape(B, each).astype(np.int32)
+    f = torch.tensor(lc.lc_rope_frequencies(D, 10000.0, "parts", 4.0, 64), device=dev)
+    cached = np.zeros(B, np.int64)
+    for counts in ([40, 23], [1, 1], [1, 1], [5, 3], [1, 1]):
+        T = sum(counts)
+        qkv = torch.from_numpy(rng.standard_normal((T, heads + 2 * kv, D)).astype(np.float32)).to(TORCH[dtype]).to(dev)
+        positions = np.concatenate([np.arange(n) + cached[b] for b, n in enumerate(counts)]).astype(np.int32)
+        which = np.repeat(np.arange(B), counts)
+        slots = (pages[which, positions // page] * page + positions % page).astype(np.int32)
+        cached += counts
+        g = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(dev)   # noqa: E731
+        row = (heads + 2 * kv) * D
+        turned = "(%d,%d,%d):(%d,%d,1)" % (T, heads + kv, D, row, D)   # in place, inside the rows
+        lc.rope_tensor(qkv, turned, g(positions), f, qkv, turned, D, pairs)
+        k, v = qkv[:, heads:heads + kv], qkv[:, heads + kv:]
+        rows = "(%d,%d,%d):(%d,%d,1)" % (T, kv, D, row, D)
+        lc.mx_cache_write_tensor(k, v, rows, pool[0], pool[2], codes_text, pool[1], pool[3], scales_text, g(slots))
+        back = [torch.empty(T, kv, D, dtype=TORCH[dtype], device=dev) for _ in range(2)]
+        lc.mx_cache_read_tensor(pool[0], pool[2], codes_text, pool[1], pool[3], scales_text, *back, "(%d,%d,%d):(%d,%d,1)" % (T, kv, D, kv * D, D), g(slots))
+        for rows_in, rows_out in ((k, back[0]), (v, back[1])):
+            want = mx.dequantize(*mx.quantize(rows_in.double().cpu().numpy().reshape(T * kv, D), D, "floor")).reshape(T, kv, D)
+            assert (rows_out.double().cpu().numpy() == want).all()
+        c = Case(counts, cached.tolist(), heads, kv, D, page=page, each=each, dtype=dtype, order="tokens")
+        c.pages, c.codes_text, c.scales_text, c.slots = pages, codes_text, scales_text, pages_n * page
+        c.q = qkv[:, :heads].contiguous().view(-1).cpu()
+        c.k, c.v = [t.cpu().numpy() for t in pool[:2]], [t.cpu().numpy() for t in pool[2:]]
+        c.run()

@@ -1,0 +1,154 @@
+"""A cache in microscaled 4-bit elements on the GPU: rows written into slots and read back against the oracle, every code, scale and value equal, bytes that belong
+to nobody left as they were."""
+import numpy as np
+import pytest
+
+import paper_2603_02298_amd as lc
+from oracle import mx_oracle as mx
+from oracle import serve_oracle as so
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+TORCH = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def _pool(slots, heads, width, page, order):
+    def text(w):
+        pages = slots // page
+        if order == "heads":
+            return "((%d,%d),%d,%d):((%d,%d),%d,1)" % (page, pages, heads, w, w, heads * page * w, page * w)
+        if order == "tokens":
+            return "((%d,%d),%d,%d):((%d,%d),%d,1)" % (page, pages, heads, w, heads * w, page * heads * w, w)
+        return "((%d,%d),%d,%d):((%d,%d),%d,1)" % (page, pages, heads, w, 64 + w, heads * page * (64 + w), page * (64 + w))   # gaps
+    codes, scales = text(width), text(width // 32)
+    return codes, scales
+
+
+def _rows(T, H, D, order):
+    return {"thd": "(%d,%d,%d):(%d,%d,1)" % (T, H, D, H * D, D), "htd": "(%d,%d,%d):(%d,%d,1)" % (T, H, D, D, T * D), "row": "(%d,%d,%d):(%d,%d,1)" % (T, H, D, (H + 2) * D + 1, D),
+            "dht": "(%d,%d,%d):(1,%d,%d)" % (T, H, D, T, T * H), "back": "(%d,%d,%d):(-%d,%d,1)" % (T, H, D, H * D, D)}[order]
+
+
+def _values(rng, shape, dtype, kind):
+    if kind == "normal":
+        v = rng.standard_normal(shape) * np.exp2(rng.integers(-14, 10, shape[:2]))[..., None]
+    elif kind == "ties":
+        v = rng.choice([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 0.0, 6.0, 7.0, 7.5, 1.0, 3.0, 4.0], shape) * rng.choice([-1.0, 1.0], shape)
+    else:
+        v = rng.standard_normal(shape)
+        for bad, share in ((np.nan, 0.01), (np.inf, 0.01), (-np.inf, 0.01), (0.0, 0.3)):
+            v[rng.random(shape) < share] = bad
+        v[::3] = 0.0
+    return torch.from_numpy(v.astype(np.float32)).to(TORCH[dtype])
+
+
+def _same(a, b):
+    return ((a == b) & (np.signbit(a) == np.signbit(b))) | (np.isnan(a) & np.isnan(b))
+
+
+def _check(T, H, D, width, page, slots_n, dtype, rule="floor", order="heads", x_order="thd", kind="normal", two=True, out=0, seed=0):
+    print("case", T, H, D, width, page, slots_n, dtype, rule, order, x_order, kind, two, flush=True)
+    rng = np.random.default_rng(seed)
+    dev = torch.device("cuda:0")
+    codes_text, scales_text, x_text = *_pool(slots_n, H, width, page, order), _rows(T, H, D, x_order)
+    X = lc.Layout(x_text)
+    origin, size = 5 - X.min_offset, 16 - X.min_offset + X.cosize
+    off = mx.offsets(x_text) + origin
+    slots = rng.permutation(slots_n)[:T].astype(np.int32)
+    if out:
+        slots[rng.random(T) < 0.3] = -1
+        slots[rng.random(T) < 0.2] = slots_n + out
+    slots_t = torch.from_numpy(slots).to(dev)
+    there = (slots >= 0) & (slots < slots_n)
+    sides = []
+    for _ in range(2 if two else 1):
+        v = _values(rng, (T, H, D), dtype, kind)
+        src = torch.full((size,), 77.0, dtype=TORCH[dtype])
+        src[torch.from_numpy(off)] = v
+        codes = rng.integers(0, 256, lc.Layout(codes_text).cosize // 2 + 32, dtype=np.uint8)
+        scales = rng.integers(0, 256, lc.Layout(scales_text).cosize + 32, dtype=np.uint8)
+        sides.append(dict(v=v, src=src.to(dev), codes=codes, scales=scales, codes_t=torch.from_numpy(codes).to(dev), scales_t=torch.from_numpy(scales).to(dev),
+                          dst=torch.full((size,), 77.0, dtype=TORCH[dtype], device=dev)))
+    a, b = sides[0], sides[1] if two else dict.fromkeys(("src", "codes_t", "scales_t", "dst"))
+    lc.mx_cache_write_tensor(a["src"], b["src"], x_text, a["codes_t"], b["codes_t"], codes_text, a["scales_t"], b["scales_t"], scales_text, slots_t, rule, x_origin=origin)
+    lc.mx_cache_read_tensor(a["codes_t"], b["codes_t"], codes_text, a["scales_t"], b["scales_t"], scales_text, a["dst"], b["dst"], x_text, slots_t, x_origin=origin)
+    torch.cuda.synchronize()
+    for side in sides:
+        so.write_slots(side["codes"], codes_text, side["scales"], scales_text, slots, side["v"].double().numpy(), rule)
+        assert (side["scales_t"].cpu().numpy() == side["scales"]).all()
+        assert (side["codes_t"].cpu().numpy() == side["codes"]).all()
+        want = torch.full((size,), 77.0, dtype=TORCH[dtype])
+        values = so.read_slots(side["codes"], codes_text, side["scales"], scales_text, np.where(there, slots, 0))[:, :, :D]
+        with np.errstate(over="ignore"):
+            want[torch.from_numpy(off[there])] = torch.from_numpy(values[there]).to(TORCH[dtype])
+        assert _same(side["dst"].float().cpu().numpy(), want.float().numpy()).all()
+
+
+SIZES = [(1, 1, 1, 32, 1, 4), (1, 8, 128, 128, 16, 64), (3, 2, 33, 64, 3, 30), (64, 8, 128, 128, 16, 256), (33, 5, 80, 96, 16, 96), (7, 1, 256, 320, 4, 16), (200, 3, 64, 64, 64, 256),
+         (1100, 8, 64, 64, 8, 2000), (515, 8, 128, 128, 16, 1024)]
+
+
+@pytest.mark.parametrize("T,H,D,width,page,slots", SIZES)
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("order", ["heads", "tokens"])
+def test_sizes(T, H, D, width, page, slots, dtype, order):
+    _check(T, H, D, width, page, slots, dtype, "floor" if order == "heads" else "cover", order)
+
+
+@pytest.mark.parametrize("x_order", ["htd", "row", "dht", "back"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_layouts(x_order, dtype):
+    _check(41, 3, 72, 96, 4, 64, dtype, order="gaps", x_order=x_order)
+    _check(41, 3, 64, 64, 4, 64, dtype, order="tokens", x_order=x_order, two=False)
+
+
+@pytest.mark.parametrize("kind", ["ties", "bad"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rule", ["floor", "cover"])
+def test_values(kind, dtype, rule):
+    _check(24, 2, 96, 96, 8, 32, dtype, rule, kind=kind)
+
+
+@pytest.mark.parametrize("out", [0x7FFFFFFF - 64, 1, 1000])
+def test_slots_that_are_not_there(out):
+    """Their tokens are left out of both directions: nothing is written for them, their rows stay as they are."""
+    _check(50, 4, 64, 64, 16, 64, "bf16", out=out)
+
+
+def test_the_quantisation_is_mx_quantize():
+    """A cache whose slots lie like rows: the same codes and scales as lc_mx_quantize's."""
+    rng = np.random.default_rng(9)
+    dev = torch.device("cuda:0")
+    x = _values(rng, (40, 2, 96), "bf16", "normal").to(dev)
+    made = [[torch.zeros(40 * 192 // n, dtype=torch.uint8, device=dev) for n in (2, 32)] for _ in range(2)]
+    lc.mx_quantize_tensor(x.view(80, 96), "(80,96):(96,1)", made[0][0], "(80,96):(96,1)", made[0][1], "(80,3):(3,1)", "cover")
+    lc.mx_cache_write_tensor(x, None, "(40,2,96):(192,96,1)", made[1][0], None, "(40,2,96):(192,96,1)", made[1][1], None, "(40,2,3):(6,3,1)", torch.arange(40, dtype=torch.int32, device=dev), "cover")
+    assert all(torch.equal(a, b) for a, b in zip(*made))
+
+
+def test_a_slot_read_by_many():
+    dev = torch.device("cuda:0")
+    rng = np.random.default_rng(10)
+    codes, scales = (torch.from_numpy(rng.integers(0, n, 4096 // m, dtype=np.uint8)).to(dev) for n, m in ((256, 2), (200, 32)))
+    slots = torch.full((70,), 31, dtype=torch.int32, device=dev)
+    y = torch.empty(70, 2, 64, device=dev)
+    lc.mx_cache_read_tensor(codes, None, "(32,2,64):(128,64,1)", scales, None, "(32,2,2):(4,2,1)", y, None, "(70,2,64):(128,64,1)", slots)
+    want = so.read_slots(codes.cpu().numpy(), "(32,2,64):(128,64,1)", scales.cpu().numpy(), "(32,2,2):(4,2,1)", np.array([31]))[0]
+    assert (y.double().cpu().numpy() == want).all()
+
+
+def test_offsets_past_32_bits():
+    """Slots whose codes lie 2^31 + 16 bytes apart."""
+    dev = torch.device("cuda:0")
+    rng = np.random.default_rng(11)
+    step = (1 << 32) + 32
+    codes_text, scales_text = "(3,1,32):(%d,32,1)" % step, "(3,1,1):(1,1,1)"
+    codes, scales = torch.zeros(step + 16, dtype=torch.uint8, device=dev), torch.zeros(3, dtype=torch.uint8, device=dev)
+    x = torch.from_numpy(rng.standard_normal((3, 1, 32)).astype(np.float32)).to(dev)
+    y = torch.empty_like(x)
+    slots = torch.tensor([2, 0, 1], dtype=torch.int32, device=dev)
+    lc.mx_cache_write_tensor(x, None, "(3,1,32):(32,32,1)", codes, None, codes_text, scales, None, scales_text, slots)
+    lc.mx_cache_read_tensor(codes, None, codes_text, scales, None, scales_text, y, None, "(3,1,32):(32,32,1)", slots)
+    want = mx.dequantize(*mx.quantize(x[:, 0].double().cpu().numpy(), 32, "floor"))
+    assert (y[:, 0].double().cpu().numpy() == want).all()
