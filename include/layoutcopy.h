@@ -503,7 +503,7 @@ lc_status_t lc_mx_cache_read(const void* k_codes, const void* v_codes, const lc_
  * Asynchronous on `hip_stream`, allocates nothing, may be recorded into a HIP graph; o and lse may overlap nothing that is read.  Results do not depend on
  * timing.
  * Errors: INVALID_ARG (ranks, Hq no multiple of Hkv, T no multiple of `sequences` without starts, page, sequences, pages_per_sequence or
- * max_queries < 1, window without causal or < 0, scale not finite, D > 256, N no multiple of page), SIZE_MISMATCH, BLOCK_LAYOUT,
+ * max_queries < 1, window without causal or < 0, scale times log2(e) not finite, D > 256, N no multiple of page), SIZE_MISMATCH, BLOCK_LAYOUT,
  * NEGATIVE_STRIDE (codes, scales), DST_ALIASES (o), UNSUPPORTED_DTYPE, TOO_LARGE (modes of 2^31 or more, more than 4 leaves, tokens of a sequence
  * of 2^31 or more, more than 65535 sequences or heads), MISALIGNED (q, o to their elements, codes to 16 bytes, lse and integers to 4),
  * WORKSPACE_TOO_SMALL, HIP. */

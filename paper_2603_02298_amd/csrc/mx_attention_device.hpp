@@ -81,9 +81,14 @@ __device__ __forceinline__ void mx_row_place(const MxAttentionParams& P, const M
 }
 
 typedef u32x4 __attribute__((aligned(2))) u32x4_at_elements;
-// Eight elements d .. d + 7 of a row of q, zeros from D on (and for no row at all).
+// Eight elements d .. d + 7 of a row of q, zeros from D on (and for no row at all), with their signs turned where the scale is negative: scores times scale_log2,
+// which is above 0, then order as the scores do.
 __device__ __forceinline__ u32x4 mx_query_vector(const MxAttentionParams& P, const unsigned char* row, uint32_t d, bool vectors) {
-  if (row && vectors && d + 8u <= P.D) return *reinterpret_cast<const u32x4_at_elements*>(row + 2u * d);
+  const uint32_t turn = P.turned ? 0x80008000u : 0u;
+  if (row && vectors && d + 8u <= P.D) {
+    u32x4 v = *reinterpret_cast<const u32x4_at_elements*>(row + 2u * d);
+    return u32x4{v[0] ^ turn, v[1] ^ turn, v[2] ^ turn, v[3] ^ turn};
+  }
   uint64_t low = 0u, high = 0u;
   if (row) {
 #pragma unroll 1   // (once a workgroup: the code's size counts)
@@ -93,7 +98,7 @@ __device__ __forceinline__ u32x4 mx_query_vector(const MxAttentionParams& P, con
       else high |= x;
     }
   }
-  return u32x4{(uint32_t)low, (uint32_t)(low >> 32), (uint32_t)high, (uint32_t)(high >> 32)};
+  return u32x4{(uint32_t)low ^ turn, (uint32_t)(low >> 32) ^ turn, (uint32_t)high ^ turn, (uint32_t)(high >> 32) ^ turn};
 }
 
 // two probabilities to 16 bits, rounded to nearest: they lie in 0 .. 1, so that a rounding is off by half a step of the type relative to the probability, as q,
@@ -110,6 +115,8 @@ __device__ __forceinline__ uint32_t mx_pair(float a, float b) {
 // are kept out of the matrix products and added one by one, for the rows that see them, in fp32.
 template <int MATH>
 constexpr uint32_t kMxLoud = MATH == kMxBf16 ? 253u : 141u;
+// A scale's byte as the conversions take it: they read its exponent field as 2^(byte - 127), 0 and 255 (NaN) included (checked for every byte and pair of codes).
+__device__ __forceinline__ float mx_scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
 // codes SEL of a dword (two of them) as q's type holds them
 template <int MATH, int SEL>
 __device__ __forceinline__ void mx_expand_pair(uint32_t codes, float scale, float* a, float* b) {

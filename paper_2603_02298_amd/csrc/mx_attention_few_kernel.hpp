@@ -12,7 +12,7 @@
 
 namespace lc {
 
-// Where the tokens of a tile lie.  RUNS: two runs of 16 tokens evenly apart, whose bases all lanes share; otherwise lane l knows those of token l % 32.
+// Where the tokens of a tile of 32 lie.  RUNS: two runs of 16 tokens evenly apart, whose bases all lanes share; otherwise lane l knows those of token l % 32.
 template <bool RUNS>
 struct MxTokens;
 template <>
@@ -57,8 +57,9 @@ __device__ __forceinline__ float mx_sum_of_row(float m) {
   return mx_float_of(b[0]) + mx_float_of(b[1]);
 }
 
+// (three workgroups a CU where the registers of a tile on its way, of another and of the sums leave that)
 template <int MATH, int NB, int RT, bool RUNS>
-__global__ __launch_bounds__(256) void mx_attention_few_kernel(MxAttentionParams P, MxAttentionTensors t, bool q_vectors, bool o_vectors) {
+__global__ __launch_bounds__(256, NB * RT <= 4 ? 3 : NB * RT <= 8 ? 2 : 1) void mx_attention_few_kernel(MxAttentionParams P, MxAttentionTensors t, bool q_vectors, bool o_vectors) {
   using Tile = MxFewTile<NB>;
   constexpr int WIDTH = 32 * NB, WAVES = 4, TOKENS = 32, CHUNK = 2 * NB;   // elements of a lane's chunk
   touch_kernel_arguments<kMxAttentionKernargs>();
@@ -70,63 +71,71 @@ __global__ __launch_bounds__(256) void mx_attention_few_kernel(MxAttentionParams
   MxAttentionWork w;
   if (!mx_attention_begin(P, t, blockIdx.x, w)) return;
 
-  // ---- where a lane's share of a token lies ----
+  // ---- where a lane's share of a token lies (blocks that a head does not have: its first one's, which meet zeros of q, or rows of O^T that nobody stores) ----
   const uint32_t k_dword = h * NB, v_code = n * CHUNK;                        // its first dword of keys' codes, its first code of values
-  uint32_t k_off[Tile::KS], ks_off[Tile::KS];
-  bool k_in[Tile::KS];
-  static_for<Tile::KS>([&](auto i) {
-    const uint32_t block = k_dword / 4u + (uint32_t)i;
-    k_in[i] = block < P.blocks;
-    const uint32_t at = k_in[i] ? block : 0u;
-    k_off[i] = (uint32_t)mx_mode_eval(P.c_b, at) + (NB == 2 ? 4u * (k_dword & 3u) : 0u);
-    ks_off[i] = (uint32_t)mx_mode_eval(P.s_b, at);
-  });
-  const uint32_t v_block = v_code / kMxBlock;
-  const bool v_in = v_block < P.blocks;
-  const uint32_t v_off = (uint32_t)mx_mode_eval(P.c_b, v_in ? v_block : 0u) + (v_code % kMxBlock) / 2u, vs_off = (uint32_t)mx_mode_eval(P.s_b, v_in ? v_block : 0u);
   const uint32_t c_step = (uint32_t)(P.c_n.n == 1 ? P.c_n.last_stride : P.c_n.stride[0]), s_step = (uint32_t)(P.s_n.n == 1 ? P.s_n.last_stride : P.s_n.stride[0]);
+  uint32_t k_off[Tile::KS], ks_off[Tile::KS], v_off[RUNS ? 4 : 1], vs_off[RUNS ? 4 : 1];   // RUNS: in a run, its first four tokens' and the lane's own
+  static_for<Tile::KS>([&](auto i) {
+    const uint32_t block = k_dword / 4u + (uint32_t)i, at = block < P.blocks ? block : 0u;
+    k_off[i] = (uint32_t)mx_mode_eval(P.c_b, at) + (NB == 2 ? 4u * (k_dword & 3u) : 0u) + (RUNS ? n * c_step : 0u);
+    ks_off[i] = (uint32_t)mx_mode_eval(P.s_b, at) + (RUNS ? n * s_step : 0u);
+  });
+  {
+    const uint32_t block = v_code / kMxBlock, at = block < P.blocks ? block : 0u;
+    v_off[0] = (uint32_t)mx_mode_eval(P.c_b, at) + (v_code % kMxBlock) / 2u + (RUNS ? 4u * h * c_step : 0u);
+    vs_off[0] = (uint32_t)mx_mode_eval(P.s_b, at) + (RUNS ? 4u * h * s_step : 0u);
+    if constexpr (RUNS) {
+      static_for<3>([&](auto i) {
+        v_off[i + 1] = v_off[i] + c_step;
+        vs_off[i + 1] = vs_off[i] + s_step;
+      });
+    }
+  }
   const unsigned char *kc = t.k_codes + mx_mode_eval(P.c_h, w.kv), *ks = t.k_scales + mx_mode_eval(P.s_h, w.kv);
   const unsigned char *vc = t.v_codes + mx_mode_eval(P.c_h, w.kv), *vs = t.v_scales + mx_mode_eval(P.s_h, w.kv);
 
-  // ---- page numbers (RUNS: of the two runs; otherwise of the lane's token): 0xFFFFFFFF past the part ----
-  auto page_of = [&](uint32_t j, uint32_t* place) -> uint32_t {
-    if (j >= w.to) { *place = 0u; return 0xFFFFFFFFu; }
-    const uint64_t at = mx_page_at(P, w.b, j, place);
-    return t.pages ? (uint32_t)t.pages[at] : (uint32_t)at;
+  // ---- where tokens lie: lane l looks up one run of 16 (RUNS), l % 2 of the wavefront's tile l / 2 from `tile` on, 32 tiles at a time, or one
+  // token, l % 32 of a tile ----
+  struct Found {
+    int64_t c, s;
+    uint32_t ok;   // RUNS: a bit for each token of the run
   };
-  struct Pages {
-    uint32_t id[2], place[2];
-  };
-  auto pages_of = [&](uint32_t j) {
-    Pages p;
-    if constexpr (RUNS) {
-      p.id[0] = page_of(j, &p.place[0]);
-      p.id[1] = page_of(j + 16u, &p.place[1]);
-    } else {
-      p.id[0] = page_of(j + (lane & 31u), &p.place[0]);
-      p.id[1] = p.place[1] = 0u;
+  auto find = [&](uint32_t j) {   // j: of the lane
+    Found f;
+    uint32_t place = 0u, id = 0xFFFFFFFFu;
+    if (j < w.to) {
+      const uint64_t at = mx_page_at(P, w.b, j, &place);
+      id = t.pages ? (uint32_t)t.pages[at] : (uint32_t)at;
     }
-    return p;
+    const bool in = id < P.pool_pages;   // (the rest of a run that is begun lies in the pool too)
+    const uint32_t slot = in ? id * P.page + place : 0u, left = w.to - j;
+    f.c = mx_mode_eval(P.c_n, slot);
+    f.s = mx_mode_eval(P.s_n, slot);
+    f.ok = !in ? 0u : !RUNS || left >= 16u ? 0xFFFFu : (1u << left) - 1u;
+    return f;
   };
-  auto tokens_of = [&](uint32_t j, const Pages& p) {
+  auto of_lane = [&](uint32_t v, uint32_t from) { return (uint32_t)__builtin_amdgcn_readlane((int)v, (int)from); };
+  auto of_lane_64 = [&](int64_t v, uint32_t from) {
+    return (int64_t)((uint64_t)of_lane((uint32_t)((uint64_t)v >> 32), from) << 32 | of_lane((uint32_t)(uint64_t)v, from));
+  };
+  auto tokens_of = [&](uint32_t tile, const Found& f) {
     MxTokens<RUNS> k;
     if constexpr (RUNS) {
-      k.ok = 0u;
+      const uint32_t at = 2u * (tile % 32u);
       static_for<2>([&](auto g) {
-        const bool in = p.id[(int)g] < P.pool_pages;   // (the rest of a run that is begun lies in the pool too)
-        const uint32_t slot = in ? p.id[(int)g] * P.page + p.place[(int)g] : 0u, left = w.to - j - 16u * (uint32_t)g;
-        k.c[(int)g] = mx_mode_eval(P.c_n, slot);
-        k.s[(int)g] = mx_mode_eval(P.s_n, slot);
-        if (in) k.ok |= (left >= 16u ? 0xFFFFu : (1u << left) - 1u) << (16 * (int)g);
+        k.c[(int)g] = of_lane_64(f.c, at + (uint32_t)g);
+        k.s[(int)g] = of_lane_64(f.s, at + (uint32_t)g);
       });
+      k.ok = of_lane(f.ok, at) | of_lane(f.ok, at + 1u) << 16;
     } else {
-      const bool in = p.id[0] < P.pool_pages;
-      const uint32_t slot = in ? p.id[0] * P.page + p.place[0] : 0u;
-      k.c = mx_mode_eval(P.c_n, slot);
-      k.s = mx_mode_eval(P.s_n, slot);
-      k.ok = (uint32_t)__ballot(in);   // (lanes 32 and more repeat the first)
+      k.c = f.c;
+      k.s = f.s;
+      k.ok = (uint32_t)__ballot(f.ok != 0u);   // (lanes 32 and more repeat the first)
     }
     return k;
+  };
+  auto first_of_lane = [&](uint32_t tile) {   // the token that a lane looks up from this tile on
+    return w.from + TOKENS * (wave + WAVES * (RUNS ? tile + lane / 2u : tile)) + (RUNS ? 16u * (lane & 1u) : lane & 31u);
   };
   auto load = [&](const MxTokens<RUNS>& k, Tile& tile) {
     auto keys = [&](auto g, const unsigned char* c, const unsigned char* s) {
@@ -144,22 +153,20 @@ __global__ __launch_bounds__(256) void mx_attention_few_kernel(MxAttentionParams
       static_for<Tile::KS>([&](auto i) { tile.ks[(int)g][(int)i] = s[ks_off[i]]; });
     };
     auto values = [&](auto e, const unsigned char* c, const unsigned char* s) {
-      if constexpr (NB == 2) tile.v[(int)e][0] = *reinterpret_cast<const uint16_t*>(c + v_off);
-      else if constexpr (NB == 4) tile.v[(int)e][0] = *reinterpret_cast<const uint32_t*>(c + v_off);
+      constexpr int AT = RUNS ? (int)decltype(e)::value % 4 : 0;
+      if constexpr (NB == 2) tile.v[(int)e][0] = *reinterpret_cast<const uint16_t*>(c + v_off[AT]);
+      else if constexpr (NB == 4) tile.v[(int)e][0] = *reinterpret_cast<const uint32_t*>(c + v_off[AT]);
       else {
         typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-        const u32x2 x = *reinterpret_cast<const u32x2*>(c + v_off);
+        const u32x2 x = *reinterpret_cast<const u32x2*>(c + v_off[AT]);
         tile.v[(int)e][0] = x[0];
         tile.v[(int)e][1] = x[1];
       }
-      tile.vs[(int)e] = s[vs_off];
+      tile.vs[(int)e] = s[vs_off[AT]];
     };
     if constexpr (RUNS) {
-      static_for<2>([&](auto g) { keys(g, kc + k.c[(int)g] + n * c_step, ks + k.s[(int)g] + n * s_step); });
-      static_for<8>([&](auto e) {
-        constexpr int g = (int)decltype(e)::value / 4, in = (int)decltype(e)::value % 4;
-        values(e, vc + k.c[g] + (4u * h + in) * c_step, vs + k.s[g] + (4u * h + in) * s_step);
-      });
+      static_for<2>([&](auto g) { keys(g, kc + k.c[(int)g], ks + k.s[(int)g]); });
+      static_for<8>([&](auto e) { values(e, vc + k.c[(int)e / 4], vs + k.s[(int)e / 4]); });
     } else {
       static_for<2>([&](auto g) {
         const uint32_t from = 16u * (uint32_t)g + n;
@@ -173,11 +180,12 @@ __global__ __launch_bounds__(256) void mx_attention_few_kernel(MxAttentionParams
   };
 
   // the first tile's way begins before the queries'
-  uint32_t j = w.from + TOKENS * wave;
-  Tile cur, next;
-  MxTokens<RUNS> at = tokens_of(j, pages_of(j));
-  Pages ahead = pages_of(j + TOKENS * WAVES);
-  if (j < w.to) load(at, cur);
+  uint32_t j = w.from + TOKENS * wave, tile = 0u;
+  Tile one, two;
+  Found found = find(first_of_lane(0u));
+  MxTokens<RUNS> at = tokens_of(0u, found);
+  if (!RUNS) found = find(first_of_lane(1u));
+  if (j < w.to) load(at, one);
 
   u32x4 q[RT][NB];
   uint32_t row_lo[RT], row_hi[RT];
@@ -198,12 +206,14 @@ __global__ __launch_bounds__(256) void mx_attention_few_kernel(MxAttentionParams
     static_for<CHUNK>([&](auto c) { acc[r][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f}; });
   });
 
-  for (; j < w.to; j += TOKENS * WAVES) {
+  // works on the tile `now` (tokens j ..) while the next one comes
+  auto step = [&](Tile& now, Tile& next) {
     const uint32_t ok = at.ok;
-    const uint32_t follows = j + TOKENS * WAVES;
-    at = tokens_of(follows, ahead);
-    ahead = pages_of(follows + TOKENS * WAVES);
-    if (follows < w.to) load(at, next);
+    ++tile;
+    if (RUNS && tile % 32u == 0u) found = find(first_of_lane(tile));
+    at = tokens_of(tile, found);
+    if (!RUNS) found = find(first_of_lane(tile + 1u));
+    if (j + TOKENS * WAVES < w.to) load(at, next);
     __builtin_amdgcn_sched_barrier(0);
 
     // ---- scores ----
@@ -212,21 +222,20 @@ __global__ __launch_bounds__(256) void mx_attention_few_kernel(MxAttentionParams
       static_for<RT>([&](auto r) { s[r][g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f}; });
       static_for<NB>([&](auto k) {
         constexpr int ks_at = Tile::KS == 2 ? (int)decltype(k)::value / 4 : 0;
-        const bool in = k_in[ks_at];
-        const u32x4 a = mx_expand<MATH>(in ? cur.k[g][k] : 0u, mx_scale_value(in ? cur.ks[g][ks_at] : 127u));
+        const u32x4 a = mx_expand<MATH>(now.k[g][k], mx_scale_of(now.ks[g][ks_at]));
         static_for<RT>([&](auto r) { s[r][g] = mfma_16x16x32<MATH>(a, q[r][k], s[r][g]); });
       });
     });
     float x[RT][8];   // of the lane's row at token 16 (e / 4) + 4 h + e % 4
-    static_for<RT>([&](auto r) { static_for<8>([&](auto e) { x[r][e] = s[r][e / 4][(int)e % 4] * P.scale_log2; }); });
+    static_for<RT>([&](auto r) { static_for<8>([&](auto e) { x[r][e] = s[r][e / 4][(int)e % 4]; }); });
     const bool whole = j >= w.all_lo && j + TOKENS <= w.all_hi && ok == 0xFFFFFFFFu;
     if (!whole) {   // what nobody sees does not enter: its score goes, and so do its values, whatever they are
       static_for<8>([&](auto e) {
         const uint32_t in = 16u * ((uint32_t)e / 4u) + 4u * h + (uint32_t)e % 4u;
         const bool seen = (ok >> in & 1u) && j + in >= w.lo;
         if (!seen) {
-          static_for<Tile::VD>([&](auto d) { cur.v[(int)e][(int)d] = 0u; });
-          cur.vs[(int)e] = 127u;
+          static_for<Tile::VD>([&](auto d) { now.v[(int)e][(int)d] = 0u; });
+          now.vs[(int)e] = 127u;
         }
         static_for<RT>([&](auto r) {
           const bool mine = seen && j + in >= row_lo[r] && j + in < row_hi[r];
@@ -242,14 +251,14 @@ __global__ __launch_bounds__(256) void mx_attention_few_kernel(MxAttentionParams
     static_for<RT>([&](auto r) {
       float m = kMinusInfinity;
       static_for<8>([&](auto e) { m = fmaxf(m, x[r][e]); });
-      m = fmaxf(top[r], mx_max_of_row(m));
+      m = fmaxf(top[r], mx_max_of_row(m) * P.scale_log2);
       const float from = m == kMinusInfinity ? 0.0f : m;   // (nothing seen so far)
       shrink[r] = __builtin_amdgcn_exp2f(top[r] - from);
       moved = moved || m != top[r];
       top[r] = m;
       float sum = 0.0f;
       static_for<8>([&](auto e) {
-        x[r][e] = __builtin_amdgcn_exp2f(x[r][e] - from);
+        x[r][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r][e], P.scale_log2, -from));
         sum += x[r][e];
       });
       total[r] = total[r] * shrink[r] + sum;
@@ -261,27 +270,21 @@ __global__ __launch_bounds__(256) void mx_attention_few_kernel(MxAttentionParams
 
     // ---- values ----
     uint32_t largest = 0u;
-    static_for<8>([&](auto e) { largest = largest > cur.vs[(int)e] ? largest : cur.vs[(int)e]; });
-    if (__ballot(v_in && largest >= kMxLoud<MATH>)) {   // (blocks that may hold infinities or NaN: rare)
-      uint32_t tokens = 0u;
-      static_for<8>([&](auto e) {
-        const uint64_t lanes = __ballot(v_in && cur.vs[(int)e] >= kMxLoud<MATH>);
-        static_for<4>([&](auto g) {
-          if (lanes >> (16 * (int)g) & 0xFFFFu) tokens |= 1u << (16 * ((int)e / 4) + 4 * (int)g + (int)e % 4);
-        });
-      });
+    static_for<8>([&](auto e) { largest = largest > now.vs[(int)e] ? largest : now.vs[(int)e]; });
+    if (__ballot(largest >= kMxLoud<MATH>)) {   // (blocks that may hold infinities or NaN: rare)
 #pragma unroll 1
-      for (; tokens; tokens &= tokens - 1u) {
-        const uint32_t in = (uint32_t)__builtin_ctz(tokens), holds = in >> 2 & 3u, e_in = (in >> 4) * 4u + (in & 3u);   // the group of lanes and their place of it
+      for (uint32_t in = 0; in < TOKENS; ++in) {
+        const uint32_t holds = in >> 2 & 3u, e_in = (in >> 4) * 4u + (in & 3u);   // the group of lanes that have the token, and its place there
         uint32_t codes[Tile::VD] = {}, byte = 127u;
         float mine[RT] = {};
         static_for<8>([&](auto e) {
           if ((uint32_t)e == e_in) {
-            static_for<Tile::VD>([&](auto d) { codes[d] = cur.v[(int)e][(int)d]; });
-            byte = v_in ? cur.vs[(int)e] : 127u;
+            static_for<Tile::VD>([&](auto d) { codes[d] = now.v[(int)e][(int)d]; });
+            byte = now.vs[(int)e];
             static_for<RT>([&](auto r) { mine[r] = x[r][e]; });
           }
         });
+        if (!__ballot(h == holds && byte >= kMxLoud<MATH>)) continue;
         float probability[RT];
         bool seen[RT];
         static_for<RT>([&](auto r) {
@@ -293,7 +296,7 @@ __global__ __launch_bounds__(256) void mx_attention_few_kernel(MxAttentionParams
           uint32_t c[Tile::VD];
           static_for<Tile::VD>([&](auto d) { c[d] = mx_from_lane(codes[d], from); });
           const uint32_t its_byte = mx_from_lane(byte, from);
-          const float its_scale = mx_scale_value(its_byte);
+          const float its_scale = mx_scale_of(its_byte);
           static_for<NB>([&](auto k) {
             float v[2];
             mx_expand_pair<MATH, (int)decltype(k)::value % 4>(c[(int)k / 4], its_scale, &v[0], &v[1]);
@@ -307,19 +310,19 @@ __global__ __launch_bounds__(256) void mx_attention_few_kernel(MxAttentionParams
         });
       }
       static_for<8>([&](auto e) {
-        if (cur.vs[(int)e] >= kMxLoud<MATH>) {
-          static_for<Tile::VD>([&](auto d) { cur.v[(int)e][(int)d] = 0u; });
-          cur.vs[(int)e] = 127u;
+        if (now.vs[(int)e] >= kMxLoud<MATH>) {
+          static_for<Tile::VD>([&](auto d) { now.v[(int)e][(int)d] = 0u; });
+          now.vs[(int)e] = 127u;
         }
       });
     }
     float scale[8];
-    static_for<8>([&](auto e) { scale[e] = mx_scale_value(v_in ? cur.vs[(int)e] : 127u); });
+    static_for<8>([&](auto e) { scale[e] = mx_scale_of(now.vs[(int)e]); });
     static_for<NB>([&](auto byte) {
       constexpr int D = (int)decltype(byte)::value / 4, SEL = (int)decltype(byte)::value % 4;
       uint32_t pairs[8];
       static_for<8>([&](auto e) {
-        const uint32_t codes = v_in ? cur.v[(int)e][D] : 0u;
+        const uint32_t codes = now.v[(int)e][D];
         if constexpr (MATH == kMxBf16) pairs[e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale[e], SEL));
         else pairs[e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale[e], SEL));
       });
@@ -331,7 +334,12 @@ __global__ __launch_bounds__(256) void mx_attention_few_kernel(MxAttentionParams
         static_for<RT>([&](auto r) { acc[r][C] = mfma_16x16x32<MATH>(a, p[r], acc[r][C]); });
       });
     });
-    cur = next;
+    j += TOKENS * WAVES;
+  };
+  while (j < w.to) {
+    step(one, two);
+    if (j >= w.to) break;
+    step(two, one);
   }
 
   // ---- the wavefronts' sums: 2 and 3 hand theirs to 0 and 1, then 1 to 0 (or one after the other to 0, where LDS has room for one's only) ----

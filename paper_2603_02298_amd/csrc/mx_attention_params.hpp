@@ -20,7 +20,8 @@ struct MxAttentionParams {
   uint32_t part_tokens, parts;           // tokens of a part (a multiple of kMxAttentionTokens), parts at most
   uint32_t window;                       // 0: none
   FastDiv page_div, group_div, parts_div, rows_div, kv_div;   // rows_div: of row_tiles
-  float scale_log2;                      // scores are exponents of two: scale * log2(e)
+  float scale_log2;                      // scores are exponents of two: |scale| * log2(e), above 0
+  int32_t turned;                        // the scale is negative
   int32_t causal, o_type;
   uint32_t queries_each;                 // of a sequence, where a call names no starts
   int32_t by_xcd;

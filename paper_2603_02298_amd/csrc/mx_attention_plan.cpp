@@ -2,6 +2,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <limits>
 #include <vector>
 
 #include "plan.hpp"
@@ -31,7 +32,7 @@ lc_status_t make_mx_attention_plan(const Layout& q, const Layout& codes, const L
   const int64_t T = q.mode(0).size(), H = q.mode(1).size(), D = q.mode(2).size(), most = int64_t(1) << 31;
   if (D > pool.padded) return LC_ERR_SIZE_MISMATCH;
   if (D > 256 || H % pool.heads) return LC_ERR_INVALID_ARG;
-  if (sequences < 1 || page < 1 || pages_each < 1 || max_queries < 1 || window < 0 || (window && !causal) || !std::isfinite(scale)) return LC_ERR_INVALID_ARG;
+  if (sequences < 1 || page < 1 || pages_each < 1 || max_queries < 1 || window < 0 || (window && !causal) || !std::isfinite(scale * 1.44269504088896341f)) return LC_ERR_INVALID_ARG;
   if (pool.slots % page) return LC_ERR_INVALID_ARG;
   if (T >= most || H > 65535 || sequences > 65535 || pages_each >= most / page || page >= most) return LC_ERR_TOO_LARGE;
   if (!modes_write_once(o.leaves)) return LC_ERR_DST_ALIASES;
@@ -76,7 +77,9 @@ lc_status_t make_mx_attention_plan(const Layout& q, const Layout& codes, const L
   P.max_queries = (uint32_t)std::min(max_queries, T);
   P.max_tokens = P.page * P.pages_each;
   P.window = (uint32_t)std::min(window, most - 1);
-  P.scale_log2 = scale * 1.44269504088896341f;
+  // (a scale of 0, and one too small for fp32's normal numbers, becomes the smallest of those: infinities and what is not seen stay what they are)
+  P.scale_log2 = std::fmax(std::fabs(scale) * 1.44269504088896341f, std::numeric_limits<float>::min());
+  P.turned = scale < 0.0f;
   P.causal = causal != 0;
   P.queries_each = (uint32_t)(T / sequences);
   P.o_type = o_dtype;

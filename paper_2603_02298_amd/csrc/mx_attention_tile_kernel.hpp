@@ -91,7 +91,7 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : 2) void mx_attention_tile_k
         // tokens that nobody sees, and blocks that are not there: zeros
         const bool in = block_in && raw.in[i] && j + token >= w.lo, loud = is_value && in && raw.byte[i][k] >= kMxLoud<MATH>;
         const u32x4 c = select_or_zero(in && !loud, raw.codes[i][k]);
-        const float scale = mx_scale_value(in && !loud ? raw.byte[i][k] : 127u);
+        const float scale = mx_scale_of(in && !loud ? raw.byte[i][k] : 127u);
         if (loud) s_loud[TOKENS * stage + token] = j;
         static_for<4>([&](auto e) {
           const uint32_t at = is_value ? K_BYTES + gemm_rdirect_lds_offset(WIDTH, token, 32u * block + 8u * (uint32_t)e)
@@ -157,7 +157,6 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : 2) void mx_attention_tile_k
           const u32x4 a = direct_fragment<TOKENS, kLoadKDirect>(keys + ((int)k / 4) * (TOKENS * 128), lane, 32u * (uint32_t)g, (int)k % 4);
           s[g] = mfma_32x32x16<MATH == kMxBf16>(a, q[k], s[g]);
         });
-        s[g] *= P.scale_log2;   // (of either sign, or 0: before what is not seen becomes minus infinity)
       });
       const bool whole = j >= all_lo && j + TOKENS <= all_hi && ok == ~uint64_t(0);
       if (!whole) {
@@ -174,7 +173,7 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : 2) void mx_attention_tile_k
       static_for<2>([&](auto g) {
         static_for<16>([&](auto e) { m = fmaxf(m, s[g][(int)e]); });
       });
-      m = fmaxf(top, mx_max_of_halves(m));
+      m = fmaxf(top, mx_max_of_halves(m) * P.scale_log2);
       const float from = m == kMinusInfinity ? 0.0f : m;
       const float shrink = __builtin_amdgcn_exp2f(top - from);
       if (__ballot(m != top)) static_for<NB>([&](auto d) { acc[d] *= shrink; });
@@ -183,7 +182,7 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : 2) void mx_attention_tile_k
       u32x4 p[4];
       static_for<2>([&](auto g) {
         static_for<16>([&](auto e) {
-          s[g][(int)e] = __builtin_amdgcn_exp2f(s[g][(int)e] - from);
+          s[g][(int)e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g][(int)e], P.scale_log2, -from));
           sum += s[g][(int)e];
         });
         static_for<8>([&](auto d) { p[2 * g + d / 4][(int)d % 4] = mx_pair<MATH>(s[g][2 * d], s[g][2 * d + 1]); });
@@ -216,7 +215,7 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : 2) void mx_attention_tile_k
           const uint32_t byte = b[mx_mode_eval(P.s_b, at)];
           if ((uint32_t)d < P.blocks && byte >= kMxLoud<MATH>) {
             const u32x4 codes = *reinterpret_cast<const u32x4*>(c + mx_mode_eval(P.c_b, at));
-            const float scale = mx_scale_value(byte);
+            const float scale = mx_scale_of(byte);
             static_for<4>([&](auto i) {   // elements 8 i + 4 h .. + 3 of the block
               const uint32_t four = codes[(int)i] >> (16u * h);
               float v[4];
