@@ -40,7 +40,7 @@ _ATTENTION = _ATTENTION_DEVICE + ["mx_attention_plan.cpp", "rope_cache_capi.cpp"
 _ROPE = ["rope_plan.cpp", "rope_kernels.hip", "rope_cache_capi.cpp"]
 _CACHE = _ATTENTION + ["mx_cache_plan.cpp", "mx_cache_kernels.hip"]
 _MX = _MX_GEMM + ["mx_plan.cpp", "mx_kernels.hip"] + _CACHE + _ROPE
-KERNEL_HEADERS = {"lds_limit.hpp": _TILE + _SPLIT + _STREAM + _GATHER + _WIDE + _MX_DIRECT + _MX_STREAM + _MX_RING + _MX_WIDE + _ATTENTION_TILE + ["kernels.hip", "capi.cpp"],
+KERNEL_HEADERS = {"lds_limit.hpp": _TILE + _SPLIT + _STREAM + _GATHER + _WIDE + _MX_DIRECT + _MX_STREAM + _MX_RING + _MX_WIDE + _ATTENTION_TILE + _ATTENTION_FEW + ["kernels.hip", "capi.cpp"],
                   "rope_params.hpp": _ROPE, "rope_plan.hpp": _ROPE, "mx_cache_params.hpp": _CACHE, "mx_cache_plan.hpp": _CACHE,
                   "mx_attention_params.hpp": _ATTENTION, "mx_attention_plan.hpp": _ATTENTION, "mx_attention_device.hpp": _ATTENTION_DEVICE,
                   "mx_attention_few_kernel.hpp": _ATTENTION_FEW, "mx_attention_tile_kernel.hpp": _ATTENTION_TILE,

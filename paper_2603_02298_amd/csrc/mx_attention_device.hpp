@@ -18,7 +18,8 @@ struct MxAttentionTensors {
   const unsigned char *q, *k_codes, *k_scales, *v_codes, *v_scales;
   const int32_t *pages, *lengths, *starts;
   unsigned char* o;
-  float *lse, *parts;
+  float *lse, *parts;   // parts: unfinished rows
+  uint32_t* bases;      // few rows: the sequences' first units, and the total (NULL: nothing is joined)
 };
 constexpr int kMxAttentionKernargs = 1024;   // (as many bytes of the arguments as are brought in at once)
 
@@ -46,6 +47,15 @@ struct MxAttentionWork {
   uint32_t parts;            // that there are (0: no tokens)
   uint32_t from, to;         // tokens of this one
 };
+// rows r0 .. r1 - 1 of a sequence: what any and every one of them sees
+__device__ __forceinline__ void mx_attention_rows(const MxAttentionParams& P, MxAttentionWork& w, uint32_t r0, uint32_t r1) {
+  uint32_t unused;
+  w.r0 = r0;
+  w.r1 = r1;
+  mx_rows_seen(P, w.s, r0, r1, &w.lo, &w.hi);
+  mx_seen(P, w.s, fd_div(r0, P.group_div), &unused, &w.all_hi);
+  mx_seen(P, w.s, fd_div(r1 - 1u, P.group_div), &w.all_lo, &unused);
+}
 __device__ __forceinline__ MxSequence mx_sequence_of(const MxAttentionParams& P, const MxAttentionTensors& t, uint32_t b) {
   const int32_t each = (int32_t)P.queries_each;
   return mx_sequence(P, t.lengths[b], t.starts ? t.starts[b] : (int32_t)b * each, t.starts ? t.starts[b + 1u] : ((int32_t)b + 1) * each);
@@ -54,17 +64,12 @@ __device__ __forceinline__ MxSequence mx_sequence_of(const MxAttentionParams& P,
 __device__ __forceinline__ bool mx_attention_begin(const MxAttentionParams& P, const MxAttentionTensors& t, uint32_t group, MxAttentionWork& w) {
   if (!mx_attention_work(P, group, &w.b, &w.kv, &w.row_tile, &w.part)) return false;
   w.s = mx_sequence_of(P, t, w.b);
-  const uint32_t rows = w.s.queries * P.group;
-  w.r0 = w.row_tile * P.tile_rows;
-  if (w.r0 >= rows) return false;
-  w.r1 = rows - w.r0 < P.tile_rows ? rows : w.r0 + P.tile_rows;
-  mx_rows_seen(P, w.s, w.r0, w.r1, &w.lo, &w.hi);
+  const uint32_t rows = w.s.queries * P.group, r0 = w.row_tile * P.tile_rows;
+  if (r0 >= rows) return false;
+  mx_attention_rows(P, w, r0, rows - r0 < P.tile_rows ? rows : r0 + P.tile_rows);
   w.parts = mx_parts(P, w.lo, w.hi);
   if (w.part && w.part >= w.parts) return false;
   mx_part(P, w.lo, w.hi, w.part, &w.from, &w.to);
-  uint32_t unused;
-  mx_seen(P, w.s, fd_div(w.r0, P.group_div), &unused, &w.all_hi);
-  mx_seen(P, w.s, fd_div(w.r1 - 1u, P.group_div), &w.all_lo, &unused);
   return true;
 }
 // the tokens that row r sees, none where it is not the workgroup's
@@ -132,8 +137,8 @@ __device__ __forceinline__ void mx_expand_pair(uint32_t codes, float scale, floa
 }
 
 // ---- rows on their way out ----
-// N sums (elements d .. d + N - 1 of a row, rounded once) to o
-template <int N>
+// N sums (elements d .. d + N - 1 of a row, rounded once) to o.  ELEMENTS: they need not be neighbours, and D may lie among them.
+template <int N, bool ELEMENTS = true>
 __device__ __forceinline__ void mx_store_o(const MxAttentionParams& P, unsigned char* row, uint32_t d, const float (&v)[N], bool vectors) {
   uint32_t bits[N];
   static_for<N>([&](auto e) {
@@ -142,7 +147,8 @@ __device__ __forceinline__ void mx_store_o(const MxAttentionParams& P, unsigned 
                                     : (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)v[e]);
   });
   const bool wide = P.o_type == LC_F32;
-  if (vectors && d + N <= P.D) {
+  if (!ELEMENTS && d >= P.D) return;
+  if (!ELEMENTS || (vectors && d + N <= P.D)) {
     typedef uint32_t words __attribute__((ext_vector_type(N)));
     typedef words __attribute__((aligned(4))) words_at_elements;
     if (wide) {
@@ -160,6 +166,7 @@ __device__ __forceinline__ void mx_store_o(const MxAttentionParams& P, unsigned 
     }
     return;
   }
+  if constexpr (!ELEMENTS) return;
 #pragma unroll 1
   for (uint32_t k = 0; k < (uint32_t)N && d + k < P.D; ++k) {
     uint32_t x = bits[0];

@@ -1,37 +1,55 @@
-// Attention of few rows (decoding, drafted tokens) over a microscaled 4-bit cache: a row tile of 16 or 32 rows and a part of their tokens per workgroup; its four
-// wavefronts take tiles of 32 tokens in turns, straight from memory into registers, and join their sums through LDS at the end.
+// Attention of few rows (decoding, drafted tokens) over a microscaled 4-bit cache: all rows (16 or 32 at most) of a sequence and key head and a part of their tokens
+// at a time.  A wavefront works alone: it has an equal share of all tiles of 32 tokens of the call (mx_share) and goes over the end of one sequence's
+// tokens, whole ones, and the beginning of another's, without a barrier; what several share is joined by a second launch.  (Workgroups that went over tokens together
+// and joined their sums through LDS at the end of each part stood still there and at the beginning of the next: 64 sequences of 512 to 8192 tokens took
+// half as long again.)
 //
-// Keys: lane l holds a quarter of token l % 16's elements, which is one run of its codes; a dword of codes is the eight elements of one k step (the order of
-// the elements inside q . k is free as long as q's registers share it).  Values: lane l holds the same few elements (chunk l % 16) of eight tokens, those
+// Codes and scales go from memory straight into LDS, a ring of two tiles per wavefront, so that as many bytes are on their way as the memory's latency
+// asks for without a register held for them.
+// Keys: lane l reads a quarter of token l % 16's elements, which is one run of its codes; a dword of codes is the eight elements of one k step (the order of
+// the elements inside q . k is free as long as q's registers share it).  Values: lane l reads the same few elements (chunk l % 16) of eight tokens, those
 // whose probabilities it has; expanded, its 8 tokens x 2 elements change places by byte permutes into the operand that wants eight tokens of
-// an element.  Nothing of the cache goes through LDS.
-// The next tile's codes and scales are on their way while a tile is worked on, and the page numbers of the one after it.
+// an element.
 // Bound by the cache's bytes, (D / 2 + D / 32) of a token and head, twice.
 #pragma once
+#include "lds_limit.hpp"
 #include "mx_attention_device.hpp"
 
 namespace lc {
 
-// Where the tokens of a tile of 32 lie.  RUNS: two runs of 16 tokens evenly apart, whose bases all lanes share; otherwise lane l knows those of token l % 32.
-template <bool RUNS>
-struct MxTokens;
-template <>
-struct MxTokens<true> {
-  int64_t c[2], s[2];   // bytes of the runs' first tokens
-  uint32_t ok;          // bit t: token t of the tile lies in the part and on a page of the pool
-};
-template <>
-struct MxTokens<false> {
-  int64_t c, s;
-  uint32_t ok;
-};
-
+// A tile of 32 tokens in LDS: keys' and values' codes and scales, two runs of 16 tokens of each.
 template <int NB>   // blocks of the kernel's width
+struct MxFewSlot {
+  static constexpr uint32_t CODES = 16u * NB * 16u, SCALES = 16u * NB * 4u;   // bytes of a run: blocks of 16 bytes, a dword for every scale
+  static constexpr uint32_t BYTES = 4u * (CODES + SCALES);
+  static constexpr int LOADS = NB == 8 ? 2 : 1;                               // instructions of 64 lanes for a run's blocks, or scales
+  static constexpr int DEPTH = 2;                               // tiles of a ring: 80 KiB a workgroup (width 64: 40)
+  static constexpr uint32_t WAVE = DEPTH * BYTES;
+  // A token is a row of NB units of 16 bytes, which neighbouring lanes load: memory is asked for whole stretches of a token.  (Lanes that load one unit of 16 tokens
+  // each would keep the vector memory path four times as long: it looks a line up for every 16 of them.)
+  // Keys: 16 lanes read one unit of 16 tokens, so units are folded by rows that share LDS's banks: unit q of row t lies at q ^ fold(t).
+  // Values: lanes of four groups h read tokens 4 h + e at once, whose rows are put into different quarters of the banks.
+  __device__ __forceinline__ static uint32_t key_fold(uint32_t token) { return NB == 8 ? token >> 1 & 7u : NB == 4 ? token >> 2 : token >> 3; }
+  __device__ __forceinline__ static uint32_t value_row(uint32_t token) { return (token & ~3u) + ((token + (token >> 2)) & 3u); }
+  __device__ __forceinline__ static uint32_t token_of_row(uint32_t row) { return (row & ~3u) + ((row - (row >> 2)) & 3u); }
+};
+// What a lane holds of a tile that is worked on.
+template <int NB>
 struct MxFewTile {
   static constexpr int KS = NB == 8 ? 2 : 1, VD = NB == 8 ? 2 : 1;   // scales of a lane's keys, dwords of its values' chunk
   uint32_t k[2][NB], ks[2][KS];
   uint32_t v[8][VD], vs[8];
 };
+
+typedef __attribute__((address_space(3))) void mx_lds_void;
+typedef __attribute__((address_space(1))) const void mx_global_void;
+// Dynamic LDS under a second name: the compiler sees no alias between what lands there and what is read, and adds no waits of its own; the kernel states them.
+template <int BYTES>
+__device__ __forceinline__ void mx_load_to_lds(const unsigned char* from, uint32_t at) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char mx_landing[];
+  if constexpr (BYTES == 16) __builtin_amdgcn_global_load_lds((mx_global_void*)from, (mx_lds_void*)(mx_landing + at), 16, 0, 0);
+  else __builtin_amdgcn_global_load_lds((mx_global_void*)from, (mx_lds_void*)(mx_landing + at), 1, 0, 0);   // (a dword, the byte in its low part)
+}
 
 // one dword of lane `from`
 __device__ __forceinline__ uint32_t mx_from_lane(uint32_t v, uint32_t from) { return (uint32_t)__builtin_amdgcn_ds_bpermute((int)(from * 4u), (int)v); }
@@ -57,48 +75,108 @@ __device__ __forceinline__ float mx_sum_of_row(float m) {
   return mx_float_of(b[0]) + mx_float_of(b[1]);
 }
 
-// (three workgroups a CU where the registers of a tile on its way, of another and of the sums leave that)
-template <int MATH, int NB, int RT, bool RUNS>
-__global__ __launch_bounds__(256, NB * RT <= 4 ? 3 : NB * RT <= 8 ? 2 : 1) void mx_attention_few_kernel(MxAttentionParams P, MxAttentionTensors t, bool q_vectors, bool o_vectors) {
+// LINEAR: everything lies as MxLinear says (lc_mx_attention_plan::linear); what a wavefront does once is short then, and short in instructions, which come from
+// memory as well: at one tile a wavefront they are most of the time.
+template <int MATH, int NB, int RT, bool LINEAR>
+__global__ __launch_bounds__(256, NB * RT == 16 ? 1 : NB * RT <= 4 ? 3 : 2) void mx_attention_few_kernel(MxAttentionParams P, MxAttentionTensors t, bool q_vectors, bool o_vectors) {
+  using Slot = MxFewSlot<NB>;
   using Tile = MxFewTile<NB>;
   constexpr int WIDTH = 32 * NB, WAVES = 4, TOKENS = 32, CHUNK = 2 * NB;   // elements of a lane's chunk
-  touch_kernel_arguments<kMxAttentionKernargs>();
-  constexpr int SLOTS = RT * CHUNK > 16 ? 1 : 2;
-  __shared__ f32x4 s_sums[SLOTS][RT * CHUNK][64];
-  __shared__ float s_top[WAVES][RT * 16], s_total[WAVES][RT * 16];
+  constexpr int LOADS = Slot::LOADS, IN_FLIGHT = 8 * LOADS;                // a tile's load instructions
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   const uint32_t lane = threadIdx.x & 63u, n = lane & 15u, h = lane >> 4;
   const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  MxAttentionWork w;
-  if (!mx_attention_begin(P, t, blockIdx.x, w)) return;
+  auto of_lane = [&](uint32_t v, uint32_t from) { return (uint32_t)__builtin_amdgcn_readlane((int)v, (int)from); };
+  auto of_lane_64 = [&](int64_t v, uint32_t from) {
+    return (int64_t)((uint64_t)of_lane((uint32_t)((uint64_t)v >> 32), from) << 32 | of_lane((uint32_t)(uint64_t)v, from));
+  };
 
-  // ---- where a lane's share of a token lies (blocks that a head does not have: its first one's, which meet zeros of q, or rows of O^T that nobody stores) ----
-  const uint32_t k_dword = h * NB, v_code = n * CHUNK;                        // its first dword of keys' codes, its first code of values
-  const uint32_t c_step = (uint32_t)(P.c_n.n == 1 ? P.c_n.last_stride : P.c_n.stride[0]), s_step = (uint32_t)(P.s_n.n == 1 ? P.s_n.last_stride : P.s_n.stride[0]);
-  uint32_t k_off[Tile::KS], ks_off[Tile::KS], v_off[RUNS ? 4 : 1], vs_off[RUNS ? 4 : 1];   // RUNS: in a run, its first four tokens' and the lane's own
-  static_for<Tile::KS>([&](auto i) {
-    const uint32_t block = k_dword / 4u + (uint32_t)i, at = block < P.blocks ? block : 0u;
-    k_off[i] = (uint32_t)mx_mode_eval(P.c_b, at) + (NB == 2 ? 4u * (k_dword & 3u) : 0u) + (RUNS ? n * c_step : 0u);
-    ks_off[i] = (uint32_t)mx_mode_eval(P.s_b, at) + (RUNS ? n * s_step : 0u);
-  });
-  {
-    const uint32_t block = v_code / kMxBlock, at = block < P.blocks ? block : 0u;
-    v_off[0] = (uint32_t)mx_mode_eval(P.c_b, at) + (v_code % kMxBlock) / 2u + (RUNS ? 4u * h * c_step : 0u);
-    vs_off[0] = (uint32_t)mx_mode_eval(P.s_b, at) + (RUNS ? 4u * h * s_step : 0u);
-    if constexpr (RUNS) {
-      static_for<3>([&](auto i) {
-        v_off[i + 1] = v_off[i] + c_step;
-        vs_off[i + 1] = vs_off[i] + s_step;
-      });
+  // ---- sequences, 64 at a time: lane l has number 64 block + l, its units and those of the lanes up to it ----
+  MxSequence mine;
+  uint32_t units_of_lane, upto, block = 0u, block_base = 0u;
+  auto look_up = [&]() -> uint32_t {   // -> the block's units
+    const uint32_t b = 64u * block + lane;
+    mine = MxSequence{0u, 0u, 0, 0u};
+    if (b < P.sequences) mine = mx_sequence_of(P, t, b);
+    units_of_lane = mx_units(P, mine);
+    upto = units_of_lane * P.groups_kv;
+    static_for<6>([&](auto k) {
+      const uint32_t other = mx_from_lane(upto, lane - (1u << (int)k));
+      upto += lane >= (1u << (int)k) ? other : 0u;
+    });
+    return of_lane(upto, 63u);
+  };
+  const uint32_t blocks = (P.sequences + 63u) / 64u;
+  uint32_t together_shift = P.together >> 1;   // 4, 2, 1: 2, 1, 0
+  const uint32_t g = blockIdx.x * (WAVES >> together_shift) + (wave >> together_shift), in_group = wave & (P.together - 1u);
+  uint32_t u, share_end, total_units = 0u;
+  for (uint32_t left = blocks; left; --left) {
+    const uint32_t sum = look_up();
+    if (g == 0u && in_group == 0u && t.bases) {   // for the join
+      if (64u * block + lane < P.sequences) t.bases[64u * block + lane] = total_units + upto - units_of_lane * P.groups_kv;
+      if (left == 1u && lane == 0u) t.bases[P.sequences] = total_units + sum;
     }
+    total_units += sum;
+    if (left > 1u) ++block;
   }
-  const unsigned char *kc = t.k_codes + mx_mode_eval(P.c_h, w.kv), *ks = t.k_scales + mx_mode_eval(P.s_h, w.kv);
-  const unsigned char *vc = t.v_codes + mx_mode_eval(P.c_h, w.kv), *vs = t.v_scales + mx_mode_eval(P.s_h, w.kv);
+  mx_share(P, total_units, g, &u, &share_end);
+  if (u >= share_end) return;
+  const uint32_t share_begin = u;
+  if (blocks > 1u) {   // back to the first
+    block = 0u;
+    (void)look_up();
+  }
 
-  // ---- where tokens lie: lane l looks up one run of 16 (RUNS), l % 2 of the wavefront's tile l / 2 from `tile` on, 32 tiles at a time, or one
+  // ---- what a lane asks memory for: unit lane + 64 i of a run (blocks that a head does not have: its first one's, which meet zeros of q, or rows of O^T that
+  // nobody stores) ----
+  auto block_or_first = [&](uint32_t k) { return k < P.blocks ? k : 0u; };
+  auto codes_block = [&](uint32_t k) { return LINEAR ? block_or_first(k) * P.line.c_b : (uint32_t)mx_mode_eval(P.c_b, block_or_first(k)); };
+  auto scales_block = [&](uint32_t k) { return LINEAR ? block_or_first(k) * P.line.s_b : (uint32_t)mx_mode_eval(P.s_b, block_or_first(k)); };
+  uint32_t k_off[LOADS], v_off[LOADS], s_off[LOADS], k_token[LOADS], v_token[LOADS];   // scales: token n, block h + 4 i
+  static_for<LOADS>([&](auto i) {
+    const uint32_t unit = lane + 64u * (uint32_t)i, row = unit / NB % 16u;
+    k_token[i] = row;
+    v_token[i] = Slot::token_of_row(row);
+    k_off[i] = codes_block(unit % NB ^ Slot::key_fold(row)) + (LINEAR ? row * P.line.c_n : 0u);
+    v_off[i] = codes_block(unit % NB) + (LINEAR ? v_token[i] * P.line.c_n : 0u);
+    s_off[i] = scales_block(h + 4u * (uint32_t)i) + (LINEAR ? n * P.line.s_n : 0u);
+  });
+  // ---- a lane's share of a tile that has landed ----
+  uint32_t k_at[Tile::KS];
+  static_for<Tile::KS>([&](auto i) { k_at[i] = 16u * (NB * n + ((h * NB / 4u + (uint32_t)i) ^ Slot::key_fold(n))) + (NB == 2 ? 8u * (h & 1u) : 0u); });
+  const uint32_t ks_at = 4u * (NB == 4 ? lane : NB == 2 ? 16u * (h >> 1) + n : 32u * h + n);
+  const uint32_t vs_at = 4u * (16u * (n * NB / 16u) + 4u * h);
+  uint32_t v_at[4];
+  static_for<4>([&](auto e) { v_at[e] = Slot::value_row(4u * h + (uint32_t)e) * (16u * NB) + n * NB; });
+
+  while (true) {
+  // ---- the share's next sequence and key head ----
+  const uint64_t behind = __ballot(u < block_base + upto);
+  if (behind == 0u) {   // (in a later block)
+    block_base += of_lane(upto, 63u);
+    ++block;
+    (void)look_up();
+    continue;
+  }
+  const uint32_t holds = (uint32_t)__builtin_ctzll(behind), units = of_lane(units_of_lane, holds);
+  MxAttentionWork w;
+  w.b = 64u * block + holds;
+  w.s = MxSequence{of_lane(mine.first, holds), of_lane(mine.queries, holds), (int32_t)of_lane((uint32_t)mine.position, holds), of_lane(mine.length, holds)};
+  const uint32_t into = u - (block_base + of_lane(upto, holds) - units * P.groups_kv), group = into / units;
+  w.kv = group * P.together + in_group;
+  const uint32_t unit = into - group * units, unit_end = units - unit < share_end - u ? units : unit + (share_end - u);
+  mx_attention_rows(P, w, 0u, w.s.queries * P.group);
+  w.from = (w.lo & ~(kMxAttentionTokens - 1u)) + unit * kMxUnitTokens;
+  w.to = unit_end == units ? w.hi : (w.lo & ~(kMxAttentionTokens - 1u)) + unit_end * kMxUnitTokens;
+  if (w.from > w.hi) w.from = w.hi;
+  const int64_t c_head = LINEAR ? w.kv * P.line.c_h : mx_mode_eval(P.c_h, w.kv), s_head = LINEAR ? w.kv * P.line.s_h : mx_mode_eval(P.s_h, w.kv);
+  const unsigned char *kc = t.k_codes + c_head, *ks = t.k_scales + s_head, *vc = t.v_codes + c_head, *vs = t.v_scales + s_head;
+
+  // ---- where tokens lie: lane l looks up one run of 16 (LINEAR), l % 2 of the wavefront's tile l / 2 from `tile` on, 32 tiles at a time, or one
   // token, l % 32 of a tile ----
   struct Found {
     int64_t c, s;
-    uint32_t ok;   // RUNS: a bit for each token of the run
+    uint32_t ok;   // LINEAR: a bit for each token of the run
   };
   auto find = [&](uint32_t j) {   // j: of the lane
     Found f;
@@ -108,84 +186,100 @@ __global__ __launch_bounds__(256, NB * RT <= 4 ? 3 : NB * RT <= 8 ? 2 : 1) void 
       id = t.pages ? (uint32_t)t.pages[at] : (uint32_t)at;
     }
     const bool in = id < P.pool_pages;   // (the rest of a run that is begun lies in the pool too)
-    const uint32_t slot = in ? id * P.page + place : 0u, left = w.to - j;
-    f.c = mx_mode_eval(P.c_n, slot);
-    f.s = mx_mode_eval(P.s_n, slot);
-    f.ok = !in ? 0u : !RUNS || left >= 16u ? 0xFFFFu : (1u << left) - 1u;
+    const uint32_t left = w.to - j;
+    if constexpr (LINEAR) {
+      f.c = in ? id * P.line.c_page + (int64_t)place * P.line.c_n : 0;
+      f.s = in ? id * P.line.s_page + (int64_t)place * P.line.s_n : 0;
+      f.ok = !in ? 0u : left >= 16u ? 0xFFFFu : (1u << left) - 1u;
+    } else {
+      const uint32_t slot = in ? id * P.page + place : 0u;
+      f.c = mx_mode_eval(P.c_n, slot);
+      f.s = mx_mode_eval(P.s_n, slot);
+      f.ok = in;
+    }
     return f;
   };
-  auto of_lane = [&](uint32_t v, uint32_t from) { return (uint32_t)__builtin_amdgcn_readlane((int)v, (int)from); };
-  auto of_lane_64 = [&](int64_t v, uint32_t from) {
-    return (int64_t)((uint64_t)of_lane((uint32_t)((uint64_t)v >> 32), from) << 32 | of_lane((uint32_t)(uint64_t)v, from));
-  };
-  auto tokens_of = [&](uint32_t tile, const Found& f) {
-    MxTokens<RUNS> k;
-    if constexpr (RUNS) {
-      const uint32_t at = 2u * (tile % 32u);
-      static_for<2>([&](auto g) {
-        k.c[(int)g] = of_lane_64(f.c, at + (uint32_t)g);
-        k.s[(int)g] = of_lane_64(f.s, at + (uint32_t)g);
-      });
-      k.ok = of_lane(f.ok, at) | of_lane(f.ok, at + 1u) << 16;
-    } else {
-      k.c = f.c;
-      k.s = f.s;
-      k.ok = (uint32_t)__ballot(f.ok != 0u);   // (lanes 32 and more repeat the first)
-    }
-    return k;
-  };
   auto first_of_lane = [&](uint32_t tile) {   // the token that a lane looks up from this tile on
-    return w.from + TOKENS * (wave + WAVES * (RUNS ? tile + lane / 2u : tile)) + (RUNS ? 16u * (lane & 1u) : lane & 31u);
+    return w.from + TOKENS * (LINEAR ? tile + lane / 2u : tile) + (LINEAR ? 16u * (lane & 1u) : lane & 31u);
   };
-  auto load = [&](const MxTokens<RUNS>& k, Tile& tile) {
-    auto keys = [&](auto g, const unsigned char* c, const unsigned char* s) {
+  Found found;
+  // Asks for a tile; it lands in the ring's slot tile % DEPTH.  -> which of its tokens lie in the part and on pages of the pool
+  auto load = [&](uint32_t tile) -> uint32_t {
+    uint32_t ok;
+    if constexpr (LINEAR) {
+      if (tile % 32u == 0u) found = find(first_of_lane(tile));
+      ok = of_lane(found.ok, 2u * (tile % 32u)) | of_lane(found.ok, 2u * (tile % 32u) + 1u) << 16;
+    } else {
+      found = find(first_of_lane(tile));
+      ok = (uint32_t)__ballot(found.ok != 0u);   // (lanes 32 and more repeat the first)
+    }
+    uint32_t to = Slot::WAVE * wave + Slot::BYTES * (tile % Slot::DEPTH);
+    static_for<2>([&](auto g) {
+      const unsigned char *pk = kc, *pv = vc, *pks = ks, *pvs = vs;
+      if constexpr (LINEAR) {
+        const int64_t c = of_lane_64(found.c, 2u * (tile % 32u) + (uint32_t)g), s = of_lane_64(found.s, 2u * (tile % 32u) + (uint32_t)g);
+        pk += c;
+        pv += c;
+        pks += s;
+        pvs += s;
+      }
+      static_for<LOADS>([&](auto i) {
+        int64_t of_key = 0, of_value = 0, of_scale = 0;
+        if constexpr (!LINEAR) {
+          of_key = mx_from_lane(found.c, 16u * (uint32_t)g + k_token[i]);
+          of_value = mx_from_lane(found.c, 16u * (uint32_t)g + v_token[i]);
+          of_scale = mx_from_lane(found.s, 16u * (uint32_t)g + n);
+        }
+        if (NB > 2 || lane < 32u) {
+          mx_load_to_lds<16>(pk + of_key + k_off[i], to + (uint32_t)g * Slot::CODES + 1024u * (uint32_t)i);
+          mx_load_to_lds<16>(pv + of_value + v_off[i], to + (2u + (uint32_t)g) * Slot::CODES + 1024u * (uint32_t)i);
+          mx_load_to_lds<1>(pks + of_scale + s_off[i], to + 4u * Slot::CODES + (uint32_t)g * Slot::SCALES + 256u * (uint32_t)i);
+          mx_load_to_lds<1>(pvs + of_scale + s_off[i], to + 4u * Slot::CODES + (2u + (uint32_t)g) * Slot::SCALES + 256u * (uint32_t)i);
+        }
+      });
+    });
+    return ok;
+  };
+  auto take = [&](uint32_t tile, Tile& now) {
+    const unsigned char* at = lds + Slot::WAVE * wave + Slot::BYTES * (tile % Slot::DEPTH);
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    static_for<2>([&](auto g) {
+      const unsigned char *codes = at + (uint32_t)g * Slot::CODES, *scales = at + 4u * Slot::CODES + (uint32_t)g * Slot::SCALES + ks_at;
       if constexpr (NB == 2) {
-        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-        const u32x2 x = *reinterpret_cast<const u32x2*>(c + k_off[0]);
-        tile.k[(int)g][0] = x[0];
-        tile.k[(int)g][1] = x[1];
+        const u32x2 x = *reinterpret_cast<const u32x2*>(codes + k_at[0]);
+        now.k[(int)g][0] = x[0];
+        now.k[(int)g][1] = x[1];
       } else {
         static_for<Tile::KS>([&](auto i) {
-          const u32x4 x = *reinterpret_cast<const u32x4*>(c + k_off[i]);
-          static_for<4>([&](auto d) { tile.k[(int)g][4 * i + d] = x[(int)d]; });
+          const u32x4 x = *reinterpret_cast<const u32x4*>(codes + k_at[i]);
+          static_for<4>([&](auto d) { now.k[(int)g][4 * i + d] = x[(int)d]; });
         });
       }
-      static_for<Tile::KS>([&](auto i) { tile.ks[(int)g][(int)i] = s[ks_off[i]]; });
-    };
-    auto values = [&](auto e, const unsigned char* c, const unsigned char* s) {
-      constexpr int AT = RUNS ? (int)decltype(e)::value % 4 : 0;
-      if constexpr (NB == 2) tile.v[(int)e][0] = *reinterpret_cast<const uint16_t*>(c + v_off[AT]);
-      else if constexpr (NB == 4) tile.v[(int)e][0] = *reinterpret_cast<const uint32_t*>(c + v_off[AT]);
-      else {
-        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-        const u32x2 x = *reinterpret_cast<const u32x2*>(c + v_off[AT]);
-        tile.v[(int)e][0] = x[0];
-        tile.v[(int)e][1] = x[1];
-      }
-      tile.vs[(int)e] = s[vs_off[AT]];
-    };
-    if constexpr (RUNS) {
-      static_for<2>([&](auto g) { keys(g, kc + k.c[(int)g], ks + k.s[(int)g]); });
-      static_for<8>([&](auto e) { values(e, vc + k.c[(int)e / 4], vs + k.s[(int)e / 4]); });
-    } else {
-      static_for<2>([&](auto g) {
-        const uint32_t from = 16u * (uint32_t)g + n;
-        keys(g, kc + mx_from_lane(k.c, from), ks + mx_from_lane(k.s, from));
+      static_for<Tile::KS>([&](auto i) { now.ks[(int)g][(int)i] = *reinterpret_cast<const uint32_t*>(scales + 64u * (uint32_t)i); });
+    });
+    static_for<2>([&](auto g) {
+      const unsigned char *codes = at + (2u + (uint32_t)g) * Slot::CODES, *scales = at + 4u * Slot::CODES + (2u + (uint32_t)g) * Slot::SCALES + vs_at;
+      const u32x4 x = *reinterpret_cast<const u32x4*>(scales);
+      static_for<4>([&](auto e) {
+        now.vs[4 * g + e] = x[(int)e];
+        if constexpr (NB == 2) now.v[4 * g + e][0] = *reinterpret_cast<const uint16_t*>(codes + v_at[e]);
+        else if constexpr (NB == 4) now.v[4 * g + e][0] = *reinterpret_cast<const uint32_t*>(codes + v_at[e]);
+        else {
+          const u32x2 y = *reinterpret_cast<const u32x2*>(codes + v_at[e]);
+          now.v[4 * g + e][0] = y[0];
+          now.v[4 * g + e][1] = y[1];
+        }
       });
-      static_for<8>([&](auto e) {
-        const uint32_t from = 16u * ((uint32_t)e / 4u) + 4u * h + (uint32_t)e % 4u;
-        values(e, vc + mx_from_lane(k.c, from), vs + mx_from_lane(k.s, from));
-      });
-    }
+    });
   };
 
-  // the first tile's way begins before the queries'
-  uint32_t j = w.from + TOKENS * wave, tile = 0u;
-  Tile one, two;
-  Found found = find(first_of_lane(0u));
-  MxTokens<RUNS> at = tokens_of(0u, found);
-  if (!RUNS) found = find(first_of_lane(1u));
-  if (j < w.to) load(at, one);
+  // the first tiles' way begins before the queries'
+  const uint32_t tiles = (w.to - w.from + TOKENS - 1u) / TOKENS;
+  uint32_t oks[Slot::DEPTH];   // of the tiles on their way, the next one's first
+  static_for<Slot::DEPTH - 1>([&](auto i) {
+    oks[i] = 0u;
+    if ((uint32_t)i < tiles) oks[i] = load((uint32_t)i);
+  });
 
   u32x4 q[RT][NB];
   uint32_t row_lo[RT], row_hi[RT];
@@ -194,8 +288,18 @@ __global__ __launch_bounds__(256, NB * RT <= 4 ? 3 : NB * RT <= 8 ? 2 : 1) void 
     mx_row_seen(P, w, row, &row_lo[r], &row_hi[r]);
     uint32_t token, head;
     mx_row_place(P, w, row < w.r1 ? row : w.r0, &token, &head);
-    const unsigned char* p = row < w.r1 ? t.q + mx_mode_eval(P.q_t, token) + mx_mode_eval(P.q_h, head) : nullptr;
-    static_for<NB>([&](auto s) { q[r][s] = mx_query_vector(P, p, 8u * (k_dword + (uint32_t)s), q_vectors); });
+    if constexpr (LINEAR) {
+      const unsigned char* p = t.q + token * P.line.q_t + head * P.line.q_h;
+      const uint32_t turn = P.turned ? 0x80008000u : 0u;
+      static_for<NB>([&](auto s) {
+        const uint32_t d = 8u * (h * NB + (uint32_t)s);
+        const u32x4 v = *reinterpret_cast<const u32x4_at_elements*>(p + 2u * (d < P.D ? d : 0u));
+        q[r][s] = select_or_zero(row < w.r1 && d < P.D, u32x4{v[0] ^ turn, v[1] ^ turn, v[2] ^ turn, v[3] ^ turn});
+      });
+    } else {
+      const unsigned char* p = row < w.r1 ? t.q + mx_mode_eval(P.q_t, token) + mx_mode_eval(P.q_h, head) : nullptr;
+      static_for<NB>([&](auto s) { q[r][s] = mx_query_vector(P, p, 8u * (h * NB + (uint32_t)s), q_vectors); });
+    }
   });
 
   float top[RT], total[RT];
@@ -206,15 +310,26 @@ __global__ __launch_bounds__(256, NB * RT <= 4 ? 3 : NB * RT <= 8 ? 2 : 1) void 
     static_for<CHUNK>([&](auto c) { acc[r][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f}; });
   });
 
-  // works on the tile `now` (tokens j ..) while the next one comes
-  auto step = [&](Tile& now, Tile& next) {
-    const uint32_t ok = at.ok;
-    ++tile;
-    if (RUNS && tile % 32u == 0u) found = find(first_of_lane(tile));
-    at = tokens_of(tile, found);
-    if (!RUNS) found = find(first_of_lane(tile + 1u));
-    if (j + TOKENS * WAVES < w.to) load(at, next);
-    __builtin_amdgcn_sched_barrier(0);
+  // s_waitcnt vmcnt(n) lgkmcnt(0): all but the n youngest loads have landed, every LDS read has returned
+  auto wait_loads_but = [](auto but) {
+    constexpr int N = decltype(but)::value;
+    static_assert(N >= 0 && N < 64, "vmcnt has six bits");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0070);
+    asm volatile("" ::: "memory");
+  };
+  for (uint32_t tile = 0u; tile < tiles; ++tile) {
+    const uint32_t j = w.from + TOKENS * tile;
+    const uint32_t ok = oks[0];
+    static_for<Slot::DEPTH - 2>([&](auto i) { oks[i] = oks[i + 1]; });
+    if (tile + Slot::DEPTH - 1u < tiles) {
+      oks[Slot::DEPTH - 2] = load(tile + Slot::DEPTH - 1u);   // (into the slot that the last tile was in)
+      wait_loads_but(std::integral_constant<int, (Slot::DEPTH - 1) * IN_FLIGHT>{});
+    } else {
+      wait_loads_but(std::integral_constant<int, 0>{});
+    }
+    Tile now;
+    take(tile, now);
 
     // ---- scores ----
     f32x4 s[RT][2];
@@ -334,93 +449,60 @@ __global__ __launch_bounds__(256, NB * RT <= 4 ? 3 : NB * RT <= 8 ? 2 : 1) void 
         static_for<RT>([&](auto r) { acc[r][C] = mfma_16x16x32<MATH>(a, p[r], acc[r][C]); });
       });
     });
-    j += TOKENS * WAVES;
-  };
-  while (j < w.to) {
-    step(one, two);
-    if (j >= w.to) break;
-    step(two, one);
   }
 
-  // ---- the wavefronts' sums: 2 and 3 hand theirs to 0 and 1, then 1 to 0 (or one after the other to 0, where LDS has room for one's only) ----
-  float factor[RT];
-  static_for<RT>([&](auto r) {
-    total[r] = mx_sum_of_row(total[r]);
-    if (h == 0u) {
-      s_top[wave][16 * r + n] = top[r];
-      s_total[wave][16 * r + n] = total[r];
-    }
-  });
-  __syncthreads();
-  static_for<RT>([&](auto r) {
-    float m = kMinusInfinity, sum = 0.0f;
-    static_for<WAVES>([&](auto k) { m = fmaxf(m, s_top[k][16 * r + n]); });
-    const float from = m == kMinusInfinity ? 0.0f : m;
-    static_for<WAVES>([&](auto k) { sum += s_total[k][16 * r + n] * __builtin_amdgcn_exp2f(s_top[k][16 * r + n] - from); });
-    factor[r] = __builtin_amdgcn_exp2f(top[r] - from);
-    top[r] = m;
-    total[r] = sum;
-  });
-  static_for<RT>([&](auto r) { static_for<CHUNK>([&](auto c) { acc[r][c] *= factor[r]; }); });
-  auto give = [&](uint32_t slot) { static_for<RT>([&](auto r) { static_for<CHUNK>([&](auto c) { s_sums[slot][CHUNK * r + c][lane] = acc[r][c]; }); }); };
-  auto take = [&](uint32_t slot) { static_for<RT>([&](auto r) { static_for<CHUNK>([&](auto c) { acc[r][c] += s_sums[slot][CHUNK * r + c][lane]; }); }); };
-  if constexpr (SLOTS == 2) {
-    if (wave >= 2u) give(wave - 2u);
-    __syncthreads();
-    if (wave < 2u) take(wave);
-    __syncthreads();
-    if (wave == 1u) give(0u);
-    __syncthreads();
-    if (wave == 0u) take(0u);
-  } else {
-    static_for<WAVES - 1>([&](auto k) {
-      if (wave == 1u + (uint32_t)k) give(0u);
-      __syncthreads();
-      if (wave == 0u) take(0u);
-      __syncthreads();
+  static_for<RT>([&](auto r) { total[r] = mx_sum_of_row(total[r]); });
+
+  // ---- out: finished, or unfinished rows for the join ----
+  {
+    const MxAttentionParams& Z = mx_attention_params_again();
+    const bool alone = unit == 0u && unit_end == units;
+    float* part = alone ? nullptr : t.parts + mx_share_tile(Z, g, u == share_begin, in_group) * Z.part_rows * (WIDTH + 2);
+    static_for<RT>([&](auto r) {
+      const uint32_t in = 16u * (uint32_t)r + n;
+      if (in < w.r1) {
+        if (alone) {
+          uint32_t token, head;
+          mx_row_place(Z, w, in, &token, &head);
+          unsigned char* o = t.o + (LINEAR ? token * Z.line.o_t + head * Z.line.o_h : mx_mode_eval(Z.o_t, token) + mx_mode_eval(Z.o_h, head));
+          const float inverse = mx_inverse(total[r]);
+          constexpr int PIECE = CHUNK < 8 ? CHUNK : 8;
+          static_for<4>([&](auto i) {
+            static_for<CHUNK / PIECE>([&](auto k) {
+              float v[PIECE];
+              static_for<PIECE>([&](auto c) { v[c] = acc[r][PIECE * k + c][(int)i] * inverse; });
+              mx_store_o<PIECE, !LINEAR>(Z, o, CHUNK * (4u * h + (uint32_t)i) + PIECE * (uint32_t)k, v, o_vectors);
+            });
+          });
+          if (t.lse && h == 0u) t.lse[(uint64_t)token * Z.heads + head] = mx_lse(top[r], total[r]);
+        } else {
+          static_for<4>([&](auto i) {
+            static_for<CHUNK / 4>([&](auto c) {
+              *reinterpret_cast<f32x4*>(part + in * WIDTH + CHUNK * (4u * h + (uint32_t)i) + 4 * (int)c) =
+                  f32x4{acc[r][4 * c][(int)i], acc[r][4 * c + 1][(int)i], acc[r][4 * c + 2][(int)i], acc[r][4 * c + 3][(int)i]};
+            });
+          });
+          if (h == 0u) {
+            part[Z.part_rows * WIDTH + in] = top[r];
+            part[Z.part_rows * WIDTH + Z.part_rows + in] = total[r];
+          }
+        }
+      }
     });
   }
-  if (wave != 0u) return;
-
-  // ---- out: finished, or a part's sums for the join ----
-  const MxAttentionParams& Z = mx_attention_params_again();
-  const bool alone = w.parts <= 1u;
-  float* part = nullptr;
-  if (!alone) part = t.parts + mx_partial_tile(Z, w.b, w.kv, w.row_tile, w.part) * Z.tile_rows * (WIDTH + 2);
-  static_for<RT>([&](auto r) {
-    const uint32_t in = 16u * (uint32_t)r + n, row = w.r0 + in;
-    if (row >= w.r1) return;
-    if (alone) {
-      uint32_t token, head;
-      mx_row_place(Z, w, row, &token, &head);
-      unsigned char* o = t.o + mx_mode_eval(Z.o_t, token) + mx_mode_eval(Z.o_h, head);
-      const float inverse = mx_inverse(total[r]);
-      static_for<4>([&](auto i) {
-        float v[CHUNK];
-        static_for<CHUNK>([&](auto c) { v[c] = acc[r][c][(int)i] * inverse; });
-        mx_store_o<CHUNK>(Z, o, CHUNK * (4u * h + (uint32_t)i), v, o_vectors);
-      });
-      if (t.lse && h == 0u) t.lse[(uint64_t)token * Z.heads + head] = mx_lse(top[r], total[r]);
-    } else {
-      static_for<4>([&](auto i) {
-        static_for<CHUNK / 4>([&](auto c) {
-          *reinterpret_cast<f32x4*>(part + in * WIDTH + CHUNK * (4u * h + (uint32_t)i) + 4 * (int)c) =
-              f32x4{acc[r][4 * c][(int)i], acc[r][4 * c + 1][(int)i], acc[r][4 * c + 2][(int)i], acc[r][4 * c + 3][(int)i]};
-        });
-      });
-      if (h == 0u) {
-        part[Z.tile_rows * WIDTH + in] = top[r];
-        part[Z.tile_rows * WIDTH + Z.tile_rows + in] = total[r];
-      }
-    }
-  });
+  u += unit_end - unit;
+  if (u >= share_end) return;
+  }
 }
 
 template <int MATH, int NB, int RT>
 hipError_t launch_mx_attention_few_as(const lc_mx_attention_plan& plan, const MxAttentionTensors& t, hipStream_t s) {
-  const bool runs = t.pages ? plan.even_table : plan.even_plain;
-  if (runs) hipLaunchKernelGGL((mx_attention_few_kernel<MATH, NB, RT, true>), dim3(plan.groups), dim3(256), 0, s, plan.params, t, plan.q_vectors, plan.o_vectors);
-  else hipLaunchKernelGGL((mx_attention_few_kernel<MATH, NB, RT, false>), dim3(plan.groups), dim3(256), 0, s, plan.params, t, plan.q_vectors, plan.o_vectors);
+  static DevicesDone raised;
+  const hipError_t e = raise_lds_limit(&raised, &mx_attention_few_kernel<MATH, NB, RT, true>, &mx_attention_few_kernel<MATH, NB, RT, false>);
+  if (e != hipSuccess) return e;
+  const uint32_t lds = 4u * MxFewSlot<NB>::WAVE;
+  if (plan.linear) hipLaunchKernelGGL((mx_attention_few_kernel<MATH, NB, RT, true>), dim3(plan.groups), dim3(256), lds, s, plan.params, t, plan.q_vectors, plan.o_vectors);
+  else hipLaunchKernelGGL((mx_attention_few_kernel<MATH, NB, RT, false>), dim3(plan.groups), dim3(256), lds, s, plan.params, t, plan.q_vectors, plan.o_vectors);
   return hipSuccess;
 }
 template <int MATH, int NB>

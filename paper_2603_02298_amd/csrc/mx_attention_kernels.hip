@@ -18,71 +18,95 @@ LC_MX_ATTENTION_LAUNCHER(launch_mx_attention_tile_f16);
 namespace {
 
 // Joins the parts of one row, a workgroup each: parts p with sums o_p, maximum m_p and total l_p (exponents of two) make o = sum_p 2^(m_p - m) o_p over
-// l = sum_p 2^(m_p - m) l_p.  Wavefront k takes parts k, k + 4, ..; the four are added in their order, so that a result does not depend on timing.
-// Bound by the latency of a few loads.
-template <int WIDTH>
+// l = sum_p 2^(m_p - m) l_p.  WIDTH / 4 lanes take a part, so the workgroup takes 1024 / WIDTH at a time, and AHEAD times as many are on their way; their
+// groups are added in order at the end, so that a result does not depend on timing.
+// FEW: the parts are shares of units (mx_share), otherwise parts of a row tile's tokens.  Bound by the latency of a few loads.
+template <int WIDTH, bool FEW>
 __global__ __launch_bounds__(256) void mx_attention_join_kernel(MxAttentionParams P, MxAttentionTensors t, bool o_vectors) {
-  constexpr int EACH = WIDTH / 64, WAVES = 4, AHEAD = 8;
+  constexpr uint32_t LANES = WIDTH / 4, GROUPS = 256 / LANES;
+  constexpr int AHEAD = 4;
   touch_kernel_arguments<kMxAttentionKernargs>();
-  __shared__ float s_sums[WAVES][WIDTH], s_top[WAVES], s_total[WAVES];
-  const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  __shared__ f32x4 s_sums[GROUPS][LANES];
+  __shared__ float s_top[GROUPS], s_total[GROUPS];
+  const uint32_t lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
   const uint32_t b = blockIdx.y, i = blockIdx.x / P.heads, head = blockIdx.x % P.heads;
   const MxSequence s = mx_sequence_of(P, t, b);
   if (i >= s.queries) return;
-  const uint32_t kv = fd_div(head, P.group_div), r = i * P.group + (head - kv * P.group), row_tile = r / P.tile_rows, in = r % P.tile_rows;
-  const uint32_t rows = s.queries * P.group, r0 = row_tile * P.tile_rows, r1 = rows - r0 < P.tile_rows ? rows : r0 + P.tile_rows;
-  uint32_t lo, hi;
-  mx_rows_seen(P, s, r0, r1, &lo, &hi);
-  const uint32_t parts = mx_parts(P, lo, hi);
+  const uint32_t kv = fd_div(head, P.group_div), r = i * P.group + (head - kv * P.group);
+  uint32_t parts, in;
+  const uint32_t part_rows = FEW ? P.part_rows : P.tile_rows;
+  const uint64_t step = (uint64_t)part_rows * (WIDTH + 2);
+  const float* first;
+  uint64_t second, stride;   // from the first part to the next; from there on they follow each other
+  if constexpr (FEW) {
+    const uint32_t group_kv = kv / P.together, all = t.bases[P.sequences], units = (t.bases[b + 1u] - t.bases[b]) / P.groups_kv, u0 = t.bases[b] + group_kv * units;
+    const uint32_t g0 = mx_share_of(P, all, u0), g1 = mx_share_of(P, all, u0 + units - 1u);
+    parts = g1 - g0 + 1u;
+    uint32_t share, unused;
+    mx_share(P, all, g0, &share, &unused);
+    const uint64_t tile = mx_share_tile(P, g0, share == u0, kv - group_kv * P.together);
+    in = r;
+    first = t.parts + tile * step;
+    second = (mx_share_tile(P, g0 + 1u, true, kv - group_kv * P.together) - tile) * step;
+    stride = 2u * P.together * step;
+  } else {
+    const uint32_t row_tile = r / P.tile_rows, rows = s.queries * P.group, r0 = row_tile * P.tile_rows, r1 = rows - r0 < P.tile_rows ? rows : r0 + P.tile_rows;
+    uint32_t lo, hi;
+    mx_rows_seen(P, s, r0, r1, &lo, &hi);
+    parts = mx_parts(P, lo, hi);
+    in = r - r0;
+    first = t.parts + mx_partial_tile(P, b, kv, row_tile, 0u) * step;
+    second = stride = step;
+  }
   if (parts <= 1u) return;   // finished already
-  const uint64_t step = (uint64_t)P.tile_rows * (WIDTH + 2);
-  const float* first = t.parts + mx_partial_tile(P, b, kv, row_tile, 0u) * step;
-  const float *tops = first + P.tile_rows * WIDTH + in, *totals = tops + P.tile_rows, *sums = first + in * WIDTH + lane * EACH;
-  float top = kMinusInfinity, total = 0.0f, o[EACH];
-  static_for<EACH>([&](auto e) { o[e] = 0.0f; });
-  for (uint32_t p = wave; p < parts; p += WAVES * AHEAD) {
-    float m[AHEAD], l[AHEAD], v[AHEAD][EACH];
+  auto place_of = [&](uint32_t p) { return p ? second + (p - 1u) * stride : 0u; };
+  const float *tops = first + part_rows * WIDTH + in, *totals = tops + part_rows, *sums = first + in * WIDTH + 4u * lane;
+  float top = kMinusInfinity, total = 0.0f;
+  f32x4 o{0.0f, 0.0f, 0.0f, 0.0f};
+  for (uint32_t p = group; p < parts; p += GROUPS * AHEAD) {
+    float m[AHEAD], l[AHEAD];
+    f32x4 v[AHEAD];
+    typedef f32x4 __attribute__((aligned(8))) f32x4_any;
     static_for<AHEAD>([&](auto k) {
-      const uint32_t at = p + WAVES * (uint32_t)k;
+      const uint32_t at = p + GROUPS * (uint32_t)k;
       const bool there = at < parts;
-      const uint64_t off = (there ? at : p) * step;
+      const uint64_t off = place_of(there ? at : p);
       m[k] = there ? tops[off] : kMinusInfinity;
       l[k] = there ? totals[off] : 0.0f;
-      static_for<EACH>([&](auto e) { v[k][e] = sums[off + (int)e]; });
+      v[k] = *reinterpret_cast<const f32x4_any*>(sums + off);
     });
     float most = top;
     static_for<AHEAD>([&](auto k) { most = fmaxf(most, m[k]); });
     const float from = most == kMinusInfinity ? 0.0f : most, shrink = __builtin_amdgcn_exp2f(top - from);
     total *= shrink;
-    static_for<EACH>([&](auto e) { o[e] *= shrink; });
+    o *= shrink;
     static_for<AHEAD>([&](auto k) {
       const float f = __builtin_amdgcn_exp2f(m[k] - from);
       total += f * l[k];
-      if (p + WAVES * (uint32_t)k < parts) static_for<EACH>([&](auto e) { o[e] += f * v[k][e]; });
+      if (p + GROUPS * (uint32_t)k < parts) o += f * v[k];
     });
     top = most;
   }
-  static_for<EACH>([&](auto e) { s_sums[wave][lane * EACH + (int)e] = o[e]; });
+  s_sums[group][lane] = o;
   if (lane == 0u) {
-    s_top[wave] = top;
-    s_total[wave] = total;
+    s_top[group] = top;
+    s_total[group] = total;
   }
   __syncthreads();
-  if (wave != 0u) return;
+  if (group != 0u) return;
   top = kMinusInfinity;
-  static_for<WAVES>([&](auto k) { top = fmaxf(top, s_top[k]); });
+  static_for<(int)GROUPS>([&](auto k) { top = fmaxf(top, s_top[k]); });
   const float from = top == kMinusInfinity ? 0.0f : top;
   total = 0.0f;
-  static_for<EACH>([&](auto e) { o[e] = 0.0f; });
-  static_for<WAVES>([&](auto k) {
+  o = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  static_for<(int)GROUPS>([&](auto k) {
     const float f = __builtin_amdgcn_exp2f(s_top[k] - from);
     total += f * s_total[k];
-    static_for<EACH>([&](auto e) { o[e] += f * s_sums[k][lane * EACH + (int)e]; });
+    o += f * s_sums[k][lane];
   });
-  const float inverse = mx_inverse(total);
-  static_for<EACH>([&](auto e) { o[e] *= inverse; });
+  const float inverse = mx_inverse(total), out[4] = {o[0] * inverse, o[1] * inverse, o[2] * inverse, o[3] * inverse};
   const uint32_t token = s.first + i;
-  mx_store_o<EACH>(P, t.o + mx_mode_eval(P.o_t, token) + mx_mode_eval(P.o_h, head), lane * EACH, o, o_vectors);
+  mx_store_o<4>(P, t.o + mx_mode_eval(P.o_t, token) + mx_mode_eval(P.o_h, head), 4u * lane, out, o_vectors);
   if (t.lse && lane == 0u) t.lse[(uint64_t)token * P.heads + head] = mx_lse(top, total);
 }
 
@@ -106,20 +130,28 @@ lc_status_t execute_mx_attention(const lc_mx_attention_plan& plan, const void* q
     return LC_ERR_MISALIGNED;
   if (plan.workspace_bytes > 0 && (!workspace || off(workspace, 16) || workspace_bytes < (size_t)plan.workspace_bytes)) return LC_ERR_WORKSPACE_TOO_SMALL;
   auto bytes = [](const void* p) { return static_cast<const unsigned char*>(p); };
-  const MxAttentionTensors t{bytes(q),    bytes(k_codes), bytes(k_scales), bytes(v_codes), bytes(v_scales), pages, lengths, starts, static_cast<unsigned char*>(o), lse,
-                             static_cast<float*>(workspace)};
+  const bool few = plan.kernel == kMxAttentionFew, joined = plan.workspace_bytes > 0;
+  unsigned char* space = static_cast<unsigned char*>(workspace);
+  const MxAttentionTensors t{bytes(q), bytes(k_codes), bytes(k_scales), bytes(v_codes), bytes(v_scales), pages, lengths, starts, static_cast<unsigned char*>(o), lse,
+                             joined ? reinterpret_cast<float*>(space + (few ? mx_bases_bytes(P.sequences) : 0u)) : nullptr,
+                             joined && few ? reinterpret_cast<uint32_t*>(space) : nullptr};
   hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
   const bool bf16 = plan.q_dtype == LC_BF16;
   hipError_t e;
-  if (plan.kernel == kMxAttentionFew) e = bf16 ? launch_mx_attention_few_bf16(plan, t, s) : launch_mx_attention_few_f16(plan, t, s);
+  if (few) e = bf16 ? launch_mx_attention_few_bf16(plan, t, s) : launch_mx_attention_few_f16(plan, t, s);
   else e = bf16 ? launch_mx_attention_tile_bf16(plan, t, s) : launch_mx_attention_tile_f16(plan, t, s);
   if (failed(e, "attention launch") || failed(hipGetLastError(), "kernel launch")) return LC_ERR_HIP;
-  if (P.parts > 1u) {
+  if (joined) {
     const dim3 grid(plan.joined_rows, P.sequences);
-    if (plan.width == 64) hipLaunchKernelGGL((mx_attention_join_kernel<64>), grid, dim3(256), 0, s, P, t, plan.o_vectors);
-    else if (plan.width == 128) hipLaunchKernelGGL((mx_attention_join_kernel<128>), grid, dim3(256), 0, s, P, t, plan.o_vectors);
-    else hipLaunchKernelGGL((mx_attention_join_kernel<256>), grid, dim3(256), 0, s, P, t, plan.o_vectors);
+    auto join = [&](auto width) {
+      constexpr int WIDTH = decltype(width)::value;
+      if (few) hipLaunchKernelGGL((mx_attention_join_kernel<WIDTH, true>), grid, dim3(256), 0, s, P, t, plan.o_vectors);
+      else hipLaunchKernelGGL((mx_attention_join_kernel<WIDTH, false>), grid, dim3(256), 0, s, P, t, plan.o_vectors);
+    };
+    if (plan.width == 64) join(std::integral_constant<int, 64>{});
+    else if (plan.width == 128) join(std::integral_constant<int, 128>{});
+    else join(std::integral_constant<int, 256>{});
     if (failed(hipGetLastError(), "kernel launch")) return LC_ERR_HIP;
   }
   return LC_OK;

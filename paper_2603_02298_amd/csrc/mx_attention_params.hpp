@@ -8,7 +8,15 @@
 
 namespace lc {
 
+// Where things lie when every mode is one stride and a page's tokens are evenly apart, in bytes; elements of a head are neighbours.
+struct MxLinear {
+  int64_t q_t, q_h, o_t, o_h;        // tokens, heads
+  int64_t c_page, c_h, s_page, s_h;  // a page of the cache, heads: codes, scales
+  uint32_t c_n, c_b, s_n, s_b;       // tokens of a page, blocks
+};
+
 struct MxAttentionParams {
+  MxLinear line;
   MxMode q_t, q_h, q_d, o_t, o_h, o_d;   // tokens, heads, elements; in bytes
   MxMode c_n, c_h, c_b;                  // the cache's slots, heads, blocks: codes
   MxMode s_n, s_h, s_b;                  // scales
@@ -25,6 +33,10 @@ struct MxAttentionParams {
   int32_t causal, o_type;
   uint32_t queries_each;                 // of a sequence, where a call names no starts
   int32_t by_xcd;
+  // few rows: shares that the call's units are dealt out in (mx_share); key heads that wavefronts of a workgroup go over side by side (1, 2 or 4), and groups of
+  // them; rows of a sequence and key head at most
+  uint32_t shares, together, groups_kv, part_rows;
+  FastDiv shares_div;
 };
 
 constexpr uint32_t kMxAttentionTokens = 64;   // parts begin and end at multiples of this many tokens
@@ -88,6 +100,37 @@ LC_HD bool mx_attention_work(const MxAttentionParams& P, uint32_t group, uint32_
   fd_divmod(P.by_xcd ? pair * kXcds + xcd : pair, P.kv_div, b, kv);
   return *b < P.sequences;
 }
+// ---- few rows: one row tile holds all rows of a sequence and key head.  Their tokens are counted in units of kMxUnitTokens.  All units of a call, sequence after
+// sequence, group of `together` key heads after group, are dealt out in even shares, whatever the sequences' lengths.  `together` wavefronts of a workgroup have
+// one share, a key head of the group each: what lies together in the cache is asked for together. ----
+constexpr uint32_t kMxUnitTokens = 32;
+// of a group of key heads of a sequence: one at least where there are queries (they get zeros where they see nothing)
+LC_HD uint32_t mx_units(const MxAttentionParams& P, const MxSequence& s) {
+  if (s.queries == 0u) return 0u;
+  uint32_t lo, hi;
+  mx_rows_seen(P, s, 0u, s.queries * P.group, &lo, &hi);
+  const uint32_t begin = lo & ~(kMxAttentionTokens - 1u);
+  return hi <= lo ? 1u : (hi - begin + kMxUnitTokens - 1u) / kMxUnitTokens;
+}
+// the units *from .. *to - 1 of `total` that share g has
+LC_HD void mx_share(const MxAttentionParams& P, uint32_t total, uint32_t g, uint32_t* from, uint32_t* to) {
+  uint32_t each, more;
+  fd_divmod(total, P.shares_div, &each, &more);
+  *from = g * each + (g < more ? g : more);
+  *to = *from + each + (g < more ? 1u : 0u);
+}
+// the share that has unit u < total
+LC_HD uint32_t mx_share_of(const MxAttentionParams& P, uint32_t total, uint32_t u) {
+  uint32_t each, more;
+  fd_divmod(total, P.shares_div, &each, &more);
+  const uint32_t longer = more * (each + 1u);
+  return u < longer ? u / (each + 1u) : more + (u - longer) / each;
+}
+// Units of a group that several shares have leave unfinished rows in the workspace, behind the sequences' first units (a dword each, and the total): the tile of
+// share g and the group's key head `in` is number 2 g together + in for what the share begins with, (2 g + 1) together + in for what it ends with; part_rows rows each.
+LC_HD uint64_t mx_share_tile(const MxAttentionParams& P, uint32_t g, bool begins, uint32_t in) { return ((uint64_t)2u * g + (begins ? 0u : 1u)) * P.together + in; }
+LC_HD uint64_t mx_bases_bytes(uint32_t sequences) { return ((uint64_t)sequences * 4u + 4u + 15u) & ~uint64_t(15); }
+
 // A part's unfinished rows in the workspace: `tile_rows` rows of `width` sums, then their maxima and totals.  Number of the part's tile:
 LC_HD uint64_t mx_partial_tile(const MxAttentionParams& P, uint32_t b, uint32_t kv, uint32_t row_tile, uint32_t part) {
   return (((uint64_t)b * P.kv_heads + kv) * P.row_tiles + row_tile) * P.parts + part;

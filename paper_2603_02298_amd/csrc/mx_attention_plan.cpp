@@ -2,6 +2,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 #include <limits>
 #include <vector>
 
@@ -10,8 +11,13 @@
 namespace lc {
 
 namespace {
-// tokens of a run of 16 slots that begins at a multiple of 16 lie evenly apart
-bool even_runs(const Modes& n) { return n.size() == 1 || n[0].extent % 16 == 0; }
+// slots that are one stride apart on a page, and pages one stride apart
+bool by_pages(const Modes& n, int64_t page, uint32_t* step, int64_t* page_step) {
+  if (n.size() > 2 || (n.size() == 2 && n[0].extent != page) || n[0].stride >= (1 << 26)) return false;
+  *step = (uint32_t)n[0].stride;
+  *page_step = n.size() == 2 ? n[1].stride : n[0].stride * page;
+  return true;
+}
 std::string texts(const Modes (&m)[3]) { return Layout::flat(m[0]).str() + " x " + Layout::flat(m[1]).str() + " x " + Layout::flat(m[2]).str(); }
 }  // namespace
 
@@ -84,24 +90,36 @@ lc_status_t make_mx_attention_plan(const Layout& q, const Layout& codes, const L
   P.queries_each = (uint32_t)(T / sequences);
   P.o_type = o_dtype;
   plan.width = D <= 64 ? 64 : D <= 128 ? 128 : 256;
-  // evenly apart: a lane's place inside 16 tokens is a multiple of one stride, and strides of 15 tokens fit 32 bits
-  const bool near_by = std::abs(P.c_n.n == 1 ? P.c_n.last_stride : P.c_n.stride[0]) < (1 << 26) && std::abs(P.s_n.n == 1 ? P.s_n.last_stride : P.s_n.stride[0]) < (1 << 26);
-  const bool runs = even_runs(cm[0]) && even_runs(sm[0]) && near_by && pool.slots >= 16;
-  plan.even_table = runs && page % 16 == 0;
-  plan.even_plain = runs && (page * pages_each) % 16 == 0;
+  // (strides between blocks of one head, times 16 tokens' strides, fit 32 bits)
+  MxLinear& line = P.line;
+  plan.linear = page % 16 == 0 && D % 8 == 0 && plan.q_vectors && plan.o_vectors && by_pages(cm[0], page, &line.c_n, &line.c_page) && by_pages(sm[0], page, &line.s_n, &line.s_page);
+  const Modes* const one_leaf[] = {&qm[0], &qm[1], &om[0], &om[1], &cm[1], &cm[2], &sm[1], &sm[2]};
+  for (const Modes* m : one_leaf) plan.linear = plan.linear && m->size() == 1;
+  plan.linear = plan.linear && cm[2][0].stride < (1 << 26) && sm[2][0].stride < (1 << 26);
+  if (plan.linear) {
+    line.q_t = 2 * qm[0][0].stride;
+    line.q_h = 2 * qm[1][0].stride;
+    line.o_t = o_es * om[0][0].stride;
+    line.o_h = o_es * om[1][0].stride;
+    line.c_h = cm[1][0].stride;
+    line.s_h = sm[1][0].stride;
+    line.c_b = (uint32_t)cm[2][0].stride;
+    line.s_b = (uint32_t)sm[2][0].stride;
+  }
 
   // Few rows: two tiles of 16 at most share their tokens' way through the registers.  More: tiles of 128 share them through LDS.
   const int64_t rows = (int64_t)P.max_queries * P.group;
   plan.kernel = rows <= 32 ? kMxAttentionFew : kMxAttentionTile;
   P.tile_rows = rows <= 16 ? 16u : rows <= 32 ? 32u : 128u;
   const int64_t row_tiles = (rows + P.tile_rows - 1) / P.tile_rows, pairs = sequences * pool.heads;
-  // Parts: as many tokens as leave every CU work at the longest lengths, a tile for every wavefront at least.
+  // Tiles, parts: as many tokens as leave every CU work at the longest lengths, four tiles at least.
   const bool few = plan.kernel == kMxAttentionFew;
   const int64_t span = P.window ? std::min<int64_t>(P.max_tokens, (int64_t)P.window + (P.tile_rows + P.group - 1) / P.group + kMxAttentionTokens) : P.max_tokens;
   const int64_t tiles = (span + kMxAttentionTokens - 1) / kMxAttentionTokens + (P.window ? 1 : 0);
-  const int64_t least = few ? 2 : 4, wanted = few ? 2048 : 768;   // tiles of a part, workgroups
-  int64_t parts = std::max<int64_t>(1, std::min((wanted + pairs * row_tiles - 1) / (pairs * row_tiles), tiles / least));
-  const int64_t part_tiles = (tiles + parts - 1) / parts;
+  const int64_t least = 4, wanted = 768;   // tiles of a part, workgroups
+  int64_t parts = few ? 1 : std::max<int64_t>(1, std::min((wanted + pairs * row_tiles - 1) / (pairs * row_tiles), tiles / least));
+  int64_t part_tiles = (tiles + parts - 1) / parts;
+  if (const char* asked = std::getenv("LC_TUNE_MX_PART")) part_tiles = std::min(tiles, std::max<int64_t>(1, std::atoll(asked) / kMxAttentionTokens));   // tokens of a part
   parts = (tiles + part_tiles - 1) / part_tiles;
   P.row_tiles = (uint32_t)row_tiles;
   P.part_tokens = (uint32_t)(part_tiles * kMxAttentionTokens);
@@ -111,14 +129,30 @@ lc_status_t make_mx_attention_plan(const Layout& q, const Layout& codes, const L
   P.parts_div = make_fastdiv(P.parts);
   P.rows_div = make_fastdiv(P.row_tiles);
   P.kv_div = make_fastdiv(P.kv_heads);
+  // Few rows: as many wavefronts as are resident at once (by the kernels' registers and LDS), fewer where there are fewer units.
+  const int resident = plan.width * (int)P.tile_rows <= 128 * 16 ? 12 : plan.width * (int)P.tile_rows <= 256 * 16 ? 8 : 4;
+  const int64_t units = (span + kMxAttentionTokens - 1 + kMxUnitTokens - 1) / kMxUnitTokens;
+  if (few && (double)pairs * (double)units >= 4294967295.0) return LC_ERR_TOO_LARGE;   // units are counted in 32 bits
+  P.together = P.kv_heads % 4 == 0 ? 4u : P.kv_heads % 2 == 0 ? 2u : 1u;
+  P.groups_kv = P.kv_heads / P.together;
+  const int64_t each = 4 / P.together;   // shares of a workgroup
+  int64_t shares = std::min<int64_t>(256 * resident / P.together, (sequences * P.groups_kv * units + each - 1) / each * each);
+  if (const char* asked = std::getenv("LC_TUNE_MX_SHARES")) shares = std::max<int64_t>(1, std::atoi(asked) / 4) * each;   // wavefronts
+  P.part_rows = (uint32_t)rows;
+  P.shares = (uint32_t)shares;
+  P.shares_div = make_fastdiv(P.shares);
   // Row tiles of a pair on one XCD, where the pairs share out evenly among the XCDs.
   P.by_xcd = row_tiles > 1 && (pairs % kXcds == 0 || pairs >= 4 * (int64_t)kXcds);
-  const double groups = (double)(P.by_xcd ? (pairs + kXcds - 1) / kXcds * kXcds : pairs) * (double)row_tiles * (double)parts;
+  const double groups = few ? (double)(shares / each) : (double)(P.by_xcd ? (pairs + kXcds - 1) / kXcds * kXcds : pairs) * (double)row_tiles * (double)parts;
   if (groups * 256.0 > 4294967295.0) return LC_ERR_TOO_LARGE;   // a grid counts its lanes in 32 bits
   plan.groups = (uint32_t)groups;
-  if (parts > 1) {
+  const int64_t tile_bytes = (int64_t)(few ? P.part_rows : P.tile_rows) * (plan.width + 2) * 4;
+  if (few && units > 1) {
     plan.joined_rows = P.max_queries * P.heads;
-    plan.workspace_bytes = pairs * row_tiles * parts * (int64_t)P.tile_rows * (plan.width + 2) * 4;
+    plan.workspace_bytes = (int64_t)mx_bases_bytes(P.sequences) + 2 * shares * P.together * tile_bytes;
+  } else if (!few && parts > 1) {
+    plan.joined_rows = P.max_queries * P.heads;
+    plan.workspace_bytes = pairs * row_tiles * parts * tile_bytes;
   }
   *out = plan;
   return LC_OK;
@@ -131,8 +165,10 @@ std::string describe(const lc_mx_attention_plan& plan) {
        std::to_string(P.sequences) + " tokens=" + std::to_string(P.max_tokens) + " page=" + std::to_string(P.page) + " max_queries=" + std::to_string(P.max_queries);
   s += std::string(P.causal ? " causal=1" : " causal=0") + " window=" + std::to_string(P.window);
   s += std::string(" kernel=") + (plan.kernel == kMxAttentionFew ? "few" : "tile") + " width=" + std::to_string(plan.width) + " rows=" + std::to_string(P.tile_rows) + " row_tiles=" +
-       std::to_string(P.row_tiles) + " parts=" + std::to_string(P.parts) + " part_tokens=" + std::to_string(P.part_tokens) + " groups=" + std::to_string(plan.groups);
-  s += std::string(" tokens_by=") + (plan.even_table ? "runs" : "one") + "/" + (plan.even_plain ? "runs" : "one") + " q_by=" + (plan.q_vectors ? "vectors" : "elements") + " o_by=" +
+       std::to_string(P.row_tiles);
+  if (plan.kernel == kMxAttentionFew) s += " shares=" + std::to_string(P.shares) + "x" + std::to_string(P.together);
+  else s += " parts=" + std::to_string(P.parts) + " part_tokens=" + std::to_string(P.part_tokens) + " groups=" + std::to_string(plan.groups);
+  s += std::string(" linear=") + (plan.linear ? "1" : "0") + " q_by=" + (plan.q_vectors ? "vectors" : "elements") + " o_by=" +
        (plan.o_vectors ? "vectors" : "elements") + " workspace=" + std::to_string(plan.workspace_bytes);
   return s + " Q=[" + plan.q_text + "] O=[" + plan.o_text + "] codes(blocks,bytes)=[" + plan.c_text + "] scales=[" + plan.s_text + "]";
 }
@@ -142,28 +178,21 @@ lc_status_t mx_attention_walk_on_host(const lc_mx_attention_plan& plan, const in
   const MxAttentionParams& P = plan.params;
   if (!pages && plan.plain_slots > plan.slots) return LC_ERR_INVALID_ARG;
   if (!starts && P.T % P.sequences) return LC_ERR_INVALID_ARG;
-  const bool runs = pages ? plan.even_table : plan.even_plain;
+  const bool runs = plan.linear && plan.kernel == kMxAttentionFew;
   bool inside = true;
   int64_t n = 0;
-  for (uint32_t group = 0; group < plan.groups && inside; ++group) {
-    uint32_t b, kv, row_tile, part;
-    if (!mx_attention_work(P, group, &b, &kv, &row_tile, &part)) continue;
-    const MxSequence s = mx_sequence(P, lengths[b], starts ? starts[b] : (int32_t)(b * P.queries_each), starts ? starts[b + 1] : (int32_t)((b + 1) * P.queries_each));
-    const uint32_t rows = s.queries * P.group, r0 = row_tile * P.tile_rows, r1 = std::min(rows, r0 + P.tile_rows);
-    if (r0 >= rows) continue;
-    uint32_t lo, hi, from, to;
-    mx_rows_seen(P, s, r0, r1, &lo, &hi);
-    if (mx_parts(P, lo, hi) > P.parts) return LC_ERR_INVALID_ARG;
-    if (part && part >= mx_parts(P, lo, hi)) continue;
-    mx_part(P, lo, hi, part, &from, &to);
-    if (P.parts > 1 && (int64_t)(mx_partial_tile(P, b, kv, row_tile, part) + 1) * P.tile_rows * (plan.width + 2) * 4 > plan.workspace_bytes) return LC_ERR_INVALID_ARG;
+  auto sequence = [&](uint32_t b) {
+    return mx_sequence(P, lengths[b], starts ? starts[b] : (int32_t)(b * P.queries_each), starts ? starts[b + 1] : (int32_t)((b + 1) * P.queries_each));
+  };
+  // rows r0 .. r1 - 1 of a sequence and key head over the tokens from .. to - 1; the first time they are gone over, their way in and out too
+  auto go_over = [&](uint32_t b, uint32_t kv, const MxSequence& s, uint32_t r0, uint32_t r1, uint32_t from, uint32_t to, bool first) {
     for (uint32_t r = r0; r < r1; ++r) {
       const uint32_t i = fd_div(r, P.group_div), head = kv * P.group + r % P.group;
       uint32_t a, z;
       mx_seen(P, s, i, &a, &z);
       a = std::max(a, from);
       z = std::min(z, to);
-      if (part == 0) {
+      if (first) {
         const int64_t qo = mx_mode_eval(P.q_t, s.first + i) + mx_mode_eval(P.q_h, head) + mx_mode_eval(P.q_d, P.D - 1);
         const int64_t oo = mx_mode_eval(P.o_t, s.first + i) + mx_mode_eval(P.o_h, head) + mx_mode_eval(P.o_d, P.D - 1);
         inside = inside && qo >= 0 && qo + 2 <= q_bytes && oo >= 0 && oo + (P.o_type == LC_F32 ? 4 : 2) <= o_bytes;
@@ -175,7 +204,7 @@ lc_status_t mx_attention_walk_on_host(const lc_mx_attention_plan& plan, const in
         ++n;
       }
     }
-    // what the kernels ask memory for: whole runs of 16 tokens where they lie evenly apart, single tokens otherwise
+    // what the kernels ask memory for: whole runs of 16 tokens where everything is linear, single tokens otherwise
     for (uint32_t j = from & ~15u; j < to; ++j) {
       uint32_t place;
       const uint32_t head_of_run = runs ? j & ~15u : j;
@@ -183,11 +212,67 @@ lc_status_t mx_attention_walk_on_host(const lc_mx_attention_plan& plan, const in
       const int64_t id = pages ? pages[at] : (int64_t)at;
       if (id < 0 || id >= P.pool_pages) continue;
       const uint32_t slot = (uint32_t)id * P.page + place;
-      const int64_t c_step = P.c_n.n == 1 ? P.c_n.last_stride : P.c_n.stride[0], s_step = P.s_n.n == 1 ? P.s_n.last_stride : P.s_n.stride[0];
-      const int64_t co = mx_mode_eval(P.c_n, slot) + mx_mode_eval(P.c_h, kv) + (runs ? (int64_t)(j & 15u) * c_step : 0);
-      const int64_t so = mx_mode_eval(P.s_n, slot) + mx_mode_eval(P.s_h, kv) + (runs ? (int64_t)(j & 15u) * s_step : 0);
-      for (uint32_t k = 0; k < P.blocks; ++k)
-        inside = inside && co + mx_mode_eval(P.c_b, k) + (int64_t)kMxBlockBytes <= c_bytes && so + mx_mode_eval(P.s_b, k) + 1 <= s_bytes;
+      const int64_t co = runs ? id * P.line.c_page + (int64_t)(place + (j & 15u)) * P.line.c_n + kv * P.line.c_h : mx_mode_eval(P.c_n, slot) + mx_mode_eval(P.c_h, kv);
+      const int64_t so = runs ? id * P.line.s_page + (int64_t)(place + (j & 15u)) * P.line.s_n + kv * P.line.s_h : mx_mode_eval(P.s_n, slot) + mx_mode_eval(P.s_h, kv);
+      for (uint32_t k = 0; k < P.blocks; ++k) {
+        const int64_t cb = runs ? (int64_t)k * P.line.c_b : mx_mode_eval(P.c_b, k), sb = runs ? (int64_t)k * P.line.s_b : mx_mode_eval(P.s_b, k);
+        inside = inside && co + cb + (int64_t)kMxBlockBytes <= c_bytes && so + sb + 1 <= s_bytes;
+        if (runs && (co != mx_mode_eval(P.c_n, slot + (j & 15u)) + mx_mode_eval(P.c_h, kv) || cb != mx_mode_eval(P.c_b, k) ||
+                     so != mx_mode_eval(P.s_n, slot + (j & 15u)) + mx_mode_eval(P.s_h, kv) || sb != mx_mode_eval(P.s_b, k)))
+          return LC_ERR_INVALID_ARG;
+      }
+    }
+  };
+  if (plan.kernel == kMxAttentionFew) {
+    std::vector<uint32_t> bases(1, 0u);
+    for (uint32_t b = 0; b < P.sequences; ++b) bases.push_back(bases.back() + mx_units(P, sequence(b)) * P.groups_kv);
+    const uint32_t total = bases.back();
+    uint32_t next = 0;
+    for (uint32_t g = 0; g < P.shares && inside; ++g) {
+      uint32_t u, end, b = 0;
+      mx_share(P, total, g, &u, &end);
+      if (u != next || end < u) return LC_ERR_INVALID_ARG;
+      next = end;
+      const uint32_t share = u;
+      while (u < end) {
+        while (u >= bases[b + 1]) ++b;
+        const MxSequence s = sequence(b);
+        const uint32_t units = mx_units(P, s), group = (u - bases[b]) / units, first = (u - bases[b]) % units, last = std::min(units, first + (end - u));
+        uint32_t lo, hi;
+        mx_rows_seen(P, s, 0u, s.queries * P.group, &lo, &hi);
+        const uint32_t begin = lo & ~(kMxAttentionTokens - 1u), from = std::min(hi, begin + first * kMxUnitTokens), to = std::min<uint64_t>(hi, (uint64_t)begin + (uint64_t)last * kMxUnitTokens);
+        if (s.queries * P.group > P.tile_rows || mx_share_of(P, total, u) != g) return LC_ERR_INVALID_ARG;
+        for (uint32_t in = 0; in < P.together; ++in) {
+          const uint32_t kv = group * P.together + in;
+          go_over(b, kv, s, 0u, s.queries * P.group, from, to, first == 0u);
+          if (last - first < units) {   // unfinished: the join has to find it
+            const uint64_t tile = mx_share_tile(P, g, u == share, in);
+            const uint32_t u0 = bases[b] + group * units, g0 = mx_share_of(P, total, u0), g1 = mx_share_of(P, total, u0 + units - 1u);
+            uint32_t mine, unused;
+            mx_share(P, total, g, &mine, &unused);
+            if (g < g0 || g > g1 || g0 == g1 || mx_share_tile(P, g, g != g0 || u0 == mine, in) != tile) return LC_ERR_INVALID_ARG;
+            if ((int64_t)mx_bases_bytes(P.sequences) + (int64_t)(tile + 1u) * P.part_rows * (plan.width + 2) * 4 > plan.workspace_bytes || s.queries * P.group > P.part_rows)
+              return LC_ERR_INVALID_ARG;
+          }
+        }
+        u += last - first;
+      }
+    }
+    if (next != total) return LC_ERR_INVALID_ARG;
+  } else {
+    for (uint32_t group = 0; group < plan.groups && inside; ++group) {
+      uint32_t b, kv, row_tile, part;
+      if (!mx_attention_work(P, group, &b, &kv, &row_tile, &part)) continue;
+      const MxSequence s = sequence(b);
+      const uint32_t rows = s.queries * P.group, r0 = row_tile * P.tile_rows, r1 = std::min(rows, r0 + P.tile_rows);
+      if (r0 >= rows) continue;
+      uint32_t lo, hi, from, to;
+      mx_rows_seen(P, s, r0, r1, &lo, &hi);
+      if (mx_parts(P, lo, hi) > P.parts) return LC_ERR_INVALID_ARG;
+      if (part && part >= mx_parts(P, lo, hi)) continue;
+      mx_part(P, lo, hi, part, &from, &to);
+      if (P.parts > 1 && (int64_t)(mx_partial_tile(P, b, kv, row_tile, part) + 1) * P.tile_rows * (plan.width + 2) * 4 > plan.workspace_bytes) return LC_ERR_INVALID_ARG;
+      go_over(b, kv, s, r0, r1, from, to, part == 0);
     }
   }
   if (pairs) *pairs = n;

@@ -13,8 +13,7 @@ struct lc_mx_attention_plan {
   lc::MxAttentionParams params{};
   MxAttentionKernel kernel = kMxAttentionFew;
   int width = 0;            // elements of a head that the kernel is made for: 64, 128 or 256
-  bool even = false;        // 16 tokens from a multiple of 16 on lie evenly apart on one page (without a table: in the sequence's slots)
-  bool even_table = false, even_plain = false;   // the same with a page table, and without
+  bool linear = false;      // everything lies as MxLinear says, 16 tokens from a multiple of 16 on are on one page
   bool q_vectors = false, o_vectors = false;     // a head's elements are neighbours
   uint32_t groups = 0, joined_rows = 0;          // joined_rows: rows of a sequence that may have parts to be joined
   int64_t workspace_bytes = 0;

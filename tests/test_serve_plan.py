@@ -328,9 +328,14 @@ def test_attention_kernel_by_rows(rows, kernel):
     assert " kernel=" + kernel in _attention(T=2 * rows, heads=2, kv=2, max_queries=rows).describe()
 
 
-def test_attention_runs_of_tokens():
-    """Runs of 16 tokens evenly apart are what pages of whole runs give; without a table a sequence's slots do."""
-    assert " tokens_by=runs/runs" in _attention(page=16).describe() and " tokens_by=runs/runs" in _attention(page=16, order="tokens").describe()
-    assert " tokens_by=one/one" in _attention(page=8, slots=64, pages_per_sequence=3).describe()
-    assert " tokens_by=one/runs" in _attention(page=8, slots=64, pages_per_sequence=4, codes="(64,2,64):(128,64,1)", scales="(64,2,2):(4,2,1)").describe()
-    assert " tokens_by=one/one" in _attention(page=24, slots=96, pages_per_sequence=2).describe()   # pages of one and a half runs, apart
+def test_attention_that_is_linear():
+    """Pages of whole runs of 16 tokens, one stride apart, everything else one stride: what the kernel of few rows has a short way for."""
+    assert " linear=1" in _attention(page=16).describe() and " linear=1" in _attention(page=16, order="tokens").describe()
+    assert " linear=1" in _attention(page=16, codes="(64,2,64):(128,64,1)", scales="(64,2,2):(4,2,1)").describe()
+    for change in (dict(page=8), dict(page=24, slots=96), dict(D=72), dict(q="((4,2),8,64):((512,4096),64,1)"), dict(o="(8,8,64):(1024,128,2)"),
+                   dict(codes="((8,8),2,64):((64,1024),512,1)", scales="(64,2,2):(4,2,1)"), dict(scales="((2,32),2,2):((4,10),2,1)")):
+        if change.get("D") == 72:
+            assert " linear=1" in _attention(**change).describe()   # (whole vectors of eight)
+        else:
+            assert " linear=0" in _attention(**change).describe(), change
+    assert " linear=0" in _attention(D=76).describe()
