@@ -27,13 +27,13 @@ __device__ __forceinline__ float mx_sum_of_halves(float m) {
 template <int WIDTH>
 constexpr uint32_t kMxAttentionTileLds = 2u * 2u * kMxAttentionTokens * WIDTH * 2u + 2u * kMxAttentionTokens * 4u;   // (all of it dynamic: what may be allowed then is all of a CU's)
 
-template <int MATH, int WIDTH>
+// LINEAR: everything lies as MxLinear says (lc_mx_attention_plan::linear).
+template <int MATH, int WIDTH, bool LINEAR>
 __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : 2) void mx_attention_tile_kernel(MxAttentionParams P, MxAttentionTensors t, bool q_vectors, bool o_vectors) {
   constexpr int NB = WIDTH / 32, TOKENS = (int)kMxAttentionTokens, STEPS = WIDTH / 16;
   constexpr uint32_t K_BYTES = TOKENS * WIDTH * 2, STAGE = 2 * K_BYTES;
   // A lane loads UNITS blocks of a tile, all of the same block of a head: of keys and values of PASSES tokens (width 64: of keys or of values)
   constexpr int PASSES = NB >= 4 ? NB / 4 : 1, TENSORS = NB >= 4 ? 2 : 1;
-  touch_kernel_arguments<kMxAttentionKernargs>();
   extern __shared__ unsigned char lds[];
   // [stage][token]: the tile whose token has values in blocks that may not be finite (kMxLoud)
   uint32_t* s_loud = reinterpret_cast<uint32_t*>(lds + 2 * STAGE);
@@ -47,7 +47,9 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : 2) void mx_attention_tile_k
   const uint32_t block = tid % NB, first_token = (tid / NB) % (256u / NB > (uint32_t)TOKENS ? (uint32_t)TOKENS : 256u / NB);
   const bool second = TENSORS == 1 && tid >= 128u;   // (width 64) values
   const bool block_in = block < P.blocks;
-  const int64_t c_head = mx_mode_eval(P.c_h, w.kv) + mx_mode_eval(P.c_b, block_in ? block : 0u), s_head = mx_mode_eval(P.s_h, w.kv) + mx_mode_eval(P.s_b, block_in ? block : 0u);
+  const uint32_t of_block = block_in ? block : 0u;
+  const int64_t c_head = LINEAR ? w.kv * P.line.c_h + (int64_t)(of_block * P.line.c_b) : mx_mode_eval(P.c_h, w.kv) + mx_mode_eval(P.c_b, of_block);
+  const int64_t s_head = LINEAR ? w.kv * P.line.s_h + (int64_t)(of_block * P.line.s_b) : mx_mode_eval(P.s_h, w.kv) + mx_mode_eval(P.s_b, of_block);
   const unsigned char *codes[2] = {(second ? t.v_codes : t.k_codes) + c_head, t.v_codes + c_head};
   const unsigned char *scales[2] = {(second ? t.v_scales : t.k_scales) + s_head, t.v_scales + s_head};
   struct Raw {
@@ -59,6 +61,19 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : 2) void mx_attention_tile_k
     if (j >= w.to) { *place = 0u; return 0xFFFFFFFFu; }
     const uint64_t at = mx_page_at(P, w.b, j, place);
     return t.pages ? (uint32_t)t.pages[at] : (uint32_t)at;
+  };
+  // where a token of page `id` lies, codes and scales
+  auto token_at = [&](uint32_t id, uint32_t place, int64_t* c, int64_t* s) {
+    const bool in = id < P.pool_pages;
+    if constexpr (LINEAR) {
+      *c = in ? id * P.line.c_page + (int64_t)place * P.line.c_n : 0;
+      *s = in ? id * P.line.s_page + (int64_t)place * P.line.s_n : 0;
+    } else {
+      const uint32_t slot = in ? id * P.page + place : 0u;
+      *c = mx_mode_eval(P.c_n, slot);
+      *s = mx_mode_eval(P.s_n, slot);
+    }
+    return in;
   };
   struct Pages {
     uint32_t id[PASSES], place[PASSES];
@@ -73,31 +88,36 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : 2) void mx_attention_tile_k
   };
   auto load = [&](const Pages& p, Raw& raw) {
     static_for<PASSES>([&](auto i) {
-      raw.in[i] = p.id[i] < P.pool_pages;
-      const uint32_t slot = raw.in[i] ? p.id[i] * P.page + p.place[i] : 0u;
-      const int64_t c = mx_mode_eval(P.c_n, slot), s = mx_mode_eval(P.s_n, slot);
+      int64_t c, s;
+      raw.in[i] = token_at(p.id[i], p.place[i], &c, &s);
       static_for<TENSORS>([&](auto k) {
         raw.codes[i][k] = *reinterpret_cast<const u32x4*>(codes[k] + c);
         raw.byte[i][k] = scales[k][s];
       });
     });
   };
+  // a block's elements go to LDS in vectors of eight: vector e of it lies at put[..] ^ 16 e (keys' and values' arrangements both fold whole vectors)
+  uint32_t put[PASSES][TENSORS];
+  static_for<PASSES>([&](auto i) {
+    static_for<TENSORS>([&](auto k) {
+      const uint32_t token = first_token + (uint32_t)i * (TOKENS / PASSES);
+      const bool is_value = TENSORS == 1 ? second : (int)decltype(k)::value == 1;
+      put[i][k] = is_value ? K_BYTES + gemm_rdirect_lds_offset(WIDTH, token, 32u * block) : (block / 2u) * (TOKENS * 128u) + gemm_lds_offset(token, 4u * (block & 1u));
+    });
+  });
   auto expand = [&](uint32_t j, uint32_t stage, Raw& raw) {
-    unsigned char* keys = lds + stage * STAGE;
+    unsigned char* tile = lds + stage * STAGE;
     static_for<PASSES>([&](auto i) {
       const uint32_t token = first_token + (uint32_t)i * (TOKENS / PASSES);
+      // tokens that nobody sees, and blocks that are not there: zeros
+      const bool in = block_in && raw.in[i] && j + token >= w.lo;
       static_for<TENSORS>([&](auto k) {
         const bool is_value = TENSORS == 1 ? second : (int)decltype(k)::value == 1;
-        // tokens that nobody sees, and blocks that are not there: zeros
-        const bool in = block_in && raw.in[i] && j + token >= w.lo, loud = is_value && in && raw.byte[i][k] >= kMxLoud<MATH>;
+        const bool loud = is_value && in && raw.byte[i][k] >= kMxLoud<MATH>;
         const u32x4 c = select_or_zero(in && !loud, raw.codes[i][k]);
         const float scale = mx_scale_of(in && !loud ? raw.byte[i][k] : 127u);
         if (loud) s_loud[TOKENS * stage + token] = j;
-        static_for<4>([&](auto e) {
-          const uint32_t at = is_value ? K_BYTES + gemm_rdirect_lds_offset(WIDTH, token, 32u * block + 8u * (uint32_t)e)
-                                       : (block / 2u) * (TOKENS * 128u) + gemm_lds_offset(token, 4u * (block & 1u) + (uint32_t)e);
-          *reinterpret_cast<u32x4*>(keys + at) = mx_expand<MATH>(c[(int)e], scale);
-        });
+        static_for<4>([&](auto e) { *reinterpret_cast<u32x4*>(tile + (put[i][k] ^ (16u * (uint32_t)e))) = mx_expand<MATH>(c[(int)e], scale); });
       });
     });
   };
@@ -117,8 +137,18 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : 2) void mx_attention_tile_k
   mx_row_place(P, w, row < w.r1 ? row : w.r0, &q_token, &q_head);
   u32x4 q[STEPS];
   {
-    const unsigned char* p = row < w.r1 ? t.q + mx_mode_eval(P.q_t, q_token) + mx_mode_eval(P.q_h, q_head) : nullptr;
-    static_for<STEPS>([&](auto s) { q[s] = mx_query_vector(P, p, 16u * (uint32_t)s + 8u * h, q_vectors); });
+    if constexpr (LINEAR) {
+      const unsigned char* p = t.q + q_token * P.line.q_t + q_head * P.line.q_h;
+      const uint32_t turn = P.turned ? 0x80008000u : 0u;
+      static_for<STEPS>([&](auto s) {
+        const uint32_t d = 16u * (uint32_t)s + 8u * h;
+        const u32x4 v = *reinterpret_cast<const u32x4_at_elements*>(p + 2u * (d < P.D ? d : 0u));
+        q[s] = select_or_zero(row < w.r1 && d < P.D, u32x4{v[0] ^ turn, v[1] ^ turn, v[2] ^ turn, v[3] ^ turn});
+      });
+    } else {
+      const unsigned char* p = row < w.r1 ? t.q + mx_mode_eval(P.q_t, q_token) + mx_mode_eval(P.q_h, q_head) : nullptr;
+      static_for<STEPS>([&](auto s) { q[s] = mx_query_vector(P, p, 16u * (uint32_t)s + 8u * h, q_vectors); });
+    }
   }
   // what the wavefront's rows see: any of them, every one of them
   uint32_t any_lo = 0u, any_hi = 0u, all_lo = 0u, all_hi = 0u;
@@ -149,22 +179,31 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : 2) void mx_attention_tile_k
     if (j < any_hi && j + TOKENS > any_lo) {   // (a wavefront whose rows see nothing of the tile has nothing to do)
       const unsigned char* keys = lds + stage * STAGE;
       const unsigned char* values = keys + K_BYTES;
-      // ---- scores ----
+      // ---- scores (both halves of the tokens in turns: neither product waits for the other) ----
       f32x16 s[2];
-      static_for<2>([&](auto g) {
-        static_for<16>([&](auto e) { s[g][(int)e] = 0.0f; });
-        static_for<STEPS>([&](auto k) {
+      static_for<2>([&](auto g) { static_for<16>([&](auto e) { s[g][(int)e] = 0.0f; }); });
+      static_for<STEPS>([&](auto k) {
+        static_for<2>([&](auto g) {
           const u32x4 a = direct_fragment<TOKENS, kLoadKDirect>(keys + ((int)k / 4) * (TOKENS * 128), lane, 32u * (uint32_t)g, (int)k % 4);
           s[g] = mfma_32x32x16<MATH == kMxBf16>(a, q[k], s[g]);
         });
       });
-      const bool whole = j >= all_lo && j + TOKENS <= all_hi && ok == ~uint64_t(0);
-      if (!whole) {
+      const bool whole = j >= all_lo && j + TOKENS <= all_hi;
+      if (!whole) {   // tokens row_lo .. row_hi - 1, counted from the lane's first one of the tile
+        const uint32_t first = row_lo - j - 4u * h, count = row_hi - row_lo;
         static_for<2>([&](auto g) {
           static_for<16>([&](auto e) {
-            const uint32_t in = 32u * (uint32_t)g + mfma_c_row(lane, (uint32_t)e);
-            const bool seen = (ok >> in & 1u) && j + in >= row_lo && j + in < row_hi;
-            s[g][(int)e] = seen ? s[g][(int)e] : kMinusInfinity;
+            constexpr uint32_t in = 32u * (uint32_t)decltype(g)::value + 8u * ((uint32_t)decltype(e)::value / 4u) + (uint32_t)decltype(e)::value % 4u;   // (of lanes h = 0)
+            s[g][(int)e] = in - first < count ? s[g][(int)e] : kMinusInfinity;
+          });
+        });
+      }
+      if (ok != ~uint64_t(0)) {   // past the part, or on no page of the pool
+        const uint64_t mine = ok >> (4u * h);
+        static_for<2>([&](auto g) {
+          static_for<16>([&](auto e) {
+            constexpr uint32_t in = 8u * ((uint32_t)decltype(e)::value / 4u) + (uint32_t)decltype(e)::value % 4u;
+            s[g][(int)e] = (uint32_t)(mine >> (32 * (int)g)) >> in & 1u ? s[g][(int)e] : kMinusInfinity;
           });
         });
       }
@@ -208,13 +247,16 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : 2) void mx_attention_tile_k
         const float probability = mx_sum_of_halves(mine);
         const bool seen = j + in >= row_lo && j + in < row_hi;
         uint32_t place;
-        const uint32_t id = page_of(j + in, &place), slot = id < P.pool_pages ? id * P.page + place : 0u;
-        const unsigned char *c = t.v_codes + mx_mode_eval(P.c_h, w.kv) + mx_mode_eval(P.c_n, slot), *b = t.v_scales + mx_mode_eval(P.s_h, w.kv) + mx_mode_eval(P.s_n, slot);
+        const uint32_t id = page_of(j + in, &place);
+        int64_t c_token, s_token;
+        token_at(id, place, &c_token, &s_token);
+        const unsigned char *c = t.v_codes + (LINEAR ? w.kv * P.line.c_h : mx_mode_eval(P.c_h, w.kv)) + c_token;
+        const unsigned char* b = t.v_scales + (LINEAR ? w.kv * P.line.s_h : mx_mode_eval(P.s_h, w.kv)) + s_token;
         static_for<NB>([&](auto d) {
           const uint32_t at = (uint32_t)d < P.blocks ? (uint32_t)d : 0u;
-          const uint32_t byte = b[mx_mode_eval(P.s_b, at)];
+          const uint32_t byte = b[LINEAR ? at * P.line.s_b : mx_mode_eval(P.s_b, at)];
           if ((uint32_t)d < P.blocks && byte >= kMxLoud<MATH>) {
-            const u32x4 codes = *reinterpret_cast<const u32x4*>(c + mx_mode_eval(P.c_b, at));
+            const u32x4 codes = *reinterpret_cast<const u32x4*>(c + (LINEAR ? at * P.line.c_b : mx_mode_eval(P.c_b, at)));
             const float scale = mx_scale_of(byte);
             static_for<4>([&](auto i) {   // elements 8 i + 4 h .. + 3 of the block
               const uint32_t four = codes[(int)i] >> (16u * h);
@@ -236,13 +278,13 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : 2) void mx_attention_tile_k
   total = mx_sum_of_halves(total);
   if (row >= w.r1) return;
   if (w.parts <= 1u) {
-    unsigned char* o = t.o + mx_mode_eval(Z.o_t, q_token) + mx_mode_eval(Z.o_h, q_head);
+    unsigned char* o = t.o + (LINEAR ? q_token * Z.line.o_t + q_head * Z.line.o_h : mx_mode_eval(Z.o_t, q_token) + mx_mode_eval(Z.o_h, q_head));
     const float inverse = mx_inverse(total);
     static_for<NB>([&](auto d) {
       static_for<4>([&](auto i) {
         float v[4];
         static_for<4>([&](auto e) { v[e] = acc[d][4 * i + e] * inverse; });
-        mx_store_o<4>(Z, o, 32u * (uint32_t)d + 8u * (uint32_t)i + 4u * h, v, o_vectors);
+        mx_store_o<4, !LINEAR>(Z, o, 32u * (uint32_t)d + 8u * (uint32_t)i + 4u * h, v, o_vectors);
       });
     });
     if (t.lse && h == 0u) t.lse[(uint64_t)q_token * Z.heads + q_head] = mx_lse(top, total);
@@ -264,9 +306,11 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : 2) void mx_attention_tile_k
 template <int MATH, int WIDTH>
 hipError_t launch_mx_attention_tile(const lc_mx_attention_plan& plan, const MxAttentionTensors& t, hipStream_t s) {
   static DevicesDone raised;
-  const hipError_t e = raise_lds_limit(&raised, &mx_attention_tile_kernel<MATH, WIDTH>);
+  const hipError_t e = raise_lds_limit(&raised, &mx_attention_tile_kernel<MATH, WIDTH, true>, &mx_attention_tile_kernel<MATH, WIDTH, false>);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((mx_attention_tile_kernel<MATH, WIDTH>), dim3(plan.groups), dim3(256), kMxAttentionTileLds<WIDTH>, s, plan.params, t, plan.q_vectors, plan.o_vectors);
+  const dim3 grid(plan.groups), block(256);
+  if (plan.linear) hipLaunchKernelGGL((mx_attention_tile_kernel<MATH, WIDTH, true>), grid, block, kMxAttentionTileLds<WIDTH>, s, plan.params, t, plan.q_vectors, plan.o_vectors);
+  else hipLaunchKernelGGL((mx_attention_tile_kernel<MATH, WIDTH, false>), grid, block, kMxAttentionTileLds<WIDTH>, s, plan.params, t, plan.q_vectors, plan.o_vectors);
   return hipSuccess;
 }
 
