@@ -60,12 +60,63 @@ __device__ __forceinline__ MxSequence mx_sequence_of(const MxAttentionParams& P,
   const int32_t each = (int32_t)P.queries_each;
   return mx_sequence(P, t.lengths[b], t.starts ? t.starts[b] : (int32_t)b * each, t.starts ? t.starts[b + 1u] : ((int32_t)b + 1) * each);
 }
-// false: nothing
-__device__ __forceinline__ bool mx_attention_begin(const MxAttentionParams& P, const MxAttentionTensors& t, uint32_t group, MxAttentionWork& w) {
-  if (!mx_attention_work(P, group, &w.b, &w.kv, &w.row_tile, &w.part)) return false;
-  w.s = mx_sequence_of(P, t, w.b);
-  const uint32_t rows = w.s.queries * P.group, r0 = w.row_tile * P.tile_rows;
-  if (r0 >= rows) return false;
+__device__ __forceinline__ uint32_t mx_of_lane(uint32_t v, uint32_t from) { return (uint32_t)__builtin_amdgcn_readlane((int)v, (int)from); }
+// one dword of another lane each
+__device__ __forceinline__ uint32_t mx_from_lane(uint32_t v, uint32_t from) { return (uint32_t)__builtin_amdgcn_ds_bpermute((int)(from * 4u), (int)v); }
+
+// A call's sequences as a wavefront counts them up, 64 at a time: lane l has number 64 block + l, how many pieces of work it makes, and how many it and the lanes below do.
+struct MxCount {
+  MxSequence mine;
+  uint32_t pieces, upto, block = 0u;
+  // -> the block's pieces; pieces_of(sequence)
+  template <typename F>
+  __device__ __forceinline__ uint32_t look_up(const MxAttentionParams& P, const MxAttentionTensors& t, uint32_t lane, F&& pieces_of) {
+    const uint32_t b = 64u * block + lane;
+    mine = MxSequence{0u, 0u, 0, 0u};
+    if (b < P.sequences) mine = mx_sequence_of(P, t, b);
+    pieces = pieces_of(mine);
+    upto = pieces;
+    static_for<6>([&](auto k) {
+      const uint32_t other = mx_from_lane(upto, lane - (1u << (int)k));
+      upto += lane >= (1u << (int)k) ? other : 0u;
+    });
+    return mx_of_lane(upto, 63u);
+  }
+  __device__ __forceinline__ MxSequence of(uint32_t holds) const {
+    return MxSequence{mx_of_lane(mine.first, holds), mx_of_lane(mine.queries, holds), (int32_t)mx_of_lane((uint32_t)mine.position, holds), mx_of_lane(mine.length, holds)};
+  }
+};
+
+// Many rows: a workgroup's tile.  false: none
+__device__ __forceinline__ bool mx_attention_begin(const MxAttentionParams& P, const MxAttentionTensors& t, uint32_t lane, MxAttentionWork& w) {
+  auto pieces_of = [&](const MxSequence& s) { return mx_row_tiles(P, s) * P.kv_heads * P.parts; };
+  MxCount count;
+  uint32_t total = 0u;
+  const uint32_t blocks = (P.sequences + 63u) / 64u;
+  for (uint32_t k = 0; k < blocks; ++k) {
+    count.block = k;
+    total += count.look_up(P, t, lane, pieces_of);
+  }
+  if (blockIdx.x >= total) return false;
+  const uint32_t u = mx_tile_of_group(blockIdx.x, total);
+  uint32_t base = 0u;
+  if (blocks > 1u) {
+    for (count.block = 0u;; ++count.block) {
+      const uint32_t sum = count.look_up(P, t, lane, pieces_of);
+      if (u < base + sum) break;
+      base += sum;
+    }
+  }
+  const uint32_t holds = (uint32_t)__builtin_ctzll(__ballot(u < base + count.upto)), pieces = mx_of_lane(count.pieces, holds);
+  w.b = 64u * count.block + holds;
+  w.s = count.of(holds);
+  uint32_t into = u - (base + mx_of_lane(count.upto, holds) - pieces), rest;
+  const uint32_t each = pieces / P.kv_heads;
+  w.kv = into / each;
+  fd_divmod(into - w.kv * each, P.parts_div, &rest, &w.part);
+  const uint32_t rows = w.s.queries * P.group;
+  w.row_tile = (rows + P.tile_rows - 1u) / P.tile_rows - 1u - rest;
+  const uint32_t r0 = w.row_tile * P.tile_rows;
   mx_attention_rows(P, w, r0, rows - r0 < P.tile_rows ? rows : r0 + P.tile_rows);
   w.parts = mx_parts(P, w.lo, w.hi);
   if (w.part && w.part >= w.parts) return false;

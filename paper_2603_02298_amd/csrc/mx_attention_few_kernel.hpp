@@ -51,8 +51,6 @@ __device__ __forceinline__ void mx_load_to_lds(const unsigned char* from, uint32
   else __builtin_amdgcn_global_load_lds((mx_global_void*)from, (mx_lds_void*)(mx_landing + at), 1, 0, 0);   // (a dword, the byte in its low part)
 }
 
-// one dword of lane `from`
-__device__ __forceinline__ uint32_t mx_from_lane(uint32_t v, uint32_t from) { return (uint32_t)__builtin_amdgcn_ds_bpermute((int)(from * 4u), (int)v); }
 __device__ __forceinline__ int64_t mx_from_lane(int64_t v, uint32_t from) {
   const uint64_t u = (uint64_t)v;
   return (int64_t)((uint64_t)mx_from_lane((uint32_t)(u >> 32), from) << 32 | mx_from_lane((uint32_t)u, from));
@@ -91,40 +89,28 @@ __global__ __launch_bounds__(256, NB * RT == 16 ? 1 : NB * RT <= 4 ? 3 : 2) void
     return (int64_t)((uint64_t)of_lane((uint32_t)((uint64_t)v >> 32), from) << 32 | of_lane((uint32_t)(uint64_t)v, from));
   };
 
-  // ---- sequences, 64 at a time: lane l has number 64 block + l, its units and those of the lanes up to it ----
-  MxSequence mine;
-  uint32_t units_of_lane, upto, block = 0u, block_base = 0u;
-  auto look_up = [&]() -> uint32_t {   // -> the block's units
-    const uint32_t b = 64u * block + lane;
-    mine = MxSequence{0u, 0u, 0, 0u};
-    if (b < P.sequences) mine = mx_sequence_of(P, t, b);
-    units_of_lane = mx_units(P, mine);
-    upto = units_of_lane * P.groups_kv;
-    static_for<6>([&](auto k) {
-      const uint32_t other = mx_from_lane(upto, lane - (1u << (int)k));
-      upto += lane >= (1u << (int)k) ? other : 0u;
-    });
-    return of_lane(upto, 63u);
-  };
+  MxCount count;
+  uint32_t block_base = 0u;   // units of the blocks before
+  auto units_of = [&](const MxSequence& s) { return mx_units(P, s) * P.groups_kv; };
   const uint32_t blocks = (P.sequences + 63u) / 64u;
-  uint32_t together_shift = P.together >> 1;   // 4, 2, 1: 2, 1, 0
+  const uint32_t together_shift = P.together >> 1;   // 4, 2, 1: 2, 1, 0
   const uint32_t g = blockIdx.x * (WAVES >> together_shift) + (wave >> together_shift), in_group = wave & (P.together - 1u);
   uint32_t u, share_end, total_units = 0u;
-  for (uint32_t left = blocks; left; --left) {
-    const uint32_t sum = look_up();
+  for (uint32_t k = 0; k < blocks; ++k) {
+    count.block = k;
+    const uint32_t sum = count.look_up(P, t, lane, units_of);
     if (g == 0u && in_group == 0u && t.bases) {   // for the join
-      if (64u * block + lane < P.sequences) t.bases[64u * block + lane] = total_units + upto - units_of_lane * P.groups_kv;
-      if (left == 1u && lane == 0u) t.bases[P.sequences] = total_units + sum;
+      if (64u * k + lane < P.sequences) t.bases[64u * k + lane] = total_units + count.upto - count.pieces;
+      if (k + 1u == blocks && lane == 0u) t.bases[P.sequences] = total_units + sum;
     }
     total_units += sum;
-    if (left > 1u) ++block;
   }
   mx_share(P, total_units, g, &u, &share_end);
   if (u >= share_end) return;
   const uint32_t share_begin = u;
   if (blocks > 1u) {   // back to the first
-    block = 0u;
-    (void)look_up();
+    count.block = 0u;
+    (void)count.look_up(P, t, lane, units_of);
   }
 
   // ---- what a lane asks memory for: unit lane + 64 i of a run (blocks that a head does not have: its first one's, which meet zeros of q, or rows of O^T that
@@ -151,18 +137,18 @@ __global__ __launch_bounds__(256, NB * RT == 16 ? 1 : NB * RT <= 4 ? 3 : 2) void
 
   while (true) {
   // ---- the share's next sequence and key head ----
-  const uint64_t behind = __ballot(u < block_base + upto);
+  const uint64_t behind = __ballot(u < block_base + count.upto);
   if (behind == 0u) {   // (in a later block)
-    block_base += of_lane(upto, 63u);
-    ++block;
-    (void)look_up();
+    block_base += of_lane(count.upto, 63u);
+    ++count.block;
+    (void)count.look_up(P, t, lane, units_of);
     continue;
   }
-  const uint32_t holds = (uint32_t)__builtin_ctzll(behind), units = of_lane(units_of_lane, holds);
+  const uint32_t holds = (uint32_t)__builtin_ctzll(behind), pieces = of_lane(count.pieces, holds), units = pieces / P.groups_kv;
   MxAttentionWork w;
-  w.b = 64u * block + holds;
-  w.s = MxSequence{of_lane(mine.first, holds), of_lane(mine.queries, holds), (int32_t)of_lane((uint32_t)mine.position, holds), of_lane(mine.length, holds)};
-  const uint32_t into = u - (block_base + of_lane(upto, holds) - units * P.groups_kv), group = into / units;
+  w.b = 64u * count.block + holds;
+  w.s = count.of(holds);
+  const uint32_t into = u - (block_base + of_lane(count.upto, holds) - pieces), group = into / units;
   w.kv = group * P.together + in_group;
   const uint32_t unit = into - group * units, unit_end = units - unit < share_end - u ? units : unit + (share_end - u);
   mx_attention_rows(P, w, 0u, w.s.queries * P.group);

@@ -27,12 +27,11 @@ struct MxAttentionParams {
   uint32_t tile_rows, row_tiles;         // row_tiles: of a sequence and key head, at most
   uint32_t part_tokens, parts;           // tokens of a part (a multiple of kMxAttentionTokens), parts at most
   uint32_t window;                       // 0: none
-  FastDiv page_div, group_div, parts_div, rows_div, kv_div;   // rows_div: of row_tiles
+  FastDiv page_div, group_div, parts_div;
   float scale_log2;                      // scores are exponents of two: |scale| * log2(e), above 0
   int32_t turned;                        // the scale is negative
   int32_t causal, o_type;
   uint32_t queries_each;                 // of a sequence, where a call names no starts
-  int32_t by_xcd;
   // few rows: shares that the call's units are dealt out in (mx_share); key heads that wavefronts of a workgroup go over side by side (1, 2 or 4), and groups of
   // them; rows of a sequence and key head at most
   uint32_t shares, together, groups_kv, part_rows;
@@ -89,17 +88,17 @@ LC_HD uint64_t mx_page_at(const MxAttentionParams& P, uint32_t b, uint32_t j, ui
   fd_divmod(j, P.page_div, &q, place);
   return (uint64_t)b * P.pages_each + q;
 }
-// Which workgroup does what.  Neighbouring workgroups go to different XCDs, each with a cache of its own.  by_xcd: those that read the same keys and values
-// (the row tiles of one sequence and key head, a pair) follow each other on one XCD, the longest (last) rows first.
-LC_HD bool mx_attention_work(const MxAttentionParams& P, uint32_t group, uint32_t* b, uint32_t* kv, uint32_t* row_tile, uint32_t* part) {
-  const uint32_t xcd = P.by_xcd ? group % kXcds : 0u, slot = P.by_xcd ? group / kXcds : group;
-  uint32_t rest, rows, pair;
-  fd_divmod(slot, P.parts_div, &rest, part);
-  fd_divmod(rest, P.rows_div, &pair, &rows);
-  *row_tile = P.row_tiles - 1u - rows;
-  fd_divmod(P.by_xcd ? pair * kXcds + xcd : pair, P.kv_div, b, kv);
-  return *b < P.sequences;
+// ---- many rows: row tiles, of which a workgroup takes one (and one part of its tokens).  All tiles of a call follow each other, sequence after sequence, key head after
+// key head, the longest (last) rows first; there are no workgroups between them that have nothing to do: those would leave some CUs more tiles than others. ----
+// of a key head of a sequence
+LC_HD uint32_t mx_row_tiles(const MxAttentionParams& P, const MxSequence& s) { return (s.queries * P.group + P.tile_rows - 1u) / P.tile_rows; }
+// Workgroup -> number of its tile of `total`; neighbouring workgroups go to different XCDs, each with a cache of its own, which gets tiles that follow each other: those that
+// read the same keys and values.
+LC_HD uint32_t mx_tile_of_group(uint32_t group, uint32_t total) {
+  const uint32_t xcd = group % kXcds, base = total / kXcds, more = total % kXcds;
+  return xcd * base + (xcd < more ? xcd : more) + group / kXcds;
 }
+
 // ---- few rows: one row tile holds all rows of a sequence and key head.  Their tokens are counted in units of kMxUnitTokens.  All units of a call, sequence after
 // sequence, group of `together` key heads after group, are dealt out in even shares, whatever the sequences' lengths.  `together` wavefronts of a workgroup have
 // one share, a key head of the group each: what lies together in the cache is asked for together. ----

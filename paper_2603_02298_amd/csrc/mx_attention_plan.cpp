@@ -127,8 +127,6 @@ lc_status_t make_mx_attention_plan(const Layout& q, const Layout& codes, const L
   P.page_div = make_fastdiv(P.page);
   P.group_div = make_fastdiv(P.group);
   P.parts_div = make_fastdiv(P.parts);
-  P.rows_div = make_fastdiv(P.row_tiles);
-  P.kv_div = make_fastdiv(P.kv_heads);
   // Few rows: as many wavefronts as are resident at once (by the kernels' registers and LDS), fewer where there are fewer units.
   const int resident = plan.width * (int)P.tile_rows <= 128 * 16 ? 12 : plan.width * (int)P.tile_rows <= 256 * 16 ? 8 : 4;
   const int64_t units = (span + kMxAttentionTokens - 1 + kMxUnitTokens - 1) / kMxUnitTokens;
@@ -141,9 +139,9 @@ lc_status_t make_mx_attention_plan(const Layout& q, const Layout& codes, const L
   P.part_rows = (uint32_t)rows;
   P.shares = (uint32_t)shares;
   P.shares_div = make_fastdiv(P.shares);
-  // Row tiles of a pair on one XCD, where the pairs share out evenly among the XCDs.
-  P.by_xcd = row_tiles > 1 && (pairs % kXcds == 0 || pairs >= 4 * (int64_t)kXcds);
-  const double groups = few ? (double)(shares / each) : (double)(P.by_xcd ? (pairs + kXcds - 1) / kXcds * kXcds : pairs) * (double)row_tiles * (double)parts;
+  // Many rows: as many workgroups as the queries can make row tiles (each sequence may begin one more).
+  const double most_tiles = std::min((double)sequences * (double)row_tiles, (double)T * (double)P.group / (double)P.tile_rows + (double)sequences);
+  const double groups = few ? (double)(shares / each) : std::floor(most_tiles) * (double)P.kv_heads * (double)parts;
   if (groups * 256.0 > 4294967295.0) return LC_ERR_TOO_LARGE;   // a grid counts its lanes in 32 bits
   plan.groups = (uint32_t)groups;
   const int64_t tile_bytes = (int64_t)(few ? P.part_rows : P.tile_rows) * (plan.width + 2) * 4;
@@ -260,12 +258,21 @@ lc_status_t mx_attention_walk_on_host(const lc_mx_attention_plan& plan, const in
     }
     if (next != total) return LC_ERR_INVALID_ARG;
   } else {
-    for (uint32_t group = 0; group < plan.groups && inside; ++group) {
-      uint32_t b, kv, row_tile, part;
-      if (!mx_attention_work(P, group, &b, &kv, &row_tile, &part)) continue;
+    std::vector<uint32_t> bases(1, 0u);
+    for (uint32_t b = 0; b < P.sequences; ++b) bases.push_back(bases.back() + mx_row_tiles(P, sequence(b)) * P.kv_heads * P.parts);
+    const uint32_t total = bases.back();
+    if (total > plan.groups) return LC_ERR_INVALID_ARG;
+    std::vector<unsigned char> taken(total);
+    for (uint32_t group = 0; group < total && inside; ++group) {
+      const uint32_t u = mx_tile_of_group(group, total);
+      if (u >= total || taken[u]++) return LC_ERR_INVALID_ARG;
+      uint32_t b = 0;
+      while (u >= bases[b + 1]) ++b;
       const MxSequence s = sequence(b);
+      const uint32_t tiles = mx_row_tiles(P, s), into = u - bases[b], kv = into / (tiles * P.parts), rest = into % (tiles * P.parts);
+      const uint32_t row_tile = tiles - 1u - rest / P.parts, part = rest % P.parts;
       const uint32_t rows = s.queries * P.group, r0 = row_tile * P.tile_rows, r1 = std::min(rows, r0 + P.tile_rows);
-      if (r0 >= rows) continue;
+      if (r0 >= rows || row_tile >= P.row_tiles) return LC_ERR_INVALID_ARG;
       uint32_t lo, hi, from, to;
       mx_rows_seen(P, s, r0, r1, &lo, &hi);
       if (mx_parts(P, lo, hi) > P.parts) return LC_ERR_INVALID_ARG;

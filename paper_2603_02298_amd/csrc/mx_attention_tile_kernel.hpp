@@ -1,7 +1,7 @@
 // Attention of many rows (prompts) over a microscaled 4-bit cache: 128 rows and a part of their tokens per workgroup, 32 rows a wavefront; tiles of 64 tokens are
 // expanded to 16 bits into LDS by all of its lanes and read by all of its wavefronts.
 //
-// LDS holds a tile twice over (the next one's codes are loaded, and expanded, under the products of the one before): keys in the arrangement of
+// LDS holds a tile twice over (the codes of the two next ones are on their way in registers, and expanded under the products of the one before): keys in the arrangement of
 // kLoadKDirect, 64 elements at a time, values in that of kLoadRDirect, whose transposing reads give a lane eight tokens of an element.
 // A lane has the scores of one row (S^T): 16 tokens of 32 each time, the others in lane + 32.
 // Bound by the matrix cores and, about as much, by the exponentials and conversions between the products.
@@ -29,33 +29,36 @@ constexpr uint32_t kMxAttentionTileLds = 2u * 2u * kMxAttentionTokens * WIDTH * 
 
 // LINEAR: everything lies as MxLinear says (lc_mx_attention_plan::linear).
 template <int MATH, int WIDTH, bool LINEAR>
-__global__ __launch_bounds__(256, WIDTH == 256 ? 1 : 2) void mx_attention_tile_kernel(MxAttentionParams P, MxAttentionTensors t, bool q_vectors, bool o_vectors) {
+__global__ __launch_bounds__(256, WIDTH == 256 ? 1 : WIDTH == 128 ? 2 : 3) void mx_attention_tile_kernel(MxAttentionParams P, MxAttentionTensors t, bool q_vectors, bool o_vectors) {
   constexpr int NB = WIDTH / 32, TOKENS = (int)kMxAttentionTokens, STEPS = WIDTH / 16;
   constexpr uint32_t K_BYTES = TOKENS * WIDTH * 2, STAGE = 2 * K_BYTES;
-  // A lane loads UNITS blocks of a tile, all of the same block of a head: of keys and values of PASSES tokens (width 64: of keys or of values)
-  constexpr int PASSES = NB >= 4 ? NB / 4 : 1, TENSORS = NB >= 4 ? 2 : 1;
+  // A lane has one token of a tile (its own number), and of it the blocks wave + 4 i of keys and of values (width 64: one block of keys, or of values).
+  // (Lanes that shared a token's blocks wrote half of them to the same banks of LDS at a time.)
+  constexpr int BLOCKS = NB >= 4 ? NB / 4 : 1, TENSORS = NB >= 4 ? 2 : 1;
   extern __shared__ unsigned char lds[];
   // [stage][token]: the tile whose token has values in blocks that may not be finite (kMxLoud)
   uint32_t* s_loud = reinterpret_cast<uint32_t*>(lds + 2 * STAGE);
   const uint32_t tid = threadIdx.x, lane = tid & 63u, n = lane & 31u, h = lane >> 5;
   const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
   MxAttentionWork w;
-  if (!mx_attention_begin(P, t, blockIdx.x, w)) return;
+  if (!mx_attention_begin(P, t, lane, w)) return;
   if (tid < 2u * TOKENS) s_loud[tid] = 0xFFFFFFFFu;
 
   // ---- a lane's blocks of a tile ----
-  const uint32_t block = tid % NB, first_token = (tid / NB) % (256u / NB > (uint32_t)TOKENS ? (uint32_t)TOKENS : 256u / NB);
-  const bool second = TENSORS == 1 && tid >= 128u;   // (width 64) values
-  const bool block_in = block < P.blocks;
-  const uint32_t of_block = block_in ? block : 0u;
-  const int64_t c_head = LINEAR ? w.kv * P.line.c_h + (int64_t)(of_block * P.line.c_b) : mx_mode_eval(P.c_h, w.kv) + mx_mode_eval(P.c_b, of_block);
-  const int64_t s_head = LINEAR ? w.kv * P.line.s_h + (int64_t)(of_block * P.line.s_b) : mx_mode_eval(P.s_h, w.kv) + mx_mode_eval(P.s_b, of_block);
-  const unsigned char *codes[2] = {(second ? t.v_codes : t.k_codes) + c_head, t.v_codes + c_head};
-  const unsigned char *scales[2] = {(second ? t.v_scales : t.k_scales) + s_head, t.v_scales + s_head};
+  const bool second = TENSORS == 1 && wave >= 2u;   // (width 64) values
+  uint32_t block[BLOCKS];
+  int64_t c_head[BLOCKS], s_head[BLOCKS];   // (of the wavefront)
+  static_for<BLOCKS>([&](auto i) {
+    block[i] = (TENSORS == 1 ? wave & 1u : wave) + 4u * (uint32_t)i;
+    const uint32_t at = block[i] < P.blocks ? block[i] : 0u;
+    c_head[i] = LINEAR ? w.kv * P.line.c_h + (int64_t)(at * P.line.c_b) : mx_mode_eval(P.c_h, w.kv) + mx_mode_eval(P.c_b, at);
+    s_head[i] = LINEAR ? w.kv * P.line.s_h + (int64_t)(at * P.line.s_b) : mx_mode_eval(P.s_h, w.kv) + mx_mode_eval(P.s_b, at);
+  });
+  const unsigned char *codes[2] = {second ? t.v_codes : t.k_codes, t.v_codes}, *scales[2] = {second ? t.v_scales : t.k_scales, t.v_scales};
   struct Raw {
-    u32x4 codes[PASSES][TENSORS];
-    uint32_t byte[PASSES][TENSORS];
-    bool in[PASSES];
+    u32x4 codes[BLOCKS][TENSORS];
+    uint32_t byte[BLOCKS][TENSORS];
+    uint64_t ok;   // bit t: token t lies in the part and on a page of the pool
   };
   auto page_of = [&](uint32_t j, uint32_t* place) -> uint32_t {
     if (j >= w.to) { *place = 0u; return 0xFFFFFFFFu; }
@@ -75,60 +78,49 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : 2) void mx_attention_tile_k
     }
     return in;
   };
-  struct Pages {
-    uint32_t id[PASSES], place[PASSES];
-    uint32_t of_lane;   // the page of token `lane` of the tile
-  };
-  auto pages_of = [&](uint32_t j) {
-    Pages p;
-    uint32_t unused;
-    static_for<PASSES>([&](auto i) { p.id[i] = page_of(j + first_token + (uint32_t)i * (TOKENS / PASSES), &p.place[i]); });
-    p.of_lane = page_of(j + lane, &unused);
-    return p;
-  };
-  auto load = [&](const Pages& p, Raw& raw) {
-    static_for<PASSES>([&](auto i) {
-      int64_t c, s;
-      raw.in[i] = token_at(p.id[i], p.place[i], &c, &s);
+  auto load = [&](uint32_t id, uint32_t place, Raw& raw) {
+    int64_t c, s;
+    raw.ok = __ballot(token_at(id, place, &c, &s));
+    static_for<BLOCKS>([&](auto i) {
       static_for<TENSORS>([&](auto k) {
-        raw.codes[i][k] = *reinterpret_cast<const u32x4*>(codes[k] + c);
-        raw.byte[i][k] = scales[k][s];
+        raw.codes[i][k] = *reinterpret_cast<const u32x4*>(codes[k] + c_head[i] + c);
+        raw.byte[i][k] = (scales[k] + s_head[i])[s];
       });
     });
   };
-  // a block's elements go to LDS in vectors of eight: vector e of it lies at put[..] ^ 16 e (keys' and values' arrangements both fold whole vectors)
-  uint32_t put[PASSES][TENSORS];
-  static_for<PASSES>([&](auto i) {
+  // A block's elements go to LDS in vectors of eight: vector e lies at put[..] ^ 16 e (keys' and values' arrangements both fold whole vectors).  Values: eight lanes' tokens
+  // have four places among the banks; every other four of them write the vectors in another order.
+  uint32_t put[BLOCKS][TENSORS];
+  const uint32_t turn = lane >> 2 & 1u;
+  static_for<BLOCKS>([&](auto i) {
     static_for<TENSORS>([&](auto k) {
-      const uint32_t token = first_token + (uint32_t)i * (TOKENS / PASSES);
       const bool is_value = TENSORS == 1 ? second : (int)decltype(k)::value == 1;
-      put[i][k] = is_value ? K_BYTES + gemm_rdirect_lds_offset(WIDTH, token, 32u * block) : (block / 2u) * (TOKENS * 128u) + gemm_lds_offset(token, 4u * (block & 1u));
+      put[i][k] = is_value ? K_BYTES + (gemm_rdirect_lds_offset(WIDTH, lane, 32u * block[i]) ^ 16u * turn)
+                           : (block[i] / 2u) * (TOKENS * 128u) + gemm_lds_offset(lane, 4u * (block[i] & 1u));
     });
   });
   auto expand = [&](uint32_t j, uint32_t stage, Raw& raw) {
     unsigned char* tile = lds + stage * STAGE;
-    static_for<PASSES>([&](auto i) {
-      const uint32_t token = first_token + (uint32_t)i * (TOKENS / PASSES);
-      // tokens that nobody sees, and blocks that are not there: zeros
-      const bool in = block_in && raw.in[i] && j + token >= w.lo;
+    const bool token_in = (raw.ok >> lane & 1u) && j + lane >= w.lo;
+    static_for<BLOCKS>([&](auto i) {
+      const bool in = token_in && block[i] < P.blocks;   // tokens that nobody sees, and blocks that are not there: zeros
       static_for<TENSORS>([&](auto k) {
         const bool is_value = TENSORS == 1 ? second : (int)decltype(k)::value == 1;
         const bool loud = is_value && in && raw.byte[i][k] >= kMxLoud<MATH>;
-        const u32x4 c = select_or_zero(in && !loud, raw.codes[i][k]);
+        u32x4 c = select_or_zero(in && !loud, raw.codes[i][k]);
+        if (is_value) c = turn ? u32x4{c[1], c[0], c[3], c[2]} : c;
         const float scale = mx_scale_of(in && !loud ? raw.byte[i][k] : 127u);
-        if (loud) s_loud[TOKENS * stage + token] = j;
+        if (loud) s_loud[TOKENS * stage + lane] = j;
         static_for<4>([&](auto e) { *reinterpret_cast<u32x4*>(tile + (put[i][k] ^ (16u * (uint32_t)e))) = mx_expand<MATH>(c[(int)e], scale); });
       });
     });
   };
 
-  Raw raw;
-  Pages ahead = pages_of(w.from);
-  uint64_t ok_next = __ballot(ahead.of_lane < P.pool_pages), ok = ok_next;
-  if (w.from < w.to) {
-    load(ahead, raw);
-    ahead = pages_of(w.from + TOKENS);
-  }
+  Raw raw[2];   // of the two tiles behind the one that is worked on: their codes are on their way
+  uint32_t id, place;
+  id = page_of(w.from + lane, &place);
+  load(id, place, raw[0]);
+  id = page_of(w.from + TOKENS + lane, &place);
 
   // ---- queries ----
   const uint32_t row = w.r0 + 32u * wave + n;
@@ -163,16 +155,18 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : 2) void mx_attention_tile_k
   static_for<NB>([&](auto d) { static_for<16>([&](auto e) { acc[d][(int)e] = 0.0f; }); });
   const uint32_t v_at = gemm_rdirect_frag_offset(WIDTH, lane, 0u, 4u * h);   // the lane's address of elements 0 .. 31 at the first 16 tokens
 
-  if (w.from < w.to) expand(w.from, 0u, raw);
+  load(id, place, raw[1]);
+  id = page_of(w.from + 2u * TOKENS + lane, &place);
+  uint64_t ok = raw[0].ok;
+  expand(w.from, 0u, raw[0]);
   __syncthreads();
-  uint32_t stage = 0u;
-  for (uint32_t j = w.from; j < w.to; j += TOKENS, stage ^= 1u) {
+  // works on tile j, in stage STAGE_AT: asks for the tile two behind it, and expands the next one at the end
+  auto step = [&](uint32_t j, auto stage_at, Raw& to_load, Raw& to_expand) {
+    constexpr uint32_t stage = decltype(stage_at)::value;
     const uint32_t follows = j + TOKENS;
-    ok = ok_next;
-    if (follows < w.to) {
-      ok_next = __ballot(ahead.of_lane < P.pool_pages);
-      load(ahead, raw);
-      ahead = pages_of(follows + TOKENS);
+    if (follows + TOKENS < w.to) {
+      load(id, place, to_load);
+      id = page_of(follows + 2u * TOKENS + lane, &place);
     }
     __builtin_amdgcn_sched_barrier(0);
 
@@ -246,10 +240,10 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : 2) void mx_attention_tile_k
         });
         const float probability = mx_sum_of_halves(mine);
         const bool seen = j + in >= row_lo && j + in < row_hi;
-        uint32_t place;
-        const uint32_t id = page_of(j + in, &place);
+        uint32_t its_place;
+        const uint32_t its_id = page_of(j + in, &its_place);
         int64_t c_token, s_token;
-        token_at(id, place, &c_token, &s_token);
+        token_at(its_id, its_place, &c_token, &s_token);
         const unsigned char *c = t.v_codes + (LINEAR ? w.kv * P.line.c_h : mx_mode_eval(P.c_h, w.kv)) + c_token;
         const unsigned char* b = t.v_scales + (LINEAR ? w.kv * P.line.s_h : mx_mode_eval(P.s_h, w.kv)) + s_token;
         static_for<NB>([&](auto d) {
@@ -269,8 +263,15 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : 2) void mx_attention_tile_k
         });
       }
     }
-    if (follows < w.to) expand(follows, stage ^ 1u, raw);
+    if (follows < w.to) {
+      ok = to_expand.ok;
+      expand(follows, stage ^ 1u, to_expand);
+    }
     __syncthreads();
+  };
+  for (uint32_t j = w.from; j < w.to; j += 2u * TOKENS) {
+    step(j, std::integral_constant<uint32_t, 0>{}, raw[0], raw[1]);
+    if (j + TOKENS < w.to) step(j + TOKENS, std::integral_constant<uint32_t, 1>{}, raw[1], raw[0]);
   }
 
   // ---- out: finished, or a part's sums for the join ----
