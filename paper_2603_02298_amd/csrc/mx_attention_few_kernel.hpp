@@ -76,7 +76,7 @@ __device__ __forceinline__ float mx_sum_of_row(float m) {
 // LINEAR: everything lies as MxLinear says (lc_mx_attention_plan::linear); what a wavefront does once is short then, and short in instructions, which come from
 // memory as well: at one tile a wavefront they are most of the time.
 template <int MATH, int NB, int RT, bool LINEAR>
-__global__ __launch_bounds__(256, NB * RT == 16 ? 1 : NB * RT <= 4 ? 3 : 2) void mx_attention_few_kernel(MxAttentionParams P, MxAttentionTensors t, bool q_vectors, bool o_vectors) {
+__global__ __launch_bounds__(256, NB * RT == 16 ? 1 : NB * RT <= 2 ? 3 : 2) void mx_attention_few_kernel(MxAttentionParams P, MxAttentionTensors t, bool q_vectors, bool o_vectors) {
   using Slot = MxFewSlot<NB>;
   using Tile = MxFewTile<NB>;
   constexpr int WIDTH = 32 * NB, WAVES = 4, TOKENS = 32, CHUNK = 2 * NB;   // elements of a lane's chunk

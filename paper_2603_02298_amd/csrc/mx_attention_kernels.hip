@@ -17,29 +17,34 @@ LC_MX_ATTENTION_LAUNCHER(launch_mx_attention_tile_f16);
 
 namespace {
 
-// Joins the parts of one row, a workgroup each: parts p with sums o_p, maximum m_p and total l_p (exponents of two) make o = sum_p 2^(m_p - m) o_p over
-// l = sum_p 2^(m_p - m) l_p.  WIDTH / 4 lanes take a part, so the workgroup takes 1024 / WIDTH at a time, and AHEAD times as many are on their way; their
-// groups are added in order at the end, so that a result does not depend on timing.
-// FEW: the parts are shares of units (mx_share), otherwise parts of a row tile's tokens.  Bound by the latency of a few loads.
-template <int WIDTH, bool FEW>
-__global__ __launch_bounds__(256) void mx_attention_join_kernel(MxAttentionParams P, MxAttentionTensors t, bool o_vectors) {
-  constexpr uint32_t LANES = WIDTH / 4, GROUPS = 256 / LANES;
-  constexpr int AHEAD = 4;
-  touch_kernel_arguments<kMxAttentionKernargs>();
-  __shared__ f32x4 s_sums[GROUPS][LANES];
-  __shared__ float s_top[GROUPS], s_total[GROUPS];
-  const uint32_t lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
-  const uint32_t b = blockIdx.y, i = blockIdx.x / P.heads, head = blockIdx.x % P.heads;
+// Joins the parts of one row: parts p with sums o_p, maximum m_p and total l_p (exponents of two) make o = sum_p 2^(m_p - m) o_p over
+// l = sum_p 2^(m_p - m) l_p.  WIDTH / 4 lanes take a part; GROUPS of them take a row's parts in turns, AHEAD of each on their way at once, and are added in order at the
+// end, so that a result does not depend on timing.  A row has a wavefront (GROUPS * WIDTH / 4 = 64: rows of few parts) or a workgroup.
+// FEW: the parts are shares of units (mx_share), otherwise parts of a row tile's tokens.
+// Bound by the latency of two loads, one after the other: where a row's parts lie, and they.
+template <int WIDTH, int GROUPS, bool FEW>
+__global__ __launch_bounds__(256) void mx_attention_join_kernel(MxAttentionParams P, MxAttentionTensors t, uint32_t rows_in_all, bool o_vectors) {
+  constexpr uint32_t LANES = WIDTH / 4, ROWS = 256u / (LANES * GROUPS);   // rows of a workgroup
+  constexpr int AHEAD = 8;
+  __shared__ f32x4 s_sums[ROWS][GROUPS][LANES];
+  __shared__ float s_top[ROWS][GROUPS], s_total[ROWS][GROUPS];
+  const uint32_t lane = threadIdx.x % LANES, group = threadIdx.x / LANES % GROUPS, row = ROWS == 1u ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / (LANES * GROUPS)));
+  const uint32_t b = blockIdx.y, in_sequence = blockIdx.x * ROWS + row;   // query by query, head by head
+  if (in_sequence >= rows_in_all) return;   // (a whole wavefront, which no other waits for)
+  uint32_t i, head, kv, in_group;
+  i = in_sequence / P.heads;
+  head = in_sequence - i * P.heads;
+  fd_divmod(head, P.group_div, &kv, &in_group);
   const MxSequence s = mx_sequence_of(P, t, b);
   if (i >= s.queries) return;
-  const uint32_t kv = fd_div(head, P.group_div), r = i * P.group + (head - kv * P.group);
+  const uint32_t r = i * P.group + in_group;
   uint32_t parts, in;
   const uint32_t part_rows = FEW ? P.part_rows : P.tile_rows;
   const uint64_t step = (uint64_t)part_rows * (WIDTH + 2);
   const float* first;
   uint64_t second, stride;   // from the first part to the next; from there on they follow each other
   if constexpr (FEW) {
-    const uint32_t group_kv = kv / P.together, all = t.bases[P.sequences], units = (t.bases[b + 1u] - t.bases[b]) / P.groups_kv, u0 = t.bases[b] + group_kv * units;
+    const uint32_t group_kv = kv / P.together, all = t.bases[P.sequences], begin = t.bases[b], units = (t.bases[b + 1u] - begin) / P.groups_kv, u0 = begin + group_kv * units;
     const uint32_t g0 = mx_share_of(P, all, u0), g1 = mx_share_of(P, all, u0 + units - 1u);
     parts = g1 - g0 + 1u;
     uint32_t share, unused;
@@ -67,14 +72,14 @@ __global__ __launch_bounds__(256) void mx_attention_join_kernel(MxAttentionParam
     float m[AHEAD], l[AHEAD];
     f32x4 v[AHEAD];
     typedef f32x4 __attribute__((aligned(8))) f32x4_any;
-    static_for<AHEAD>([&](auto k) {
+    static_for<AHEAD>([&](auto k) {   // (no branch between the loads: what is not there is the group's first again, and counts for nothing)
       const uint32_t at = p + GROUPS * (uint32_t)k;
-      const bool there = at < parts;
-      const uint64_t off = place_of(there ? at : p);
-      m[k] = there ? tops[off] : kMinusInfinity;
-      l[k] = there ? totals[off] : 0.0f;
+      const uint64_t off = place_of(at < parts ? at : p);
+      m[k] = tops[off];
+      l[k] = totals[off];
       v[k] = *reinterpret_cast<const f32x4_any*>(sums + off);
     });
+    static_for<AHEAD>([&](auto k) { m[k] = p + GROUPS * (uint32_t)k < parts ? m[k] : kMinusInfinity; });
     float most = top;
     static_for<AHEAD>([&](auto k) { most = fmaxf(most, m[k]); });
     const float from = most == kMinusInfinity ? 0.0f : most, shrink = __builtin_amdgcn_exp2f(top - from);
@@ -82,28 +87,36 @@ __global__ __launch_bounds__(256) void mx_attention_join_kernel(MxAttentionParam
     o *= shrink;
     static_for<AHEAD>([&](auto k) {
       const float f = __builtin_amdgcn_exp2f(m[k] - from);
-      total += f * l[k];
-      if (p + GROUPS * (uint32_t)k < parts) o += f * v[k];
+      if (p + GROUPS * (uint32_t)k < parts) {
+        total += f * l[k];
+        o += f * v[k];
+      }
     });
     top = most;
   }
-  s_sums[group][lane] = o;
-  if (lane == 0u) {
-    s_top[group] = top;
-    s_total[group] = total;
+  if constexpr (GROUPS > 1) {
+    s_sums[row][group][lane] = o;
+    if (lane == 0u) {
+      s_top[row][group] = top;
+      s_total[row][group] = total;
+    }
+    if constexpr (ROWS == 1u) __syncthreads();
+    else {   // (a wavefront's own, in its order)
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_wave_barrier();
+    }
+    if (group != 0u) return;
+    top = kMinusInfinity;
+    static_for<GROUPS>([&](auto k) { top = fmaxf(top, s_top[row][k]); });
+    const float from = top == kMinusInfinity ? 0.0f : top;
+    total = 0.0f;
+    o = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    static_for<GROUPS>([&](auto k) {
+      const float f = __builtin_amdgcn_exp2f(s_top[row][k] - from);
+      total += f * s_total[row][k];
+      o += f * s_sums[row][k][lane];
+    });
   }
-  __syncthreads();
-  if (group != 0u) return;
-  top = kMinusInfinity;
-  static_for<(int)GROUPS>([&](auto k) { top = fmaxf(top, s_top[k]); });
-  const float from = top == kMinusInfinity ? 0.0f : top;
-  total = 0.0f;
-  o = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  static_for<(int)GROUPS>([&](auto k) {
-    const float f = __builtin_amdgcn_exp2f(s_top[k] - from);
-    total += f * s_total[k];
-    o += f * s_sums[k][lane];
-  });
   const float inverse = mx_inverse(total), out[4] = {o[0] * inverse, o[1] * inverse, o[2] * inverse, o[3] * inverse};
   const uint32_t token = s.first + i;
   mx_store_o<4>(P, t.o + mx_mode_eval(P.o_t, token) + mx_mode_eval(P.o_h, head), 4u * lane, out, o_vectors);
@@ -143,11 +156,20 @@ lc_status_t execute_mx_attention(const lc_mx_attention_plan& plan, const void* q
   else e = bf16 ? launch_mx_attention_tile_bf16(plan, t, s) : launch_mx_attention_tile_f16(plan, t, s);
   if (failed(e, "attention launch") || failed(hipGetLastError(), "kernel launch")) return LC_ERR_HIP;
   if (joined) {
-    const dim3 grid(plan.joined_rows, P.sequences);
     auto join = [&](auto width) {
-      constexpr int WIDTH = decltype(width)::value;
-      if (few) hipLaunchKernelGGL((mx_attention_join_kernel<WIDTH, true>), grid, dim3(256), 0, s, P, t, plan.o_vectors);
-      else hipLaunchKernelGGL((mx_attention_join_kernel<WIDTH, false>), grid, dim3(256), 0, s, P, t, plan.o_vectors);
+      constexpr int WIDTH = decltype(width)::value, WAVE = 256 / WIDTH, GROUP = 1024 / WIDTH;   // groups of lanes for a row: of a wavefront, of a workgroup
+      auto launch = [&](auto groups, auto of_few) {
+        constexpr int GROUPS = decltype(groups)::value;
+        const uint32_t rows = GROUPS == GROUP ? 1u : 4u;
+        hipLaunchKernelGGL((mx_attention_join_kernel<WIDTH, GROUPS, decltype(of_few)::value>), dim3((plan.joined_rows + rows - 1u) / rows, P.sequences), dim3(256), 0, s, P, t, plan.joined_rows,
+                           plan.o_vectors);
+      };
+      // (a row's parts, were they all as many: four times what a wavefront has on its way at once, or more)
+      const bool many = (few ? (int64_t)P.shares / ((int64_t)P.sequences * P.groups_kv) : (int64_t)P.parts) >= 32 * WAVE;
+      if (few && many) launch(std::integral_constant<int, GROUP>{}, std::true_type{});
+      else if (few) launch(std::integral_constant<int, WAVE>{}, std::true_type{});
+      else if (many) launch(std::integral_constant<int, GROUP>{}, std::false_type{});
+      else launch(std::integral_constant<int, WAVE>{}, std::false_type{});
     };
     if (plan.width == 64) join(std::integral_constant<int, 64>{});
     else if (plan.width == 128) join(std::integral_constant<int, 128>{});

@@ -128,7 +128,7 @@ lc_status_t make_mx_attention_plan(const Layout& q, const Layout& codes, const L
   P.group_div = make_fastdiv(P.group);
   P.parts_div = make_fastdiv(P.parts);
   // Few rows: as many wavefronts as are resident at once (by the kernels' registers and LDS), fewer where there are fewer units.
-  const int resident = plan.width * (int)P.tile_rows <= 128 * 16 ? 12 : plan.width * (int)P.tile_rows <= 256 * 16 ? 8 : 4;
+  const int resident = plan.width * (int)P.tile_rows <= 64 * 16 ? 12 : plan.width * (int)P.tile_rows <= 256 * 16 ? 8 : 4;
   const int64_t units = (span + kMxAttentionTokens - 1 + kMxUnitTokens - 1) / kMxUnitTokens;
   if (few && (double)pairs * (double)units >= 4294967295.0) return LC_ERR_TOO_LARGE;   // units are counted in 32 bits
   P.together = P.kv_heads % 4 == 0 ? 4u : P.kv_heads % 2 == 0 ? 2u : 1u;
