@@ -8,7 +8,6 @@
 #include <hip/hip_runtime.h>
 
 #include "gemm_device.hpp"
-#include "kernarg.hpp"
 #include "mx_attention_plan.hpp"
 #include "mx_gemm_device.hpp"
 
@@ -21,7 +20,6 @@ struct MxAttentionTensors {
   float *lse, *parts;   // parts: unfinished rows
   uint32_t* bases;      // few rows: the sequences' first units, and the total (NULL: nothing is joined)
 };
-constexpr int kMxAttentionKernargs = 1024;   // (as many bytes of the arguments as are brought in at once)
 
 // The kernel's arguments again, through a pointer that the compiler cannot trace back to them: what only the end of a kernel needs is loaded there, and
 // not kept in scalar registers through the loop.  (MxAttentionParams is the first argument.)
@@ -227,6 +225,7 @@ __device__ __forceinline__ void mx_store_o(const MxAttentionParams& P, unsigned 
     else *reinterpret_cast<uint16_t*>(p) = (uint16_t)x;
   }
 }
+typedef f32x4 __attribute__((aligned(8))) f32x4_of_part;   // (a part's tiles begin at multiples of WIDTH + 2 dwords)
 __device__ __forceinline__ float mx_lse(float top, float total) { return total > 0.0f || total != total ? (top + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : kMinusInfinity; }
 __device__ __forceinline__ float mx_inverse(float total) { return total == 0.0f ? 0.0f : 1.0f / total; }
 

@@ -191,6 +191,7 @@ __global__ __launch_bounds__(256, NB * RT == 16 ? 1 : NB * RT <= 2 ? 3 : 2) void
   Found found;
   // Asks for a tile; it lands in the ring's slot tile % DEPTH.  -> which of its tokens lie in the part and on pages of the pool
   auto load = [&](uint32_t tile) -> uint32_t {
+    asm volatile("" ::: "memory");   // (after the reads of the slot's last tile, whose results have been used)
     uint32_t ok;
     if constexpr (LINEAR) {
       if (tile % 32u == 0u) found = find(first_of_lane(tile));
@@ -464,7 +465,7 @@ __global__ __launch_bounds__(256, NB * RT == 16 ? 1 : NB * RT <= 2 ? 3 : 2) void
         } else {
           static_for<4>([&](auto i) {
             static_for<CHUNK / 4>([&](auto c) {
-              *reinterpret_cast<f32x4*>(part + in * WIDTH + CHUNK * (4u * h + (uint32_t)i) + 4 * (int)c) =
+              *reinterpret_cast<f32x4_of_part*>(part + in * WIDTH + CHUNK * (4u * h + (uint32_t)i) + 4 * (int)c) =
                   f32x4{acc[r][4 * c][(int)i], acc[r][4 * c + 1][(int)i], acc[r][4 * c + 2][(int)i], acc[r][4 * c + 3][(int)i]};
             });
           });

@@ -71,13 +71,12 @@ __global__ __launch_bounds__(256) void mx_attention_join_kernel(MxAttentionParam
   for (uint32_t p = group; p < parts; p += GROUPS * AHEAD) {
     float m[AHEAD], l[AHEAD];
     f32x4 v[AHEAD];
-    typedef f32x4 __attribute__((aligned(8))) f32x4_any;
     static_for<AHEAD>([&](auto k) {   // (no branch between the loads: what is not there is the group's first again, and counts for nothing)
       const uint32_t at = p + GROUPS * (uint32_t)k;
       const uint64_t off = place_of(at < parts ? at : p);
       m[k] = tops[off];
       l[k] = totals[off];
-      v[k] = *reinterpret_cast<const f32x4_any*>(sums + off);
+      v[k] = *reinterpret_cast<const f32x4_of_part*>(sums + off);
     });
     static_for<AHEAD>([&](auto k) { m[k] = p + GROUPS * (uint32_t)k < parts ? m[k] : kMinusInfinity; });
     float most = top;

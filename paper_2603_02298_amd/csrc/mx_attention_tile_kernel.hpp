@@ -24,6 +24,19 @@ __device__ __forceinline__ float mx_sum_of_halves(float m) {
   return mx_float_of(a[0]) + mx_float_of(a[1]);
 }
 
+// PRODUCTS matrix instructions, each with READS reads of LDS for it: four products' are on their way at once.  (Left to itself the compiler reads one's and waits: 4096
+// queries of 32 heads on 16384 tokens took 1000 us and take 963 us.  Not for width 64, three of whose workgroups share a CU: 1500 queries of 12 heads took 70 us and not 64 us.)
+template <int PRODUCTS, int READS>
+__device__ __forceinline__ void mx_reads_ahead() {
+  constexpr int AHEAD = 4;
+  __builtin_amdgcn_sched_group_barrier(0x100, READS * AHEAD, 0);
+  static_for<PRODUCTS - AHEAD>([&](auto) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+  });
+  __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+}
+
 template <int WIDTH>
 constexpr uint32_t kMxAttentionTileLds = 2u * 2u * kMxAttentionTokens * WIDTH * 2u + 2u * kMxAttentionTokens * 4u;   // (all of it dynamic: what may be allowed then is all of a CU's)
 
@@ -182,6 +195,7 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : WIDTH == 128 ? 2 : 3) void 
           s[g] = mfma_32x32x16<MATH == kMxBf16>(a, q[k], s[g]);
         });
       });
+      if constexpr (WIDTH >= 128) mx_reads_ahead<2 * STEPS, 1>();
       const bool whole = j >= all_lo && j + TOKENS <= all_hi;
       if (!whole) {   // tokens row_lo .. row_hi - 1, counted from the lane's first one of the tile
         const uint32_t first = row_lo - j - 4u * h, count = row_hi - row_lo;
@@ -229,6 +243,7 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : WIDTH == 128 ? 2 : 3) void 
         return u32x4{a[0], a[1], b[0], b[1]};
       };
       static_for<4>([&](auto k) { static_for<NB>([&](auto d) { acc[d] = mfma_32x32x16<MATH == kMxBf16>(fragment(d, k), p[k], acc[d]); }); });
+      if constexpr (WIDTH >= 128) mx_reads_ahead<4 * NB, 2>();
       uint64_t tokens = __ballot(s_loud[TOKENS * stage + lane] == j);
 #pragma unroll 1
       for (; tokens; tokens &= tokens - 1u) {   // (rare)
@@ -294,7 +309,7 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : WIDTH == 128 ? 2 : 3) void 
     const uint32_t in = 32u * wave + n;
     static_for<NB>([&](auto d) {
       static_for<4>([&](auto i) {
-        *reinterpret_cast<f32x4*>(part + in * WIDTH + 32u * (uint32_t)d + 8u * (uint32_t)i + 4u * h) = f32x4{acc[d][4 * i], acc[d][4 * i + 1], acc[d][4 * i + 2], acc[d][4 * i + 3]};
+        *reinterpret_cast<f32x4_of_part*>(part + in * WIDTH + 32u * (uint32_t)d + 8u * (uint32_t)i + 4u * h) = f32x4{acc[d][4 * i], acc[d][4 * i + 1], acc[d][4 * i + 2], acc[d][4 * i + 3]};
       });
     });
     if (h == 0u) {
