@@ -484,7 +484,8 @@ lc_status_t lc_mx_cache_read(const void* k_codes, const void* v_codes, const lc_
 /* Attention over that cache: o(t,h) = sum_j p_j v(j) / sum_j p_j with p_j = exp(scale q(t,h) . k(j)) over the cached tokens j that query t
  * sees, of head h / (Hq / Hkv).  q over (T,Hq,D) in bf16 or fp16, o over (T,Hq,D) in q's type or fp32; keys' and values' codes over (N,Hkv,P),
  * scales over (N,Hkv,P/32), D <= 256, the same layouts for both.
- *   starts   (sequences + 1) tokens: sequence b's queries are rows starts[b] .. starts[b + 1] - 1 of q.  NULL: T / sequences each (T a multiple).
+ *   starts   (sequences + 1) tokens, none below the one before: sequence b's queries are rows starts[b] .. starts[b + 1] - 1 of q.  NULL: T / sequences each (T
+ *            a multiple).
  *   lengths  (sequences) cached tokens of each, its queries' own among them: query i of n stands at position length - n + i.
  *   pages    (sequences, pages_per_sequence): token j of sequence b lies in slot pages[b, j / page] * page + j % page.  NULL: in slot
  *            b * pages_per_sequence * page + j (then sequences * pages_per_sequence * page <= N).
@@ -493,7 +494,7 @@ lc_status_t lc_mx_cache_read(const void* k_codes, const void* v_codes, const lc_
  * A query that sees nothing (none cached, or a position before the first) gets zeros, and minus infinity in lse.  So does one whose
  * every score is minus infinity.  Rows of q outside every sequence leave o and lse as they were.
  * Numbers that do not fit are cut to what does: lengths to 0 .. pages_per_sequence * page, starts to 0 .. T, a sequence's queries to its
- * first max_queries (the rows of the others are left as they were); tokens on a page outside 0 .. N / page - 1 are seen by nobody.
+ * first max_queries (the rows of the others are left as they were; where starts decrease, rows of o and lse may hold anything); tokens on a page outside 0 .. N / page - 1 are seen by nobody.
  * Keys and values are rounded to q's type before they are multiplied (see lc_mx_gemm: exact in bf16 below 2^128); scores, sums and o's parts are
  * fp32, probabilities are rounded to q's type.  Elements of a block past D have to be finite in q's type.  What nobody sees (slots behind a sequence's
  * length, masked tokens) may hold anything, scales of 255 among it.

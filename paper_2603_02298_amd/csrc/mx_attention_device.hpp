@@ -101,11 +101,13 @@ __device__ __forceinline__ bool mx_attention_begin(const MxAttentionParams& P, c
   if (blocks > 1u) {
     for (count.block = 0u;; ++count.block) {
       const uint32_t sum = count.look_up(P, t, lane, pieces_of);
-      if (u < base + sum) break;
+      if (u < base + sum || count.block + 1u >= blocks) break;
       base += sum;
     }
   }
-  const uint32_t holds = (uint32_t)__builtin_ctzll(__ballot(u < base + count.upto)), pieces = mx_of_lane(count.pieces, holds);
+  const uint64_t behind = __ballot(u < base + count.upto);
+  if (behind == 0u) return false;   // (starts that decrease can make more tiles than are counted)
+  const uint32_t holds = (uint32_t)__builtin_ctzll(behind), pieces = mx_of_lane(count.pieces, holds);
   w.b = 64u * count.block + holds;
   w.s = count.of(holds);
   uint32_t into = u - (base + mx_of_lane(count.upto, holds) - pieces), rest;

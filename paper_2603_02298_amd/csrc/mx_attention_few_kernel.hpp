@@ -140,7 +140,7 @@ __global__ __launch_bounds__(256, NB * RT == 16 ? 1 : NB * RT <= 2 ? 3 : 2) void
   const uint64_t behind = __ballot(u < block_base + count.upto);
   if (behind == 0u) {   // (in a later block)
     block_base += of_lane(count.upto, 63u);
-    ++count.block;
+    if (++count.block >= blocks) return;   // (the call's arrays changed meanwhile)
     (void)count.look_up(P, t, lane, units_of);
     continue;
   }

@@ -308,6 +308,40 @@ def test_long_sequences_in_parts():
     Case([40], [6000], 4, 1, 64, page=64, dtype="f16").run()
 
 
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("queries,forced", [(1, "8"), (1, "64"), (1, "4096"), (9, "64"), (20, "64"), (20, "4096"), (70, "64"), (70, "1024")])
+def test_parts_of_any_number(queries, forced, D, monkeypatch):
+    """Few rows: wavefronts that a call's tokens are dealt out to; many rows: tokens of a part.  From one part of a row to one for each 32 or 64 tokens."""
+    monkeypatch.setenv("LC_TUNE_MX_SHARES", forced)
+    monkeypatch.setenv("LC_TUNE_MX_PART", forced)
+    Case([queries, queries], [5000, 33 + queries], 2, 2, D, page=32).run()
+
+
+@pytest.mark.parametrize("B", [64, 65, 128, 200])
+@pytest.mark.parametrize("most", [1, 5, 60])
+def test_more_sequences_than_a_wavefront_has_lanes(B, most):
+    rng = np.random.default_rng(B)
+    queries = rng.integers(0, most + 1, B).tolist()
+    queries[B // 2] = most
+    lengths = rng.integers(0, 150, B).tolist()
+    lengths[B - 1] = 700
+    Case(queries, lengths, 6, 3 if most > 5 else 2, 64, page=16, max_queries=most).run()
+
+
+@pytest.mark.parametrize("queries", [1, 40])
+def test_starts_that_decrease_end(queries):
+    """Such a call's rows may hold anything, and nothing else is written."""
+    B = 70
+    c = Case([queries] * B, [100] * B, 2, 1, 64, extra_rows=5)
+    c.starts = np.array([0, c.T - 5] * (B // 2) + [0], np.int32)
+    c.max_queries = queries
+    o, _ = c.on_gpu()
+    off = mx.offsets(c.o_text)
+    rest = np.ones(len(o), bool)
+    rest[off[:c.T - 5].reshape(-1)] = False
+    assert (o.float().cpu().numpy()[rest] == 77.0).all()
+
+
 def test_offsets_past_32_bits():
     """A pool whose pages lie 2^28 + 1024 bytes apart."""
     dev = torch.device("cuda:0")
