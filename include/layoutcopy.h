@@ -438,8 +438,8 @@ typedef enum { LC_ROPE_PLAIN = 0, LC_ROPE_LINEAR = 1, LC_ROPE_BASE = 2, LC_ROPE_
 lc_status_t lc_rope_frequencies(int rotary, double base, lc_rope_stretch_t rule, double stretch, int64_t context, double slow, double fast, float* out);
 
 /* x and y over (T,H,D), strides of either sign, in fp32, fp16 or bf16 (the same for both).  Errors: INVALID_ARG (ranks; rotary odd, < 2 or > D),
- * SIZE_MISMATCH, UNSUPPORTED_DTYPE, DST_ALIASES (two coordinates of y share an offset), TOO_LARGE (a mode of 2^31 or more, or of more than 4
- * leaves after coalescing). */
+ * SIZE_MISMATCH, UNSUPPORTED_DTYPE, DST_ALIASES (two coordinates of y share an offset), TOO_LARGE (D > 4096, another mode of 2^31
+ * or more, a mode of more than 4 leaves after coalescing). */
 lc_status_t lc_rope_plan_create(const lc_layout_t* x, const lc_layout_t* y, lc_dtype_t dtype, int rotary, lc_rope_pairs_t pairs, int transposed,
                                 lc_rope_plan_t** out);
 lc_status_t lc_rope_plan_describe(const lc_rope_plan_t* plan, char* buf, size_t cap, size_t* needed);
@@ -494,7 +494,8 @@ lc_status_t lc_mx_cache_read(const void* k_codes, const void* v_codes, const lc_
  * A query that sees nothing (none cached, or a position before the first) gets zeros, and minus infinity in lse.  So does one whose
  * every score is minus infinity.  Rows of q outside every sequence leave o and lse as they were.
  * Numbers that do not fit are cut to what does: lengths to 0 .. pages_per_sequence * page, starts to 0 .. T, a sequence's queries to its
- * first max_queries (the rows of the others are left as they were; where starts decrease, rows of o and lse may hold anything); tokens on a page outside 0 .. N / page - 1 are seen by nobody.
+ * first max_queries (the rows of the others are left as they were; where starts decrease, rows of o and lse may hold anything); tokens on a page
+ * outside 0 .. N / page - 1 are seen by nobody.
  * Keys and values are rounded to q's type before they are multiplied (see lc_mx_gemm: exact in bf16 below 2^128); scores, sums and o's parts are
  * fp32, probabilities are rounded to q's type.  Elements of a block past D have to be finite in q's type.  What nobody sees (slots behind a sequence's
  * length, masked tokens) may hold anything, scales of 255 among it.

@@ -152,3 +152,42 @@ def test_offsets_past_32_bits():
     lc.mx_cache_read_tensor(codes, None, codes_text, scales, None, scales_text, y, None, "(3,1,32):(32,32,1)", slots)
     want = mx.dequantize(*mx.quantize(x[:, 0].double().cpu().numpy(), 32, "floor"))
     assert (y[:, 0].double().cpu().numpy() == want).all()
+
+
+def test_a_graph_follows_its_slots():
+    """Rows written into the cache and read back, captured on a stream of their own: replays follow the arrays, with eager work between them."""
+    dev = torch.device("cuda:0")
+    rng = np.random.default_rng(12)
+    T, N = 9, 24
+    codes_text, scales_text, x_text = "(24,2,64):(128,64,1)", "(24,2,2):(4,2,1)", "(9,2,64):(128,64,1)"
+    x, v = (torch.from_numpy(rng.standard_normal((T, 2, 64)).astype(np.float32)).bfloat16().to(dev) for _ in range(2))
+    slots = torch.arange(T, dtype=torch.int32, device=dev)
+    pools = [[torch.zeros(n, dtype=torch.uint8, device=dev) for n in (N * 64, N * 4)] for _ in range(4)]   # keys and values, of the graph and of the eager calls
+    y = [torch.zeros_like(x) for _ in range(4)]
+
+    def call(i):
+        (kc, ks), (vc, vs) = pools[i], pools[i + 1]
+        lc.mx_cache_write_tensor(x, v, x_text, kc, vc, codes_text, ks, vs, scales_text, slots)
+        lc.mx_cache_read_tensor(kc, vc, codes_text, ks, vs, scales_text, y[i], y[i + 1], x_text, slots)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call(0)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        call(0)
+    for t in (*[p for pair in pools for p in pair], *y):
+        t.zero_()
+    for round_ in range(4):
+        slots.copy_(torch.from_numpy(rng.permutation(N)[:T].astype(np.int32)))
+        if round_ == 2:
+            slots[3] = -1
+        x.mul_(-1.5)
+        torch.cuda.synchronize()
+        graph.replay()
+        call(2)
+        torch.cuda.synchronize()
+        for a, b in ((pools[0], pools[2]), (pools[1], pools[3])):
+            assert all(torch.equal(p, q) for p, q in zip(a, b))
+        assert torch.equal(y[0], y[2]) and torch.equal(y[1], y[3]) and y[0].abs().max() > 0
