@@ -70,7 +70,7 @@ __global__ __launch_bounds__(256) void mx_cache_write_kernel(MxCacheParams P, Ca
   });
 }
 
-template <int DT, bool VECTORS, int UNROLL>
+template <int DT, bool VECTORS, int UNROLL, bool PAST>
 __global__ __launch_bounds__(256) void mx_cache_read_kernel(MxCacheParams P, CacheTensors to, const int32_t* __restrict__ slots) {
   constexpr int ES = kElemBytes<DT>, DW = 2 * ES;
   touch_kernel_arguments<kMxCacheKernargs>();
@@ -104,7 +104,7 @@ __global__ __launch_bounds__(256) void mx_cache_read_kernel(MxCacheParams P, Cac
     });
     unsigned char* p = x + mx_mode_eval(P.x_t, token + (uint32_t)u * step);
     if (VECTORS && d0 + 8u <= P.D) {
-      static_for<DW / 4>([&](auto d) { store_vector<false>(p + d0 * ES + 16 * (int)d, u32x4{v[4 * d], v[4 * d + 1], v[4 * d + 2], v[4 * d + 3]}); });
+      static_for<DW / 4>([&](auto d) { store_vector<PAST>(p + d0 * ES + 16 * (int)d, u32x4{v[4 * d], v[4 * d + 1], v[4 * d + 2], v[4 * d + 3]}); });
     } else {
       static_for<8>([&](auto j) {
         const uint32_t d = d0 + (uint32_t)j;
@@ -117,8 +117,11 @@ __global__ __launch_bounds__(256) void mx_cache_read_kernel(MxCacheParams P, Cac
 template <int DT, bool VECTORS, int UNROLL>
 void launch_cache(const lc_mx_cache_plan& plan, const CacheTensors& to, int tensors, const int32_t* slots, hipStream_t st) {
   const dim3 grid(plan.groups, tensors), block(256);
+  bool past = plan.large_lines;
+  for (int i = 0; i < tensors; ++i) past = past && reinterpret_cast<uintptr_t>(to.x[i]) % kMxLine == 0;
   if (plan.write) hipLaunchKernelGGL((mx_cache_write_kernel<DT, VECTORS, UNROLL>), grid, block, 0, st, plan.params, to, slots);
-  else hipLaunchKernelGGL((mx_cache_read_kernel<DT, VECTORS, UNROLL>), grid, block, 0, st, plan.params, to, slots);
+  else if (VECTORS && DT != LC_F32 && UNROLL != 1 && past) hipLaunchKernelGGL((mx_cache_read_kernel<DT, VECTORS, UNROLL, VECTORS && DT != LC_F32 && UNROLL != 1>), grid, block, 0, st, plan.params, to, slots);
+  else hipLaunchKernelGGL((mx_cache_read_kernel<DT, VECTORS, UNROLL, false>), grid, block, 0, st, plan.params, to, slots);
 }
 template <int DT>
 void launch_cache_of(const lc_mx_cache_plan& plan, const CacheTensors& to, int tensors, const int32_t* slots, hipStream_t st) {

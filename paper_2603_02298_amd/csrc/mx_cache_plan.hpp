@@ -9,6 +9,7 @@ struct lc_mx_cache_plan {
   bool write = false;
   int dtype = 0;
   bool vectors = false;      // a head's elements are neighbours in x
+  bool large_lines = false;  // read: rows go past the caches where x begins on a line (make_mx_cache_plan)
   lc::MxCacheParams params{};
   uint32_t groups = 0;
   int64_t x_min = 0, x_cosize = 0, q_cosize = 0, s_cosize = 0;

@@ -191,3 +191,28 @@ def test_a_graph_follows_its_slots():
         for a, b in ((pools[0], pools[2]), (pools[1], pools[3])):
             assert all(torch.equal(p, q) for p, q in zip(a, b))
         assert torch.equal(y[0], y[2]) and torch.equal(y[1], y[3]) and y[0].abs().max() > 0
+
+
+@pytest.mark.parametrize("dtype,H,D,shift", [("bf16", 16, 128, 0), ("f16", 32, 64, 0), ("bf16", 16, 128, 8), ("f16", 16, 96, 0), ("f32", 8, 128, 0)])
+def test_large_reads(dtype, H, D, shift):
+    """Rows as large as the caches, which are written past them where they make whole lines, against the values of a few tokens at a time."""
+    dev = torch.device("cuda:0")
+    rng = np.random.default_rng(13)
+    T, N = 16384, 20000
+    codes = torch.from_numpy(rng.integers(0, 256, N * H * D // 2, dtype=np.uint8)).to(dev)
+    scales = torch.from_numpy(rng.integers(120, 130, N * H * D // 32, dtype=np.uint8)).to(dev)
+    texts = "(%d,%d,%d):(%d,%d,1)" % (N, H, D, H * D, D), "(%d,%d,%d):(%d,%d,1)" % (N, H, D // 32, H * D // 32, D // 32)
+    slots = rng.permutation(N)[:T].astype(np.int32)
+    slots[5] = -1
+    k, v = (torch.full((shift + T * H * D,), 77.0, dtype=TORCH[dtype], device=dev) for _ in range(2))
+    lc.mx_cache_read_tensor(codes, codes, texts[0], scales, scales, texts[1], k, v, "(%d,%d,%d):(%d,%d,1)" % (T, H, D, H * D, D), torch.from_numpy(slots).to(dev), x_origin=shift)
+    assert torch.equal(k, v) and (k[:shift] == 77.0).all()
+    got = k[shift:].view(T, H, D)
+    assert (got[5] == 77.0).all()
+    table = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6, -0.0, -0.5, -1, -1.5, -2, -3, -4, -6], device=dev)
+    at = torch.from_numpy(slots).to(dev).long().clamp(min=0)
+    c = codes.view(N, -1)[at]
+    want = table[torch.stack([c & 15, c >> 4], -1).long()].view(T, H * D // 32, 32) * torch.exp2(scales.view(N, -1)[at].float() - 127)[..., None]   # (exact in every type)
+    want = want.view(T, H, D).to(TORCH[dtype])
+    want[5] = 77.0
+    assert torch.equal(got, want)
