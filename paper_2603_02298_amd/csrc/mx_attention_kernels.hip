@@ -21,8 +21,8 @@ namespace {
 // l = sum_p 2^(m_p - m) l_p.  WIDTH / 4 lanes take a part; GROUPS of them take a row's parts in turns, AHEAD of each on their way at once, and are added in order at the
 // end, so that a result does not depend on timing.  A row has a wavefront (GROUPS * WIDTH / 4 = 64: rows of few parts) or a workgroup.
 // FEW: the parts are shares of units (mx_share), otherwise parts of a row tile's tokens.
-// Bound by the latency of two loads, one after the other: where a row's parts lie, and they (one sequence's 32 rows of 32 parts 5 us of its call's 11; 64 sequences' 64 rows
-// 6.7 us, a workgroup for each row 12).
+// Bound by the latency of two loads, one after the other: where a row's parts lie, and they (one sequence's 32 rows of 32 parts 5.8 us; 64 sequences' 64 rows
+// 6.7 us, 12 with a workgroup for each row).
 template <int WIDTH, int GROUPS, bool FEW>
 __global__ __launch_bounds__(256) void mx_attention_join_kernel(MxAttentionParams P, MxAttentionTensors t, uint32_t rows_in_all, bool o_vectors) {
   constexpr uint32_t LANES = WIDTH / 4, ROWS = 256u / (LANES * GROUPS);   // rows of a workgroup
@@ -43,7 +43,7 @@ __global__ __launch_bounds__(256) void mx_attention_join_kernel(MxAttentionParam
     end = t.bases[b + 1u];
   }
   const MxSequence s = mx_sequence_of(P, t, b);
-  asm volatile("" ::"s"(all), "s"(begin), "s"(end));   // (loaded with the sequence's numbers, not behind what they decide: 1 us of 6)
+  asm volatile("" ::"s"(all), "s"(begin), "s"(end));   // (loaded with the sequence's numbers, not behind what they decide: one sequence's token 12 -> 11 us)
   if (i >= s.queries) return;
   const uint32_t r = i * P.group + in_group;
   uint32_t parts, in;

