@@ -55,19 +55,23 @@ lc_status_t make_rope_plan(const Layout& x, const Layout& y, int dtype, int rota
   // A workgroup's units: one a lane, of whole heads, of as many heads of a token as there are (its angles are worked out once per workgroup), then of more
   // tokens.  (Four a lane, whose loads are all on their way at once, take longer although they work out fewer angles: 16384 x 32 x 128 in fp16
   // 56 us and not 50, 65536 x 8 x 64 32 and not 27, 64 x 40 x 128 5.4 and not 4.5.  Only heads of more than 256 units have them.)
-  const uint32_t most = kRopeLanes;
-  P.heads = most / P.units;
-  if (P.heads < 1u) P.heads = 1u;
-  if (P.heads > P.H) P.heads = P.H;
-  P.groups_h = (P.H + P.heads - 1u) / P.heads;
-  P.heads = (P.H + P.groups_h - 1u) / P.groups_h;   // shared out evenly
-  P.tokens = most / (P.heads * P.units);
-  if (P.tokens < 1u) P.tokens = 1u;
-  const uint32_t fits = 4096u / (P.turn_units * V);   // angles in 32 KiB of LDS
-  if (P.tokens > (fits ? fits : 1u)) P.tokens = fits ? fits : 1u;
-  if (P.tokens > P.T) P.tokens = P.T;
-  const uint64_t groups = (uint64_t)((P.T + P.tokens - 1u) / P.tokens) * P.groups_h;
-  if (groups * kRopeLanes > 0xFFFFFFFFull) return LC_ERR_TOO_LARGE;   // a grid counts its lanes in 32 bits
+  // And copies of so many that a grid, which counts its lanes in 32 bits, does not hold them otherwise.
+  uint64_t groups = 0;
+  for (uint32_t most : {kRopeLanes, kRopeLanes * kRopeUnroll}) {
+    P.heads = most / P.units;
+    if (P.heads < 1u) P.heads = 1u;
+    if (P.heads > P.H) P.heads = P.H;
+    P.groups_h = (P.H + P.heads - 1u) / P.heads;
+    P.heads = (P.H + P.groups_h - 1u) / P.groups_h;   // shared out evenly
+    P.tokens = most / (P.heads * P.units);
+    if (P.tokens < 1u) P.tokens = 1u;
+    const uint32_t fits = 4096u / (P.turn_units * V);   // angles in 32 KiB of LDS
+    if (P.tokens > (fits ? fits : 1u)) P.tokens = fits ? fits : 1u;
+    if (P.tokens > P.T) P.tokens = P.T;
+    groups = (uint64_t)((P.T + P.tokens - 1u) / P.tokens) * P.groups_h;
+    if (groups * kRopeLanes <= 0xFFFFFFFFull) break;
+  }
+  if (groups * kRopeLanes > 0xFFFFFFFFull) return LC_ERR_TOO_LARGE;
   plan.groups = (uint32_t)groups;
   P.units_div = make_fastdiv(P.units);
   P.heads_div = make_fastdiv(P.heads);

@@ -131,6 +131,12 @@ def test_rope_refused(x, y, dtype, rotary, status):
     _refused(status, lambda: lc.RopePlan(x, y, dtype, rotary))
 
 
+def test_rope_of_more_workgroups_than_a_grid_holds():
+    """One unit a lane would need a grid of more than 2^32 lanes: four are taken."""
+    assert "T=20000000" in lc.RopePlan(_dense(20000000, 32, 64), _dense(20000000, 32, 64), "f16", 64).describe()
+    _refused("TOO_LARGE", lambda: lc.RopePlan(_dense(200000000, 32, 64), _dense(200000000, 32, 64), "f16", 64))
+
+
 # ---- plans of the cache ----
 def _pool(slots, heads, width, page=None, order="heads"):
     """Layouts of codes and scales."""
