@@ -118,8 +118,8 @@ __global__ __launch_bounds__(256, NB * RT == 16 ? 1 : NB * RT <= 2 ? 3 : 2) void
     (void)count.look_up(P, t, lane, units_of);
   }
 
-  // ---- what a lane asks memory for: unit lane + 64 i of a run (blocks that a head does not have: its first one's, which meet zeros of q, or rows of O^T that
-  // nobody stores) ----
+  // ---- what a lane asks memory for: unit lane + 64 i of a run (blocks that a head does not have: its first one's; keys' meet zeros of q, under a scale of 1 for they must
+  // be finite then, values' make rows of O^T that nobody stores) ----
   auto block_or_first = [&](uint32_t k) { return k < P.blocks ? k : 0u; };
   auto codes_block = [&](uint32_t k) { return LINEAR ? block_or_first(k) * P.line.c_b : (uint32_t)mx_mode_eval(P.c_b, block_or_first(k)); };
   auto scales_block = [&](uint32_t k) { return LINEAR ? block_or_first(k) * P.line.s_b : (uint32_t)mx_mode_eval(P.s_b, block_or_first(k)); };
@@ -137,6 +137,8 @@ __global__ __launch_bounds__(256, NB * RT == 16 ? 1 : NB * RT <= 2 ? 3 : 2) void
   static_for<Tile::KS>([&](auto i) { k_at[i] = 16u * (NB * n + ((h * NB / 4u + (uint32_t)i) ^ Slot::key_fold(n))) + (NB == 2 ? 8u * (h & 1u) : 0u); });
   const uint32_t ks_at = 4u * (NB == 4 ? lane : NB == 2 ? 16u * (h >> 1) + n : 32u * h + n);
   const uint32_t vs_at = 4u * (16u * (n * NB / 16u) + 4u * h);
+  bool k_there[Tile::KS];   // the head has the block
+  static_for<Tile::KS>([&](auto i) { k_there[i] = (NB == 8 ? 2u * h + (uint32_t)i : h * NB / 4u) < P.blocks; });
   uint32_t v_at[4];
   static_for<4>([&](auto e) { v_at[e] = Slot::value_row(4u * h + (uint32_t)e) * (16u * NB) + n * NB; });
 
@@ -247,7 +249,7 @@ __global__ __launch_bounds__(256, NB * RT == 16 ? 1 : NB * RT <= 2 ? 3 : 2) void
           static_for<4>([&](auto d) { now.k[(int)g][4 * i + d] = x[(int)d]; });
         });
       }
-      static_for<Tile::KS>([&](auto i) { now.ks[(int)g][(int)i] = *reinterpret_cast<const uint32_t*>(scales + 64u * (uint32_t)i); });
+      static_for<Tile::KS>([&](auto i) { now.ks[(int)g][(int)i] = k_there[i] ? *reinterpret_cast<const uint32_t*>(scales + 64u * (uint32_t)i) : 127u; });
     });
     static_for<2>([&](auto g) {
       const unsigned char *codes = at + (2u + (uint32_t)g) * Slot::CODES, *scales = at + 4u * Slot::CODES + (2u + (uint32_t)g) * Slot::SCALES + vs_at;

@@ -226,6 +226,33 @@ def test_nan_and_infinities_of_keys_and_queries(queries, what):
     c.run()
 
 
+@pytest.mark.parametrize("queries", [1, 5, 40])
+@pytest.mark.parametrize("D", [33, 64, 96, 160, 192, 256])
+@pytest.mark.parametrize("dtype,byte", [("bf16", 254), ("f16", 150)])
+@pytest.mark.parametrize("block", [0, -1])
+def test_a_score_of_minus_infinity_is_nothing(queries, D, dtype, byte, block):
+    """A token whose key makes every score minus infinity leaves the bits as they are without it, also where the kernel's width is more than a head's blocks."""
+    c = Case([queries, queries], [40, 39], 4, 2, D, dtype=dtype, causal=False)
+    c.q = c.q.abs() + 0.5
+    slot = c.used[0][39]
+    codes, scales = mx.mode_offsets(c.codes_text), mx.mode_offsets(c.scales_text)
+    d = block % len(scales[2])
+    for head in range(2):
+        at = (codes[0][slot] + codes[1][head] + codes[2][32 * d]) // 2
+        c.k[0][at:at + 16] = 0xFF   # (all -6, those past D zeros: they have to be finite)
+        left = D - 32 * d
+        if left < 32:
+            c.k[0][at + left // 2:at + 16] = 0
+            if left % 2:
+                c.k[0][at + left // 2] = 0x0F
+        c.k[1][scales[0][slot] + scales[1][head] + scales[2][d]] = byte
+    got = c.on_gpu()
+    c.lengths[0] = 39
+    want = c.on_gpu()
+    assert not torch.isnan(want[0][:c.T * 4 * D]).any()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 @pytest.mark.parametrize("queries", [1, 4, 70])
 @pytest.mark.parametrize("page", [4, 16])
 def test_pages_outside_the_pool_are_seen_by_nobody(queries, page):
