@@ -28,6 +28,15 @@ lc_status_t describe_into(const Plan* plan, char* buf, size_t cap, size_t* neede
     return LC_ERR_INVALID_ARG;
   }
 }
+// no exception leaves a C entry
+template <typename Call>
+lc_status_t guarded(Call&& call) {
+  try {
+    return call();
+  } catch (...) {
+    return LC_ERR_INVALID_ARG;
+  }
+}
 // make(Plan*) into a fresh handle
 template <typename Plan, typename Make>
 lc_status_t create(Plan** out, Make&& make) {
@@ -75,7 +84,7 @@ void lc_rope_plan_destroy(lc_rope_plan_t* plan) { delete plan; }
 lc_status_t lc_rope_plan_execute(const lc_rope_plan_t* plan, const void* x, const int32_t* positions, const float* frequencies, void* y, double factor,
                                  void* hip_stream) {
   if (!plan) return LC_ERR_INVALID_ARG;
-  return lc::execute_rope(*plan, x, positions, frequencies, y, factor, hip_stream);
+  return guarded([&] { return lc::execute_rope(*plan, x, positions, frequencies, y, factor, hip_stream); });
 }
 lc_status_t lc_rope(const void* x, const lc_layout_t* x_layout, const int32_t* positions, const float* frequencies, void* y, const lc_layout_t* y_layout,
                     lc_dtype_t dtype, int rotary, lc_rope_pairs_t pairs, int transposed, double factor, void* hip_stream) {
@@ -106,12 +115,12 @@ void lc_mx_cache_plan_destroy(lc_mx_cache_plan_t* plan) { delete plan; }
 lc_status_t lc_mx_cache_write_plan_execute(const lc_mx_cache_plan_t* plan, const void* k, void* k_codes, void* k_scales, const void* v, void* v_codes,
                                            void* v_scales, const int32_t* slots, void* hip_stream) {
   if (!plan) return LC_ERR_INVALID_ARG;
-  return lc::execute_mx_cache(*plan, true, k, k_codes, k_scales, v, v_codes, v_scales, slots, hip_stream);
+  return guarded([&] { return lc::execute_mx_cache(*plan, true, k, k_codes, k_scales, v, v_codes, v_scales, slots, hip_stream); });
 }
 lc_status_t lc_mx_cache_read_plan_execute(const lc_mx_cache_plan_t* plan, const void* k_codes, const void* k_scales, void* k, const void* v_codes,
                                           const void* v_scales, void* v, const int32_t* slots, void* hip_stream) {
   if (!plan) return LC_ERR_INVALID_ARG;
-  return lc::execute_mx_cache(*plan, false, k, k_codes, k_scales, v, v_codes, v_scales, slots, hip_stream);
+  return guarded([&] { return lc::execute_mx_cache(*plan, false, k, k_codes, k_scales, v, v_codes, v_scales, slots, hip_stream); });
 }
 static lc_status_t cache_call(bool write, const void* k, const void* v, const lc_layout_t* x_layout, const void* k_codes, const void* v_codes,
                               const lc_layout_t* codes_layout, const void* k_scales, const void* v_scales, const lc_layout_t* scales_layout, const int32_t* slots,
@@ -154,7 +163,7 @@ lc_status_t lc_mx_attention_plan_execute(const lc_mx_attention_plan_t* plan, con
                                          const void* v_scales, const int32_t* pages, const int32_t* lengths, const int32_t* starts, void* o, float* lse,
                                          void* workspace, size_t workspace_bytes, void* hip_stream) {
   if (!plan) return LC_ERR_INVALID_ARG;
-  return lc::execute_mx_attention(*plan, q, k_codes, k_scales, v_codes, v_scales, pages, lengths, starts, o, lse, workspace, workspace_bytes, hip_stream);
+  return guarded([&] { return lc::execute_mx_attention(*plan, q, k_codes, k_scales, v_codes, v_scales, pages, lengths, starts, o, lse, workspace, workspace_bytes, hip_stream); });
 }
 
 // Checking devices for tests: walk a plan's accesses on the host against the sizes of the buffers.  Not in the public header.
