@@ -59,6 +59,7 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : WIDTH == 128 ? 2 : 3) void 
   MxAttentionWork w;
   if (!mx_attention_begin(P, t, lane, w)) return;
   if (tid < 2u * TOKENS) s_loud[tid] = 0xFFFFFFFFu;
+  __syncthreads();   // (before any wavefront marks a token of the first tile: a mark must not be followed by another wavefront's store of none)
 
   // ---- a lane's blocks of a tile ----
   const bool second = TENSORS == 1 && wave >= 2u;   // (width 64) values

@@ -212,6 +212,25 @@ def test_values_that_are_not_finite_reach_only_rows_that_see_them(queries, windo
     c.run()
 
 
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_values_that_are_not_finite_in_the_first_tile(D, dtype):
+    """Workgroups by the hundred, every wavefront of which finds a block of NaN in the first tile that it expands, each in a token of its own."""
+    B, n, heads, blocks = 24, 130, 8, D // 32
+    c = Case([n] * B, [64] * B, heads, heads, D, dtype=dtype, causal=False)
+    s = mx.mode_offsets(c.scales_text)
+    nan = np.zeros((B, heads, blocks), bool)
+    for b in range(B):
+        for h in range(heads):
+            for block in range(blocks):
+                if (b + h + block) % 3:
+                    c.v[1][s[0][c.used[b][(7 * b + 13 * h + 8 * block) % 64]] + s[1][h] + s[2][block]] = 255
+                    nan[b, h, block] = True
+    o, _ = c.on_gpu()
+    got = torch.isnan(o).cpu().numpy()[mx.offsets(c.o_text)].reshape(B, n, heads, blocks, 32)
+    assert (got == nan[:, None, :, :, None]).all()
+
+
 @pytest.mark.parametrize("queries", [1, 3, 60])
 @pytest.mark.parametrize("what", ["k", "q"])
 def test_nan_and_infinities_of_keys_and_queries(queries, what):
