@@ -157,7 +157,29 @@ __device__ __forceinline__ u32x4 mx_query_vector(const MxAttentionParams& P, con
   return u32x4{(uint32_t)low ^ turn, (uint32_t)(low >> 32) ^ turn, (uint32_t)high ^ turn, (uint32_t)(high >> 32) ^ turn};
 }
 
-// two probabilities to 16 bits, rounded to nearest: they lie in 0 .. 1, so that a rounding is off by half a step of the type relative to the probability, as q,
+// ---- what a row's exponents are counted from ----
+// A row's probabilities are 2^((x - top) * scale_log2), top the largest score so far.  Near 0 that is one fma, of x and the rounded product top * scale_log2, and the largest
+// one's exponent is that product's rounding error: 2^-15 at most for products up to 2^10, the same in every probability and in their sum.  Beyond, the error would grow with the scores
+// until the largest probability is 0 or infinite, and top is taken off the scores before they are multiplied: `base`, 0 otherwise.  (Always: one more instruction a score.)
+constexpr float kMxFar = 1024.0f;
+struct MxFrom {
+  float base = 0.0f, less = 0.0f;   // of the scores; of the exponents
+};
+__device__ __forceinline__ MxFrom mx_from(const MxAttentionParams& P, float top) {
+  const float product = top * P.scale_log2;
+  const bool far = fabsf(product) > kMxFar;
+  MxFrom f;
+  f.base = far && top != kMinusInfinity ? top : 0.0f;   // (nothing seen so far: minus infinity stays itself)
+  f.less = far ? 0.0f : product;
+  return f;
+}
+__device__ __forceinline__ float mx_exponent(const MxAttentionParams& P, float from_base, const MxFrom& f) { return __builtin_fmaf(from_base, P.scale_log2, -f.less); }
+// what sums counted from `old`, of a row whose largest score was `top`, are multiplied by to be counted from `now`
+__device__ __forceinline__ float mx_shrink(const MxAttentionParams& P, float top, const MxFrom& old, const MxFrom& now) {
+  return top == kMinusInfinity ? 0.0f : __builtin_amdgcn_exp2f(__builtin_fmaf(old.base - now.base, P.scale_log2, old.less - now.less));
+}
+
+// two probabilities to 16 bits, rounded to nearest: they lie in 0 .. 1 (2^-15 more at most), so that a rounding is off by half a step of the type relative to the probability, as q,
 // k and v are.  (The sums that they are divided by are those of the unrounded ones.)
 template <int MATH>
 __device__ __forceinline__ uint32_t mx_pair(float a, float b) {
@@ -228,7 +250,11 @@ __device__ __forceinline__ void mx_store_o(const MxAttentionParams& P, unsigned 
   }
 }
 typedef f32x4 __attribute__((aligned(8))) f32x4_of_part;   // (a part's tiles begin at multiples of WIDTH + 2 dwords)
-__device__ __forceinline__ float mx_lse(float top, float total) { return total > 0.0f || total != total ? (top + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : kMinusInfinity; }
+__device__ __forceinline__ float mx_lse(const MxAttentionParams& P, float top, float total) {
+  constexpr float kLn2 = 0.6931471805599453f;
+  const MxFrom f = mx_from(P, top);
+  return total > 0.0f || total != total ? __builtin_fmaf(f.base, P.scale_log2 * kLn2, (f.less + __builtin_amdgcn_logf(total)) * kLn2) : kMinusInfinity;
+}
 __device__ __forceinline__ float mx_inverse(float total) { return total == 0.0f ? 0.0f : 1.0f / total; }
 
 }  // namespace lc

@@ -297,6 +297,7 @@ __global__ __launch_bounds__(256, NB * RT == 16 ? 1 : NB * RT <= 2 ? 3 : 2) void
   });
 
   float top[RT], total[RT];
+  MxFrom from[RT];
   f32x4 acc[RT][CHUNK];
   static_for<RT>([&](auto r) {
     top[r] = kMinusInfinity;
@@ -356,26 +357,35 @@ __global__ __launch_bounds__(256, NB * RT == 16 ? 1 : NB * RT <= 2 ? 3 : 2) void
     // ---- probabilities: x becomes them ----
     u32x4 p[RT];
     bool moved = false;
-    float shrink[RT];
+    float shrink[RT], most[RT];
     static_for<RT>([&](auto r) {
       float m = kMinusInfinity;
       static_for<8>([&](auto e) { m = fmaxf(m, x[r][e]); });
-      m = fmaxf(top[r], mx_max_of_row(m) * P.scale_log2);
-      const float from = m == kMinusInfinity ? 0.0f : m;   // (nothing seen so far)
-      shrink[r] = __builtin_amdgcn_exp2f(top[r] - from);
-      moved = moved || m != top[r];
-      top[r] = m;
+      most[r] = fmaxf(top[r], mx_max_of_row(m));
+      shrink[r] = 1.0f;
+      moved = moved || most[r] != top[r];
+    });
+    if (__ballot(moved)) {
+      static_for<RT>([&](auto r) {
+        const MxFrom now = mx_from(P, most[r]);
+        shrink[r] = mx_shrink(P, top[r], from[r], now);
+        from[r] = now;
+        top[r] = most[r];
+        static_for<CHUNK>([&](auto c) { acc[r][c] *= shrink[r]; });
+      });
+    }
+    bool far = false;
+    static_for<RT>([&](auto r) { far = far || from[r].base != 0.0f; });
+    if (__ballot(far)) static_for<RT>([&](auto r) { static_for<8>([&](auto e) { x[r][e] -= from[r].base; }); });   // (rare)
+    static_for<RT>([&](auto r) {
       float sum = 0.0f;
       static_for<8>([&](auto e) {
-        x[r][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r][e], P.scale_log2, -from));
+        x[r][e] = __builtin_amdgcn_exp2f(mx_exponent(P, x[r][e], from[r]));
         sum += x[r][e];
       });
       total[r] = total[r] * shrink[r] + sum;
       static_for<4>([&](auto d) { p[r][(int)d] = mx_pair<MATH>(x[r][2 * d], x[r][2 * d + 1]); });
     });
-    if (__ballot(moved)) {
-      static_for<RT>([&](auto r) { static_for<CHUNK>([&](auto c) { acc[r][c] *= shrink[r]; }); });
-    }
 
     // ---- values ----
     uint32_t largest = 0u;
@@ -468,7 +478,7 @@ __global__ __launch_bounds__(256, NB * RT == 16 ? 1 : NB * RT <= 2 ? 3 : 2) void
               mx_store_o<PIECE, !LINEAR>(Z, o, CHUNK * (4u * h + (uint32_t)i) + PIECE * (uint32_t)k, v, o_vectors);
             });
           });
-          if (t.lse && h == 0u) t.lse[(uint64_t)token * Z.heads + head] = mx_lse(top[r], total[r]);
+          if (t.lse && h == 0u) t.lse[(uint64_t)token * Z.heads + head] = mx_lse(Z, top[r], total[r]);
         } else {
           static_for<4>([&](auto i) {
             static_for<CHUNK / 4>([&](auto c) {

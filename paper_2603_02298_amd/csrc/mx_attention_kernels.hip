@@ -17,8 +17,7 @@ LC_MX_ATTENTION_LAUNCHER(launch_mx_attention_tile_f16);
 
 namespace {
 
-// Joins the parts of one row: parts p with sums o_p, maximum m_p and total l_p (exponents of two) make o = sum_p 2^(m_p - m) o_p over
-// l = sum_p 2^(m_p - m) l_p.  WIDTH / 4 lanes take a part; GROUPS of them take a row's parts in turns, AHEAD of each on their way at once, and are added in order at the
+// Joins the parts of one row: parts p with sums o_p, largest score m_p and total l_p make o = sum_p f_p o_p over l = sum_p f_p l_p, f_p = 2^((m_p - m) scale_log2) (mx_shrink).  WIDTH / 4 lanes take a part; GROUPS of them take a row's parts in turns, AHEAD of each on their way at once, and are added in order at the
 // end, so that a result does not depend on timing.  A row has a wavefront (GROUPS * WIDTH / 4 = 64: rows of few parts) or a workgroup.
 // FEW: the parts are shares of units (mx_share), otherwise parts of a row tile's tokens.
 // Bound by the latency of two loads, one after the other: where a row's parts lie, and they (one sequence's 32 rows of 32 parts 5.8 us; 64 sequences' 64 rows
@@ -89,11 +88,12 @@ __global__ __launch_bounds__(256) void mx_attention_join_kernel(MxAttentionParam
     static_for<AHEAD>([&](auto k) { m[k] = p + GROUPS * (uint32_t)k < parts ? m[k] : kMinusInfinity; });
     float most = top;
     static_for<AHEAD>([&](auto k) { most = fmaxf(most, m[k]); });
-    const float from = most == kMinusInfinity ? 0.0f : most, shrink = __builtin_amdgcn_exp2f(top - from);
+    const MxFrom now = mx_from(P, most);
+    const float shrink = mx_shrink(P, top, mx_from(P, top), now);
     total *= shrink;
     o *= shrink;
     static_for<AHEAD>([&](auto k) {
-      const float f = __builtin_amdgcn_exp2f(m[k] - from);
+      const float f = mx_shrink(P, m[k], mx_from(P, m[k]), now);
       if (p + GROUPS * (uint32_t)k < parts) {
         total += f * l[k];
         o += f * v[k];
@@ -115,11 +115,11 @@ __global__ __launch_bounds__(256) void mx_attention_join_kernel(MxAttentionParam
     if (group != 0u) return;
     top = kMinusInfinity;
     static_for<GROUPS>([&](auto k) { top = fmaxf(top, s_top[row][k]); });
-    const float from = top == kMinusInfinity ? 0.0f : top;
+    const MxFrom now = mx_from(P, top);
     total = 0.0f;
     o = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     static_for<GROUPS>([&](auto k) {
-      const float f = __builtin_amdgcn_exp2f(s_top[row][k] - from);
+      const float f = mx_shrink(P, s_top[row][k], mx_from(P, s_top[row][k]), now);
       total += f * s_total[row][k];
       o += f * s_sums[row][k][lane];
     });
@@ -127,7 +127,7 @@ __global__ __launch_bounds__(256) void mx_attention_join_kernel(MxAttentionParam
   const float inverse = mx_inverse(total), out[4] = {o[0] * inverse, o[1] * inverse, o[2] * inverse, o[3] * inverse};
   const uint32_t token = s.first + i;
   mx_store_o<4>(P, t.o + mx_mode_eval(P.o_t, token) + mx_mode_eval(P.o_h, head), 4u * lane, out, o_vectors);
-  if (t.lse && lane == 0u) t.lse[(uint64_t)token * P.heads + head] = mx_lse(top, total);
+  if (t.lse && lane == 0u) t.lse[(uint64_t)token * P.heads + head] = mx_lse(P, top, total);
 }
 
 bool failed(hipError_t e, const char* what) {

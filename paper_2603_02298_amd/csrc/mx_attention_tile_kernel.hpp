@@ -168,6 +168,7 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : WIDTH == 128 ? 2 : 3) void 
   }
 
   float top = kMinusInfinity, total = 0.0f;
+  MxFrom from;
   f32x16 acc[NB];
   static_for<NB>([&](auto d) { static_for<16>([&](auto e) { acc[d][(int)e] = 0.0f; }); });
   const uint32_t v_at = gemm_rdirect_frag_offset(WIDTH, lane, 0u, 4u * h);   // the lane's address of elements 0 .. 31 at the first 16 tokens
@@ -224,16 +225,21 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : WIDTH == 128 ? 2 : 3) void 
       static_for<2>([&](auto g) {
         static_for<16>([&](auto e) { m = fmaxf(m, s[g][(int)e]); });
       });
-      m = fmaxf(top, mx_max_of_halves(m) * P.scale_log2);
-      const float from = m == kMinusInfinity ? 0.0f : m;
-      const float shrink = __builtin_amdgcn_exp2f(top - from);
-      if (__ballot(m != top)) static_for<NB>([&](auto d) { acc[d] *= shrink; });
-      top = m;
+      m = fmaxf(top, mx_max_of_halves(m));
+      float shrink = 1.0f;
+      if (__ballot(m != top)) {
+        const MxFrom now = mx_from(P, m);
+        shrink = mx_shrink(P, top, from, now);
+        from = now;
+        top = m;
+        static_for<NB>([&](auto d) { acc[d] *= shrink; });
+      }
+      if (__ballot(from.base != 0.0f)) static_for<2>([&](auto g) { static_for<16>([&](auto e) { s[g][(int)e] -= from.base; }); });   // (rare)
       float sum = 0.0f;
       u32x4 p[4];
       static_for<2>([&](auto g) {
         static_for<16>([&](auto e) {
-          s[g][(int)e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g][(int)e], P.scale_log2, -from));
+          s[g][(int)e] = __builtin_amdgcn_exp2f(mx_exponent(P, s[g][(int)e], from));
           sum += s[g][(int)e];
         });
         static_for<8>([&](auto d) { p[2 * g + d / 4][(int)d % 4] = mx_pair<MATH>(s[g][2 * d], s[g][2 * d + 1]); });
@@ -307,7 +313,7 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : WIDTH == 128 ? 2 : 3) void 
         mx_store_o<4, !LINEAR>(Z, o, 32u * (uint32_t)d + 8u * (uint32_t)i + 4u * h, v, o_vectors);
       });
     });
-    if (t.lse && h == 0u) t.lse[(uint64_t)q_token * Z.heads + q_head] = mx_lse(top, total);
+    if (t.lse && h == 0u) t.lse[(uint64_t)q_token * Z.heads + q_head] = mx_lse(Z, top, total);
   } else {
     float* part = t.parts + mx_partial_tile(Z, w.b, w.kv, w.row_tile, w.part) * Z.tile_rows * (WIDTH + 2);
     const uint32_t in = 32u * wave + n;

@@ -309,6 +309,68 @@ def test_scores_of_every_size():
             Case([queries], [700], 4, 2, 64, scale=scale, low=126, high=131).run()
 
 
+def _levels(rng, n):
+    """Codes of n tokens, all of a token's elements alike: the largest and the smallest are shared by 2^k tokens each, in tiles of their own where there are several."""
+    if n <= 2:
+        yield np.full(n, rng.integers(9, 16))
+        yield np.full(n, rng.integers(1, 8))
+        return
+    level = rng.choice([0, 1, 2, 3, 4, 5, 6, 9, 10, 11, 12, 13, 14], n)
+    level[[70, n - 1]] = 7
+    level[[3, 64, 130, 131]] = 15
+    yield level
+    level = rng.choice([9, 10, 11, 12, 13, 14], n)   # scores that reach 0 late, from far below (or begin at their largest)
+    level[:64] = 15
+    level[100:104] = 0
+    yield level
+
+
+@pytest.mark.parametrize("D,page,order", [(64, 16, "heads"), (128, 16, "tokens"), (256, 16, "heads"), (128, 3, "gaps")])
+@pytest.mark.parametrize("queries", [1, 6, 40])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_scores_of_large_magnitude(D, page, order, queries, dtype, monkeypatch):
+    """Scores of 1e3 to 3e38 of either sign, so far apart that only those that equal the largest count: the answer is the mean of 2^k values, exactly where the largest score's
+    exponent of two lies beyond 2^10.  Up to there the exponent that is left of it is the rounding error of a product of that size, u times the exponent, 2^-14 u / u = 2^-15 at most: every
+    probability that counts is 2^that, less than a quarter of a 16-bit step (2^-11) from 1, and is rounded to 1, and their sum holds it: the answer is off by ln 2 times it, u |score|,
+    relative, and by 16 u of the mean magnitude for the sums, the reciprocal and the product with it.  (At 1e3 neighbouring scores are 24 apart, and the others' probabilities, e^-24 each, are allowed for twice.)
+    lse: the scale's product with log2(e) (2 u), its product with a constant (2 u) and with the score (u), and one sum: 6 u."""
+    values = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0, -0.0, -0.5, -1.0, -1.5, -2.0, -3.0, -4.0, -6.0])
+    rng = np.random.default_rng(D + queries)
+    for size in (1e3, 1e4, 1e6, 1e9, 1e12, 1e30, 3e38):
+        for n, forced in ((1, None), (2, None), (200, None), (200, "64")):
+            if forced:
+                monkeypatch.setenv("LC_TUNE_MX_SHARES", forced)
+                monkeypatch.setenv("LC_TUNE_MX_PART", forced)
+            for byte in (127, 217) if dtype == "bf16" else (127,):   # large by the scale, or by the keys
+                for level in _levels(rng, n):
+                    scale = float(np.float32(size * rng.uniform(0.5, 1) / (10.5 * D) * 2.0 ** (127 - byte)))
+                    c = Case([queries], [n], 8, 2, D, page=page, order=order, dtype=dtype, o_dtype="f32", causal=False, scale=scale, low=125, high=129)
+                    codes, scales = mx.mode_offsets(c.codes_text), mx.mode_offsets(c.scales_text)
+                    at = (codes[0][c.used[0]][:, None, None] + codes[1][None, :, None] + codes[2][None, None, ::2]) // 2
+                    c.k[0][at] = (level | level << 4)[:, None, None]
+                    c.k[1][scales[0][c.used[0]][:, None, None] + scales[1][None, :, None] + scales[2][None, None, :]] = byte
+                    a = rng.choice([1, 1.25, 1.5, 1.75, -1, -1.25, -1.5, -1.75], (queries, 8))
+                    off = mx.offsets(c.q_text)
+                    q = np.zeros(off.max() + 1, np.float32)
+                    q[off] = a[:, :, None]
+                    c.q = torch.from_numpy(q).to(TORCH[dtype])
+                    score = scale * 2.0 ** (byte - 127) * D * a[:, :, None] * values[level]   # (queries, heads, tokens)
+                    top = score == score.max(-1, keepdims=True)
+                    v = so.Pool(c.v[0], c.codes_text, c.v[1], c.scales_text, D)(c.used[0])    # (tokens, key heads, D)
+                    want = np.einsum("ihj,jhd->ihd", top / top.sum(-1, keepdims=True), np.repeat(v, 4, 1))
+                    o, lse = c.on_gpu()
+                    exponent = np.abs(score.max(-1))[..., None] / np.log(2.0)
+                    mass = np.einsum("ihj,jhd->ihd", top / top.sum(-1, keepdims=True), np.repeat(np.abs(v), 4, 1))
+                    tol = np.where(exponent <= 1024 * (1 + 4 * U), U * exponent * np.log(2.0) * np.abs(want) + 16 * U * mass, 0.0)
+                    others = np.where(top, 0.0, np.exp(score - score.max(-1, keepdims=True)))
+                    tol = tol + 2 * np.einsum("ihj,jhd->ihd", others, np.repeat(np.abs(v), 4, 1) + np.abs(v).max())
+                    assert (np.abs(o.double().cpu().numpy()[mx.offsets(c.o_text)] - want) <= tol).all(), (size, n, forced, byte)
+                    want = score.max(-1) + np.log(top.sum(-1))
+                    assert (np.abs(lse.double().cpu().numpy() - want) <= 6.1 * U * np.abs(want) + others.sum(-1)).all(), (size, n, forced, byte)
+            monkeypatch.delenv("LC_TUNE_MX_SHARES", raising=False)
+            monkeypatch.delenv("LC_TUNE_MX_PART", raising=False)
+
+
 # ---- layouts, types, rows that are nobody's ----
 @pytest.mark.parametrize("q_order,o_order", [("htd", "thd"), ("row", "htd"), ("dht", "thd"), ("thd", "dht"), ("thd", "row")])
 @pytest.mark.parametrize("queries", [1, 5, 40])
