@@ -121,9 +121,10 @@ __global__ __launch_bounds__(256, NB * RT == 16 ? 1 : NB * RT <= 2 ? 3 : 2) void
   // ---- what a lane asks memory for: unit lane + 64 i of a run (blocks that a head does not have: its first one's; keys' meet zeros of q, under a scale of 1 for they must
   // be finite then, values' make rows of O^T that nobody stores) ----
   auto block_or_first = [&](uint32_t k) { return k < P.blocks ? k : 0u; };
-  auto codes_block = [&](uint32_t k) { return LINEAR ? block_or_first(k) * P.line.c_b : (uint32_t)mx_mode_eval(P.c_b, block_or_first(k)); };
-  auto scales_block = [&](uint32_t k) { return LINEAR ? block_or_first(k) * P.line.s_b : (uint32_t)mx_mode_eval(P.s_b, block_or_first(k)); };
-  uint32_t k_off[LOADS], v_off[LOADS], s_off[LOADS], k_token[LOADS], v_token[LOADS];   // scales: token n, block h + 4 i
+  auto codes_block = [&](uint32_t k) { return mx_codes_block<LINEAR>(P, block_or_first(k)); };
+  auto scales_block = [&](uint32_t k) { return mx_scales_block<LINEAR>(P, block_or_first(k)); };
+  MxBlockOffset<LINEAR> k_off[LOADS], v_off[LOADS], s_off[LOADS];
+  uint32_t k_token[LOADS], v_token[LOADS];   // scales: token n, block h + 4 i
   static_for<LOADS>([&](auto i) {
     const uint32_t unit = lane + 64u * (uint32_t)i, row = unit / NB % 16u;
     k_token[i] = row;

@@ -4,6 +4,8 @@
 // A sequence's rows are its queries' heads that share keys and values: row r of sequence b and key head k is query r / group of the sequence, head
 // k * group + r % group.  A workgroup takes `tile_rows` rows of one sequence and key head, and one part of the tokens that they see.
 #pragma once
+#include <type_traits>
+
 #include "mx_params.hpp"
 
 namespace lc {
@@ -129,6 +131,20 @@ LC_HD uint32_t mx_share_of(const MxAttentionParams& P, uint32_t total, uint32_t 
 // share g and the group's key head `in` is number 2 g together + in for what the share begins with, (2 g + 1) together + in for what it ends with; part_rows rows each.
 LC_HD uint64_t mx_share_tile(const MxAttentionParams& P, uint32_t g, bool begins, uint32_t in) { return ((uint64_t)2u * g + (begins ? 0u : 1u)) * P.together + in; }
 LC_HD uint64_t mx_bases_bytes(uint32_t sequences) { return ((uint64_t)sequences * 4u + 4u + 15u) & ~uint64_t(15); }
+
+// Where a block of a head lies from its first one on.  LINEAR: below 2^29 bytes, by the plan's bounds; otherwise blocks may be as far apart as the pool is long.
+template <bool LINEAR>
+using MxBlockOffset = std::conditional_t<LINEAR, uint32_t, int64_t>;
+template <bool LINEAR>
+LC_HD MxBlockOffset<LINEAR> mx_codes_block(const MxAttentionParams& P, uint32_t k) {
+  if constexpr (LINEAR) return k * P.line.c_b;
+  else return mx_mode_eval(P.c_b, k);
+}
+template <bool LINEAR>
+LC_HD MxBlockOffset<LINEAR> mx_scales_block(const MxAttentionParams& P, uint32_t k) {
+  if constexpr (LINEAR) return k * P.line.s_b;
+  else return mx_mode_eval(P.s_b, k);
+}
 
 // A part's unfinished rows in the workspace: `tile_rows` rows of `width` sums, then their maxima and totals.  Number of the part's tile:
 LC_HD uint64_t mx_partial_tile(const MxAttentionParams& P, uint32_t b, uint32_t kv, uint32_t row_tile, uint32_t part) {

@@ -228,11 +228,11 @@ lc_status_t mx_attention_walk_on_host(const lc_mx_attention_plan& plan, const in
       const int64_t co = runs ? id * P.line.c_page + (int64_t)(place + (j & 15u)) * P.line.c_n + kv * P.line.c_h : mx_mode_eval(P.c_n, slot) + mx_mode_eval(P.c_h, kv);
       const int64_t so = runs ? id * P.line.s_page + (int64_t)(place + (j & 15u)) * P.line.s_n + kv * P.line.s_h : mx_mode_eval(P.s_n, slot) + mx_mode_eval(P.s_h, kv);
       for (uint32_t k = 0; k < P.blocks; ++k) {
-        const int64_t cb = runs ? (int64_t)k * P.line.c_b : mx_mode_eval(P.c_b, k), sb = runs ? (int64_t)k * P.line.s_b : mx_mode_eval(P.s_b, k);
-        inside = inside && co + cb + (int64_t)kMxBlockBytes <= c_bytes && so + sb + 1 <= s_bytes;
-        if (runs && (co != mx_mode_eval(P.c_n, slot + (j & 15u)) + mx_mode_eval(P.c_h, kv) || cb != mx_mode_eval(P.c_b, k) ||
-                     so != mx_mode_eval(P.s_n, slot + (j & 15u)) + mx_mode_eval(P.s_h, kv) || sb != mx_mode_eval(P.s_b, k)))
-          return LC_ERR_INVALID_ARG;
+        const int64_t cb = runs ? (int64_t)mx_codes_block<true>(P, k) : (int64_t)mx_codes_block<false>(P, k);
+        const int64_t sb = runs ? (int64_t)mx_scales_block<true>(P, k) : (int64_t)mx_scales_block<false>(P, k);
+        inside = inside && co + cb + (int64_t)kMxBlockBytes <= c_bytes && so + sb + 1 <= s_bytes && cb == mx_mode_eval(P.c_b, k) && sb == mx_mode_eval(P.s_b, k);
+        if (runs)
+          inside = inside && co == mx_mode_eval(P.c_n, slot + (j & 15u)) + mx_mode_eval(P.c_h, kv) && so == mx_mode_eval(P.s_n, slot + (j & 15u)) + mx_mode_eval(P.s_h, kv);
       }
     }
   };

@@ -478,6 +478,34 @@ def test_offsets_past_32_bits():
         assert torch.equal(o, o2)
 
 
+@pytest.mark.parametrize("queries", [1, 5, 40])
+def test_blocks_past_32_bits(queries):
+    """A pool of 8 GiB whose heads have their eight blocks 2^30 bytes apart, scales 2^26 bytes: the bits of the same tokens in a small one."""
+    dev = torch.device("cuda:0")
+    rng = np.random.default_rng(5)
+    slots, kv, D, page, each = 1 << 22, 16, 256, 16, 5
+    far, far_scales = "(%d,%d,(32,8)):(%d,32,(1,%d))" % (slots, kv, 32 * kv, slots * kv * 32), "(%d,%d,8):(%d,1,%d)" % (slots, kv, kv, slots * kv)
+    near, near_scales = "(%d,%d,%d):(%d,%d,1)" % (page * each, kv, D, kv * D, D), "(%d,%d,8):(%d,8,1)" % (page * each, kv, 8 * kv)
+    codes = rng.integers(0, 256, (page * each, kv, 8, 16), dtype=np.uint8)
+    scales = rng.integers(122, 126, (page * each, kv, 8), dtype=np.uint8)
+    g = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(dev)   # noqa: E731
+    q = g(rng.standard_normal((queries, 2 * kv, D)).astype(np.float32)).bfloat16()
+    lengths, table = g(np.array([page * each - 3], np.int32)), rng.permutation(slots // page)[:each]
+    big, big_scales = torch.zeros(8, slots, kv, 16, dtype=torch.uint8, device=dev), torch.full((8, slots, kv), 255, dtype=torch.uint8, device=dev)
+    for i, at in enumerate(table):   # page i of the small pool is page `at` of the large one
+        big[:, page * at:page * (at + 1)] = g(codes[page * i:page * (i + 1)].transpose(2, 0, 1, 3))
+        big_scales[:, page * at:page * (at + 1)] = g(scales[page * i:page * (i + 1)].transpose(2, 0, 1))
+    outs = []
+    for c_text, s_text, c, s, pages in ((far, far_scales, big.view(-1), big_scales.view(-1), table), (near, near_scales, g(codes).view(-1), g(scales).view(-1), np.arange(each))):
+        text = "(%d,%d,%d):(%d,%d,1)" % (queries, 2 * kv, D, 2 * kv * D, D)
+        plan = lc.MxAttentionPlan(text, c_text, s_text, text, "bf16", "f32", sequences=1, page=page, pages_per_sequence=each, max_queries=queries, scale=0.0625)
+        print(plan.describe(), flush=True)
+        o = torch.full((queries, 2 * kv, D), 77.0, device=dev)
+        lc.mx_attention_tensor(plan, q, c, s, c, s, lengths, o, g(pages[None].astype(np.int32)))
+        outs.append(o)
+    assert not (torch.isnan(outs[1]) | (outs[1] == 77.0)).any() and torch.equal(*outs)
+
+
 def test_two_calls_at_once_and_a_captured_one():
     """A graph follows the arrays that it was captured with; an eager call on another stream with a workspace of its own does not disturb it."""
     dev = torch.device("cuda:0")

@@ -329,6 +329,20 @@ def test_attention_walk(B, queries, lengths, heads, kv, page, each, window, caus
         assert plan.debug_walk_on_host(pages, lengths, starts, *sizes) == want
 
 
+@pytest.mark.parametrize("codes,scales", [("(4194304,2,(32,8)):(64,32,(1,2147483648))", "(4194304,2,8):(16,8,1)"), ("(64,2,(32,8)):(64,32,(1,17179869184))", "(64,2,8):(16,8,1)"),
+                                          ("(64,2,256):(512,256,1)", "(64,2,8):(2,1,4294967296)")])
+@pytest.mark.parametrize("queries", [1, 40])
+def test_attention_walk_of_blocks_far_apart(codes, scales, queries):
+    """A head's blocks lie as far apart as the pool is long: their offsets pass 32 bits."""
+    L, M = lc.Layout(codes), lc.Layout(scales)
+    plan = lc.MxAttentionPlan(_dense(queries, 4, 256), codes, scales, _dense(queries, 4, 256), "bf16", sequences=1, page=16, pages_per_sequence=4, max_queries=queries, scale=1.0)
+    assert " linear=0" in plan.describe()
+    pages, lengths = np.array([[3, 0, 2, 1]], np.int32), np.array([60], np.int32)
+    sizes = (queries * 4 * 256 * 2, L.cosize // 2, M.cosize, queries * 4 * 256 * 2)
+    want = _pairs(queries, 1, 16, 4, queries, lengths, None, 2, 4, True, 0)
+    assert plan.debug_walk_on_host(pages, lengths, None, *sizes) == want
+
+
 @pytest.mark.parametrize("rows,kernel", [(1, "few"), (16, "few"), (17, "few"), (32, "few"), (33, "tile"), (4096, "tile")])
 def test_attention_kernel_by_rows(rows, kernel):
     assert " kernel=" + kernel in _attention(T=2 * rows, heads=2, kv=2, max_queries=rows).describe()
