@@ -255,6 +255,11 @@ __device__ __forceinline__ float mx_lse(const MxAttentionParams& P, float top, f
   const MxFrom f = mx_from(P, top);
   return total > 0.0f || total != total ? __builtin_fmaf(f.base, P.scale_log2 * kLn2, (f.less + __builtin_amdgcn_logf(total)) * kLn2) : kMinusInfinity;
 }
-__device__ __forceinline__ float mx_inverse(float total) { return total == 0.0f ? 0.0f : 1.0f / total; }
+// a row's sums over its total: zeros where nothing counts (sums of zeros; or NaN, where every score is minus infinity and a value is not finite)
+struct MxOver {
+  float total, inverse;
+  __device__ __forceinline__ explicit MxOver(float t) : total(t), inverse(1.0f / t) {}
+  __device__ __forceinline__ float operator()(float sum) const { return total == 0.0f ? 0.0f : sum * inverse; }
+};
 
 }  // namespace lc

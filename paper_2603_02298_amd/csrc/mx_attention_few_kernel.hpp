@@ -470,12 +470,12 @@ __global__ __launch_bounds__(256, NB * RT == 16 ? 1 : NB * RT <= 2 ? 3 : 2) void
           uint32_t token, head;
           mx_row_place(Z, w, in, &token, &head);
           unsigned char* o = t.o + (LINEAR ? token * Z.line.o_t + head * Z.line.o_h : mx_mode_eval(Z.o_t, token) + mx_mode_eval(Z.o_h, head));
-          const float inverse = mx_inverse(total[r]);
+          const MxOver over(total[r]);
           constexpr int PIECE = CHUNK < 8 ? CHUNK : 8;
           static_for<4>([&](auto i) {
             static_for<CHUNK / PIECE>([&](auto k) {
               float v[PIECE];
-              static_for<PIECE>([&](auto c) { v[c] = acc[r][PIECE * k + c][(int)i] * inverse; });
+              static_for<PIECE>([&](auto c) { v[c] = over(acc[r][PIECE * k + c][(int)i]); });
               mx_store_o<PIECE, !LINEAR>(Z, o, CHUNK * (4u * h + (uint32_t)i) + PIECE * (uint32_t)k, v, o_vectors);
             });
           });

@@ -124,7 +124,8 @@ __global__ __launch_bounds__(256) void mx_attention_join_kernel(MxAttentionParam
       o += f * s_sums[row][k][lane];
     });
   }
-  const float inverse = mx_inverse(total), out[4] = {o[0] * inverse, o[1] * inverse, o[2] * inverse, o[3] * inverse};
+  const MxOver over(total);
+  const float out[4] = {over(o[0]), over(o[1]), over(o[2]), over(o[3])};
   const uint32_t token = s.first + i;
   mx_store_o<4>(P, t.o + mx_mode_eval(P.o_t, token) + mx_mode_eval(P.o_h, head), 4u * lane, out, o_vectors);
   if (t.lse && lane == 0u) t.lse[(uint64_t)token * P.heads + head] = mx_lse(P, top, total);

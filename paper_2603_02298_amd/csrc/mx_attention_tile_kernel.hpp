@@ -305,11 +305,11 @@ __global__ __launch_bounds__(256, WIDTH == 256 ? 1 : WIDTH == 128 ? 2 : 3) void 
   if (row >= w.r1) return;
   if (w.parts <= 1u) {
     unsigned char* o = t.o + (LINEAR ? q_token * Z.line.o_t + q_head * Z.line.o_h : mx_mode_eval(Z.o_t, q_token) + mx_mode_eval(Z.o_h, q_head));
-    const float inverse = mx_inverse(total);
+    const MxOver over(total);
     static_for<NB>([&](auto d) {
       static_for<4>([&](auto i) {
         float v[4];
-        static_for<4>([&](auto e) { v[e] = acc[d][4 * i + e] * inverse; });
+        static_for<4>([&](auto e) { v[e] = over(acc[d][4 * i + e]); });
         mx_store_o<4, !LINEAR>(Z, o, 32u * (uint32_t)d + 8u * (uint32_t)i + 4u * h, v, o_vectors);
       });
     });

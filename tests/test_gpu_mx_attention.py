@@ -272,6 +272,32 @@ def test_a_score_of_minus_infinity_is_nothing(queries, D, dtype, byte, block):
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+@pytest.mark.parametrize("queries", [1, 5, 40])
+@pytest.mark.parametrize("dtype,byte", [("bf16", 254), ("f16", 150)])
+@pytest.mark.parametrize("forced", [None, "64"])
+def test_every_score_minus_infinity_gives_zeros_whatever_the_values(queries, dtype, byte, forced, monkeypatch):
+    if forced:
+        monkeypatch.setenv("LC_TUNE_MX_SHARES", forced)
+        monkeypatch.setenv("LC_TUNE_MX_PART", forced)
+    for D, page, order in ((64, 16, "heads"), (128, 3, "gaps"), (256, 16, "tokens")):
+        c = Case([queries, queries], [200, 70], 4, 2, D, page=page, order=order, dtype=dtype, causal=False)
+        off = mx.offsets(c.q_text)
+        c.q = c.q.abs() + 0.5
+        c.q[off[queries - 1, 3].reshape(-1)] *= -1   # one row's scores are infinite the other way: NaN
+        codes, scales = mx.mode_offsets(c.codes_text), mx.mode_offsets(c.scales_text)
+        c.k[0][(codes[0][c.used[0]][:, None, None] + codes[1][None, :, None] + codes[2][None, None, ::2]) // 2] = 0xFF
+        c.k[1][scales[0][c.used[0]][:, None, None] + scales[1][None, :, None] + scales[2][None, None, :]] = byte
+        for j, scale in ((0, 255), (64, byte), (199, 255)):
+            c.v[1][scales[0][c.used[0][j]] + scales[1] + scales[2][j % 2]] = scale
+        o, lse = c.on_gpu()
+        o = o.double().cpu().numpy()[mx.offsets(c.o_text)]
+        zero = np.ones((2 * queries, 4), bool)
+        zero[queries - 1, 3] = False
+        zero[queries:] = False
+        assert (o[zero] == 0.0).all() and (lse.cpu().numpy()[zero] == -np.inf).all()
+        assert np.isnan(o[queries - 1, 3]).all() and np.isfinite(o[queries:]).all()
+
+
 @pytest.mark.parametrize("queries", [1, 4, 70])
 @pytest.mark.parametrize("page", [4, 16])
 def test_pages_outside_the_pool_are_seen_by_nobody(queries, page):
