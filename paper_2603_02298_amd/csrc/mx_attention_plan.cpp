@@ -97,8 +97,8 @@ lc_status_t make_mx_attention_plan(const Layout& q, const Layout& codes, const L
   P.max_queries = (uint32_t)std::min(max_queries, T);
   P.max_tokens = P.page * P.pages_each;
   P.window = (uint32_t)std::min(window, most - 1);
-  // (a scale of 0, and one too small for fp32's normal numbers, becomes the smallest of those: infinities and what is not seen stay what they are)
-  P.scale_log2 = std::fmax(std::fabs(scale) * 1.44269504088896341f, std::numeric_limits<float>::min());
+  // (a scale of 0 becomes fp32's smallest number, 2^-149: infinities and what is not seen stay what they are, and scores as far apart as fp32 goes weigh the same to within 2^-20)
+  P.scale_log2 = std::fmax(std::fabs(scale) * 1.44269504088896341f, std::numeric_limits<float>::denorm_min());
   P.turned = scale < 0.0f;
   P.causal = causal != 0;
   P.queries_each = (uint32_t)(T / sequences);

@@ -320,6 +320,20 @@ def test_equal_scores_give_the_mean():
         assert (np.abs(lse_t.double().cpu().numpy() - lse) <= 4 * U * np.abs(lse)).all()
 
 
+@pytest.mark.parametrize("scale", [0.0, -0.0, 1e-42])
+def test_a_scale_of_nothing_gives_the_mean(scale):
+    """Scores of up to 1e35, none further from 0 than 2^-24 once they are scaled: as in the test above; what is masked stays so."""
+    for queries in (1, 40):
+        c = Case([queries], [256 + queries - 1], 4, 2, 64, causal=True, window=256, dtype="bf16", o_dtype="f32", low=127, high=128, scale=scale)
+        c.q = c.q.clamp(-2, 2) * 2.0 ** 50 / (1 if abs(scale) < 1e-44 else 2 ** 20)
+        c.k[1][mx.offsets(c.scales_text)[c.used[0]]] = 127 + 55
+        o_t, lse_t = c.on_gpu()
+        v = so.Pool(c.v[0], c.codes_text, c.v[1], c.scales_text, 64)(c.used[0])
+        want = np.stack([np.repeat(v[i:i + 256].mean(0), 2, 0) for i in range(queries)])
+        assert (o_t.double().cpu().numpy()[mx.offsets(c.o_text)] == want).all()
+        assert (np.abs(lse_t.double().cpu().numpy() - np.log(256.0)) <= 4 * U * np.log(256.0)).all()
+
+
 def test_one_cached_token_is_the_answer():
     for queries in (1, 40):
         c = Case([1] if queries == 1 else [1, queries], [1] if queries == 1 else [1, 1], 4, 2, 96, causal=False, low=120, high=134)
