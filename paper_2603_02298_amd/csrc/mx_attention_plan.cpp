@@ -144,7 +144,7 @@ lc_status_t make_mx_attention_plan(const Layout& q, const Layout& codes, const L
   // Few rows: as many wavefronts of a CU as are fastest, fewer where there are fewer units.  (Width 64 of 16 rows, 64 sequences of 512 to 8192 tokens, 64 heads on 8: 12 of them 50 us, 8
   // 53; width 128 of 32 rows, 16 sequences of 2048 to 8191: 8 of them 45 us, 4 46 and 12 52, 64 sequences 116 and 132; width 256 of 16 rows, 64 sequences: 8 of them 180 us, 4 166.)
   const int resident = plan.width == 256 ? 4 : plan.width * (int)P.tile_rows <= 64 * 16 ? 12 : 8;
-  const int64_t units = (span + kMxAttentionTokens - 1 + kMxUnitTokens - 1) / kMxUnitTokens;
+  const int64_t units = (span + kMxUnitTokens - 1) / kMxUnitTokens;   // (a window's span holds what lies before it in its first tile)
   if (few && (double)pairs * (double)units >= 4294967295.0) return LC_ERR_TOO_LARGE;   // units are counted in 32 bits
   P.together = P.kv_heads % 4 == 0 ? 4u : P.kv_heads % 2 == 0 ? 2u : 1u;
   P.groups_kv = P.kv_heads / P.together;
@@ -160,7 +160,7 @@ lc_status_t make_mx_attention_plan(const Layout& q, const Layout& codes, const L
   if (groups * 256.0 > 4294967295.0) return LC_ERR_TOO_LARGE;   // a grid counts its lanes in 32 bits
   plan.groups = (uint32_t)groups;
   const int64_t tile_bytes = (int64_t)(few ? P.part_rows : P.tile_rows) * (plan.width + 2) * 4;
-  if (few && units > 1) {
+  if (few && units > 1) {   // (a single unit is never shared)
     plan.joined_rows = P.max_queries * P.heads;
     plan.workspace_bytes = (int64_t)mx_bases_bytes(P.sequences) + 2 * shares * P.together * tile_bytes;
   } else if (!few && parts > 1) {

@@ -451,6 +451,15 @@ def test_the_workspace_is_the_calls_alone(queries):
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
 
 
+@pytest.mark.parametrize("queries", [1, 8])
+@pytest.mark.parametrize("page,each,D", [(16, 2, 64), (1, 32, 128), (16, 1, 256)])
+def test_short_caches_need_no_workspace(queries, page, each, D):
+    n = page * each
+    c = Case([queries, queries, 0, queries], [n, 1, 3, n - 1], 8, 2, D, page=page, each=each, order="flat")
+    assert c.plan().workspace_bytes == 0
+    c.run()
+
+
 def test_long_sequences_in_parts():
     Case([1, 1], [20000, 9999], 8, 2, 128, page=64).run()
     Case([40], [6000], 4, 1, 64, page=64, dtype="f16").run()

@@ -343,6 +343,19 @@ def test_attention_walk_of_blocks_far_apart(codes, scales, queries):
     assert plan.debug_walk_on_host(pages, lengths, None, *sizes) == want
 
 
+@pytest.mark.parametrize("page,each,window,none", [(16, 1, 0, True), (16, 2, 0, True), (32, 1, 5, True), (1, 32, 0, True), (11, 3, 0, False), (16, 3, 0, False), (64, 1, 1, False), (16, 200, 1, False)])
+def test_attention_of_one_unit_needs_no_workspace(page, each, window, none):
+    """32 cached tokens at most are never shared out, so nothing is joined.  (A window's first tile may begin before it.)"""
+    for queries in (1, 8):
+        plan = _attention(T=2 * queries, slots=page * 2 * each, page=page, pages_per_sequence=each, max_queries=queries, window=window)
+        assert (plan.workspace_bytes == 0) == none and " kernel=few" in plan.describe()
+        sizes = [t.cosize for t in (plan.q_layout, plan.codes_layout, plan.scales_layout, plan.o_layout)]
+        starts, pages = np.array([0, queries, 2 * queries], np.int32), np.arange(2 * each, dtype=np.int32).reshape(2, each)
+        for lengths in ([page * each] * 2, [1, page * each], [0, 1], [max(1, page * each // 2)] * 2):
+            want = _pairs(2 * queries, 2, page, each, queries, lengths, starts, 4, 8, True, window)
+            assert plan.debug_walk_on_host(pages, np.array(lengths, np.int32), starts, 2 * sizes[0], sizes[1] // 2, sizes[2], 2 * sizes[3]) == want
+
+
 @pytest.mark.parametrize("rows,kernel", [(1, "few"), (16, "few"), (17, "few"), (32, "few"), (33, "tile"), (4096, "tile")])
 def test_attention_kernel_by_rows(rows, kernel):
     assert " kernel=" + kernel in _attention(T=2 * rows, heads=2, kv=2, max_queries=rows).describe()
