@@ -419,8 +419,8 @@ lc_status_t lc_mx_gemm_plan_time(const lc_mx_gemm_plan_t* plan, const void* a, c
  *   HALF        element i with element i + rotary / 2
  *   NEIGHBOURS  element 2 i with element 2 i + 1
  * Positions: 32-bit integers of either sign, one per token.  Frequencies: rotary / 2 fp32 numbers (radians a position).  Both are device
- * arrays read by the call.  The angle is the exact product of the two, reduced in 64 bits; c and s are within 2^-24 of it in
- * fp32 (|factor| <= 1), each result is rounded once.
+ * arrays read by the call.  The angle is the exact product of the two, reduced in 64 bits (to within 2^-40 for angles of up to 2^64); c and s are
+ * within 2^-24 of it in fp32 (|factor| <= 1).  One of a result's two products is rounded to fp32, then the sum with the other, then that to the type.
  * ------------------------------------------------------------------------------------------- */
 typedef enum { LC_ROPE_HALF = 0, LC_ROPE_NEIGHBOURS = 1 } lc_rope_pairs_t;
 
@@ -439,7 +439,7 @@ lc_status_t lc_rope_frequencies(int rotary, double base, lc_rope_stretch_t rule,
 
 /* x and y over (T,H,D), strides of either sign, in fp32, fp16 or bf16 (the same for both).  Errors: INVALID_ARG (ranks; rotary odd, < 2 or > D),
  * SIZE_MISMATCH, UNSUPPORTED_DTYPE, DST_ALIASES (two coordinates of y share an offset), TOO_LARGE (D > 4096, another mode of 2^31
- * or more, a mode of more than 4 leaves after coalescing). */
+ * or more, a mode of more than 4 leaves after coalescing, more elements than 2^24 workgroups go over: some 2^38). */
 lc_status_t lc_rope_plan_create(const lc_layout_t* x, const lc_layout_t* y, lc_dtype_t dtype, int rotary, lc_rope_pairs_t pairs, int transposed,
                                 lc_rope_plan_t** out);
 lc_status_t lc_rope_plan_describe(const lc_rope_plan_t* plan, char* buf, size_t cap, size_t* needed);
@@ -462,7 +462,8 @@ lc_status_t lc_rope(const void* x, const lc_layout_t* x_layout, const int32_t* p
  * A slot must not be named twice by one write: its blocks then hold the codes of one and the scale of one of the tokens, not always the same one's.
  * One call takes keys and values, both under the plan's layouts, or one tensor (the second's three pointers NULL).
  * Asynchronous on `hip_stream`, allocate nothing, may be recorded into a HIP graph; tensors written may overlap none that is read.
- * Errors: those of lc_mx_quantize / lc_mx_dequantize; ranks are 3. x: strides of either sign.  TOO_LARGE: modes of 2^31 or more.
+ * Errors: those of lc_mx_quantize / lc_mx_dequantize; ranks are 3. x: strides of either sign.  TOO_LARGE: modes, or a token's blocks, of 2^31 or more; more
+ * blocks than 2^24 workgroups go over (some 2^32).
  * ------------------------------------------------------------------------------------------- */
 lc_status_t lc_mx_cache_write_plan_create(const lc_layout_t* x, const lc_layout_t* codes, const lc_layout_t* scales, lc_dtype_t x_dtype, lc_mx_rule_t rule,
                                           lc_mx_cache_plan_t** out);
@@ -492,7 +493,7 @@ lc_status_t lc_mx_cache_read(const void* k_codes, const void* v_codes, const lc_
  * All three are device arrays of 32-bit integers, read by the call: a captured call follows them.
  * causal: a query sees no token behind its position; window > 0 (only with causal): and none before the last `window` up to its own.
  * A query that sees nothing (none cached, or a position before the first) gets zeros, and minus infinity in lse.  So does one whose
- * every score is minus infinity.  Rows of q outside every sequence leave o and lse as they were.
+ * every score is minus infinity, whatever the values are.  Rows of q outside every sequence leave o and lse as they were.
  * Numbers that do not fit are cut to what does: lengths to 0 .. pages_per_sequence * page, starts to 0 .. T, a sequence's queries to its
  * first max_queries (the rows of the others are left as they were; where starts decrease, rows of o and lse may hold anything); tokens on a page
  * outside 0 .. N / page - 1 are seen by nobody.

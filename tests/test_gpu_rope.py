@@ -158,3 +158,18 @@ def test_another_stream_and_a_graph():
         eager = torch.empty_like(x)
         lc.rope_tensor(x, text, p, f, eager, text, D)
         assert torch.equal(eager, y)
+
+
+@pytest.mark.parametrize("pairs", ["half", "neighbours"])
+def test_angles_up_to_the_largest(pairs):
+    """Angles of 2^20 to 2^64 radians, whose products with 23 bits of position and 24 of frequency 64 bits hold exactly: 2^-40 more than elsewhere."""
+    rng = np.random.default_rng(7)
+    dev = torch.device("cuda:0")
+    T, rotary = 64, 88
+    positions = (rng.integers(1 << 22, 1 << 23, T) << 8).astype(np.int32) * rng.choice([-1, 1], T).astype(np.int32)
+    frequencies = np.ldexp(rng.uniform(1, 2, rotary // 2).astype(np.float32), np.arange(rotary // 2) - 11).astype(np.float32)
+    x = rng.standard_normal((T, 2, rotary)).astype(np.float32)
+    want, size = so.rotate(x, positions, frequencies, rotary, pairs)
+    y, text = torch.empty(T, 2, rotary, device=dev), "(%d,2,%d):(%d,%d,1)" % (T, rotary, 2 * rotary, rotary)
+    lc.rope_tensor(torch.from_numpy(x).to(dev), text, torch.from_numpy(positions).to(dev), torch.from_numpy(frequencies).to(dev), y, text, rotary, pairs)
+    assert (np.abs(y.double().cpu().numpy() - want) <= _tolerance(want, size, "f32") + 2.0 ** -40 * 2 * np.abs(x).max()).all()
