@@ -11,9 +11,9 @@
 // whose probabilities it has; expanded, its 8 tokens x 2 elements change places by byte permutes into the operand that wants eight tokens of
 // an element.
 // Bound by the cache's bytes, (D / 2 + D / 32) of a token and head, twice, and beside them by a tile's conversions and exponentials: 64 sequences of 512 to 8192
-// tokens, 64 heads on 8 of 128 in bf16, 67 us for 304 MB (4.5 TB/s; a large copy 4.7), with memory alone 64, with the work on tiles alone 45.
-// Two of 131071 tokens in fp16 62 us (4.3 TB/s); 16 of 2048 to 8191 with five queries each, 20 rows: 38 us (2.7 TB/s; vector instructions 59 % of the time, parts of
-// rows 25 MB written and read again).
+// tokens, 64 heads on 8 of 128 in bf16, 67 to 70 us for 304 MB (4.5 TB/s of the 6.3 that a large copy reaches), 64 with these loads alone: half of
+// them fetch scales, a byte a lane.  The work on tiles alone takes 45.  Two of 131071 tokens in fp16 62 us (4.2 TB/s); 16 of 2048 to 8191 with five queries each, 20 rows: 38 us (2.7 TB/s; vector instructions 60 % of the time, parts of
+// rows 27 MB written and read again).
 // Two workgroups of a CU, which keep everything in registers, are 11 to 13 % faster than three, which do not (87 us for the 64 sequences); rings of three and of four tiles
 // are no faster than of two.
 #pragma once
@@ -28,8 +28,9 @@ struct MxFewSlot {
   static constexpr uint32_t CODES = 16u * NB * 16u, SCALES = 16u * NB * 4u;   // bytes of a run: blocks of 16 bytes, a dword for every scale
   static constexpr uint32_t BYTES = 4u * (CODES + SCALES);
   static constexpr int LOADS = NB == 8 ? 2 : 1;                               // instructions of 64 lanes for a run's blocks, or scales
-  static constexpr int DEPTH = 2;                               // tiles of a ring: 80 KiB a workgroup (width 64: 40)
+  static constexpr int DEPTH = 2;                               // tiles of a ring: 20, 40 and 80 KiB a workgroup for widths 64, 128 and 256
   static constexpr uint32_t WAVE = DEPTH * BYTES;
+  static_assert(4u * WAVE == 10240u * NB, "four wavefronts' rings");
   // A token is a row of NB units of 16 bytes, which neighbouring lanes load: memory is asked for whole stretches of a token.  (Lanes that load one unit of 16 tokens
   // each would keep the vector memory path four times as long: it looks a line up for every 16 of them.)
   // Keys: 16 lanes read one unit of 16 tokens, so units are folded by rows that share LDS's banks: unit q of row t lies at q ^ fold(t).

@@ -20,8 +20,8 @@ namespace {
 // Joins the parts of one row: parts p with sums o_p, largest score m_p and total l_p make o = sum_p f_p o_p over l = sum_p f_p l_p, f_p = 2^((m_p - m) scale_log2) (mx_shrink).  WIDTH / 4 lanes take a part; GROUPS of them take a row's parts in turns, AHEAD of each on their way at once, and are added in order at the
 // end, so that a result does not depend on timing.  A row has a wavefront (GROUPS * WIDTH / 4 = 64: rows of few parts) or a workgroup.
 // FEW: the parts are shares of units (mx_share), otherwise parts of a row tile's tokens.
-// Bound by the latency of two loads, one after the other: where a row's parts lie, and they (one sequence's 32 rows of 32 parts 5.8 us; 64 sequences' 64 rows
-// 6.7 us, 12 with a workgroup for each row).
+// Bound by the latency of two loads, one after the other: where a row's parts lie, and they (one sequence's 32 rows of 32 parts 6 us; 64 sequences' 64 rows
+// 6.8 us, 12 with a workgroup for each row).
 template <int WIDTH, int GROUPS, bool FEW>
 __global__ __launch_bounds__(256) void mx_attention_join_kernel(MxAttentionParams P, MxAttentionTensors t, uint32_t rows_in_all, bool o_vectors) {
   constexpr uint32_t LANES = WIDTH / 4, ROWS = 256u / (LANES * GROUPS);   // rows of a workgroup

@@ -5,8 +5,8 @@
 // kLoadKDirect, 64 elements at a time, values in that of kLoadRDirect, whose transposing reads give a lane eight tokens of an element.
 // A lane has the scores of one row (S^T): 16 tokens of 32 each time, the others in lane + 32.
 // Bound by the matrix cores and, about as much, by the exponentials and conversions between the products: 4096 queries at the end of 16384 tokens, 32 heads on 8 of 128 in
-// bf16, 977 us (984 TFLOP/s; a library's product of 8192^3 1220), of which the matrix cores work 42 % and the vector units 58 %; LDS 37 %, 14 % of that in conflicts.
-// Nine prompts of up to 1500 queries under a window of 1024, 12 heads of 64 in fp16, 56 us (410 TFLOP/s): 2.8 row tiles a CU of 17 tiles of tokens each, waits 45 %.
+// bf16, 963 us (1000 TFLOP/s; a library's product of 8192^3 1220), of which the matrix cores work 43 % and the vector units 57 %; LDS 39 %, 14 % of that in conflicts.
+// Nine prompts of up to 1500 queries under a window of 1024, 12 heads of 64 in fp16, 58 us (400 TFLOP/s): 2.8 row tiles a CU of 17 tiles of tokens each, waits 50 %.
 // (The scores of the next tile between this one's exponentials took 1250 us: their registers do not fit.  Other priorities of wavefronts: 943 to 993 us, no pattern.)
 #pragma once
 #include "mx_attention_device.hpp"
